@@ -232,7 +232,7 @@ def prepare(case, seed):
         s["cmass"] = torch.exp(2.0 * _randn(g, B, Hkv, cap))
         # slots hold positions in no order: evicted ones were written over by later tokens
         order = torch.rand((B, Hkv, cap), generator=g, device="cuda").argsort(-1).argsort(-1)
-        held = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        held = torch.tensor(lens, dtype=torch.int32, device="cuda")[:, None].repeat(1, Hkv)
         s["clen"] = held
         s["cpos"] = (2 * order).to(torch.int32)
         s["pos_new"] = torch.full((B,), 2 * cap, dtype=torch.int32, device="cuda")
@@ -261,7 +261,7 @@ def _new_cache(s, dt, n_seqs, cap, Hkv, dh):
     s["vc"] = torch.zeros((n_seqs, cap, Hkv, dh), dtype=dt, device="cuda")
     s["cmass"] = torch.zeros((n_seqs, Hkv, cap), device="cuda")
     s["cpos"] = torch.full((n_seqs, Hkv, cap), -1, dtype=torch.int32, device="cuda")
-    s["clen"] = torch.zeros(n_seqs, dtype=torch.int32, device="cuda")
+    s["clen"] = torch.zeros((n_seqs, Hkv), dtype=torch.int32, device="cuda")
 
 
 # ------------------------------------------------------------------------------------------ one pass
@@ -374,7 +374,7 @@ def _plain_evict(s):
     s["vc"][si, ti, hi] = v[r, hi]
     s["cmass"][si, hi, ti] = s["mass"][hi, r]
     s["cpos"][si, hi, ti] = s["pos"][r]
-    s["clen"].copy_(keep)
+    s["clen"].copy_(keep[:, None].expand(S, Hkv))
     return {name: s[name] for name in ("kc", "vc", "cmass", "cpos", "clen")}
 
 
@@ -391,19 +391,19 @@ def _plain_step(s):
     H, budget, dev = s["n_heads"], s["budget"], "cuda"
     G = H // Hkv
     at = torch.arange(cap, device=dev)
-    held = s["clen"][:, None, None]
+    held = s["clen"][..., None]                                                  # every head has its own length
     # the lightest slot that is not among the newest `recent` positions; the lowest of equal ones
     free = (at < held) & (s["cpos"] < s["pos_new"][:, None, None] - s["recent"])
     weight = torch.where(free, s["cmass"], math.inf)
     victim = torch.where(weight == weight.amin(-1, keepdim=True), at, cap).amin(-1)
     full = s["clen"] >= budget
-    slot = torch.where(full[:, None], victim, s["clen"][:, None].expand(B, Hkv).long())
-    gone = torch.where(full[:, None], s["cpos"].gather(-1, slot[..., None]).squeeze(-1), -1)
+    slot = torch.where(full, victim, s["clen"].long())
+    gone = torch.where(full, s["cpos"].gather(-1, slot[..., None]).squeeze(-1), -1)
     bi, hi = torch.arange(B, device=dev)[:, None], torch.arange(Hkv, device=dev)[None]
     s["kc"][bi, slot, hi] = s["k_new"].view(B, Hkv, dh)
     s["vc"][bi, slot, hi] = s["v_new"].view(B, Hkv, dh)
     length = torch.where(full, s["clen"], s["clen"] + 1)
-    there = (at < length[:, None])[:, None]                                     # [B, 1, cap]
+    there = at < length[..., None]                                               # [B, Hkv, cap]
     k, v = s["kc"].float().permute(0, 2, 3, 1), s["vc"].float().permute(0, 2, 1, 3)
     x = torch.matmul(s["q"].float().view(B, Hkv, G, dh), k) * (1.0 / math.sqrt(dh))
     w = _softmax(x, there[:, :, None])
