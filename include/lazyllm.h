@@ -256,7 +256,8 @@ int lazy_sync_status(lazy_ctx *ctx, void *stream);
 int lazy_device_status(void *stream);
 /* Where the latest non-OK device status taken by this process came from: *where = code of the wait or
  * check that failed (1..4 GEMM roles, 5 gather index, 6 Aux look-up, 7 token id, 8 selection, 9 decode
- * planning, 10 RoPE position, 11..13 attention roles, 14 split-wave counter wait, 15 wait self-test),
+ * planning, 10 RoPE position, 11..13 attention roles, 14 split-wave counter wait, 15 wait self-test,
+ * 16 eviction and bounded caches, 17 shared-prefix attention, 18 draft verification, 19 attention weight),
  * *a / *b two integers of context (CTA and parity for a wait, row and value for a check).  Any pointer
  * may be NULL.  Plumbing: no counterpart in the paper. */
 int lazy_status_detail(int32_t *where, int32_t *a, int32_t *b);
@@ -389,6 +390,83 @@ int lazy_k_select_threshold(void *stream, const float *scores, const int32_t *d_
  * src has src_rows rows (indices outside are reported, not dereferenced). */
 int lazy_k_gather_rows(void *stream, const void *src, const int32_t *idx, void *dst, int32_t n,
                        int32_t row_bytes, int32_t src_rows);
+
+/* ---- bounded and shared caches ------------------------------------------------------------ */
+/* Steps for serving many requests from caches that do not grow: a prompt's keys weighed by the attention
+ * they received (a window of rows instead of Eq. 1's last row, per key/value head instead of the head mean), the cache cut
+ * to a budget by that weight, one token at a time on such a cache, a batch of requests over one shared
+ * prefix, and the check of drafted tokens.  The paper has no counterpart (its selection is Section 3.2's, above);
+ * they combine with it: a pruned prompt's rows can be cut further, or be the shared prefix.
+ * For all of them: head_dim a multiple of 32 in 32..256; n_kv_heads divides n_heads (0 = n_heads); rows that hold
+ * heads side by side start on 16-byte boundaries (base address and pitch); caches kc / vc are [n_seqs, cap, n_kv_heads,
+ * head_dim], cmass / cpos [n_seqs, n_kv_heads, cap], clen [n_seqs, n_kv_heads]; device tables that do not fit the
+ * sizes given are reported through the status word (LAZY_E_BADARG unless stated otherwise) and that sequence is
+ * skipped.  Outputs must not overlap inputs except where stated.  Scratch need not be initialised, keeps nothing from
+ * one call for the next, and must not be shared by calls that may run at the same time (two replayed graphs included). */
+
+/* Accumulated attention weight of prompts: mass[g][r] (fp32 [n_kv_heads, n_total]) = sum over the last `window` rows
+ * i >= r of r's sequence (0 = all its rows) and over the query heads h of key/value head g of
+ * softmax_r(q_i,h . k_r,g / sqrt(head_dim)), causal.  q rows of pitch ldq, k rows of pitch ldkv elements, packed sequences,
+ * the longest of max_len rows.  Sums in fp32 in a fixed order (the same bits every call). */
+size_t lazy_k_attention_mass_scratch_floats(int32_t n_seqs, int32_t n_total, int32_t max_len, int32_t n_heads,
+                                            int32_t n_kv_heads, int32_t window);
+int lazy_k_attention_mass(void *stream, int32_t dtype, const void *q, int32_t ldq, const void *k, int32_t ldkv,
+                          const int32_t *d_cu_seqlens, int32_t n_seqs, int32_t max_len, int32_t n_total,
+                          int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t window, float *scratch,
+                          size_t scratch_floats, float *mass);
+/* Cuts prompts to bounded caches.  Every key/value head of a sequence of n rows keeps min(n, budget) of them: the
+ * newest n_recent (0 <= n_recent <= budget <= cap), and of the older ones those with the largest mass[g][r], equal ones to the
+ * lower row (NaN is less than everything).  Kept rows go to slots 0, 1, ... in row order: K and V rows, their
+ * weights, their positions pos[r], and clen; slots behind them keep what they held.  k, v packed rows of pitch ldkv. */
+size_t lazy_k_evict_scratch_ints(int32_t n_seqs, int32_t n_kv_heads, int32_t budget);
+int lazy_k_evict(void *stream, int32_t dtype, const void *k, const void *v, int32_t ldkv, const int32_t *pos,
+                 const float *mass, const int32_t *d_cu_seqlens, int32_t n_seqs, int32_t max_len, int32_t n_total,
+                 int32_t n_kv_heads, int32_t head_dim, int32_t budget, int32_t n_recent, int32_t *scratch,
+                 size_t scratch_ints, void *kc, void *vc, float *cmass, int32_t *cpos, int32_t *clen, int32_t cap);
+/* One token per sequence on bounded caches (n_recent < budget <= cap; 0 <= len_in <= budget, else LAZY_E_CAPACITY is reported
+ * and that head skipped: its o is zero, its slot and gone -1, its cache untouched).  Per sequence and key/value head: with
+ * len_in < budget the new token is appended; else it takes the slot of the least weight among those with position <
+ * pos_new - n_recent (equal ones: the lowest slot; NaN least of all; no such slot: slot 0).  Then o [n_seqs, n_heads *
+ * head_dim] = attention of q over the slots held, and every held slot's weight grows by the weights that the
+ * group's heads gave it (the new token's from 0).  k_new / v_new: rotated rows of pitch ld_new.  kc / vc are updated in place;
+ * mass_out, pos_out and len_out may each be the array read (in place) or another one, which leaves the old state for a
+ * step that is to be taken back (behind the held slots they keep what they held).  slot, gone (int32 [n_seqs,
+ * n_kv_heads]): the slot taken, the position evicted from it or -1. */
+size_t lazy_k_evict_step_scratch_floats(int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                        int32_t budget);
+int lazy_k_evict_step(void *stream, int32_t dtype, const void *q, int32_t ldq, const void *k_new, const void *v_new,
+                      int32_t ld_new, const int32_t *pos_new, void *kc, void *vc, int32_t cap, const float *mass_in,
+                      float *mass_out, const int32_t *pos_in, int32_t *pos_out, const int32_t *len_in,
+                      int32_t *len_out, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                      int32_t budget, int32_t n_recent, float *scratch, size_t scratch_floats, void *o, int32_t *slot,
+                      int32_t *gone);
+/* Attention of a batch over one shared prefix.  Sequence s has query rows [cu_q[s], cu_q[s+1]) (at most max_q: one, or a
+ * token and its drafted successors) of n_rows in all, and its own keys kv_idx[cu_kv[s] .. cu_kv[s+1]) (at most max_kv),
+ * rows of the buffers k / v (kv_rows rows of pitch ldkv) in the order of their positions, its new rows' own keys last.  Row i of
+ * T sees all n_pre rows of k_pre / v_pre (pitch ld_pre; the slots of one bounded cache serve too) and its own keys j
+ * <= C - T + i of C; a row that sees nothing gives zeros.  The prefix is read once for the batch.  A row index outside
+ * [0, kv_rows) is reported and that key skipped.  n_rows <= 65535.  o [n_rows, n_heads * head_dim]. */
+size_t lazy_k_attention_prefix_scratch_floats(int32_t n_rows, int32_t n_seqs, int32_t max_q, int32_t n_pre,
+                                              int32_t max_kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+int lazy_k_attention_prefix(void *stream, int32_t dtype, const void *q, int32_t ldq, const int32_t *d_cu_q,
+                            int32_t n_rows, int32_t n_seqs, int32_t max_q, const void *k_pre, const void *v_pre,
+                            int32_t ld_pre, int32_t n_pre, const void *k, const void *v, int32_t ldkv, int32_t kv_rows,
+                            const int32_t *kv_idx, const int32_t *d_cu_kv, int32_t n_kv, int32_t max_kv,
+                            int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float *scratch,
+                            size_t scratch_floats, void *o);
+/* Verification of drafted tokens.  Sequence s drafted draft[d_cu_draft[s] .. d_cu_draft[s+1]) (T_s <= max_draft tokens; n_draft in
+ * all); row t of q (pitch ldq) holds the draft model's probabilities that draft t was drawn from, NULL if the
+ * drafts were chosen outright (probability 1); rows d_cu_draft[s] + s + t, t = 0..T_s, of p (pitch ldp) the target's at draft t
+ * and, for t = T_s, behind the last one.  Draft t is accepted iff u_accept[t] q(x) < p(x) and all before it were
+ * (u_accept fp32 [n_draft], u_sample fp32 [n_seqs], uniform in [0, 1)).  The token behind the accepted ones is the first id
+ * whose running sum of w exceeds u_sample times their total, w = max(p - q, 0) after a rejection (p without the rejected id
+ * if q is NULL; p if that leaves nothing), w = p behind the last draft: the sequence is then distributed as the target's.
+ * tokens int32 [n_seqs, max_draft + 1]: accepted drafts, that token, then -1; n_accept int32 [n_seqs].  Sums in 64
+ * bits.  A drafted id outside [0, vocab) is reported and rejected; a row without any positive probability is
+ * reported and gives token -1.  p and q may be any rows; negative and NaN entries weigh nothing. */
+int lazy_k_verify(void *stream, const float *p, int32_t ldp, const float *q, int32_t ldq, const int32_t *draft,
+                  const int32_t *d_cu_draft, int32_t n_seqs, int32_t n_draft, int32_t max_draft, int32_t vocab,
+                  const float *u_accept, const float *u_sample, int32_t *n_accept, int32_t *tokens);
 
 #ifdef __cplusplus
 }

@@ -120,6 +120,17 @@ _SIGNATURES = {
     "lazy_k_select_threshold": (_I, [_P, _P, _P, _I, C.c_uint32, _P, _P, _P]),
     "lazy_k_gather_rows": (_I, [_P, _P, _P, _P, _I, _I, _I]),
     "lazy_keep_count": (_I, [_I, _U, _I]),
+    "lazy_k_attention_mass_scratch_floats": (_Z, [_I] * 6),
+    "lazy_k_attention_mass": (_I, [_P, _I, _P, _I, _P, _I, _P] + [_I] * 7 + [_P, _Z, _P]),
+    "lazy_k_evict_scratch_ints": (_Z, [_I] * 3),
+    "lazy_k_evict": (_I, [_P, _I, _P, _P, _I, _P, _P, _P] + [_I] * 7 + [_P, _Z, _P, _P, _P, _P, _P, _I]),
+    "lazy_k_evict_step_scratch_floats": (_Z, [_I] * 5),
+    "lazy_k_evict_step": (_I, [_P, _I, _P, _I, _P, _P, _I, _P, _P, _P, _I] + [_P] * 6 + [_I] * 6 +
+                          [_P, _Z, _P, _P, _P]),
+    "lazy_k_attention_prefix_scratch_floats": (_Z, [_I] * 8),
+    "lazy_k_attention_prefix": (_I, [_P, _I, _P, _I, _P, _I, _I, _I, _P, _P, _I, _I, _P, _P, _I, _I, _P, _P] +
+                                [_I] * 5 + [_P, _Z, _P]),
+    "lazy_k_verify": (_I, [_P, _P, _I, _P, _I, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P]),
     "lazy_status_detail": (_I, [C.POINTER(_I), C.POINTER(_I), C.POINTER(_I)]),
     "lazy_k_wait_selftest": (_I, [_P, _I, _U]),
 }
@@ -568,3 +579,211 @@ def lazy_prune_op(x: torch.Tensor, pos: torch.Tensor, w_qkv: torch.Tensor, w_o: 
         _ptr(o["aux_hidden"]), _ptr(o["aux_pos"]), base, nbytes))
     o["n_keep"], o["n_drop"], o["workspace"] = n_keep, n_drop, workspace
     return o
+
+
+# ------------------------------------------------------------------------------- bounded and shared caches
+def _dense(t: torch.Tensor, dev: int, dtype: torch.dtype, name: str) -> int:
+    """Address of a contiguous tensor of the current device and the given type."""
+    if t.get_device() != dev or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor on the current CUDA device is wanted")
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, dev: int, dtype: torch.dtype, width: int, name: str) -> Tuple[int, int]:
+    """(address, pitch) of a matrix whose rows lie `pitch` elements apart, each of them contiguous."""
+    if t.get_device() != dev or t.dtype != dtype or t.dim() != 2 or t.shape[1] != width or \
+            (t.shape[0] > 0 and t.stride(1) != 1):
+        raise ValueError(f"{name}: {dtype} rows of {width} elements on the current CUDA device are wanted")
+    pitch = t.stride(0) if t.shape[0] > 1 else width
+    if pitch < width or pitch > 0x7fffffff:
+        raise ValueError(f"{name}: rows overlap or lie too far apart")
+    return t.data_ptr(), pitch
+
+
+def _same(a: int, b: int, what: str) -> None:
+    if a != b:
+        raise ValueError(f"{what}: {a} and {b} do not agree")
+
+
+def _scratch(n: int, dtype: torch.dtype, device="cuda") -> torch.Tensor:
+    return torch.empty(max(int(n), 1), dtype=dtype, device=device)
+
+
+def lazy_k_attention_mass_scratch(n_seqs: int, n_total: int, max_len: int, n_heads: int, n_kv_heads: int,
+                                  window: int = 0) -> torch.Tensor:
+    """Scratch for the `scratch=` argument of lazy_k_attention_mass."""
+    return _scratch(lib().lazy_k_attention_mass_scratch_floats(n_seqs, n_total, max_len, n_heads, n_kv_heads, window),
+                    torch.float32)
+
+
+def lazy_k_attention_mass(q: torch.Tensor, k: torch.Tensor, cu_seqlens: torch.Tensor, max_len: int, n_heads: int,
+                          n_kv_heads: int, head_dim: int, window: int = 0, scratch: Optional[torch.Tensor] = None,
+                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """mass fp32 [n_kv_heads, n_total]; q [n_total, n_heads * head_dim], k [n_total, n_kv_heads * head_dim], any row
+    pitch (parts of a fused projection's rows)."""
+    dev, n_total, n_seqs = torch.cuda.current_device(), q.shape[0], cu_seqlens.numel() - 1
+    n_kv_heads = n_kv_heads or n_heads
+    pq, ldq = _rows(q, dev, q.dtype, n_heads * head_dim, "q")
+    pk, ldk = _rows(k, dev, q.dtype, n_kv_heads * head_dim, "k")
+    _same(k.shape[0], n_total, "rows of q and k")
+    if out is None:
+        out = torch.empty((n_kv_heads, n_total), dtype=torch.float32, device=q.device)
+    _same(out.numel(), n_kv_heads * n_total, "size of out")
+    if scratch is None:
+        scratch = lazy_k_attention_mass_scratch(n_seqs, n_total, max_len, n_heads, n_kv_heads, window)
+    _check("lazy_k_attention_mass", lib().lazy_k_attention_mass(
+        _stream(), dtype_code(q.dtype), pq, ldq, pk, ldk, _dense(cu_seqlens, dev, torch.int32, "cu_seqlens"), n_seqs,
+        max_len, n_total, n_heads, n_kv_heads, head_dim, window, _dense(scratch, dev, torch.float32, "scratch"),
+        scratch.numel(), _dense(out, dev, torch.float32, "out")))
+    return out
+
+
+def lazy_k_evict_scratch(n_seqs: int, n_kv_heads: int, budget: int) -> torch.Tensor:
+    """Scratch for the `scratch=` argument of lazy_k_evict."""
+    return _scratch(lib().lazy_k_evict_scratch_ints(n_seqs, n_kv_heads, budget), torch.int32)
+
+
+def _cache_ptrs(dev: int, kc, vc, dtype):
+    if kc.dim() != 4 or kc.shape != vc.shape:
+        raise ValueError("kc, vc: [n_seqs, cap, n_kv_heads, head_dim] are wanted")
+    return _dense(kc, dev, dtype, "kc"), _dense(vc, dev, dtype, "vc")
+
+
+def lazy_k_evict(k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, mass: torch.Tensor, cu_seqlens: torch.Tensor,
+                 max_len: int, budget: int, n_recent: int, kc: torch.Tensor, vc: torch.Tensor, cmass: torch.Tensor,
+                 cpos: torch.Tensor, clen: torch.Tensor, scratch: Optional[torch.Tensor] = None) -> None:
+    """Fills the bounded cache (kc, vc, cmass, cpos, clen) from packed prompt rows k, v and their weights."""
+    dev, n_total, n_seqs = torch.cuda.current_device(), k.shape[0], cu_seqlens.numel() - 1
+    pkc, pvc = _cache_ptrs(dev, kc, vc, k.dtype)
+    _, cap, n_kv_heads, head_dim = kc.shape
+    pk, ldk = _rows(k, dev, k.dtype, n_kv_heads * head_dim, "k")
+    pv, ldv = _rows(v, dev, k.dtype, n_kv_heads * head_dim, "v")
+    _same(ldk, ldv, "row pitches of k and v")
+    _same(v.shape[0], n_total, "rows of k and v")
+    _same(kc.shape[0], n_seqs, "sequences")
+    _same(pos.numel(), n_total, "size of pos")
+    _same(mass.numel(), n_kv_heads * n_total, "size of mass")
+    _same(cmass.numel(), n_seqs * n_kv_heads * cap, "size of cmass")
+    _same(cpos.numel(), n_seqs * n_kv_heads * cap, "size of cpos")
+    _same(clen.numel(), n_seqs * n_kv_heads, "size of clen")
+    if scratch is None:
+        scratch = lazy_k_evict_scratch(n_seqs, n_kv_heads, budget)
+    i32, f32 = torch.int32, torch.float32
+    _check("lazy_k_evict", lib().lazy_k_evict(
+        _stream(), dtype_code(k.dtype), pk, pv, ldk, _dense(pos, dev, i32, "pos"), _dense(mass, dev, f32, "mass"),
+        _dense(cu_seqlens, dev, i32, "cu_seqlens"), n_seqs, max_len, n_total, n_kv_heads, head_dim, budget, n_recent,
+        _dense(scratch, dev, i32, "scratch"), scratch.numel(), pkc, pvc, _dense(cmass, dev, f32, "cmass"),
+        _dense(cpos, dev, i32, "cpos"), _dense(clen, dev, i32, "clen"), cap))
+
+
+def lazy_k_evict_step_scratch(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, budget: int) -> torch.Tensor:
+    """Scratch for the `scratch=` argument of lazy_k_evict_step."""
+    return _scratch(lib().lazy_k_evict_step_scratch_floats(n_seqs, n_heads, n_kv_heads, head_dim, budget),
+                    torch.float32)
+
+
+def lazy_k_evict_step(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, pos_new: torch.Tensor,
+                      kc: torch.Tensor, vc: torch.Tensor, cmass: torch.Tensor, cpos: torch.Tensor, clen: torch.Tensor,
+                      n_heads: int, budget: int, n_recent: int, mass_out: Optional[torch.Tensor] = None,
+                      pos_out: Optional[torch.Tensor] = None, len_out: Optional[torch.Tensor] = None,
+                      scratch: Optional[torch.Tensor] = None,
+                      out: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None):
+    """(o [n_seqs, n_heads * head_dim], slot, gone int32 [n_seqs, n_kv_heads]).  Without mass_out / pos_out / len_out
+    the cache's own cmass / cpos / clen are updated in place, as kc and vc always are."""
+    dev, dt = torch.cuda.current_device(), q.dtype
+    pkc, pvc = _cache_ptrs(dev, kc, vc, dt)
+    n_seqs, cap, n_kv_heads, head_dim = kc.shape
+    pq, ldq = _rows(q, dev, dt, n_heads * head_dim, "q")
+    pkn, ldn = _rows(k_new, dev, dt, n_kv_heads * head_dim, "k_new")
+    pvn, ldv = _rows(v_new, dev, dt, n_kv_heads * head_dim, "v_new")
+    _same(ldn, ldv, "row pitches of k_new and v_new")
+    mass_out = cmass if mass_out is None else mass_out
+    pos_out = cpos if pos_out is None else pos_out
+    len_out = clen if len_out is None else len_out
+    heads = n_seqs * n_kv_heads
+    if not (q.shape[0] == k_new.shape[0] == v_new.shape[0] == pos_new.numel() == n_seqs and
+            cmass.numel() == mass_out.numel() == cpos.numel() == pos_out.numel() == heads * cap and
+            clen.numel() == len_out.numel() == heads):
+        raise ValueError("q, k_new, v_new, pos_new and the cache's arrays: sizes do not agree")
+    if out is None:
+        out = (torch.empty((n_seqs, n_heads * head_dim), dtype=dt, device=q.device),
+               torch.empty((n_seqs, n_kv_heads), dtype=torch.int32, device=q.device),
+               torch.empty((n_seqs, n_kv_heads), dtype=torch.int32, device=q.device))
+    o, slot, gone = out
+    if o.numel() != n_seqs * n_heads * head_dim or slot.numel() != heads or gone.numel() != heads:
+        raise ValueError("out: sizes do not agree")
+    if scratch is None:
+        scratch = lazy_k_evict_step_scratch(n_seqs, n_heads, n_kv_heads, head_dim, budget)
+    i32, f32 = torch.int32, torch.float32
+    _check("lazy_k_evict_step", lib().lazy_k_evict_step(
+        _stream(), dtype_code(dt), pq, ldq, pkn, pvn, ldn, _dense(pos_new, dev, i32, "pos_new"), pkc, pvc, cap,
+        _dense(cmass, dev, f32, "cmass"), _dense(mass_out, dev, f32, "mass_out"), _dense(cpos, dev, i32, "cpos"),
+        _dense(pos_out, dev, i32, "pos_out"), _dense(clen, dev, i32, "clen"), _dense(len_out, dev, i32, "len_out"),
+        n_seqs, n_heads, n_kv_heads, head_dim, budget, n_recent, _dense(scratch, dev, f32, "scratch"), scratch.numel(),
+        _dense(o, dev, dt, "o"), _dense(slot, dev, i32, "slot"), _dense(gone, dev, i32, "gone")))
+    return out
+
+
+def lazy_k_attention_prefix_scratch(n_rows: int, n_seqs: int, max_q: int, n_pre: int, max_kv: int, n_heads: int,
+                                    n_kv_heads: int, head_dim: int) -> torch.Tensor:
+    """Scratch for the `scratch=` argument of lazy_k_attention_prefix."""
+    return _scratch(lib().lazy_k_attention_prefix_scratch_floats(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads,
+                                                                 n_kv_heads, head_dim), torch.float32)
+
+
+def lazy_k_attention_prefix(q: torch.Tensor, cu_q: torch.Tensor, max_q: int, k_pre: torch.Tensor,
+                            v_pre: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv_idx: torch.Tensor,
+                            cu_kv: torch.Tensor, max_kv: int, n_heads: int, n_kv_heads: int, head_dim: int,
+                            scratch: Optional[torch.Tensor] = None,
+                            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """o [n_rows, n_heads * head_dim]; k_pre, v_pre [n_pre, n_kv_heads * head_dim] shared by the batch; k, v buffers of
+    rows, of which sequence s owns kv_idx[cu_kv[s]:cu_kv[s + 1]]."""
+    dev, dt, n_rows, n_seqs = torch.cuda.current_device(), q.dtype, q.shape[0], cu_q.numel() - 1
+    n_kv_heads = n_kv_heads or n_heads
+    width = n_kv_heads * head_dim
+    pq, ldq = _rows(q, dev, dt, n_heads * head_dim, "q")
+    pkp, ldp = _rows(k_pre, dev, dt, width, "k_pre")
+    pvp, ldvp = _rows(v_pre, dev, dt, width, "v_pre")
+    pk, ldk = _rows(k, dev, dt, width, "k")
+    pv, ldv = _rows(v, dev, dt, width, "v")
+    if ldp != ldvp or ldk != ldv or k_pre.shape[0] != v_pre.shape[0] or k.shape[0] != v.shape[0]:
+        raise ValueError("keys and values: numbers of rows or pitches do not agree")
+    _same(cu_kv.numel(), n_seqs + 1, "sizes of cu_q and cu_kv")
+    if out is None:
+        out = torch.empty((n_rows, n_heads * head_dim), dtype=dt, device=q.device)
+    _same(out.numel(), n_rows * n_heads * head_dim, "size of out")
+    n_pre = k_pre.shape[0]
+    if scratch is None:
+        scratch = lazy_k_attention_prefix_scratch(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads, n_kv_heads, head_dim)
+    i32 = torch.int32
+    _check("lazy_k_attention_prefix", lib().lazy_k_attention_prefix(
+        _stream(), dtype_code(dt), pq, ldq, _dense(cu_q, dev, i32, "cu_q"), n_rows, n_seqs, max_q, pkp, pvp, ldp, n_pre,
+        pk, pv, ldk, k.shape[0], _dense(kv_idx, dev, i32, "kv_idx"), _dense(cu_kv, dev, i32, "cu_kv"), kv_idx.numel(),
+        max_kv, n_heads, n_kv_heads, head_dim, _dense(scratch, dev, torch.float32, "scratch"), scratch.numel(),
+        _dense(out, dev, dt, "out")))
+    return out
+
+
+def lazy_k_verify(p: torch.Tensor, draft: torch.Tensor, cu_draft: torch.Tensor, max_draft: int,
+                  u_accept: torch.Tensor, u_sample: torch.Tensor, q: Optional[torch.Tensor] = None,
+                  out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+    """(n_accept int32 [n_seqs], tokens int32 [n_seqs, max_draft + 1]); p [n_draft + n_seqs, vocab], q [n_draft, vocab]
+    or None for drafts chosen outright."""
+    dev, f32, i32 = torch.cuda.current_device(), torch.float32, torch.int32
+    n_seqs, n_draft, vocab = cu_draft.numel() - 1, draft.numel(), p.shape[-1]
+    pp, ldp = _rows(p, dev, f32, vocab, "p")
+    pq, ldq = (None, 0) if q is None or n_draft == 0 else _rows(q, dev, f32, vocab, "q")
+    if p.shape[0] != n_draft + n_seqs or u_accept.numel() != n_draft or u_sample.numel() != n_seqs or \
+            (q is not None and q.shape[0] != n_draft):
+        raise ValueError("p, q, draft, u_accept, u_sample: sizes do not agree")
+    if out is None:
+        out = (torch.empty(n_seqs, dtype=i32, device=p.device),
+               torch.empty((n_seqs, max_draft + 1), dtype=i32, device=p.device))
+    n_accept, tokens = out
+    if n_accept.numel() != n_seqs or tokens.numel() != n_seqs * (max_draft + 1):
+        raise ValueError("out: sizes do not agree")
+    _check("lazy_k_verify", lib().lazy_k_verify(
+        _stream(), pp, ldp, pq, ldq, _dense(draft, dev, i32, "draft"), _dense(cu_draft, dev, i32, "cu_draft"), n_seqs,
+        n_draft, max_draft, vocab, _dense(u_accept, dev, f32, "u_accept"), _dense(u_sample, dev, f32, "u_sample"),
+        _dense(n_accept, dev, i32, "n_accept"), _dense(tokens, dev, i32, "tokens")))
+    return out

@@ -1,0 +1,102 @@
+// Pieces shared by the operators on bounded and shared caches: checks of device-side length tables, the
+// order of accumulated weights, per-device kernel attributes, launch shapes with clusters.
+#pragma once
+#include <atomic>
+
+#include "common.cuh"
+
+namespace lazy {
+
+constexpr float CO_LOG2E = 1.4426950408889634f;
+
+// Rows [start, start + n) of sequence s in a table of cumulative lengths.  A table that is not ascending, leaves
+// [0, n_total] or holds a sequence longer than max_len is reported; the caller then skips the sequence.
+__device__ __forceinline__ bool co_span(const int32_t *cu, int s, int n_total, int max_len, DevStatus *status,
+                                        int where, int &start, int &n) {
+  const int a = cu[s], b = cu[s + 1];
+  start = a;
+  n = b - a;
+  const bool ok = a >= 0 && b >= a && b <= n_total && b - a <= max_len;
+  if (!ok && threadIdx.x == 0) dev_fail(status, LAZY_E_BADARG, where, s, b);
+  return ok;
+}
+
+// Unsigned key whose order is that of the weights: -0 counts as 0, NaN as less than everything.
+__device__ __forceinline__ uint32_t co_weight_key(float w) {
+  if (w != w) return 0u;
+  const uint32_t u = __float_as_uint(w + 0.f);  // -0 + 0 = +0
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// Opts a kernel in to `bytes` of dynamic shared memory, once per device (the attribute belongs to the device's
+// context).  More than 64 devices simply set it again each time.
+template <auto Kernel>
+inline int co_allow_smem(int bytes) {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  LAZY_CUDA_OK(cudaGetDevice(&dev));
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+  if (done.load(std::memory_order_acquire) & bit) return LAZY_OK;
+  LAZY_CUDA_OK(cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  done.fetch_or(bit, std::memory_order_release);
+  return LAZY_OK;
+}
+
+// Launch with a cluster of `cluster` CTAs along x and, on request, as a programmatic dependent.
+template <typename... KArgs, typename... Args>
+inline int co_launch(void (*kfn)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, int cluster, bool pdl,
+                     Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (cluster > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = cluster;
+    attr[n].val.clusterDim.y = 1;
+    attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (pdl) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kfn, static_cast<KArgs>(args)...);
+  LAZY_COUNT_LAUNCH();
+  return e == cudaSuccess ? LAZY_OK : LAZY_E_CUDA;
+}
+
+__device__ __forceinline__ uint32_t co_cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t co_cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+// All threads of all CTAs of the cluster; shared-memory writes before it are visible cluster-wide after it.
+__device__ __forceinline__ void co_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// Address of `p` (this CTA's shared memory) in CTA `rank` of the cluster.
+template <typename T>
+__device__ __forceinline__ T *co_map_shared(T *p, uint32_t rank) {
+  uint64_t out;
+  asm volatile("mapa.u64 %0, %1, %2;" : "=l"(out) : "l"((uint64_t)p), "r"(rank));
+  return reinterpret_cast<T *>(out);
+}
+
+// Pitch and base of rows that are read in 16-byte pieces.
+inline bool co_rows_ok(const void *p, long long ld, int dtype) {
+  return !((uintptr_t)p & 15) && ld % (dtype == LAZY_F32 ? 4 : 8) == 0;
+}
+
+}  // namespace lazy

@@ -34,6 +34,10 @@ enum DevWhere {
   W_ATTN_SOFTMAX = 13,
   W_GEMM_TAIL = 14,
   W_WAIT_SELFTEST = 15,
+  W_EVICT = 16,
+  W_PREFIX = 17,
+  W_VERIFY = 18,
+  W_MASS = 19,
 };
 
 __device__ __forceinline__ void dev_fail(DevStatus *st, int code, int where, int a = 0, int b = 0) {
@@ -317,6 +321,58 @@ int launch_gather_rows(cudaStream_t st, const void *src, const int32_t *idx, voi
 int launch_gather_i32(cudaStream_t st, const int32_t *src, const int32_t *idx, int32_t *dst, int n);
 int launch_lm_head(cudaStream_t st, int dtype, const void *h, const void *w, float *logits,
                    int n_rows, int d, int vocab, bool w_const = false);
+// ---- bounded and shared caches (evict.cu, evict_step.cu, attention_mass.cu, attention_prefix.cu, verify.cu) ----
+// Accumulated attention weight of prompts; scratch: attention_mass_scratch_floats().
+size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window);
+int launch_attention_mass(cudaStream_t st, int dtype, const void *q, int ldq, const void *k, int ldkv,
+                          const int32_t *cu, int n_seqs, int max_len, int n_total, int n_heads, int n_kv_heads,
+                          int head_dim, int window, float *scratch, float *mass, DevStatus *status);
+// Compaction of prompts' K / V rows to the heaviest and newest; idx: evict_scratch_ints().
+size_t evict_scratch_ints(int n_seqs, int n_kv_heads, int budget);
+int launch_evict(cudaStream_t st, int dtype, const void *k, const void *v, int ldkv, const int32_t *pos,
+                 const float *mass, const int32_t *cu, int n_seqs, int max_len, int n_total, int n_kv_heads,
+                 int head_dim, int budget, int n_recent, int32_t *idx, void *kc, void *vc, float *cmass, int32_t *cpos,
+                 int32_t *clen, int cap, DevStatus *status);
+// One token per sequence on such a cache.
+struct EvictStepArgs {
+  const void *q, *k_new, *v_new;
+  int ldq, ld_new;
+  const int32_t *pos_new;
+  void *kc, *vc;
+  int cap;
+  const float *mass_in;
+  float *mass_out;
+  const int32_t *pos_in;
+  int32_t *pos_out;
+  const int32_t *len_in;
+  int32_t *len_out;
+  int n_seqs, n_heads, n_kv_heads, head_dim, budget, n_recent;
+  void *o;
+  int32_t *slot, *gone;
+};
+size_t evict_step_scratch_floats(int n_seqs, int n_heads, int n_kv_heads, int head_dim, int budget);
+int launch_evict_step(cudaStream_t st, int dtype, const EvictStepArgs &a, float *scratch, DevStatus *status);
+// Rows of a batch over one shared prefix and each sequence's own key list.
+struct PrefixArgs {
+  const void *q;
+  int ldq;
+  const int32_t *cu_q;
+  int n_rows, n_seqs, max_q;
+  const void *k_pre, *v_pre;
+  int ld_pre, n_pre;
+  const void *k, *v;
+  int ldkv, kv_rows;
+  const int32_t *kv_idx, *cu_kv;
+  int n_kv, max_kv;
+  int n_heads, n_kv_heads, head_dim;
+  void *o;
+};
+size_t attention_prefix_scratch_floats(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv, int n_heads,
+                                       int n_kv_heads, int head_dim);
+int launch_attention_prefix(cudaStream_t st, int dtype, const PrefixArgs &a, float *scratch, DevStatus *status);
+int launch_verify(cudaStream_t st, const float *p, int ldp, const float *q, int ldq, const int32_t *draft,
+                  const int32_t *cu_draft, int n_seqs, int n_draft, int max_draft, int vocab, const float *u_accept,
+                  const float *u_sample, int32_t *n_accept, int32_t *tokens, DevStatus *status);
 int launch_argmax(cudaStream_t st, const float *logits, int32_t *out, int n_rows, int vocab);
 int launch_fill_i32(cudaStream_t st, int32_t *p, int32_t v, size_t n);
 int launch_iota_pos(cudaStream_t st, int32_t *pos, const int32_t *cu, int n_seqs, int n_total);
