@@ -6,6 +6,7 @@
 //
 // A "lane" is one (row, head of the group) pair; lanes of a key/value head are numbered row-major, f = row * group +
 // head.  lse[g][f] (log2 units) of all rows of the batch is the scratch between the passes.
+#include "attn_common.cuh"
 #include "cache_ops.cuh"
 
 namespace lazy {
@@ -148,17 +149,337 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
   return launch_ok();
 }
 
+
+// ---- tensor-core form: bf16, head width 64 or 128 -----------------------------------------------------------------
+// One CTA holds 128 rows of one side (pass 1: lanes, pass 2: keys) in shared memory as the M side of the product and
+// streams 128-row tiles of the other side past them; a logit tile S (128 x 128, fp32) lands in TMEM and is consumed from
+// there, so every row's reduction stays inside one thread: pass 1 keeps a lane's running maximum and sum, pass 2 a
+// key's running sum.  Warp roles:
+//   warp 0     TMA: the stationary tile once, the streamed tiles through a two-stage ring (and, in pass 2, their
+//              lanes' log-sum-exps through a four-stage ring);
+//   warp 1     owns TMEM and issues S_j = A B_j^T (M128 N128 K16) from one lane into two buffers of 128 columns;
+//   warps 2-9  two threads per TMEM lane, 64 columns each: tcgen05.ld, then one exponential per logit.
+// Two CTAs share an SM.  The bound is the special-function unit: one exponential per (row, key, head) and pass is 1024 clocks
+// per tile against 512 of the tensor cores (head width 128).
+// Lane tiles hold R = 128 / group rows x group heads, loaded as one 3-d box; with a group that does not divide 128
+// the last lanes of a tile are unused.  A short grid is filled up by clusters: the CTAs of a cluster share a
+// stationary tile, split the streamed tiles and add their parts in rank order through distributed shared memory.
+constexpr int MT = 128;                       // tile rows of either side, columns of S
+constexpr int MT_STAGES = 2, MT_LSE_STAGES = 4, MT_MAX_CLUSTER = 8;
+constexpr int MT_THREADS = 320;
+constexpr int MT_TMEM_COLS = 256;
+
+struct __align__(16) MassShared {
+  float lse[MT_LSE_STAGES][MT];
+  float part_m[2][MT], part_l[2][MT];  // per column half: a lane's (maximum, sum), a key's sum
+  unsigned long long a_full, b_full[MT_STAGES], b_empty[MT_STAGES], s_full[2], s_free[2], l_full[MT_LSE_STAGES],
+      l_free[MT_LSE_STAGES];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+template <int HD>
+constexpr int mass_smem_bytes() {
+  return (1 + MT_STAGES) * MT * HD * 2 + 1024 + (int)sizeof(MassShared);
+}
+
+// grid (n_kv_heads * cluster, tiles, n_seqs).  lse: tiles of 128 floats, tile t of sequence s of key/value head g at
+// ((g * seq_tiles) + start_s / R + s + t) * 128: sequences' tiles cannot overlap and every tile is 512-byte aligned.
+template <int PASS, int HD>
+__global__ void __launch_bounds__(MT_THREADS, 2)
+mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+               const int32_t *__restrict__ cu, int max_len, int n_total, int group, int rows_per_tile, int window,
+               float *lse, int seq_tiles, float *__restrict__ mass, DevStatus *status) {
+  extern __shared__ uint8_t mass_smem_raw[];
+  constexpr int CH = HD / 64;                // 64-column chunks of the head
+  constexpr int CHUNK = MT * 128;            // bytes of one chunk of a tile
+  const uint32_t raw_addr = smem_u32(mass_smem_raw);
+  uint8_t *smem = mass_smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
+  const uint32_t sA = smem_u32(smem), sB = sA + CH * CHUNK;
+  MassShared *sh = reinterpret_cast<MassShared *>(smem + (1 + MT_STAGES) * CH * CHUNK);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)co_cluster_rank(), csize = (int)co_cluster_size();
+  const int g = blockIdx.x / csize, s = blockIdx.z, R = rows_per_tile;
+  if (PASS == 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  int start, n;
+  if (!co_span(cu, s, n_total, max_len, status, W_MASS, start, n)) return;  // the whole cluster alike
+  const int first = window > 0 ? max(n - window, 0) : 0;
+  const int lane_tiles = (n - first + R - 1) / R, key_tiles = (n + MT - 1) / MT;
+  const int a_tiles = PASS == 1 ? lane_tiles : key_tiles;
+  if ((int)blockIdx.y >= a_tiles) return;
+  const int at = PASS == 1 ? a_tiles - 1 - (int)blockIdx.y : (int)blockIdx.y;  // most work first
+  // streamed tiles [b0, b1) of this CTA
+  const int all0 = PASS == 1 ? 0 : max(at * MT - first, 0) / R;
+  const int all1 = PASS == 1 ? min(key_tiles, (min(first + (at + 1) * R, n) + MT - 1) / MT) : lane_tiles;
+  const int per = (all1 - all0 + csize - 1) / csize;
+  const int b0 = min(all0 + rank * per, all1), b1 = min(b0 + per, all1), nb = b1 - b0;
+  const size_t lse_base = ((size_t)g * seq_tiles + start / R + s) * MT;
+
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&sh->a_full), 1);
+    for (int i = 0; i < MT_STAGES; ++i) {
+      mbar_init(smem_u32(&sh->b_full[i]), 1);
+      mbar_init(smem_u32(&sh->b_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sh->s_full[i]), 1);
+      mbar_init(smem_u32(&sh->s_free[i]), 8);
+    }
+    for (int i = 0; i < MT_LSE_STAGES; ++i) {
+      mbar_init(smem_u32(&sh->l_full[i]), 1);
+      mbar_init(smem_u32(&sh->l_free[i]), 8);
+    }
+    sh->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tma_prefetch_desc(&map_q);
+    tma_prefetch_desc(&map_k);
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
+                 "r"((uint32_t)MT_TMEM_COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(&sh->tmem_base);
+  volatile int *abort_flag = &sh->abort_flag;
+
+  if (warp == 0) {
+    if (lane == 0 && nb > 0) {
+      const uint32_t lane_bytes = (uint32_t)(R * group * 128 * CH), key_bytes = (uint32_t)(CH * CHUNK);
+      auto load = [&](bool lanes, int tile, uint32_t dst, uint32_t bar) {
+        mbar_expect_tx(bar, lanes ? lane_bytes : key_bytes);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          if (lanes) tma_load_3d(dst + c * CHUNK, &map_q, bar, c * 64, g * group, start + first + tile * R);
+          else tma_load_2d(dst + c * CHUNK, &map_k, bar, g * HD + c * 64, start + tile * MT);
+        }
+      };
+      load(PASS == 1, at, sA, smem_u32(&sh->a_full));
+      if (PASS == 2) asm volatile("griddepcontrol.wait;" ::: "memory");  // the log-sum-exps of pass 1
+      for (int j = 0; j < nb; ++j) {
+        const int st = j % MT_STAGES;
+        if (!mbar_wait(smem_u32(&sh->b_empty[st]), (uint32_t)((j / MT_STAGES) & 1) ^ 1u, abort_flag, status, W_MASS)) break;
+        load(PASS == 2, b0 + j, sB + st * CH * CHUNK, smem_u32(&sh->b_full[st]));
+        if (PASS == 2) {
+          const int ls = j % MT_LSE_STAGES;
+          if (!mbar_wait(smem_u32(&sh->l_free[ls]), (uint32_t)((j / MT_LSE_STAGES) & 1) ^ 1u, abort_flag, status, W_MASS))
+            break;
+          mbar_expect_tx(smem_u32(&sh->l_full[ls]), MT * 4);
+          bulk_load(smem_u32(sh->lse[ls]), lse + lse_base + (size_t)(b0 + j) * MT, MT * 4, smem_u32(&sh->l_full[ls]));
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && nb > 0) {
+      const uint32_t idesc = idesc_bf16(MT, MT, 0, 0);
+      bool ok = mbar_wait(smem_u32(&sh->a_full), 0, abort_flag, status, W_MASS);
+      for (int j = 0; j < nb && ok; ++j) {
+        const int st = j % MT_STAGES, sb = j & 1;
+        ok = mbar_wait(smem_u32(&sh->b_full[st]), (uint32_t)((j / MT_STAGES) & 1), abort_flag, status, W_MASS);
+        if (!ok) break;
+        ok = mbar_wait(smem_u32(&sh->s_free[sb]), (uint32_t)((j >> 1) & 1) ^ 1u, abort_flag, status, W_MASS);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint64_t ad = umma_smem_desc(sA + (k >> 2) * CHUNK + (k & 3) * 32);
+          const uint64_t bd = umma_smem_desc(sB + st * CH * CHUNK + (k >> 2) * CHUNK + (k & 3) * 32);
+          umma_bf16(tmem_base + (uint32_t)(sb * MT), ad, bd, idesc, k != 0 ? 1u : 0u);
+        }
+        umma_commit(smem_u32(&sh->b_empty[st]));
+        umma_commit(smem_u32(&sh->s_full[sb]));
+      }
+    }
+  } else {
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t t_s = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 64);
+    const int row = quarter * 32 + lane;  // row of the stationary tile
+    const float sl2 = rsqrtf((float)HD) * CO_LOG2E;
+    const unsigned long long sl2x2 = f32x2_pack(sl2, sl2);
+    // pass 1: this lane's row inside the sequence, -1 for a lane that does not exist (it sees no key)
+    int own = PASS == 1 ? first + at * R + row / group : at * MT + row;
+    if (PASS == 1 && (row >= R * group || own >= n)) own = -1;
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int j = 0; j < nb && ok; ++j) {
+      const int sb = j & 1;
+      ok = mbar_wait(smem_u32(&sh->s_full[sb]), (uint32_t)((j >> 1) & 1), abort_flag, status, W_MASS);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t raw[64];
+      tmem_ld_32x32_raw(t_s + (uint32_t)(sb * MT), raw);
+      tmem_ld_32x32_raw(t_s + (uint32_t)(sb * MT) + 32u, raw + 32);
+      tmem_ld_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh->s_free[sb]));
+      // columns [lo, hi) of this thread's 64 are seen
+      int lo = 0, hi = 64;
+      if (PASS == 1) hi = own + 1 - ((b0 + j) * MT + half * 64);
+      else {
+        const int row0 = first + (b0 + j) * R;  // first row of the streamed tile
+        lo = (own - row0) * group - half * 64;
+        hi = min(R, n - row0) * group - half * 64;
+      }
+      if (PASS == 1) {
+        if (hi < 64) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c >= hi) raw[c] = 0xff800000u;  // -inf
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < 64; c += 8) {
+          mx[0] = fmax3(mx[0], __uint_as_float(raw[c]), __uint_as_float(raw[c + 1]));
+          mx[1] = fmax3(mx[1], __uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3]));
+          mx[2] = fmax3(mx[2], __uint_as_float(raw[c + 4]), __uint_as_float(raw[c + 5]));
+          mx[3] = fmax3(mx[3], __uint_as_float(raw[c + 6]), __uint_as_float(raw[c + 7]));
+        }
+        const float mt = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2);
+        const float ref = mt == -INFINITY ? 0.f : mt;
+        const unsigned long long neg = f32x2_pack(-ref, -ref);
+        unsigned long long sum0 = 0ull, sum1 = 0ull;
+#pragma unroll
+        for (int c = 0; c < 64; c += 4) {
+          float x0, x1, x2, x3;
+          f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2, neg), x0, x1);
+          f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])), sl2x2, neg), x2, x3);
+          sum0 = f32x2_add(sum0, f32x2_pack(ex2_approx(x0), ex2_approx(x1)));
+          sum1 = f32x2_add(sum1, f32x2_pack(ex2_approx(x2), ex2_approx(x3)));
+        }
+        float u0, u1;
+        f32x2_unpack(f32x2_add(sum0, sum1), u0, u1);
+        l = l * ex2_approx(m - ref) + (u0 + u1);
+        m = mt;
+      } else {
+        const int ls = j % MT_LSE_STAGES;
+        ok = mbar_wait(smem_u32(&sh->l_full[ls]), (uint32_t)((j / MT_LSE_STAGES) & 1), abort_flag, status, W_MASS);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const float4 *le = reinterpret_cast<const float4 *>(sh->lse[ls] + half * 64);
+        if (lo <= 0 && hi >= 64) {
+          unsigned long long sum0 = 0ull, sum1 = 0ull;
+#pragma unroll
+          for (int c = 0; c < 64; c += 4) {
+            const float4 e = le[c >> 2];  // minus the log-sum-exp
+            float x0, x1, x2, x3;
+            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2,
+                                   f32x2_pack(e.x, e.y)), x0, x1);
+            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])), sl2x2,
+                                   f32x2_pack(e.z, e.w)), x2, x3);
+            sum0 = f32x2_add(sum0, f32x2_pack(ex2_approx(x0), ex2_approx(x1)));
+            sum1 = f32x2_add(sum1, f32x2_pack(ex2_approx(x2), ex2_approx(x3)));
+          }
+          float u0, u1;
+          f32x2_unpack(f32x2_add(sum0, sum1), u0, u1);
+          l += u0 + u1;
+        } else {  // a tile on the diagonal or at the end: unseen columns are left out, whatever they hold
+          float sum = 0.f;
+#pragma unroll
+          for (int c = 0; c < 64; ++c) {
+            const float x = fmaf(__uint_as_float(raw[c]), sl2, sh->lse[ls][half * 64 + c]);
+            sum += c >= lo && c < hi ? ex2_approx(x) : 0.f;
+          }
+          l += sum;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh->l_free[ls]));
+      }
+    }
+    if (!ok) l = NAN;  // a wait ran out (reported): nothing that looks like a result
+    sh->part_m[half][row] = m;
+    sh->part_l[half][row] = l;
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)MT_TMEM_COLS)
+                 : "memory");
+  }
+  if (csize > 1) co_cluster_sync();
+  if (rank == 0 && threadIdx.x < MT) {
+    const int row = threadIdx.x;
+    float m = -INFINITY, l = 0.f;
+    for (int r = 0; r < csize; ++r)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float lr = *co_map_shared(&sh->part_l[h][row], r);
+        if (PASS == 1) {
+          const float mr = *co_map_shared(&sh->part_m[h][row], r);
+          const float mt = fmaxf(m, mr), ref = mt == -INFINITY ? 0.f : mt;
+          l = l * ex2_approx(m - ref) + lr * ex2_approx(mr - ref);
+          m = mt;
+        } else {
+          l += lr;
+        }
+      }
+    if (PASS == 1) lse[lse_base + (size_t)at * MT + row] = -(m + log2f(l));  // lanes that do not exist: never looked at
+    else if (at * MT + row < n) mass[(size_t)g * n_total + start + at * MT + row] = l;
+  }
+  if (csize > 1) co_cluster_sync();  // nobody leaves while its parts are being read
+}
+
+bool mass_tc_eligible(int dtype, int head_dim, int group) {
+  return dtype == LAZY_BF16 && (head_dim == 64 || head_dim == 128) && group <= MT;
+}
+int mass_seq_tiles(int n_seqs, int n_total, int group) { return n_total / (MT / group) + n_seqs + 1; }
+
+// CTAs per stationary tile: the next power of two that still finds room for every CTA at once (two per SM), while each
+// keeps at least two streamed tiles.
+int mass_cluster(long long tiles, int streamed) {
+  int c = 1;
+  while (c < MT_MAX_CLUSTER && tiles * c * 2 <= 2LL * sm_count() && streamed >= 4 * c) c *= 2;
+  return c;
+}
+
+template <int HD>
+int mass_tc(cudaStream_t st, const void *q, int ldq, const void *k, int ldkv, const int32_t *cu, int n_seqs, int max_len,
+            int n_total, int n_heads, int n_kv_heads, int window, float *lse, float *mass, DevStatus *status) {
+  const int group = n_heads / n_kv_heads, R = MT / group;
+  CUtensorMap mq, mk;
+  LAZY_TRY(tma_map_heads_bf16(&mq, q, n_total, n_heads, HD, ldq, group, R));
+  LAZY_TRY(tma_map_2d_bf16(&mk, k, n_total, n_kv_heads * HD, ldkv, 64, MT));
+  LAZY_TRY((co_allow_smem<mass_tc_kernel<1, HD>>(mass_smem_bytes<HD>())));
+  LAZY_TRY((co_allow_smem<mass_tc_kernel<2, HD>>(mass_smem_bytes<HD>())));
+  const int rows = window > 0 && window < max_len ? window : max_len;
+  const int lane_tiles = cdiv(rows, R), key_tiles = cdiv(max_len, MT), seq_tiles = mass_seq_tiles(n_seqs, n_total, group);
+  if (lane_tiles > 65535 || key_tiles > 65535) return LAZY_E_CAPACITY;
+  const long long per_tile = (long long)n_kv_heads * n_seqs;
+  const int c1 = mass_cluster(lane_tiles * per_tile, key_tiles), c2 = mass_cluster(key_tiles * per_tile, lane_tiles);
+  LAZY_TRY(co_launch(mass_tc_kernel<1, HD>, dim3(n_kv_heads * c1, lane_tiles, n_seqs), dim3(MT_THREADS),
+                     mass_smem_bytes<HD>(), st, c1, false, mq, mk, cu, max_len, n_total, group, R, window, lse, seq_tiles,
+                     mass, status));
+  return co_launch(mass_tc_kernel<2, HD>, dim3(n_kv_heads * c2, key_tiles, n_seqs), dim3(MT_THREADS),
+                   mass_smem_bytes<HD>(), st, c2, true, mq, mk, cu, max_len, n_total, group, R, window, lse, seq_tiles,
+                   mass, status);
+}
+
 }  // namespace
 
 size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window) {
-  (void)n_seqs, (void)max_len, (void)n_kv_heads, (void)window;
-  return (size_t)n_total * n_heads;
+  (void)max_len, (void)window;
+  const int group = n_heads / n_kv_heads;
+  const size_t general = (size_t)n_total * n_heads;
+  if (group > MT) return general;
+  const size_t tiled = (size_t)n_kv_heads * mass_seq_tiles(n_seqs, n_total, group) * MT;
+  return (general > tiled ? general : tiled) + 4;  // + 4: tiles start on a 16-byte boundary
 }
 
 int launch_attention_mass(cudaStream_t st, int dtype, const void *q, int ldq, const void *k, int ldkv,
                           const int32_t *cu, int n_seqs, int max_len, int n_total, int n_heads, int n_kv_heads,
                           int head_dim, int window, float *scratch, float *mass, DevStatus *status) {
   if (n_seqs == 0 || max_len == 0) return LAZY_OK;
+  if (mass_tc_eligible(dtype, head_dim, n_heads / n_kv_heads)) {
+    float *lse = reinterpret_cast<float *>(align_up((uintptr_t)scratch, 16));
+    return head_dim == 64 ? mass_tc<64>(st, q, ldq, k, ldkv, cu, n_seqs, max_len, n_total, n_heads, n_kv_heads, window, lse,
+                                        mass, status)
+                          : mass_tc<128>(st, q, ldq, k, ldkv, cu, n_seqs, max_len, n_total, n_heads, n_kv_heads, window,
+                                         lse, mass, status);
+  }
   if (dtype == LAZY_F32)
     return mass_general<float>(st, (const float *)q, ldq, (const float *)k, ldkv, cu, n_seqs, max_len, n_total, n_heads,
                                n_kv_heads, head_dim, window, scratch, mass, status);

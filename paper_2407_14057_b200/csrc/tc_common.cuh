@@ -66,6 +66,19 @@ __device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const CUtensorMap
       ::"r"(smem_dst), "l"(map), "r"(bar), "r"(x), "r"(y)
       : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const CUtensorMap *map, uint32_t bar, int x, int y,
+                                            int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(smem_dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+// Untiled copy global -> shared; both addresses and the size multiples of 16 bytes.
+__device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void *src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
 // Tile store shared -> global (bulk async-group completion): the box of `map` at (x, y) is written from
 // shared memory; parts of the box outside the tensor are dropped.  x * element size must be a multiple of 16.
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t smem_src, int x, int y) {
@@ -252,6 +265,23 @@ inline int tma_map_2d(CUtensorMap *map, const void *base, long long rows, int co
 inline int tma_map_2d_bf16(CUtensorMap *map, const void *base, long long rows, int cols, long long ld,
                            int box_cols, int box_rows) {
   return tma_map_2d(map, base, rows, cols, ld, box_cols, box_rows, 2);
+}
+
+// Rows of heads side by side as a 3-d bf16 tensor [rows][heads][head_dim] (row pitch `ld` elements): box = 64 columns x
+// box_heads x box_rows with 128-byte swizzle, so that consecutive (row, head) pairs become consecutive 128-byte
+// rows of a K-major operand tile; out-of-range reads give 0.
+inline int tma_map_heads_bf16(CUtensorMap *map, const void *base, long long rows, int heads, int head_dim, long long ld,
+                              int box_heads, int box_rows) {
+  EncodeTiledFn fn = tma_encode_fn();
+  if (!fn) return LAZY_E_CUDA;
+  cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)rows};
+  cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)ld * 2};
+  cuuint32_t box[3] = {64u, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? LAZY_OK : LAZY_E_CUDA;
 }
 
 }  // namespace lazy
