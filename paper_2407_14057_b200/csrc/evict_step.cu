@@ -6,6 +6,7 @@
 // The choice depends on the weights before the step alone, so it needs no attention result, and the caches are
 // read once.  bytes: K and V rows of the held slots (the bound), 16 bytes of weight and position per slot.
 #include "attn_split.cuh"
+#include "rows_mma.cuh"
 
 namespace lazy {
 
@@ -158,14 +159,262 @@ int step_general(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevSta
   return launch_ok();
 }
 
+
+// ---- one launch: bf16, head width 64 or 128, up to 16 query heads per key/value head ------------------------------
+// A cluster of CTAs holds one (sequence, key/value head), each CTA a contiguous part of the slots, each warp every
+// fourth group of 16 of them.  The first groups' rows are requested before anything else, the choice of the slot
+// (a minimum over the part's weights, then over the cluster) runs underneath; the new token's row replaces the chosen slot's in
+// shared memory when its group comes up.  The parts' maxima, sums and outputs meet in distributed shared memory, and
+// every CTA adds the final weights of its own slots to their masses from the logits it kept (in shared memory, or in
+// the scratch when a part is too long).
+constexpr int SF_WARPS = 4, SF_THREADS = SF_WARPS * 32, SF_STAGES = 3, SF_MAX_CLUSTER = 8;
+constexpr int SF_LOGIT_BYTES = 8192;  // of a part's logits in shared memory; two CTAs fit on an SM with it
+
+template <int HD, int NT>
+struct StepShared {
+  float m[NT * 8], l[NT * 8];       // this CTA's maxima and sums, read by the cluster
+  float o[NT * 8][HD];              // its unnormalised outputs against those maxima
+  float wm[SF_WARPS][NT * 8], wl[SF_WARPS][NT * 8];
+  float fm[NT * 8], finv[NT * 8];   // final
+  unsigned long long best;
+  unsigned long long wbest[SF_WARPS];
+};
+template <int HD, int NT>
+constexpr int step_stage_bytes = SF_WARPS * SF_STAGES * RowsMma<HD, NT>::STAGE;
+
+template <int HD, int NT>
+__global__ void __launch_bounds__(SF_THREADS)
+step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_in_smem, float *__restrict__ scratch,
+                  DevStatus *status) {
+  using Rows = RowsMma<HD, NT>;
+  extern __shared__ __align__(128) uint8_t step_smem[];
+  __shared__ StepShared<HD, NT> sh;
+  const int rank = (int)co_cluster_rank(), csize = (int)co_cluster_size();
+  const int sg = blockIdx.x / csize, s = sg / a.n_kv_heads, g = sg - s * a.n_kv_heads;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int len = a.len_in[sg];
+  bf16 *o = (bf16 *)a.o + ((size_t)s * a.n_heads + (size_t)g * group) * HD;
+  if (len < 0 || len > a.budget) {  // the whole cluster alike
+    if (rank == 0) {
+      for (int i = threadIdx.x; i < group * HD; i += SF_THREADS) o[i] = __float2bfloat16_rn(0.f);
+      if (threadIdx.x == 0) {
+        dev_fail(status, LAZY_E_CAPACITY, W_EVICT, sg, len);
+        a.slot[sg] = a.gone[sg] = -1;
+      }
+    }
+    return;
+  }
+  const bool full = len >= a.budget;
+  const int n = full ? len : len + 1;
+  const int lo = min(rank * part_slots, n), hi = min(lo + part_slots, n);  // this CTA's slots
+  const int groups = (hi - lo + RM_KEYS - 1) / RM_KEYS;
+  const size_t ld = (size_t)a.n_kv_heads * HD;
+  bf16 *kc = (bf16 *)a.kc + (size_t)s * a.cap * ld + (size_t)g * HD, *vc = (bf16 *)a.vc + (size_t)s * a.cap * ld + (size_t)g * HD;
+  const uint32_t stages = smem_u32(step_smem) + warp * SF_STAGES * Rows::STAGE;
+  Rows rows;
+  auto request = [&](int i) {  // group warp + 4 i of this CTA
+    const int j0 = lo + (warp + i * SF_WARPS) * RM_KEYS;
+    if (j0 < hi)
+      rows.load(stages + (i % SF_STAGES) * Rows::STAGE, [&](int r, const bf16 *&kr, const bf16 *&vr) {
+        const int j = min(j0 + r, max(len - 1, 0));
+        kr = kc + j * ld;
+        vr = vc + j * ld;
+        return j0 + r < len;  // the slot being appended holds nothing yet
+      });
+    rm_cp_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < SF_STAGES - 1; ++i) request(i);
+  rows.init([&](int c) -> const bf16 * {
+    return c < group ? (const bf16 *)a.q + (size_t)s * a.ldq + (size_t)(g * group + c) * HD : nullptr;
+  });
+  // ---- the slot
+  const float *mi = a.mass_in + (size_t)sg * a.cap;
+  const int32_t *pi = a.pos_in + (size_t)sg * a.cap;
+  float *mo = a.mass_out + (size_t)sg * a.cap;
+  int32_t *po = a.pos_out + (size_t)sg * a.cap;
+  const int p_new = a.pos_new[s];
+  int slot = len;
+  if (full || po != pi) {
+    const long long first_recent = (long long)p_new - a.n_recent;
+    unsigned long long best = ~0ull;
+    for (int j = lo + threadIdx.x; j < min(hi, len); j += SF_THREADS) {
+      const int p = pi[j];
+      if (full) best = min_u64(best, step_rank(mi[j], p, first_recent, j));
+      if (po != pi) po[j] = p;
+    }
+    if (full) {
+#pragma unroll
+      for (int k = 16; k > 0; k >>= 1) best = min_u64(best, __shfl_xor_sync(0xffffffffu, best, k));
+      if (lane == 0) sh.wbest[warp] = best;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        for (int w = 1; w < SF_WARPS; ++w) best = min_u64(best, sh.wbest[w]);
+        sh.best = best;
+      }
+      co_cluster_sync();
+      best = ~0ull;
+      for (int r = 0; r < csize; ++r) best = min_u64(best, *co_map_shared(&sh.best, r));
+      slot = (int)(uint32_t)best;
+    } else {
+      __syncthreads();
+    }
+  }
+  if (threadIdx.x == 0 && slot >= lo && slot < hi) {  // every thread of the CTA has read the old position
+    a.slot[sg] = slot;
+    a.gone[sg] = full ? pi[slot] : -1;
+    po[slot] = p_new;
+  }
+  // ---- attention over this CTA's slots; logits [slot][columns of the group, an even number]
+  const int lcols = (group + 1) & ~1;
+  float *lg = logits_in_smem ? reinterpret_cast<float *>(step_smem + step_stage_bytes<HD, NT>)
+                             : scratch + ((size_t)sg * csize + rank) * part_slots * lcols;
+  for (int i = 0; warp + i * SF_WARPS < groups; ++i) {
+    request(i + SF_STAGES - 1);
+    rm_cp_wait<SF_STAGES - 1>();
+    __syncwarp();
+    const uint32_t stage = stages + (i % SF_STAGES) * Rows::STAGE;
+    const int j0 = lo + (warp + i * SF_WARPS) * RM_KEYS;
+    if (slot >= j0 && slot < j0 + RM_KEYS) {  // the new row: into the stage and the cache
+      if ((lane & 15) < Rows::CHUNKS) {
+        const int c = lane & 15, r = slot - j0;
+        const bool is_v = lane >= 16;
+        const bf16 *src = (const bf16 *)(is_v ? a.v_new : a.k_new) + (size_t)s * a.ld_new + (size_t)g * HD + c * 8;
+        const uint4 x = *reinterpret_cast<const uint4 *>(src);
+        const uint32_t dst = stage + (is_v ? Rows::HALF : 0) + Rows::at(r, c);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+        *reinterpret_cast<uint4 *>((is_v ? vc : kc) + slot * ld + c * 8) = x;
+      }
+      __syncwarp();
+    }
+    int vis[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) vis[t][0] = vis[t][1] = hi - j0;
+    rows.process(stage, vis, [&](int t, int r, float x0, float x1) {
+      const int c = t * 8 + (lane & 3) * 2;
+      if (c < lcols && j0 + r < hi) *reinterpret_cast<float2 *>(lg + (size_t)(j0 - lo + r) * lcols + c) = make_float2(x0, x1);
+    });
+    __syncwarp();  // the stage may be requested again
+  }
+  rm_cp_wait<0>();
+  rows.finish();
+  // ---- the CTA's part: warps' outputs against the common maximum, added in warp order
+  if (lane < 4) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        sh.wm[warp][t * 8 + lane * 2 + i] = rows.m[t][i];
+        sh.wl[warp][t * 8 + lane * 2 + i] = rows.l[t][i];
+      }
+  }
+  __syncthreads();  // also: no warp reads its stages any more
+  float *wo = reinterpret_cast<float *>(step_smem);  // [warp][column][HD]
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = t * 8 + (lane & 3) * 2 + i;
+      float mx = sh.wm[0][c];
+#pragma unroll
+      for (int w = 1; w < SF_WARPS; ++w) mx = fmaxf(mx, sh.wm[w][c]);
+      const float ref = mx == -INFINITY ? 0.f : mx;
+      const float f = ex2_approx(rows.m[t][i] - ref);
+#pragma unroll
+      for (int k = 0; k < HD / 16; ++k) {
+        wo[((size_t)warp * NT * 8 + c) * HD + k * 16 + (lane >> 2)] = rows.o[t][k][i] * f;
+        wo[((size_t)warp * NT * 8 + c) * HD + k * 16 + 8 + (lane >> 2)] = rows.o[t][k][2 + i] * f;
+      }
+      if (warp == 0 && lane < 4) {
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < SF_WARPS; ++w) sum += sh.wl[w][c] * ex2_approx(sh.wm[w][c] - ref);
+        sh.m[c] = mx;
+        sh.l[c] = sum;
+      }
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < group * HD; i += SF_THREADS) {
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < SF_WARPS; ++w) sum += wo[(size_t)w * NT * 8 * HD + i];
+    sh.o[i / HD][i % HD] = sum;
+  }
+  if (csize > 1) co_cluster_sync();
+  else __syncthreads();
+  // ---- the final maxima and sums, the same in every CTA; this CTA's share of the outputs
+  if (threadIdx.x < group) {
+    const int c = threadIdx.x;
+    float mx = -INFINITY;
+    for (int r = 0; r < csize; ++r) mx = fmaxf(mx, *co_map_shared(&sh.m[c], r));
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    float sum = 0.f;
+    for (int r = 0; r < csize; ++r) sum += *co_map_shared(&sh.l[c], r) * ex2_approx(*co_map_shared(&sh.m[c], r) - ref);
+    sh.fm[c] = ref;
+    sh.finv[c] = 1.f / sum;
+  }
+  __syncthreads();
+  for (int i = rank * SF_THREADS + threadIdx.x; i < group * HD; i += csize * SF_THREADS) {
+    const int c = i / HD, d = i % HD;
+    float sum = 0.f;
+    for (int r = 0; r < csize; ++r)
+      sum += *co_map_shared(&sh.o[c][d], r) * ex2_approx(*co_map_shared(&sh.m[c], r) - sh.fm[c]);
+    o[i] = __float2bfloat16_rn(sum * sh.finv[c]);
+  }
+  // ---- the slots' masses
+  for (int j = lo + threadIdx.x; j < hi; j += SF_THREADS) {
+    float w = 0.f;
+    for (int c = 0; c < group; ++c) w = fmaf(ex2_approx(lg[(size_t)(j - lo) * lcols + c] - sh.fm[c]), sh.finv[c], w);
+    mo[j] = (j == slot ? 0.f : mi[j]) + w;
+  }
+  if (rank == 0 && threadIdx.x == 0) a.len_out[sg] = n;  // the cluster has read the old length long ago
+  if (csize > 1) co_cluster_sync();                      // nobody leaves while its parts are being read
+}
+
+bool step_fused_eligible(int dtype, int head_dim, int group) {
+  return dtype == LAZY_BF16 && (head_dim == 64 || head_dim == 128) && group <= 16;
+}
+
+// CTAs per (sequence, head): the next power of two that still leaves every warp a group of 16 slots and room for
+// all CTAs at once at two per SM.
+int step_cluster(long long heads, int budget) {
+  int c = 1;
+  while (c < SF_MAX_CLUSTER && heads * c * 2 <= 2LL * sm_count() && budget > c * SF_WARPS * RM_KEYS) c *= 2;
+  return c;
+}
+int step_part_slots(int budget, int cluster) { return cdiv(cdiv(budget, RM_KEYS), cluster) * RM_KEYS; }
+
+template <int HD, int NT>
+int step_fused(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevStatus *status) {
+  const int group = a.n_heads / a.n_kv_heads;
+  const long long heads = (long long)a.n_seqs * a.n_kv_heads;
+  const int cluster = step_cluster(heads, a.budget), part = step_part_slots(a.budget, cluster);
+  const long long logit_bytes = (long long)part * ((group + 1) & ~1) * 4;
+  const int in_smem = logit_bytes <= SF_LOGIT_BYTES;
+  const int smem = step_stage_bytes<HD, NT> + (in_smem ? (int)logit_bytes : 0);
+  LAZY_TRY((co_allow_smem<step_fused_kernel<HD, NT>>(step_stage_bytes<HD, NT> + SF_LOGIT_BYTES)));
+  return co_launch(step_fused_kernel<HD, NT>, dim3((unsigned)(heads * cluster)), dim3(SF_THREADS), smem, st, cluster, false,
+                   a, group, part, in_smem, scratch, status);
+}
+
 }  // namespace
 
 size_t evict_step_scratch_floats(int n_seqs, int n_heads, int n_kv_heads, int head_dim, int budget) {
-  return step_scratch(n_seqs, n_heads, n_kv_heads, head_dim, budget).total;
+  const size_t general = step_scratch(n_seqs, n_heads, n_kv_heads, head_dim, budget).total;
+  // the one-launch form keeps at most every slot's logits, an even number of columns, parts rounded up to 16 slots
+  const size_t heads = (size_t)n_seqs * n_kv_heads, group = n_heads / n_kv_heads;
+  const size_t fused = heads * ((size_t)budget + SF_MAX_CLUSTER * RM_KEYS) * ((group + 1) & ~(size_t)1);
+  return general > fused ? general : fused;
 }
 
 int launch_evict_step(cudaStream_t st, int dtype, const EvictStepArgs &a, float *scratch, DevStatus *status) {
   if (a.n_seqs == 0) return LAZY_OK;
+  const int group = a.n_heads / a.n_kv_heads;
+  if (step_fused_eligible(dtype, a.head_dim, group)) {
+    if (a.head_dim == 64)
+      return group <= 8 ? step_fused<64, 1>(st, a, scratch, status) : step_fused<64, 2>(st, a, scratch, status);
+    return group <= 8 ? step_fused<128, 1>(st, a, scratch, status) : step_fused<128, 2>(st, a, scratch, status);
+  }
   return dtype == LAZY_F32 ? step_general<float>(st, a, scratch, status) : step_general<bf16>(st, a, scratch, status);
 }
 
