@@ -1,7 +1,14 @@
 // Attention of a batch of requests that share one prefix.  Every query row sees the whole prefix and the first part of
 // its request's own key list (row i of T rows: keys j <= C - T + i of C), so the prefix part is one product of all
 // rows with the prefix's keys: it is computed for the batch together and read once, not once per request.
+//
+// bf16, head width 64 or 128: three launches.  (1) The prefix on tcgen05: the batch's (row, head) pairs of one
+// key/value head are the lanes of 128-lane tiles, the prefix's keys are cut into ranges, every CTA leaves the partial
+// softmax of its lanes over its range.  (2) The requests' own keys on the warp-level path of rows_mma.cuh, launched as a
+// dependent that does not wait for (1), so that its CTAs fill the SMs as the first ones leave.  (3) A merge of
+// the parts, one warp per (row, head).
 #include "attn_split.cuh"
+#include "rows_mma.cuh"
 
 namespace lazy {
 
@@ -23,7 +30,7 @@ __device__ __forceinline__ int px_own_keys(const PrefixArgs &a, int r, int *firs
   const int s = px_seq_of_row(a.cu_q, a.n_seqs, r);
   const int q0 = a.cu_q[s], q1 = a.cu_q[s + 1], c0 = a.cu_kv[s], c1 = a.cu_kv[s + 1];
   *first = c0;
-  if (r < q0 || r >= q1 || q1 - q0 > a.max_q || c0 < 0 || c1 < c0 || c1 > a.n_kv || c1 - c0 > a.max_kv) {
+  if (q0 < 0 || q1 > a.n_rows || r < q0 || r >= q1 || q1 - q0 > a.max_q || c0 < 0 || c1 < c0 || c1 > a.n_kv || c1 - c0 > a.max_kv) {
     dev_fail(status, LAZY_E_BADARG, W_PREFIX, r, s);
     return 0;
   }
@@ -83,16 +90,606 @@ int prefix_general(cudaStream_t st, const PrefixArgs &a, float *scratch, DevStat
   return launch_ok();
 }
 
+
+// ---- (1) the prefix on tcgen05 ------------------------------------------------------------------------------------
+// One CTA: TILES lane tiles (one or two) of 128 lanes = R rows x group heads of one key/value head, 64 keys at a time.
+//   warp 0      TMA: the queries as one 3-d box per tile, then K and V tiles through a ring each (lanes 0 and 1);
+//   warp 1      owns TMEM, issues S = Q K^T (M128 N64) of every tile as soon as its logits have been taken to registers;
+//   warp 2      issues O += P V (M128 N = head width, P from TMEM);
+//   warps 4..   softmax, one thread per lane; running maximum raised only when it grows by more than 2^8.
+// TMEM columns of a tile: S (64) | P high (32) | P low (32) | O (head width).  P enters as the sum of two bf16 numbers, so
+// that the output's only rounding is its own: the part is bound by reading K and V up to 256 lanes, where the third
+// product's time is free.  Two lane tiles in one CTA share the K and V tiles in shared memory.
+constexpr int PT_Q = 128, PT_K = 64;
+constexpr float PT_RESCALE = 8.f;
+
+template <int HD, int TILES>
+struct PrefixShape {
+  static constexpr int CH = HD / 64;
+  static constexpr int Q_CHUNK = PT_Q * 128, Q_BYTES = CH * Q_CHUNK;
+  static constexpr int KV_CHUNK = PT_K * 128, KV_BYTES = CH * KV_CHUNK;
+  static constexpr int STAGES = TILES == 1 ? 2 : 4;     // 96 KiB of two CTAs per SM, 192 KiB of one (head width 128)
+  static constexpr int THREADS = 128 + TILES * 128;
+  static constexpr int TMEM_COLS = 256 * TILES;
+  static constexpr int RING = TILES * Q_BYTES;          // offset of the K ring, the V ring behind it
+  static constexpr int BARRIERS = RING + 2 * STAGES * KV_BYTES;
+};
+template <int STAGES, int TILES>
+struct __align__(8) PrefixBarriers {
+  unsigned long long q_full, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES];
+  unsigned long long s_full[TILES], s_free[TILES], p_full[TILES], pv_done[TILES];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+template <int HD, int TILES>
+constexpr int prefix_smem = PrefixShape<HD, TILES>::BARRIERS + 1024 +
+                            (int)sizeof(PrefixBarriers<PrefixShape<HD, TILES>::STAGES, TILES>);
+
+// grid (n_kv_heads, lane groups of TILES tiles, splits).  Parts: part_o [split][n_rows * n_heads][HD], part_ml
+// [split][n_rows * n_heads] (maximum in log2 units, sum); pair (row, head) at row * n_heads + head.
+template <int HD, int TILES>
+__global__ void __launch_bounds__(PrefixShape<HD, TILES>::THREADS, TILES == 1 ? 2 : 1)
+prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                 const __grid_constant__ CUtensorMap map_v, int n_rows, int group, int rows_per_tile, int n_pre,
+                 int tiles_per_split, float *__restrict__ part_o, float2 *__restrict__ part_ml, DevStatus *status) {
+  using Shape = PrefixShape<HD, TILES>;
+  constexpr int STAGES = Shape::STAGES;
+  extern __shared__ uint8_t prefix_smem_raw[];
+  const uint32_t raw_addr = smem_u32(prefix_smem_raw);
+  uint8_t *smem = prefix_smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
+  const uint32_t sQ = smem_u32(smem), sK = sQ + Shape::RING, sV = sK + STAGES * Shape::KV_BYTES;
+  auto *bars = reinterpret_cast<PrefixBarriers<STAGES, TILES> *>(smem + Shape::BARRIERS);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = blockIdx.x, R = rows_per_tile, H = gridDim.x * group;
+  const int row0 = blockIdx.y * TILES * R;  // first row of the CTA's first tile
+  const int t0 = blockIdx.z * tiles_per_split, nt = min(tiles_per_split, (n_pre + PT_K - 1) / PT_K - t0);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&bars->q_full), 1);
+    for (int i = 0; i < STAGES; ++i) {
+      mbar_init(smem_u32(&bars->k_full[i]), 1);
+      mbar_init(smem_u32(&bars->k_empty[i]), 1);
+      mbar_init(smem_u32(&bars->v_full[i]), 1);
+      mbar_init(smem_u32(&bars->v_empty[i]), 1);
+    }
+    for (int t = 0; t < TILES; ++t) {
+      mbar_init(smem_u32(&bars->s_full[t]), 1);
+      mbar_init(smem_u32(&bars->s_free[t]), 4);
+      mbar_init(smem_u32(&bars->p_full[t]), 4);
+      mbar_init(smem_u32(&bars->pv_done[t]), 1);
+    }
+    bars->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tma_prefetch_desc(&map_q);
+    tma_prefetch_desc(&map_k);
+    tma_prefetch_desc(&map_v);
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)),
+                 "r"((uint32_t)Shape::TMEM_COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(&bars->tmem_base);
+  volatile int *abort_flag = &bars->abort_flag;
+
+  if (warp == 0) {
+    if (lane < 2) {
+      const CUtensorMap *map = lane == 0 ? &map_k : &map_v;
+      const uint32_t ring = lane == 0 ? sK : sV;
+      unsigned long long *fulls = lane == 0 ? bars->k_full : bars->v_full, *empties = lane == 0 ? bars->k_empty : bars->v_empty;
+      if (lane == 0) {
+        const uint32_t qf = smem_u32(&bars->q_full);
+        mbar_expect_tx(qf, (uint32_t)(TILES * Shape::CH * R * group * 128));
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+          for (int c = 0; c < Shape::CH; ++c)
+            tma_load_3d(sQ + t * Shape::Q_BYTES + c * Shape::Q_CHUNK, &map_q, qf, c * 64, g * group, row0 + t * R);
+      }
+      for (int j = 0; j < nt; ++j) {
+        const int st = j % STAGES;
+        if (!mbar_wait(smem_u32(&empties[st]), (uint32_t)((j / STAGES) & 1) ^ 1u, abort_flag, status, W_PREFIX)) break;
+        const uint32_t full = smem_u32(&fulls[st]);
+        mbar_expect_tx(full, Shape::KV_BYTES);
+#pragma unroll
+        for (int c = 0; c < Shape::CH; ++c)
+          tma_load_2d(ring + st * Shape::KV_BYTES + c * Shape::KV_CHUNK, map, full, g * HD + c * 64, (t0 + j) * PT_K);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = idesc_bf16(PT_Q, PT_K, 0, 0);
+      bool ok = mbar_wait(smem_u32(&bars->q_full), 0, abort_flag, status, W_PREFIX);
+      for (int j = 0; j < nt && ok; ++j) {
+        const int st = j % STAGES;
+        ok = mbar_wait(smem_u32(&bars->k_full[st]), (uint32_t)((j / STAGES) & 1), abort_flag, status, W_PREFIX);
+        for (int t = 0; t < TILES && ok; ++t) {
+          ok = mbar_wait(smem_u32(&bars->s_free[t]), (uint32_t)(j & 1) ^ 1u, abort_flag, status, W_PREFIX);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) {
+            const uint64_t ad = umma_smem_desc(sQ + t * Shape::Q_BYTES + (k >> 2) * Shape::Q_CHUNK + (k & 3) * 32);
+            const uint64_t bd = umma_smem_desc(sK + st * Shape::KV_BYTES + (k >> 2) * Shape::KV_CHUNK + (k & 3) * 32);
+            umma_bf16(tmem_base + (uint32_t)(t * 256), ad, bd, idesc, k != 0 ? 1u : 0u);
+          }
+          umma_commit(smem_u32(&bars->s_full[t]));
+        }
+        if (ok) umma_commit(smem_u32(&bars->k_empty[st]));
+      }
+    }
+  } else if (warp == 2) {
+    if (lane == 0) {
+      const uint32_t idesc = idesc_bf16(PT_Q, HD, 0, 1);
+      bool ok = true;
+      for (int j = 0; j < nt && ok; ++j) {
+        const int st = j % STAGES;
+        ok = mbar_wait(smem_u32(&bars->v_full[st]), (uint32_t)((j / STAGES) & 1), abort_flag, status, W_PREFIX);
+        for (int t = 0; t < TILES && ok; ++t) {
+          ok = mbar_wait(smem_u32(&bars->p_full[t]), (uint32_t)(j & 1), abort_flag, status, W_PREFIX);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t tile = tmem_base + (uint32_t)(t * 256);
+#pragma unroll
+          for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int k = 0; k < PT_K / 16; ++k) {
+              const uint64_t vd = umma_smem_desc_mn(sV + st * Shape::KV_BYTES + k * 2048, Shape::KV_CHUNK, 1024);
+              umma_bf16_a_tmem(tile + 128u, tile + 64u + (uint32_t)(part * 32 + k * 8), vd, idesc, (j | part | k) != 0 ? 1u : 0u);
+            }
+          umma_commit(smem_u32(&bars->pv_done[t]));
+        }
+        if (ok) umma_commit(smem_u32(&bars->v_empty[st]));
+      }
+    }
+  } else if (warp >= 4) {
+    const int t = (warp - 4) >> 2, quarter = warp & 3;
+    const uint32_t tile = tmem_base + (uint32_t)(t * 256) + ((uint32_t)(quarter * 32) << 16);
+    const int f = quarter * 32 + lane;  // lane of the tile
+    const int row = row0 + t * R + f / group;
+    const bool used = f < R * group && row < n_rows;
+    const bool warp_used = __any_sync(0xffffffffu, used);  // a warp without lanes only keeps the hand-over going
+    const float sl2 = rsqrtf((float)HD) * CO_LOG2E;
+    const unsigned long long sl2x2 = f32x2_pack(sl2, sl2);
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int j = 0; j < nt && ok; ++j) {
+      ok = mbar_wait(smem_u32(&bars->s_full[t]), (uint32_t)(j & 1), abort_flag, status, W_PREFIX);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      if (!warp_used) {
+        // not before the phase of P_{j-1} is over: the arrival would count for that one
+        if (j > 0) {
+          ok = mbar_wait(smem_u32(&bars->pv_done[t]), (uint32_t)((j - 1) & 1), abort_flag, status, W_PREFIX);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&bars->s_free[t]));
+          mbar_arrive(smem_u32(&bars->p_full[t]));
+        }
+        continue;
+      }
+      uint32_t raw[64];
+      tmem_ld_32x32_raw(tile, raw);
+      tmem_ld_32x32_raw(tile + 32u, raw + 32);
+      tmem_ld_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->s_free[t]));
+      const int there = n_pre - (t0 + j) * PT_K;  // keys of this tile
+      if (there < PT_K) {
+#pragma unroll
+        for (int c = 0; c < 64; ++c)
+          if (c >= there) raw[c] = 0xff800000u;  // -inf
+      }
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int c = 0; c < 64; c += 8) {
+        mx[0] = fmax3(mx[0], __uint_as_float(raw[c]), __uint_as_float(raw[c + 1]));
+        mx[1] = fmax3(mx[1], __uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3]));
+        mx[2] = fmax3(mx[2], __uint_as_float(raw[c + 4]), __uint_as_float(raw[c + 5]));
+        mx[3] = fmax3(mx[3], __uint_as_float(raw[c + 6]), __uint_as_float(raw[c + 7]));
+      }
+      const float mj = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
+      float alpha = 1.f;
+      if (j == 0) m = mj;
+      else {
+        // P_{j-1} V_{j-1} has to be done before P is overwritten, and before O is rescaled
+        ok = mbar_wait(smem_u32(&bars->pv_done[t]), (uint32_t)((j - 1) & 1), abort_flag, status, W_PREFIX);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const bool need = mj - m > PT_RESCALE;
+        if (need) {
+          alpha = ex2_approx(m - mj);
+          m = mj;
+        }
+        if (__any_sync(0xffffffffu, need)) {
+#pragma unroll 1
+          for (int c = 0; c < HD; c += 32) {
+            uint32_t ov[32];
+            tmem_ld_32x32_raw(tile + 128u + (uint32_t)c, ov);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * alpha);
+            tmem_st_32x32(tile + 128u + (uint32_t)c, ov);
+          }
+          tmem_st_wait();
+        }
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      const unsigned long long neg = f32x2_pack(-ref, -ref);
+      float sm[2] = {0.f, 0.f};
+      uint32_t hi[32];
+#pragma unroll
+      for (int c = 0; c < 64; c += 2) {
+        float x0, x1, h0, h1;
+        f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2, neg), x0, x1);
+        const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+        sm[0] += p0;
+        sm[1] += p1;
+        hi[c >> 1] = bf16x2_pack(p0, p1);
+        bf16x2_unpack(hi[c >> 1], h0, h1);
+        raw[c >> 1] = bf16x2_pack(p0 - h0, p1 - h1);  // entry c / 2 has been used by now
+      }
+      l = l * alpha + (sm[0] + sm[1]);
+      tmem_st_32x32(tile + 64u, hi);
+      tmem_st_32x32(tile + 96u, raw);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->p_full[t]));
+    }
+    if (ok && nt > 0) {
+      ok = mbar_wait(smem_u32(&bars->pv_done[t]), (uint32_t)((nt - 1) & 1), abort_flag, status, W_PREFIX);
+      ok = __all_sync(0xffffffffu, ok);
+    }
+    if (warp_used) {
+      tc_fence_after();
+      const size_t pair = (size_t)blockIdx.z * n_rows * H + (size_t)row * H + g * group + f % group;
+      if (used) part_ml[pair] = make_float2(m, ok ? l : NAN);  // a wait ran out (reported): nothing like a result
+      if (ok) {
+#pragma unroll 1
+        for (int c = 0; c < HD; c += 32) {
+          float v[32];
+          tmem_ld_32x32(tile + 128u + (uint32_t)c, v);
+          if (used) {
+            float4 *dst = reinterpret_cast<float4 *>(part_o + pair * HD + c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dst[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          }
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)Shape::TMEM_COLS)
+                 : "memory");
+  }
+}
+
+// ---- (2) the requests' own keys -----------------------------------------------------------------------------------
+// One CTA: 8 NT columns (row, head) of one (request, key/value head) over one range of its list; warps take every fourth group of
+// 16 keys, and their parts are added in shared memory.
+constexpr int PO_WARPS = 4, PO_THREADS = PO_WARPS * 32, PO_STAGES = 3;
+
+template <int HD, int NT>
+struct PrefixOwnShared {
+  float wm[PO_WARPS][NT * 8], wl[PO_WARPS][NT * 8];
+};
+
+// grid (n_kv_heads * column blocks, splits, n_seqs)
+template <int HD, int NT>
+__global__ void __launch_bounds__(PO_THREADS)
+prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, float *__restrict__ part_o,
+                  float2 *__restrict__ part_ml, DevStatus *status) {
+  using Rows = RowsMma<HD, NT>;
+  extern __shared__ __align__(128) uint8_t own_smem[];
+  __shared__ PrefixOwnShared<HD, NT> sh;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int g = blockIdx.x / col_blocks, cb = blockIdx.x - g * col_blocks, s = blockIdx.z;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int q0 = a.cu_q[s], T = a.cu_q[s + 1] - q0, c0 = a.cu_kv[s], C = a.cu_kv[s + 1] - c0;
+  const bool fits = q0 >= 0 && T >= 0 && q0 + T <= a.n_rows && T <= a.max_q && c0 >= 0 && C >= 0 && c0 + C <= a.n_kv &&
+                    C <= a.max_kv;
+  if (!fits && threadIdx.x == 0) dev_fail(status, LAZY_E_BADARG, W_PREFIX, s, -1);
+  const int n_cols = T * group, col0 = cb * NT * 8;
+  const int lo = blockIdx.y * per_split, hi = min(lo + per_split, C);
+  if (fits && col0 < n_cols) {
+    const uint32_t stages = smem_u32(own_smem) + warp * PO_STAGES * Rows::STAGE;
+    Rows rows;
+    rows.init([&](int c) -> const bf16 * {
+      const int f = col0 + c;
+      return f < n_cols ? (const bf16 *)a.q + (size_t)(q0 + f / group) * a.ldq + (size_t)(g * group + f % group) * HD : nullptr;
+    });
+    int vis[NT][2];  // keys of the list that this lane's columns see
+    int least = C, most = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int f = col0 + t * 8 + (lane & 3) * 2 + i;
+        vis[t][i] = f < n_cols ? max(C - T + f / group + 1, 0) : 0;
+      }
+    {  // the block's first and last column bound all of them
+      const int last = min(col0 + NT * 8, n_cols) - 1;
+      least = max(C - T + col0 / group + 1, 0);
+      most = max(C - T + last / group + 1, 0);
+    }
+    const int end = min(hi, most);
+    const bf16 *kb = (const bf16 *)a.k + (size_t)g * HD, *vb = (const bf16 *)a.v + (size_t)g * HD;
+    // list entry of key lane % 16 of group warp + 4 i (-1: not there or out of range), fetched one group ahead
+    auto entry = [&](int i) {
+      const int j = lo + (warp + i * PO_WARPS) * RM_KEYS + (lane & 15);
+      int e = -1;
+      if (j < end) {
+        e = a.kv_idx[c0 + j];
+        if (e < 0 || e >= a.kv_rows) {
+          dev_fail(status, LAZY_E_BADARG, W_PREFIX, c0 + j, e);
+          e = -1;
+        }
+      }
+      return e;
+    };
+    uint32_t there[PO_STAGES];  // by stage, kept in registers: every index below is a compile-time one
+    auto request = [&](int i, int e, uint32_t &mask) {
+      const int j0 = lo + (warp + i * PO_WARPS) * RM_KEYS;
+      mask = __ballot_sync(0xffffffffu, e >= 0) & 0xffffu;
+      if (j0 < end)
+        rows.load(stages + (i % PO_STAGES) * Rows::STAGE, [&](int r, const bf16 *&kr, const bf16 *&vr) {
+          const int row = __shfl_sync(0xffffffffu, e, r);
+          const size_t at = (size_t)max(row, 0) * a.ldkv;
+          kr = kb + at;
+          vr = vb + at;
+          return row >= 0;
+        });
+      rm_cp_commit();
+    };
+    static_assert(PO_STAGES == 3, "the loop below is unrolled by hand over three stages");
+    request(0, entry(0), there[0]);
+    request(1, entry(1), there[1]);
+    int e_next = entry(2);
+    auto step = [&](int i, uint32_t mask, uint32_t &mask_next) {
+      request(i + 2, e_next, mask_next);
+      e_next = entry(i + 3);
+      rm_cp_wait<PO_STAGES - 1>();
+      __syncwarp();
+      const int j0 = lo + (warp + i * PO_WARPS) * RM_KEYS;
+      int seen[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) seen[t][k] = min(vis[t][k], hi) - j0;
+      const uint32_t stage = stages + (i % PO_STAGES) * Rows::STAGE;
+      auto none = [](int, int, float, float) {};
+      if (least >= min(j0 + RM_KEYS, end)) rows.template process<false>(stage, seen, mask, none);
+      else rows.template process<true>(stage, seen, mask, none);
+      __syncwarp();
+    };
+    for (int i = 0; lo + (warp + i * PO_WARPS) * RM_KEYS < end; i += 3) {
+      step(i, there[0], there[2]);
+      if (lo + (warp + (i + 1) * PO_WARPS) * RM_KEYS >= end) break;
+      step(i + 1, there[1], there[0]);
+      if (lo + (warp + (i + 2) * PO_WARPS) * RM_KEYS >= end) break;
+      step(i + 2, there[2], there[1]);
+    }
+    rm_cp_wait<0>();
+    rows.finish();
+    if (lane < 4) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          sh.wm[warp][t * 8 + lane * 2 + i] = rows.m[t][i];
+          sh.wl[warp][t * 8 + lane * 2 + i] = rows.l[t][i];
+        }
+    }
+    __syncthreads();  // also: no warp reads its stages any more
+    float *wo = reinterpret_cast<float *>(own_smem);  // [warp][column][HD]
+    const size_t base = (size_t)blockIdx.y * a.n_rows * a.n_heads;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int c = t * 8 + (lane & 3) * 2 + i;
+        float mx = sh.wm[0][c];
+#pragma unroll
+        for (int w = 1; w < PO_WARPS; ++w) mx = fmaxf(mx, sh.wm[w][c]);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        const float scale = ex2_approx(rows.m[t][i] - ref);
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          wo[((size_t)warp * NT * 8 + c) * HD + k * 16 + (lane >> 2)] = rows.o[t][k][i] * scale;
+          wo[((size_t)warp * NT * 8 + c) * HD + k * 16 + 8 + (lane >> 2)] = rows.o[t][k][2 + i] * scale;
+        }
+        const int f = col0 + c;
+        if (warp == 0 && lane < 4 && f < n_cols) {
+          float sum = 0.f;
+#pragma unroll
+          for (int w = 0; w < PO_WARPS; ++w) sum += sh.wl[w][c] * ex2_approx(sh.wm[w][c] - ref);
+          part_ml[base + (size_t)(q0 + f / group) * a.n_heads + g * group + f % group] = make_float2(mx, sum);
+        }
+      }
+    __syncthreads();
+    for (int i = threadIdx.x; i < min(NT * 8, n_cols - col0) * HD; i += PO_THREADS) {
+      const int f = col0 + i / HD;
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < PO_WARPS; ++w) sum += wo[(size_t)w * NT * 8 * HD + i];
+      part_o[(base + (size_t)(q0 + f / group) * a.n_heads + g * group + f % group) * HD + i % HD] = sum;
+    }
+  }
+  // the merge waits for this kernel alone: its end has to mean the end of the one before it.  One CTA sees to that; the
+  // others leave their SMs to the next ones.
+  if (blockIdx.x + blockIdx.y + blockIdx.z == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// ---- (3) the merge: one warp per (row, head) ------------------------------------------------------------------------
+template <int HD>
+__global__ void __launch_bounds__(128)
+prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, const float2 *__restrict__ part_ml, int n_pre_parts,
+                       int n_parts, int own_split, DevStatus *status) {
+  constexpr int V = HD / 32;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31;
+  const long long pairs = (long long)a.n_rows * a.n_heads, pair = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (pair >= pairs) return;
+  int first;
+  const int own = px_own_keys(a, (int)(pair / a.n_heads), &first, status);
+  // parts of own keys that hold any for this row (the others may not have been written)
+  const int n = n_pre_parts + (own > 0 ? min((own + own_split - 1) / own_split, n_parts - n_pre_parts) : 0);
+  float m = -INFINITY, l = 0.f;
+  bool bad = false;
+  for (int i = lane; i < n; i += 32) {
+    const float2 ml = part_ml[i * pairs + pair];
+    bad |= ml.y != ml.y;
+    if (ml.y > 0.f) m = fmaxf(m, ml.x);
+  }
+  m = warp_max(m);
+  bad = __any_sync(0xffffffffu, bad);
+  float acc[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] = 0.f;
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    float w = 0.f;
+    if (i0 + lane < n) {
+      const float2 ml = part_ml[(i0 + lane) * pairs + pair];
+      if (ml.y > 0.f) {
+        w = ex2_approx(ml.x - m);
+        l = fmaf(ml.y, w, l);
+      }
+    }
+    const int cnt = min(32, n - i0);
+#pragma unroll 4
+    for (int i = 0; i < cnt; ++i) {
+      const float wi = __shfl_sync(0xffffffffu, w, i);
+      const float *p = part_o + ((i0 + i) * pairs + pair) * HD + lane * V;
+      float x[V];
+      if (V == 4) *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(p);
+      else *reinterpret_cast<float2 *>(x) = *reinterpret_cast<const float2 *>(p);
+      if (wi != 0.f) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) acc[k] = fmaf(x[k], wi, acc[k]);
+      }
+    }
+  }
+  l = warp_sum(l);
+  const float inv = bad ? NAN : (l > 0.f ? 1.f / l : 0.f);
+  bf16 *o = (bf16 *)a.o + pair * HD + lane * V;
+  if (V == 4) *reinterpret_cast<uint2 *>(o) = make_uint2(bf16x2_pack(acc[0] * inv, acc[1] * inv), bf16x2_pack(acc[2] * inv, acc[3] * inv));
+  else *reinterpret_cast<uint32_t *>(o) = bf16x2_pack(acc[0] * inv, acc[1] * inv);
+}
+
+bool prefix_tc_eligible(int dtype, int head_dim, int group) {
+  return dtype == LAZY_BF16 && (head_dim == 64 || head_dim == 128) && group <= PT_Q;
+}
+
+// How the work is cut: key ranges of the prefix and of the own lists, so that every launch fills the machine once.
+struct PrefixPlan {
+  int tiles, lane_groups, pre_parts, tiles_per_split, nt, col_blocks, own_parts, own_split;
+  size_t pairs, parts;
+};
+PrefixPlan prefix_plan(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv, int n_heads, int n_kv_heads) {
+  PrefixPlan p;
+  const int group = n_heads / n_kv_heads, R = PT_Q / group;
+  const int lane_tiles = cdiv(n_rows, R), key_tiles = cdiv(n_pre, PT_K);
+  p.tiles = lane_tiles > 1 ? 2 : 1;
+  p.lane_groups = cdiv(lane_tiles, p.tiles);
+  p.pre_parts = p.tiles_per_split = 0;
+  if (key_tiles > 0) {
+    const long long ctas = (long long)n_kv_heads * p.lane_groups, slots = (p.tiles == 1 ? 2LL : 1LL) * sm_count();
+    long long want = slots / ctas;
+    if (want < 1) want = 1;
+    if (want > key_tiles) want = key_tiles;
+    p.tiles_per_split = cdiv(key_tiles, (int)want);
+    p.pre_parts = cdiv(key_tiles, p.tiles_per_split);
+  }
+  p.nt = max_q * group <= 8 ? 1 : 2;
+  p.col_blocks = cdiv(max_q * group, p.nt * 8);
+  p.own_parts = p.own_split = 0;
+  if (max_kv > 0) {
+    const long long ctas = (long long)n_kv_heads * p.col_blocks * n_seqs;
+    long long want = (2LL * sm_count() + ctas - 1) / ctas;
+    const int most = cdiv(max_kv, PO_WARPS * RM_KEYS * 2);  // two groups of keys per warp at least
+    if (want > most) want = most;
+    p.own_split = cdiv(cdiv(max_kv, (int)want), RM_KEYS) * RM_KEYS;
+    p.own_parts = cdiv(max_kv, p.own_split);
+  }
+  p.pairs = (size_t)n_rows * n_heads;
+  p.parts = (size_t)p.pre_parts + p.own_parts;
+  return p;
+}
+
+template <int HD, int TILES>
+int prefix_tc_launch(cudaStream_t st, const PrefixArgs &a, const PrefixPlan &p, int group, float *part_o, float2 *part_ml,
+                     DevStatus *status) {
+  const int R = PT_Q / group;
+  CUtensorMap mq, mk, mv;
+  LAZY_TRY(tma_map_heads_bf16(&mq, a.q, a.n_rows, a.n_heads, HD, a.ldq, group, R));
+  LAZY_TRY(tma_map_2d_bf16(&mk, a.k_pre, a.n_pre, a.n_kv_heads * HD, a.ld_pre, 64, PT_K));
+  LAZY_TRY(tma_map_2d_bf16(&mv, a.v_pre, a.n_pre, a.n_kv_heads * HD, a.ld_pre, 64, PT_K));
+  LAZY_TRY((co_allow_smem<prefix_tc_kernel<HD, TILES>>(prefix_smem<HD, TILES>)));
+  return co_launch(prefix_tc_kernel<HD, TILES>, dim3(a.n_kv_heads, p.lane_groups, p.pre_parts),
+                   dim3(PrefixShape<HD, TILES>::THREADS), prefix_smem<HD, TILES>, st, 1, false, mq, mk, mv, a.n_rows, group, R,
+                   a.n_pre, p.tiles_per_split, part_o, part_ml, status);
+}
+template <int HD, int NT>
+int prefix_own_launch(cudaStream_t st, const PrefixArgs &a, const PrefixPlan &p, int group, float *part_o, float2 *part_ml,
+                      DevStatus *status) {
+  constexpr int SMEM = PO_WARPS * PO_STAGES * RowsMma<HD, NT>::STAGE;
+  LAZY_TRY((co_allow_smem<prefix_own_kernel<HD, NT>>(SMEM)));
+  return co_launch(prefix_own_kernel<HD, NT>, dim3(a.n_kv_heads * p.col_blocks, p.own_parts, a.n_seqs), dim3(PO_THREADS), SMEM,
+                   st, 1, p.pre_parts > 0, a, group, p.col_blocks, p.own_split, part_o, part_ml, status);
+}
+
+template <int HD>
+int prefix_tc(cudaStream_t st, const PrefixArgs &a, float *scratch, DevStatus *status) {
+  const int group = a.n_heads / a.n_kv_heads;
+  const PrefixPlan p = prefix_plan(a.n_rows, a.n_seqs, a.max_q, a.n_pre, a.max_kv, a.n_heads, a.n_kv_heads);
+  float *part_o = reinterpret_cast<float *>(align_up((uintptr_t)scratch, 16));
+  float2 *part_ml = reinterpret_cast<float2 *>(part_o + p.parts * p.pairs * HD);
+  if (p.pre_parts > 0)
+    LAZY_TRY((p.tiles == 1 ? prefix_tc_launch<HD, 1>(st, a, p, group, part_o, part_ml, status)
+                           : prefix_tc_launch<HD, 2>(st, a, p, group, part_o, part_ml, status)));
+  if (p.own_parts > 0) {
+    float *own_o = part_o + (size_t)p.pre_parts * p.pairs * HD;
+    float2 *own_ml = part_ml + (size_t)p.pre_parts * p.pairs;
+    LAZY_TRY((p.nt == 1 ? prefix_own_launch<HD, 1>(st, a, p, group, own_o, own_ml, status)
+                        : prefix_own_launch<HD, 2>(st, a, p, group, own_o, own_ml, status)));
+  }
+  const long long warps = (long long)p.pairs;
+  return co_launch(prefix_tc_merge_kernel<HD>, dim3((unsigned)((warps + 3) / 4)), dim3(128), 0, st, 1, p.parts > 0, a,
+                   (const float *)part_o, (const float2 *)part_ml, p.pre_parts, (int)p.parts, p.own_split > 0 ? p.own_split : 1,
+                   status);
+}
+
 }  // namespace
 
 size_t attention_prefix_scratch_floats(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv, int n_heads,
                                        int n_kv_heads, int head_dim) {
-  (void)n_seqs, (void)max_q, (void)n_kv_heads;
-  return (size_t)n_rows * n_heads * attn_split_count((long long)n_rows * n_heads, n_pre + max_kv) * (head_dim + 2);
+  const size_t general =
+      (size_t)n_rows * n_heads * attn_split_count((long long)n_rows * n_heads, n_pre + max_kv) * (head_dim + 2);
+  if (n_heads / n_kv_heads > PT_Q || max_q < 1 || n_seqs < 1) return general;
+  const PrefixPlan p = prefix_plan(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads, n_kv_heads);
+  const size_t tiled = p.parts * p.pairs * (head_dim + 2) + 4;  // + 4: parts start on a 16-byte boundary
+  return general > tiled ? general : tiled;
 }
 
 int launch_attention_prefix(cudaStream_t st, int dtype, const PrefixArgs &a, float *scratch, DevStatus *status) {
   if (a.n_rows == 0) return LAZY_OK;
+  if (prefix_tc_eligible(dtype, a.head_dim, a.n_heads / a.n_kv_heads))
+    return a.head_dim == 64 ? prefix_tc<64>(st, a, scratch, status) : prefix_tc<128>(st, a, scratch, status);
   return dtype == LAZY_F32 ? prefix_general<float>(st, a, scratch, status) : prefix_general<bf16>(st, a, scratch, status);
 }
 

@@ -290,7 +290,7 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
     int vis[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t) vis[t][0] = vis[t][1] = hi - j0;
-    rows.process(stage, vis, [&](int t, int r, float x0, float x1) {
+    rows.template process<false>(stage, vis, 0xffffu, [&](int t, int r, float x0, float x1) {
       const int c = t * 8 + (lane & 3) * 2;
       if (c < lcols && j0 + r < hi) *reinterpret_cast<float2 *>(lg + (size_t)(j0 - lo + r) * lcols + c) = make_float2(x0, x1);
     });
