@@ -582,19 +582,28 @@ def lazy_prune_op(x: torch.Tensor, pos: torch.Tensor, w_qkv: torch.Tensor, w_o: 
 
 
 # ------------------------------------------------------------------------------- bounded and shared caches
-def _dense(t: torch.Tensor, dev: int, dtype: torch.dtype, name: str) -> int:
-    """Address of a contiguous tensor of the current device and the given type."""
-    if t.get_device() != dev or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous {dtype} tensor on the current CUDA device is wanted")
-    return t.data_ptr()
+def _stream_of(dev: int) -> int:
+    """The current stream's handle on device `dev`, without building a stream object (3 us less per call)."""
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _dense(dev: int, dtype: torch.dtype, names: str, *tensors: torch.Tensor) -> List[int]:
+    """Addresses of contiguous tensors of the current device and the given type."""
+    out = []
+    for t in tensors:
+        if t.get_device() != dev or t.dtype is not dtype or not t.is_contiguous():
+            raise ValueError(f"{names.split()[len(out)]}: a contiguous {dtype} tensor on the current CUDA device is wanted")
+        out.append(t.data_ptr())
+    return out
 
 
 def _rows(t: torch.Tensor, dev: int, dtype: torch.dtype, width: int, name: str) -> Tuple[int, int]:
     """(address, pitch) of a matrix whose rows lie `pitch` elements apart, each of them contiguous."""
-    if t.get_device() != dev or t.dtype != dtype or t.dim() != 2 or t.shape[1] != width or \
-            (t.shape[0] > 0 and t.stride(1) != 1):
+    shape, stride = t.shape, t.stride()
+    if t.get_device() != dev or t.dtype is not dtype or len(shape) != 2 or shape[1] != width or \
+            (stride[1] != 1 and shape[0] > 0 and width > 1):
         raise ValueError(f"{name}: {dtype} rows of {width} elements on the current CUDA device are wanted")
-    pitch = t.stride(0) if t.shape[0] > 1 else width
+    pitch = stride[0] if shape[0] > 1 else width
     if pitch < width or pitch > 0x7fffffff:
         raise ValueError(f"{name}: rows overlap or lie too far apart")
     return t.data_ptr(), pitch
@@ -631,10 +640,11 @@ def lazy_k_attention_mass(q: torch.Tensor, k: torch.Tensor, cu_seqlens: torch.Te
     _same(out.numel(), n_kv_heads * n_total, "size of out")
     if scratch is None:
         scratch = lazy_k_attention_mass_scratch(n_seqs, n_total, max_len, n_heads, n_kv_heads, window)
+    pcu, = _dense(dev, torch.int32, "cu_seqlens", cu_seqlens)
+    pscr, pout = _dense(dev, torch.float32, "scratch out", scratch, out)
     _check("lazy_k_attention_mass", lib().lazy_k_attention_mass(
-        _stream(), dtype_code(q.dtype), pq, ldq, pk, ldk, _dense(cu_seqlens, dev, torch.int32, "cu_seqlens"), n_seqs,
-        max_len, n_total, n_heads, n_kv_heads, head_dim, window, _dense(scratch, dev, torch.float32, "scratch"),
-        scratch.numel(), _dense(out, dev, torch.float32, "out")))
+        _stream_of(dev), dtype_code(q.dtype), pq, ldq, pk, ldk, pcu, n_seqs, max_len, n_total, n_heads, n_kv_heads,
+        head_dim, window, pscr, scratch.numel(), pout))
     return out
 
 
@@ -646,7 +656,7 @@ def lazy_k_evict_scratch(n_seqs: int, n_kv_heads: int, budget: int) -> torch.Ten
 def _cache_ptrs(dev: int, kc, vc, dtype):
     if kc.dim() != 4 or kc.shape != vc.shape:
         raise ValueError("kc, vc: [n_seqs, cap, n_kv_heads, head_dim] are wanted")
-    return _dense(kc, dev, dtype, "kc"), _dense(vc, dev, dtype, "vc")
+    return _dense(dev, dtype, "kc vc", kc, vc)
 
 
 def lazy_k_evict(k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, mass: torch.Tensor, cu_seqlens: torch.Tensor,
@@ -668,12 +678,12 @@ def lazy_k_evict(k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, mass: torc
     _same(clen.numel(), n_seqs * n_kv_heads, "size of clen")
     if scratch is None:
         scratch = lazy_k_evict_scratch(n_seqs, n_kv_heads, budget)
-    i32, f32 = torch.int32, torch.float32
+    ppos, pcu, pscr, pcpos, pclen = _dense(dev, torch.int32, "pos cu_seqlens scratch cpos clen", pos, cu_seqlens, scratch,
+                                           cpos, clen)
+    pmass, pcmass = _dense(dev, torch.float32, "mass cmass", mass, cmass)
     _check("lazy_k_evict", lib().lazy_k_evict(
-        _stream(), dtype_code(k.dtype), pk, pv, ldk, _dense(pos, dev, i32, "pos"), _dense(mass, dev, f32, "mass"),
-        _dense(cu_seqlens, dev, i32, "cu_seqlens"), n_seqs, max_len, n_total, n_kv_heads, head_dim, budget, n_recent,
-        _dense(scratch, dev, i32, "scratch"), scratch.numel(), pkc, pvc, _dense(cmass, dev, f32, "cmass"),
-        _dense(cpos, dev, i32, "cpos"), _dense(clen, dev, i32, "clen"), cap))
+        _stream_of(dev), dtype_code(k.dtype), pk, pv, ldk, ppos, pmass, pcu, n_seqs, max_len, n_total, n_kv_heads, head_dim,
+        budget, n_recent, pscr, scratch.numel(), pkc, pvc, pcmass, pcpos, pclen, cap))
 
 
 def lazy_k_evict_step_scratch(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, budget: int) -> torch.Tensor:
@@ -714,13 +724,13 @@ def lazy_k_evict_step(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
         raise ValueError("out: sizes do not agree")
     if scratch is None:
         scratch = lazy_k_evict_step_scratch(n_seqs, n_heads, n_kv_heads, head_dim, budget)
-    i32, f32 = torch.int32, torch.float32
+    pposn, ppos, pposo, plen, pleno, pslot, pgone = _dense(
+        dev, torch.int32, "pos_new cpos pos_out clen len_out slot gone", pos_new, cpos, pos_out, clen, len_out, slot, gone)
+    pmass, pmasso, pscr = _dense(dev, torch.float32, "cmass mass_out scratch", cmass, mass_out, scratch)
+    po, = _dense(dev, dt, "o", o)
     _check("lazy_k_evict_step", lib().lazy_k_evict_step(
-        _stream(), dtype_code(dt), pq, ldq, pkn, pvn, ldn, _dense(pos_new, dev, i32, "pos_new"), pkc, pvc, cap,
-        _dense(cmass, dev, f32, "cmass"), _dense(mass_out, dev, f32, "mass_out"), _dense(cpos, dev, i32, "cpos"),
-        _dense(pos_out, dev, i32, "pos_out"), _dense(clen, dev, i32, "clen"), _dense(len_out, dev, i32, "len_out"),
-        n_seqs, n_heads, n_kv_heads, head_dim, budget, n_recent, _dense(scratch, dev, f32, "scratch"), scratch.numel(),
-        _dense(o, dev, dt, "o"), _dense(slot, dev, i32, "slot"), _dense(gone, dev, i32, "gone")))
+        _stream_of(dev), dtype_code(dt), pq, ldq, pkn, pvn, ldn, pposn, pkc, pvc, cap, pmass, pmasso, ppos, pposo, plen,
+        pleno, n_seqs, n_heads, n_kv_heads, head_dim, budget, n_recent, pscr, scratch.numel(), po, pslot, pgone))
     return out
 
 
@@ -755,12 +765,12 @@ def lazy_k_attention_prefix(q: torch.Tensor, cu_q: torch.Tensor, max_q: int, k_p
     n_pre = k_pre.shape[0]
     if scratch is None:
         scratch = lazy_k_attention_prefix_scratch(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads, n_kv_heads, head_dim)
-    i32 = torch.int32
+    pcq, pidx, pckv = _dense(dev, torch.int32, "cu_q kv_idx cu_kv", cu_q, kv_idx, cu_kv)
+    pscr, = _dense(dev, torch.float32, "scratch", scratch)
+    pout, = _dense(dev, dt, "out", out)
     _check("lazy_k_attention_prefix", lib().lazy_k_attention_prefix(
-        _stream(), dtype_code(dt), pq, ldq, _dense(cu_q, dev, i32, "cu_q"), n_rows, n_seqs, max_q, pkp, pvp, ldp, n_pre,
-        pk, pv, ldk, k.shape[0], _dense(kv_idx, dev, i32, "kv_idx"), _dense(cu_kv, dev, i32, "cu_kv"), kv_idx.numel(),
-        max_kv, n_heads, n_kv_heads, head_dim, _dense(scratch, dev, torch.float32, "scratch"), scratch.numel(),
-        _dense(out, dev, dt, "out")))
+        _stream_of(dev), dtype_code(dt), pq, ldq, pcq, n_rows, n_seqs, max_q, pkp, pvp, ldp, n_pre, pk, pv, ldk, k.shape[0],
+        pidx, pckv, kv_idx.numel(), max_kv, n_heads, n_kv_heads, head_dim, pscr, scratch.numel(), pout))
     return out
 
 
@@ -782,8 +792,8 @@ def lazy_k_verify(p: torch.Tensor, draft: torch.Tensor, cu_draft: torch.Tensor, 
     n_accept, tokens = out
     if n_accept.numel() != n_seqs or tokens.numel() != n_seqs * (max_draft + 1):
         raise ValueError("out: sizes do not agree")
+    pdraft, pcu, pacc, ptok = _dense(dev, i32, "draft cu_draft n_accept tokens", draft, cu_draft, n_accept, tokens)
+    pua, pus = _dense(dev, f32, "u_accept u_sample", u_accept, u_sample)
     _check("lazy_k_verify", lib().lazy_k_verify(
-        _stream(), pp, ldp, pq, ldq, _dense(draft, dev, i32, "draft"), _dense(cu_draft, dev, i32, "cu_draft"), n_seqs,
-        n_draft, max_draft, vocab, _dense(u_accept, dev, f32, "u_accept"), _dense(u_sample, dev, f32, "u_sample"),
-        _dense(n_accept, dev, i32, "n_accept"), _dense(tokens, dev, i32, "tokens")))
+        _stream_of(dev), pp, ldp, pq, ldq, pdraft, pcu, n_seqs, n_draft, max_draft, vocab, pua, pus, pacc, ptok))
     return out
