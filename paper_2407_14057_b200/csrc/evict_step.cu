@@ -167,13 +167,14 @@ int step_general(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevSta
 // shared memory when its group comes up.  The parts' maxima, sums and outputs meet in distributed shared memory, and
 // every CTA adds the final weights of its own slots to their masses from the logits it kept (in shared memory, or in
 // the scratch when a part is too long).
-constexpr int SF_WARPS = 4, SF_THREADS = SF_WARPS * 32, SF_STAGES = 3, SF_MAX_CLUSTER = 8;
-constexpr int SF_LOGIT_BYTES = 8192;  // of a part's logits in shared memory; two CTAs fit on an SM with it
+constexpr int SF_WARPS = 4, SF_THREADS = SF_WARPS * 32, SF_STAGES = 2, SF_CTAS = 3, SF_MAX_CLUSTER = 8;
+// A part's logits stay in shared memory up to this size: with three CTAs on an SM, with two or one
+constexpr int SF_LOGIT_BYTES = 8192, SF_LOGIT_BYTES_2 = 40960;
+constexpr int SF_BATCH = 8;           // slots a thread has in flight in the loops over weights
 
 template <int HD, int NT>
 struct StepShared {
   float m[NT * 8], l[NT * 8];       // this CTA's maxima and sums, read by the cluster
-  float o[NT * 8][HD];              // its unnormalised outputs against those maxima
   float wm[SF_WARPS][NT * 8], wl[SF_WARPS][NT * 8];
   float fm[NT * 8], finv[NT * 8];   // final
   unsigned long long best;
@@ -183,7 +184,7 @@ template <int HD, int NT>
 constexpr int step_stage_bytes = SF_WARPS * SF_STAGES * RowsMma<HD, NT>::STAGE;
 
 template <int HD, int NT>
-__global__ void __launch_bounds__(SF_THREADS)
+__global__ void __launch_bounds__(SF_THREADS, SF_CTAS)
 step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_in_smem, float *__restrict__ scratch,
                   DevStatus *status) {
   using Rows = RowsMma<HD, NT>;
@@ -192,6 +193,25 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
   const int rank = (int)co_cluster_rank(), csize = (int)co_cluster_size();
   const int sg = blockIdx.x / csize, s = sg / a.n_kv_heads, g = sg - s * a.n_kv_heads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float *mi = a.mass_in + (size_t)sg * a.cap;
+  const int32_t *pi = a.pos_in + (size_t)sg * a.cap;
+  float *mo = a.mass_out + (size_t)sg * a.cap;
+  int32_t *po = a.pos_out + (size_t)sg * a.cap;
+  // The first batch of weights and positions of this CTA's slots is asked for before anything else: the rows would
+  // hold it up, and it need not wait for the length (what lies behind it is not looked at).
+  const int lo = rank * part_slots, behind = min(lo + part_slots, a.budget);
+  int bp[SF_BATCH];
+  float bw[SF_BATCH];
+  auto fetch = [&](int j0, int end) {
+#pragma unroll
+    for (int i = 0; i < SF_BATCH; ++i) {
+      const int j = j0 + i * SF_THREADS;
+      bp[i] = j < end ? pi[j] : 0;
+      bw[i] = j < end ? mi[j] : 0.f;
+    }
+  };
+  fetch(lo + threadIdx.x, behind);
+  const int p_new = a.pos_new[s];
   const int len = a.len_in[sg];
   bf16 *o = (bf16 *)a.o + ((size_t)s * a.n_heads + (size_t)g * group) * HD;
   if (len < 0 || len > a.budget) {  // the whole cluster alike
@@ -206,7 +226,7 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
   }
   const bool full = len >= a.budget;
   const int n = full ? len : len + 1;
-  const int lo = min(rank * part_slots, n), hi = min(lo + part_slots, n);  // this CTA's slots
+  const int hi = max(min(behind, n), lo), end = min(hi, len);  // this CTA's slots: [lo, hi), [lo, end) of them held before
   const int groups = (hi - lo + RM_KEYS - 1) / RM_KEYS;
   const size_t ld = (size_t)a.n_kv_heads * HD;
   bf16 *kc = (bf16 *)a.kc + (size_t)s * a.cap * ld + (size_t)g * HD, *vc = (bf16 *)a.vc + (size_t)s * a.cap * ld + (size_t)g * HD;
@@ -223,25 +243,31 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
       });
     rm_cp_commit();
   };
+  // ---- the slot
+  int slot = len;
+  const bool look = full || po != pi;
+  const long long first_recent = (long long)p_new - a.n_recent;
+  unsigned long long best = ~0ull;
+  auto take = [&](int j0) {
+#pragma unroll
+    for (int i = 0; i < SF_BATCH; ++i) {
+      const int j = j0 + i * SF_THREADS;
+      if (j < end) {
+        best = min_u64(best, step_rank(bw[i], bp[i], first_recent, j));
+        if (po != pi) po[j] = bp[i];
+      }
+    }
+  };
 #pragma unroll
   for (int i = 0; i < SF_STAGES - 1; ++i) request(i);
   rows.init([&](int c) -> const bf16 * {
     return c < group ? (const bf16 *)a.q + (size_t)s * a.ldq + (size_t)(g * group + c) * HD : nullptr;
   });
-  // ---- the slot
-  const float *mi = a.mass_in + (size_t)sg * a.cap;
-  const int32_t *pi = a.pos_in + (size_t)sg * a.cap;
-  float *mo = a.mass_out + (size_t)sg * a.cap;
-  int32_t *po = a.pos_out + (size_t)sg * a.cap;
-  const int p_new = a.pos_new[s];
-  int slot = len;
-  if (full || po != pi) {
-    const long long first_recent = (long long)p_new - a.n_recent;
-    unsigned long long best = ~0ull;
-    for (int j = lo + threadIdx.x; j < min(hi, len); j += SF_THREADS) {
-      const int p = pi[j];
-      if (full) best = min_u64(best, step_rank(mi[j], p, first_recent, j));
-      if (po != pi) po[j] = p;
+  if (look) {
+    take(lo + threadIdx.x);
+    for (int j0 = lo + threadIdx.x + SF_THREADS * SF_BATCH; j0 < end; j0 += SF_THREADS * SF_BATCH) {
+      fetch(j0, end);
+      take(j0);
     }
     if (full) {
 #pragma unroll
@@ -252,9 +278,15 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
         for (int w = 1; w < SF_WARPS; ++w) best = min_u64(best, sh.wbest[w]);
         sh.best = best;
       }
-      co_cluster_sync();
-      best = ~0ull;
-      for (int r = 0; r < csize; ++r) best = min_u64(best, *co_map_shared(&sh.best, r));
+      if (csize > 1) {
+        co_cluster_sync();
+        best = *co_map_shared(&sh.best, lane & (csize - 1));  // csize is a power of two
+#pragma unroll
+        for (int k = SF_MAX_CLUSTER / 2; k > 0; k >>= 1) best = min_u64(best, __shfl_xor_sync(0xffffffffu, best, k));
+      } else {
+        __syncthreads();
+        best = sh.best;
+      }
       slot = (int)(uint32_t)best;
     } else {
       __syncthreads();
@@ -298,6 +330,14 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
   }
   rm_cp_wait<0>();
   rows.finish();
+  auto old_masses = [&](int j0) {
+#pragma unroll
+    for (int i = 0; i < SF_BATCH; ++i) {
+      const int j = j0 + i * SF_THREADS;
+      bw[i] = j < end ? mi[j] : 0.f;
+    }
+  };
+  old_masses(lo + threadIdx.x);  // on their way during the exchange
   // ---- the CTA's part: warps' outputs against the common maximum, added in warp order
   if (lane < 4) {
 #pragma unroll
@@ -310,6 +350,8 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
   }
   __syncthreads();  // also: no warp reads its stages any more
   float *wo = reinterpret_cast<float *>(step_smem);  // [warp][column][HD]
+  float *co = wo + SF_WARPS * NT * 8 * HD;           // [column][HD]: the CTA's outputs against its maxima, read by the cluster
+  static_assert((SF_WARPS + 1) * NT * 8 * HD * 4 <= step_stage_bytes<HD, NT>, "the stages hold the outputs in the end");
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -338,34 +380,68 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
     float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < SF_WARPS; ++w) sum += wo[(size_t)w * NT * 8 * HD + i];
-    sh.o[i / HD][i % HD] = sum;
+    co[i] = sum;
   }
   if (csize > 1) co_cluster_sync();
   else __syncthreads();
-  // ---- the final maxima and sums, the same in every CTA; this CTA's share of the outputs
+  // ---- the final maxima and sums, the same in every thread that needs them; this CTA's share of the outputs.  All
+  // reads of the other CTAs' memory are in flight together.
+  auto gather = [&](int c, float &ref, float &inv, float *scale) {
+    float rm[SF_MAX_CLUSTER], rl[SF_MAX_CLUSTER], mx = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < SF_MAX_CLUSTER; ++r) {
+      rm[r] = r < csize ? *co_map_shared(&sh.m[c], r) : -INFINITY;
+      rl[r] = r < csize ? *co_map_shared(&sh.l[c], r) : 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < SF_MAX_CLUSTER; ++r) mx = fmaxf(mx, rm[r]);
+    ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+    for (int r = 0; r < SF_MAX_CLUSTER; ++r) {
+      scale[r] = ex2_approx(rm[r] - ref);
+      sum += rl[r] * scale[r];
+    }
+    inv = 1.f / sum;
+  };
+  for (int i = rank * SF_THREADS + threadIdx.x; i < group * HD; i += csize * SF_THREADS) {
+    float part[SF_MAX_CLUSTER], scale[SF_MAX_CLUSTER], ref, inv, sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < SF_MAX_CLUSTER; ++r) part[r] = r < csize ? *co_map_shared(co + i, r) : 0.f;
+    gather(i / HD, ref, inv, scale);
+#pragma unroll
+    for (int r = 0; r < SF_MAX_CLUSTER; ++r) sum += part[r] * scale[r];  // ranks that do not exist: 0 x 0
+    o[i] = __float2bfloat16_rn(sum * inv);
+  }
   if (threadIdx.x < group) {
-    const int c = threadIdx.x;
-    float mx = -INFINITY;
-    for (int r = 0; r < csize; ++r) mx = fmaxf(mx, *co_map_shared(&sh.m[c], r));
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    float sum = 0.f;
-    for (int r = 0; r < csize; ++r) sum += *co_map_shared(&sh.l[c], r) * ex2_approx(*co_map_shared(&sh.m[c], r) - ref);
-    sh.fm[c] = ref;
-    sh.finv[c] = 1.f / sum;
+    float scale[SF_MAX_CLUSTER], ref, inv;
+    gather(threadIdx.x, ref, inv, scale);
+    sh.fm[threadIdx.x] = ref;
+    sh.finv[threadIdx.x] = inv;
   }
   __syncthreads();
-  for (int i = rank * SF_THREADS + threadIdx.x; i < group * HD; i += csize * SF_THREADS) {
-    const int c = i / HD, d = i % HD;
-    float sum = 0.f;
-    for (int r = 0; r < csize; ++r)
-      sum += *co_map_shared(&sh.o[c][d], r) * ex2_approx(*co_map_shared(&sh.m[c], r) - sh.fm[c]);
-    o[i] = __float2bfloat16_rn(sum * sh.finv[c]);
-  }
   // ---- the slots' masses
-  for (int j = lo + threadIdx.x; j < hi; j += SF_THREADS) {
-    float w = 0.f;
-    for (int c = 0; c < group; ++c) w = fmaf(ex2_approx(lg[(size_t)(j - lo) * lcols + c] - sh.fm[c]), sh.finv[c], w);
-    mo[j] = (j == slot ? 0.f : mi[j]) + w;
+  for (int j0 = lo + threadIdx.x; j0 < hi; j0 += SF_THREADS * SF_BATCH) {
+    float w[SF_BATCH];
+    int j[SF_BATCH];
+    if (j0 >= lo + SF_THREADS * SF_BATCH) old_masses(j0);
+#pragma unroll
+    for (int i = 0; i < SF_BATCH; ++i) {
+      j[i] = min(j0 + i * SF_THREADS, hi - 1);
+      w[i] = 0.f;
+    }
+#pragma unroll 2
+    for (int c = 0; c < lcols; c += 2) {
+      const float m0 = sh.fm[c], f0 = sh.finv[c], m1 = sh.fm[c + 1], f1 = sh.finv[c + 1];
+#pragma unroll
+      for (int i = 0; i < SF_BATCH; ++i) {
+        const float2 x = *reinterpret_cast<const float2 *>(lg + (size_t)(j[i] - lo) * lcols + c);
+        w[i] = fmaf(ex2_approx(x.x - m0), f0, w[i]);
+        if (c + 1 < group) w[i] = fmaf(ex2_approx(x.y - m1), f1, w[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < SF_BATCH; ++i)
+      if (j0 + i * SF_THREADS < hi) mo[j[i]] = (j[i] == slot ? 0.f : bw[i]) + w[i];
   }
   if (rank == 0 && threadIdx.x == 0) a.len_out[sg] = n;  // the cluster has read the old length long ago
   if (csize > 1) co_cluster_sync();                      // nobody leaves while its parts are being read
@@ -376,10 +452,11 @@ bool step_fused_eligible(int dtype, int head_dim, int group) {
 }
 
 // CTAs per (sequence, head): the next power of two that still leaves every warp a group of 16 slots and room for
-// all CTAs at once at two per SM.
+// all CTAs at once at three per SM.  A second wave costs more than it spreads: 32 sequences of 2048 slots on 8 heads
+// take 47 us with one CTA each, 61 us with two, 63 us with four.
 int step_cluster(long long heads, int budget) {
   int c = 1;
-  while (c < SF_MAX_CLUSTER && heads * c * 2 <= 2LL * sm_count() && budget > c * SF_WARPS * RM_KEYS) c *= 2;
+  while (c < SF_MAX_CLUSTER && heads * c * 2 <= (long long)SF_CTAS * sm_count() && budget > c * SF_WARPS * RM_KEYS) c *= 2;
   return c;
 }
 int step_part_slots(int budget, int cluster) { return cdiv(cdiv(budget, RM_KEYS), cluster) * RM_KEYS; }
@@ -390,9 +467,9 @@ int step_fused(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevStatu
   const long long heads = (long long)a.n_seqs * a.n_kv_heads;
   const int cluster = step_cluster(heads, a.budget), part = step_part_slots(a.budget, cluster);
   const long long logit_bytes = (long long)part * ((group + 1) & ~1) * 4;
-  const int in_smem = logit_bytes <= SF_LOGIT_BYTES;
+  const int in_smem = logit_bytes <= (heads * cluster <= 2LL * sm_count() ? SF_LOGIT_BYTES_2 : SF_LOGIT_BYTES);
   const int smem = step_stage_bytes<HD, NT> + (in_smem ? (int)logit_bytes : 0);
-  LAZY_TRY((co_allow_smem<step_fused_kernel<HD, NT>>(step_stage_bytes<HD, NT> + SF_LOGIT_BYTES)));
+  LAZY_TRY((co_allow_smem<step_fused_kernel<HD, NT>>(step_stage_bytes<HD, NT> + SF_LOGIT_BYTES_2)));
   return co_launch(step_fused_kernel<HD, NT>, dim3((unsigned)(heads * cluster)), dim3(SF_THREADS), smem, st, cluster, false,
                    a, group, part, in_smem, scratch, status);
 }
