@@ -2,10 +2,11 @@
 // n_recent rows stay, and of the older ones those with the largest weight, up to the budget; equal weights go
 // to the lower row.  Heads choose for themselves, so slot t of two heads may hold different tokens.
 //
-// Two launches.  Select: one CTA per (sequence, head) finds the weight at the last kept rank by a radix select
-// over order-preserving keys, held in shared memory, then walks the rows in order and writes each kept row's
-// index, weight and position to its slot.  Gather: the whole grid copies the kept K and V rows, 16 bytes a
-// thread (the part that is bound by memory: kept rows are read and written once).
+// Two launches.  Select: one CTA per (sequence, head) finds the weight at the last kept rank by a radix select over
+// order-preserving keys held in shared memory; then every warp counts, and after one scan over the warps writes, the kept
+// rows of its contiguous part, so the list comes out in row order without a barrier per chunk.  Gather: the
+// whole grid copies the kept rows' K, V, weights and positions (the part that is bound by memory: kept rows are read and
+// written once); its CTAs are set up while the selection runs.
 #include "cache_ops.cuh"
 
 namespace lazy {
@@ -13,12 +14,15 @@ namespace lazy {
 namespace {
 
 constexpr int ES_THREADS = 1024, ES_WARPS = ES_THREADS / 32;
-constexpr int ES_BITS = 11, ES_BINS = 1 << ES_BITS;
-constexpr int ES_KEYS = 49152;  // keys held in shared memory (192 KiB); longer sequences are read again per pass
-constexpr int ES_SMEM = ES_KEYS * 4;
+constexpr int ES_BINS = 2048;      // 11-bit digits
+constexpr int ES_COPIES = 4;       // of the histogram, by lane: weights crowd in a few exponents
+constexpr int ES_KEYS = 45056;     // keys held in shared memory (176 KiB); longer sequences are read again per pass
+constexpr int ES_HIST = ES_COPIES * ES_BINS;
+constexpr int ES_SMEM = (ES_HIST + ES_KEYS) * 4;
+constexpr int ES_BATCH = 8;        // loads in flight per thread
 
-// Exclusive prefix sum over the CTA's threads of one value each; *total receives the sum.
-__device__ __forceinline__ int block_exclusive(int v, int *warp_sums, int *total) {
+// Exclusive prefix sum over the CTA's threads of one value each.
+__device__ __forceinline__ int block_exclusive(int v, int *warp_sums) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int incl = v;
 #pragma unroll
@@ -26,131 +30,168 @@ __device__ __forceinline__ int block_exclusive(int v, int *warp_sums, int *total
     const int up = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += up;
   }
-  __syncthreads();  // warp_sums may still be read from the call before
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
-  int w = lane < ES_WARPS ? warp_sums[lane] : 0;
+  int w = warp_sums[lane];
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int up = __shfl_up_sync(0xffffffffu, w, o);
     if (lane >= o) w += up;
   }
-  *total = __shfl_sync(0xffffffffu, w, ES_WARPS - 1);
-  const int before = warp ? __shfl_sync(0xffffffffu, w, warp - 1) : 0;
-  return before + incl - v;
+  const int before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+  return (warp ? before : 0) + incl - v;
 }
 
-// grid (n_kv_heads, n_seqs)
+// grid (n_kv_heads, n_seqs).  idx[s, g]: `budget` entries for the kept rows, then their number (0: nothing to copy).
 __global__ void __launch_bounds__(ES_THREADS)
-evict_select_kernel(const float *__restrict__ mass, int n_total, const int32_t *__restrict__ pos,
-                    const int32_t *__restrict__ cu, int max_len, int budget, int n_recent, int cap,
-                    int32_t *__restrict__ idx, float *__restrict__ cmass, int32_t *__restrict__ cpos,
-                    int32_t *__restrict__ clen, DevStatus *status) {
-  extern __shared__ uint32_t es_keys[];
-  __shared__ int hist[ES_BINS];
-  __shared__ int warp_sums[ES_WARPS];
+evict_select_kernel(const float *__restrict__ mass, int n_total, const int32_t *__restrict__ cu, int max_len, int budget,
+                    int n_recent, int32_t *__restrict__ idx, int32_t *__restrict__ clen, DevStatus *status) {
+  extern __shared__ uint32_t es_smem[];
+  int *hist = reinterpret_cast<int *>(es_smem);
+  uint32_t *keys = es_smem + ES_HIST;
+  __shared__ int warp_sums[2][ES_WARPS];
   __shared__ int s_bin, s_above;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int g = blockIdx.x, s = blockIdx.y, Hkv = gridDim.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const size_t sg = (size_t)s * Hkv + g;
+  int32_t *list = idx + sg * (budget + 1);
   int start, n;
   const bool ok = co_span(cu, s, n_total, max_len, status, W_EVICT, start, n);
   const int keep = ok ? min(n, budget) : 0;
-  // what the copying kernel goes by (the heads' common length may be overwritten by a later step)
   if (threadIdx.x == 0) {
-    idx[sg * (budget + 1) + budget] = keep;
+    list[budget] = keep;
     if (ok) clen[sg] = keep;
   }
   if (keep == 0) return;
   const float *m = mass + (size_t)g * n_total + start;
   const int old = n - min(n_recent, keep);  // rows that compete
   const int need = keep - (n - old);        // how many of them stay
-  uint32_t bar = 0u;                        // keys above it stay; `ties` of those equal to it, lowest rows first
-  int ties = 0;
-  if (need == old) {
-    ties = 0x7fffffff;  // all stay
-  } else if (need == 0) {
-    bar = 0xffffffffu;
-  } else {
-    const bool held = old <= ES_KEYS;
-    if (held)
-      for (int i = threadIdx.x; i < old; i += ES_THREADS) es_keys[i] = co_weight_key(m[i]);
-    uint32_t prefix = 0u, mask = 0u;
-    int left = need;
-    for (int pass = 0; pass < 3; ++pass) {  // digits of 11, 11 and 10 bits from the top
-      const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : ES_BINS;
-      for (int i = threadIdx.x; i < bins; i += ES_THREADS) hist[i] = 0;
-      __syncthreads();
-      for (int i = threadIdx.x; i < old; i += ES_THREADS) {
-        const uint32_t key = held ? es_keys[i] : co_weight_key(m[i]);
-        if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1)], 1);
-      }
-      __syncthreads();
-      // counts from the top: thread t owns the two bins at 2 t and 2 t + 1 counted downwards
-      const int b0 = bins - 1 - 2 * (int)threadIdx.x, b1 = b0 - 1;
-      const int c0 = b0 >= 0 ? hist[b0] : 0, c1 = b1 >= 0 ? hist[b1] : 0;
-      int total;
-      const int above = block_exclusive(c0 + c1, warp_sums, &total);
-      if (c0 && above < left && left <= above + c0) {
-        s_bin = b0;
-        s_above = above;
-      } else if (c1 && above + c0 < left && left <= above + c0 + c1) {
-        s_bin = b1;
-        s_above = above + c0;
-      }
-      __syncthreads();
-      left -= s_above;
-      prefix |= (uint32_t)s_bin << shift;
-      mask |= (uint32_t)(bins - 1) << shift;
-      __syncthreads();
-    }
-    bar = prefix;
-    ties = left;
+  if (need == old) {                        // all of them
+    for (int i = threadIdx.x; i < n; i += ES_THREADS) list[i] = start + i;
+    return;
   }
-  // ---- in row order: which rows stay, and where
-  int placed = 0, tied = 0;
-  for (int i0 = 0; i0 < n; i0 += ES_THREADS) {
-    const int i = i0 + threadIdx.x;
-    float w = 0.f;
-    bool above = false, equal = false;
-    if (i < n) {
-      w = m[i];
-      const uint32_t key = co_weight_key(w);
-      above = i >= old || need == old || key > bar;
-      equal = !above && key == bar && need > 0;
+  for (int i = threadIdx.x; i < n - old; i += ES_THREADS) list[need + i] = start + old + i;  // the newest
+  if (need == 0) return;
+  const bool held = old <= ES_KEYS;
+  if (held)
+    for (int i0 = threadIdx.x; i0 < old; i0 += ES_THREADS * ES_BATCH) {
+      float w[ES_BATCH];
+#pragma unroll
+      for (int i = 0; i < ES_BATCH; ++i) w[i] = i0 + i * ES_THREADS < old ? m[i0 + i * ES_THREADS] : 0.f;
+#pragma unroll
+      for (int i = 0; i < ES_BATCH; ++i)
+        if (i0 + i * ES_THREADS < old) keys[i0 + i * ES_THREADS] = co_weight_key(w[i]);
     }
-    int total;
-    const int mine = block_exclusive((above ? 1 : 0) | (equal ? 1 << 16 : 0), warp_sums, &total);
-    const int ties_before = tied + (mine >> 16);
-    const bool stays = above || (equal && ties_before < ties);
-    if (stays) {
-      const int slot = placed + (mine & 0xffff) + min(ties_before, ties) - min(tied, ties);
-      idx[sg * (budget + 1) + slot] = start + i;
-      cmass[sg * cap + slot] = w;
-      cpos[sg * cap + slot] = pos[start + i];
+  auto key_of = [&](int i) { return held ? keys[i] : co_weight_key(m[i]); };
+  uint32_t prefix = 0u, mask = 0u;
+  int left = need;
+  for (int pass = 0; pass < 3; ++pass) {  // digits of 11, 11 and 10 bits from the top
+    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : ES_BINS;
+    for (int i = threadIdx.x; i < ES_HIST; i += ES_THREADS) hist[i] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = threadIdx.x; i < old; i += ES_THREADS) {
+      const uint32_t key = key_of(i);
+      if ((key & mask) == prefix) atomicAdd(&hist[(lane & (ES_COPIES - 1)) * ES_BINS + ((key >> shift) & (bins - 1))], 1);
     }
-    placed += (total & 0xffff) + min(tied + (total >> 16), ties) - min(tied, ties);
-    tied += total >> 16;
+    __syncthreads();
+    // counts from the top: thread t owns the two bins at 2 t and 2 t + 1 counted downwards
+    const int b0 = bins - 1 - 2 * (int)threadIdx.x, b1 = b0 - 1;
+    int c0 = 0, c1 = 0;
+    if (b0 >= 0) {
+#pragma unroll
+      for (int k = 0; k < ES_COPIES; ++k) {
+        c0 += hist[k * ES_BINS + b0];
+        c1 += hist[k * ES_BINS + b1];
+      }
+    }
+    const int above = block_exclusive(c0 + c1, warp_sums[pass & 1]);
+    if (c0 && above < left && left <= above + c0) {
+      s_bin = b0;
+      s_above = above;
+    } else if (c1 && above + c0 < left && left <= above + c0 + c1) {
+      s_bin = b1;
+      s_above = above + c0;
+    }
+    __syncthreads();
+    left -= s_above;
+    prefix |= (uint32_t)s_bin << shift;
+    mask |= (uint32_t)(bins - 1) << shift;
+  }
+  // ---- keys above `prefix` stay, and of those equal to it the first `left`; warp w walks rows [w part, (w + 1) part)
+  const int part = ((old + ES_WARPS - 1) / ES_WARPS + 31) / 32 * 32;
+  const int begin = min(warp * part, old), end = min(begin + part, old);
+  int n_above = 0, n_equal = 0;
+  for (int i0 = begin; i0 < end; i0 += 32) {
+    const int i = i0 + lane;
+    const uint32_t key = i < end ? key_of(i) : 0u;
+    n_above += __popc(__ballot_sync(0xffffffffu, i < end && key > prefix));
+    n_equal += __popc(__ballot_sync(0xffffffffu, i < end && key == prefix));
+  }
+  __syncthreads();  // warp_sums may still be read from the last pass
+  if (lane == 0) {
+    warp_sums[0][warp] = n_above;
+    warp_sums[1][warp] = n_equal;
+  }
+  __syncthreads();
+  int at = 0, ties = 0;  // rows above, and equal ones, before this warp's
+  {
+    int a = lane < warp ? warp_sums[0][lane] : 0, e = lane < warp ? warp_sums[1][lane] : 0;
+    at = __reduce_add_sync(0xffffffffu, a);
+    ties = __reduce_add_sync(0xffffffffu, e);
+  }
+  const uint32_t below = (1u << lane) - 1u;
+  for (int i0 = begin; i0 < end; i0 += 32) {
+    const int i = i0 + lane;
+    const uint32_t key = i < end ? key_of(i) : 0u;
+    const uint32_t above = __ballot_sync(0xffffffffu, i < end && key > prefix);
+    const uint32_t equal = __ballot_sync(0xffffffffu, i < end && key == prefix);
+    const int my_ties = ties + __popc(equal & below);
+    if ((above >> lane & 1u) || ((equal >> lane & 1u) && my_ties < left))
+      list[at + __popc(above & below) + min(my_ties, left)] = start + i;
+    at += __popc(above);
+    ties += __popc(equal);
   }
 }
 
 // grid (slot groups, n_kv_heads, n_seqs); vecs 16-byte pieces per row
-__global__ void __launch_bounds__(256)
+constexpr int EG_THREADS = 256, EG_PIECES = 2;  // pieces of K and of V that a thread has in flight
+__global__ void __launch_bounds__(EG_THREADS)
 evict_gather_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long ld, int vecs,
+                    const float *__restrict__ mass, const int32_t *__restrict__ pos, int n_total,
                     const int32_t *__restrict__ idx, int budget, uint4 *__restrict__ kc, uint4 *__restrict__ vc,
-                    int cap, int per_block) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+                    float *__restrict__ cmass, int32_t *__restrict__ cpos, int cap, int per_block) {
   const int g = blockIdx.y, s = blockIdx.z, Hkv = gridDim.y;
   const size_t sg = (size_t)s * Hkv + g;
   const int32_t *list = idx + sg * (budget + 1);
-  const int keep = list[budget];
-  const int first = blockIdx.x * per_block, last = min(first + per_block, keep);
-  for (int i = threadIdx.x; i < (last - first) * vecs; i += blockDim.x) {
-    const int slot = first + i / vecs, c = i % vecs;
-    const size_t from = (size_t)list[slot] * ld + (size_t)g * vecs + c;
-    const size_t to = (((size_t)s * cap + slot) * Hkv + g) * vecs + c;
-    kc[to] = k[from];
-    vc[to] = v[from];
+  const int first = blockIdx.x * per_block;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int last = min(first + per_block, list[budget]);
+  const int pieces = (last - first) * vecs;
+  for (int i0 = threadIdx.x; i0 < pieces; i0 += EG_THREADS * EG_PIECES) {
+    uint4 a[EG_PIECES], b[EG_PIECES];
+    size_t to[EG_PIECES];
+#pragma unroll
+    for (int p = 0; p < EG_PIECES; ++p) {
+      const int i = min(i0 + p * EG_THREADS, pieces - 1);
+      const int slot = first + i / vecs, c = i % vecs;
+      const size_t from = (size_t)list[slot] * ld + (size_t)g * vecs + c;
+      to[p] = (((size_t)s * cap + slot) * Hkv + g) * vecs + c;
+      a[p] = k[from];
+      b[p] = v[from];
+    }
+#pragma unroll
+    for (int p = 0; p < EG_PIECES; ++p)
+      if (i0 + p * EG_THREADS < pieces) {
+        kc[to[p]] = a[p];
+        vc[to[p]] = b[p];
+      }
+  }
+  for (int slot = first + threadIdx.x; slot < last; slot += EG_THREADS) {
+    const int row = list[slot];
+    cmass[sg * cap + slot] = mass[(size_t)g * n_total + row];
+    cpos[sg * cap + slot] = pos[row];
   }
 }
 
@@ -166,16 +207,16 @@ int launch_evict(cudaStream_t st, int dtype, const void *k, const void *v, int l
                  int32_t *clen, int cap, DevStatus *status) {
   if (n_seqs == 0) return LAZY_OK;
   LAZY_TRY(co_allow_smem<evict_select_kernel>(ES_SMEM));
-  const size_t smem = (size_t)(max_len < ES_KEYS ? max_len : ES_KEYS) * 4;
-  LAZY_TRY(co_launch(evict_select_kernel, dim3(n_kv_heads, n_seqs), dim3(ES_THREADS), smem, st, 1, false, mass, n_total, pos,
-                     cu, max_len, budget, n_recent, cap, idx, cmass, cpos, clen, status));
+  const size_t smem = (size_t)(ES_HIST + (max_len < ES_KEYS ? max_len : ES_KEYS)) * 4;
+  LAZY_TRY(co_launch(evict_select_kernel, dim3(n_kv_heads, n_seqs), dim3(ES_THREADS), smem, st, 1, false, mass, n_total, cu,
+                     max_len, budget, n_recent, idx, clen, status));
   const int most = budget < max_len ? budget : max_len;
-  const int vecs = head_dim * elem_bytes(dtype) / 16;
-  const int per_block = cdiv(2048, vecs);  // eight 16-byte pieces of K and of V per thread
   if (most == 0) return LAZY_OK;
-  return co_launch(evict_gather_kernel, dim3(cdiv(most, per_block), n_kv_heads, n_seqs), dim3(256), 0, st, 1, true,
-                   (const uint4 *)k, (const uint4 *)v, (long long)ldkv * elem_bytes(dtype) / 16, vecs,
-                   (const int32_t *)idx, budget, (uint4 *)kc, (uint4 *)vc, cap, per_block);
+  const int vecs = head_dim * elem_bytes(dtype) / 16;
+  const int per_block = cdiv(EG_THREADS * EG_PIECES, vecs);
+  return co_launch(evict_gather_kernel, dim3(cdiv(most, per_block), n_kv_heads, n_seqs), dim3(EG_THREADS), 0, st, 1, true,
+                   (const uint4 *)k, (const uint4 *)v, (long long)ldkv * elem_bytes(dtype) / 16, vecs, mass, pos, n_total,
+                   (const int32_t *)idx, budget, (uint4 *)kc, (uint4 *)vc, cmass, cpos, cap, per_block);
 }
 
 }  // namespace lazy
