@@ -2,11 +2,11 @@
 // n_recent rows stay, and of the older ones those with the largest weight, up to the budget; equal weights go
 // to the lower row.  Heads choose for themselves, so slot t of two heads may hold different tokens.
 //
-// Two launches.  Select: one CTA per (sequence, head) finds the weight at the last kept rank by a radix select over
-// order-preserving keys held in shared memory; then every warp counts, and after one scan over the warps writes, the kept
-// rows of its contiguous part, so the list comes out in row order without a barrier per chunk.  Gather: the
-// whole grid copies the kept rows' K, V, weights and positions (the part that is bound by memory: kept rows are read and
-// written once); its CTAs are set up while the selection runs.
+// One launch, a few CTAs per (sequence, head).  Each of them makes the whole selection for itself (which needs no word
+// between them): a radix select over order-preserving keys held in shared memory finds the weight at the last kept
+// rank, every warp counts the kept rows of its contiguous part, and after one scan over the warps the rows are listed
+// in row order without a barrier per chunk.  A CTA lists and then copies only its share of the slots.  The copy is what
+// is bound by memory: kept rows are read and written once.
 #include "cache_ops.cuh"
 
 namespace lazy {
@@ -17,9 +17,12 @@ constexpr int ES_THREADS = 1024, ES_WARPS = ES_THREADS / 32;
 constexpr int ES_BINS = 2048;      // 11-bit digits
 constexpr int ES_COPIES = 4;       // of the histogram, by lane: weights crowd in a few exponents
 constexpr int ES_KEYS = 45056;     // keys held in shared memory (176 KiB); longer sequences are read again per pass
-constexpr int ES_HIST = ES_COPIES * ES_BINS;
+constexpr int ES_PITCH = ES_BINS + 8;  // copies start 8 banks apart
+constexpr int ES_HIST = ES_COPIES * ES_PITCH;
 constexpr int ES_SMEM = (ES_HIST + ES_KEYS) * 4;
-constexpr int ES_BATCH = 8;        // loads in flight per thread
+constexpr int ES_BATCH = 8;        // weights in flight per thread
+constexpr int EG_PIECES = 4;       // 16-byte pieces of K and of V in flight per thread
+constexpr int ES_MAX_PARTS = 8;    // CTAs per (sequence, head)
 
 // Exclusive prefix sum over the CTA's threads of one value each.
 __device__ __forceinline__ int block_exclusive(int v, int *warp_sums) {
@@ -42,37 +45,35 @@ __device__ __forceinline__ int block_exclusive(int v, int *warp_sums) {
   return (warp ? before : 0) + incl - v;
 }
 
-// grid (n_kv_heads, n_seqs).  idx[s, g]: `budget` entries for the kept rows, then their number (0: nothing to copy).
-__global__ void __launch_bounds__(ES_THREADS)
-evict_select_kernel(const float *__restrict__ mass, int n_total, const int32_t *__restrict__ cu, int max_len, int budget,
-                    int n_recent, int32_t *__restrict__ idx, int32_t *__restrict__ clen, DevStatus *status) {
+// grid (parts, n_kv_heads, n_seqs).  idx[s, g]: the kept rows by slot; vecs: 16-byte pieces per row.
+__global__ void __launch_bounds__(ES_THREADS, 1)
+evict_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long ld, int vecs,
+             const int32_t *__restrict__ pos, const float *__restrict__ mass, int n_total, const int32_t *__restrict__ cu,
+             int max_len, int budget, int n_recent, int32_t *__restrict__ idx, uint4 *__restrict__ kc,
+             uint4 *__restrict__ vc, float *__restrict__ cmass, int32_t *__restrict__ cpos, int32_t *__restrict__ clen, int cap,
+             DevStatus *status) {
   extern __shared__ uint32_t es_smem[];
   int *hist = reinterpret_cast<int *>(es_smem);
   uint32_t *keys = es_smem + ES_HIST;
   __shared__ int warp_sums[2][ES_WARPS];
   __shared__ int s_bin, s_above;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int g = blockIdx.x, s = blockIdx.y, Hkv = gridDim.x;
+  const int g = blockIdx.y, s = blockIdx.z, Hkv = gridDim.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const size_t sg = (size_t)s * Hkv + g;
-  int32_t *list = idx + sg * (budget + 1);
+  int32_t *list = idx + sg * budget;
   int start, n;
-  const bool ok = co_span(cu, s, n_total, max_len, status, W_EVICT, start, n);
-  const int keep = ok ? min(n, budget) : 0;
-  if (threadIdx.x == 0) {
-    list[budget] = keep;
-    if (ok) clen[sg] = keep;
-  }
-  if (keep == 0) return;
+  if (!co_span(cu, s, n_total, max_len, status, W_EVICT, start, n)) return;
+  const int keep = min(n, budget);
+  if (blockIdx.x == 0 && threadIdx.x == 0) clen[sg] = keep;
+  const int share = (keep + gridDim.x - 1) / gridDim.x;
+  const int first = min((int)blockIdx.x * share, keep), last = min(first + share, keep);  // this CTA's slots
+  if (first == last) return;
   const float *m = mass + (size_t)g * n_total + start;
   const int old = n - min(n_recent, keep);  // rows that compete
   const int need = keep - (n - old);        // how many of them stay
-  if (need == old) {                        // all of them
-    for (int i = threadIdx.x; i < n; i += ES_THREADS) list[i] = start + i;
-    return;
-  }
-  for (int i = threadIdx.x; i < n - old; i += ES_THREADS) list[need + i] = start + old + i;  // the newest
-  if (need == 0) return;
+  // the newest rows, and all rows where all stay: slot t holds row t + (n - keep)
+  for (int t = max(first, need == old ? 0 : need) + threadIdx.x; t < last; t += ES_THREADS) list[t] = start + n - keep + t;
+  if (need > 0 && need < old && first < need) {
   const bool held = old <= ES_KEYS;
   if (held)
     for (int i0 = threadIdx.x; i0 < old; i0 += ES_THREADS * ES_BATCH) {
@@ -93,7 +94,7 @@ evict_select_kernel(const float *__restrict__ mass, int n_total, const int32_t *
 #pragma unroll 4
     for (int i = threadIdx.x; i < old; i += ES_THREADS) {
       const uint32_t key = key_of(i);
-      if ((key & mask) == prefix) atomicAdd(&hist[(lane & (ES_COPIES - 1)) * ES_BINS + ((key >> shift) & (bins - 1))], 1);
+      if ((key & mask) == prefix) atomicAdd(&hist[(lane & (ES_COPIES - 1)) * ES_PITCH + ((key >> shift) & (bins - 1))], 1);
     }
     __syncthreads();
     // counts from the top: thread t owns the two bins at 2 t and 2 t + 1 counted downwards
@@ -102,8 +103,8 @@ evict_select_kernel(const float *__restrict__ mass, int n_total, const int32_t *
     if (b0 >= 0) {
 #pragma unroll
       for (int k = 0; k < ES_COPIES; ++k) {
-        c0 += hist[k * ES_BINS + b0];
-        c1 += hist[k * ES_BINS + b1];
+        c0 += hist[k * ES_PITCH + b0];
+        c1 += hist[k * ES_PITCH + b1];
       }
     }
     const int above = block_exclusive(c0 + c1, warp_sums[pass & 1]);
@@ -148,47 +149,35 @@ evict_select_kernel(const float *__restrict__ mass, int n_total, const int32_t *
     const uint32_t above = __ballot_sync(0xffffffffu, i < end && key > prefix);
     const uint32_t equal = __ballot_sync(0xffffffffu, i < end && key == prefix);
     const int my_ties = ties + __popc(equal & below);
-    if ((above >> lane & 1u) || ((equal >> lane & 1u) && my_ties < left))
-      list[at + __popc(above & below) + min(my_ties, left)] = start + i;
+    const int slot = at + __popc(above & below) + min(my_ties, left);
+    if (((above >> lane & 1u) || ((equal >> lane & 1u) && my_ties < left)) && slot >= first && slot < last)
+      list[slot] = start + i;
     at += __popc(above);
     ties += __popc(equal);
   }
-}
-
-// grid (slot groups, n_kv_heads, n_seqs); vecs 16-byte pieces per row
-constexpr int EG_THREADS = 256, EG_PIECES = 2;  // pieces of K and of V that a thread has in flight
-__global__ void __launch_bounds__(EG_THREADS)
-evict_gather_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long ld, int vecs,
-                    const float *__restrict__ mass, const int32_t *__restrict__ pos, int n_total,
-                    const int32_t *__restrict__ idx, int budget, uint4 *__restrict__ kc, uint4 *__restrict__ vc,
-                    float *__restrict__ cmass, int32_t *__restrict__ cpos, int cap, int per_block) {
-  const int g = blockIdx.y, s = blockIdx.z, Hkv = gridDim.y;
-  const size_t sg = (size_t)s * Hkv + g;
-  const int32_t *list = idx + sg * (budget + 1);
-  const int first = blockIdx.x * per_block;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int last = min(first + per_block, list[budget]);
+  }
+  __syncthreads();  // the share's list is complete
   const int pieces = (last - first) * vecs;
-  for (int i0 = threadIdx.x; i0 < pieces; i0 += EG_THREADS * EG_PIECES) {
+  for (int i0 = threadIdx.x; i0 < pieces; i0 += ES_THREADS * EG_PIECES) {
     uint4 a[EG_PIECES], b[EG_PIECES];
-    size_t to[EG_PIECES];
 #pragma unroll
     for (int p = 0; p < EG_PIECES; ++p) {
-      const int i = min(i0 + p * EG_THREADS, pieces - 1);
-      const int slot = first + i / vecs, c = i % vecs;
-      const size_t from = (size_t)list[slot] * ld + (size_t)g * vecs + c;
-      to[p] = (((size_t)s * cap + slot) * Hkv + g) * vecs + c;
+      const int i = min(i0 + p * ES_THREADS, pieces - 1);
+      const size_t from = (size_t)list[first + i / vecs] * ld + (size_t)g * vecs + i % vecs;
       a[p] = k[from];
       b[p] = v[from];
     }
 #pragma unroll
-    for (int p = 0; p < EG_PIECES; ++p)
-      if (i0 + p * EG_THREADS < pieces) {
-        kc[to[p]] = a[p];
-        vc[to[p]] = b[p];
+    for (int p = 0; p < EG_PIECES; ++p) {
+      const int i = i0 + p * ES_THREADS;
+      if (i < pieces) {
+        const size_t to = (((size_t)s * cap + first + i / vecs) * Hkv + g) * vecs + i % vecs;
+        kc[to] = a[p];
+        vc[to] = b[p];
       }
+    }
   }
-  for (int slot = first + threadIdx.x; slot < last; slot += EG_THREADS) {
+  for (int slot = first + threadIdx.x; slot < last; slot += ES_THREADS) {
     const int row = list[slot];
     cmass[sg * cap + slot] = mass[(size_t)g * n_total + row];
     cpos[sg * cap + slot] = pos[row];
@@ -198,7 +187,7 @@ evict_gather_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, lo
 }  // namespace
 
 size_t evict_scratch_ints(int n_seqs, int n_kv_heads, int budget) {
-  return (size_t)n_seqs * n_kv_heads * ((size_t)budget + 1);
+  return (size_t)n_seqs * n_kv_heads * budget;
 }
 
 int launch_evict(cudaStream_t st, int dtype, const void *k, const void *v, int ldkv, const int32_t *pos,
@@ -206,17 +195,19 @@ int launch_evict(cudaStream_t st, int dtype, const void *k, const void *v, int l
                  int head_dim, int budget, int n_recent, int32_t *idx, void *kc, void *vc, float *cmass, int32_t *cpos,
                  int32_t *clen, int cap, DevStatus *status) {
   if (n_seqs == 0) return LAZY_OK;
-  LAZY_TRY(co_allow_smem<evict_select_kernel>(ES_SMEM));
+  LAZY_TRY(co_allow_smem<evict_kernel>(ES_SMEM));
   const size_t smem = (size_t)(ES_HIST + (max_len < ES_KEYS ? max_len : ES_KEYS)) * 4;
-  LAZY_TRY(co_launch(evict_select_kernel, dim3(n_kv_heads, n_seqs), dim3(ES_THREADS), smem, st, 1, false, mass, n_total, cu,
-                     max_len, budget, n_recent, idx, clen, status));
+  // as many CTAs per (sequence, head) as run at once on the machine, one per SM; a part copies 64 slots at least
+  const long long heads = (long long)n_seqs * n_kv_heads;
   const int most = budget < max_len ? budget : max_len;
-  if (most == 0) return LAZY_OK;
-  const int vecs = head_dim * elem_bytes(dtype) / 16;
-  const int per_block = cdiv(EG_THREADS * EG_PIECES, vecs);
-  return co_launch(evict_gather_kernel, dim3(cdiv(most, per_block), n_kv_heads, n_seqs), dim3(EG_THREADS), 0, st, 1, true,
-                   (const uint4 *)k, (const uint4 *)v, (long long)ldkv * elem_bytes(dtype) / 16, vecs, mass, pos, n_total,
-                   (const int32_t *)idx, budget, (uint4 *)kc, (uint4 *)vc, cmass, cpos, cap, per_block);
+  long long parts = sm_count() / heads;
+  if (parts > ES_MAX_PARTS) parts = ES_MAX_PARTS;
+  if (parts > cdiv(most, 64)) parts = cdiv(most, 64);
+  if (parts < 1) parts = 1;
+  return co_launch(evict_kernel, dim3((unsigned)parts, n_kv_heads, n_seqs), dim3(ES_THREADS), smem, st, 1, false,
+                   (const uint4 *)k, (const uint4 *)v, (long long)ldkv * elem_bytes(dtype) / 16,
+                   head_dim * elem_bytes(dtype) / 16, pos, mass, n_total, cu, max_len, budget, n_recent, idx, (uint4 *)kc,
+                   (uint4 *)vc, cmass, cpos, clen, cap, status);
 }
 
 }  // namespace lazy

@@ -18,7 +18,7 @@ def lib():
 MASS = dict(stream=None, dtype=0, q=X, ldq=256, k=X, ldkv=128, cu=X, n_seqs=1, max_len=8, n_total=8, H=4, Hkv=2,
             dh=64, window=0, scratch=X, floats=32, mass=X)
 EVICT = dict(stream=None, dtype=0, k=X, v=X, ldkv=128, pos=X, mass=X, cu=X, n_seqs=1, max_len=8, n_total=8, Hkv=2,
-             dh=64, budget=4, recent=2, scratch=X, ints=10, kc=X, vc=X, cmass=X, cpos=X, clen=X, cap=4)
+             dh=64, budget=4, recent=2, scratch=X, ints=8, kc=X, vc=X, cmass=X, cpos=X, clen=X, cap=4)
 STEP = dict(stream=None, dtype=0, q=X, ldq=256, k_new=X, v_new=X, ld_new=128, pos_new=X, kc=X, vc=X, cap=5, mass_in=X,
             mass_out=X, pos_in=X, pos_out=X, len_in=X, len_out=X, n_seqs=1, H=4, Hkv=2, dh=64, budget=4, recent=2,
             scratch=X, floats=1 << 20, o=X, slot=X, gone=X)
@@ -59,7 +59,7 @@ def test_evict_refuses(lib):
              dict(ldkv=120), dict(ldkv=129), dict(budget=0), dict(recent=-1), dict(recent=5), dict(cap=3),
              dict(n_seqs=-1), dict(max_len=-1), dict(max_len=0), dict(n_total=-1)]:
         refuse(f, EVICT, BADARG, **change)
-    refuse(f, EVICT, CAPACITY, ints=9)
+    refuse(f, EVICT, CAPACITY, ints=7)
     refuse(f, EVICT, CAPACITY, n_seqs=65536, ints=1 << 40)
     refuse(f, EVICT, 0, n_seqs=0)
     assert lib.lazy_k_evict_scratch_ints(1, 2, 0) == 0
