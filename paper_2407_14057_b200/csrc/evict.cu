@@ -24,25 +24,47 @@ constexpr int ES_BATCH = 8;        // weights in flight per thread
 constexpr int EG_PIECES = 4;       // 16-byte pieces of K and of V in flight per thread
 constexpr int ES_MAX_PARTS = 8;    // CTAs per (sequence, head)
 
-// Exclusive prefix sum over the CTA's threads of one value each.
-__device__ __forceinline__ int block_exclusive(int v, int *warp_sums) {
+// The bin that holds rank `left` (1 = the largest) when counted from the top, by the first ES_SCAN threads (all 1024 would
+// take four times as long: the scan is bound by instruction issue).  Writes {bin, rows above it, rows in it} to found.
+constexpr int ES_SCAN = 256, ES_PER = ES_BINS / ES_SCAN;
+__device__ __forceinline__ void find_bin(const int *hist, int copies, int bins, int left, int *warp_sums, int *found) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int incl = v;
+  const int b0 = bins - ES_PER * ((int)threadIdx.x + 1);  // this thread's bins: [b0, b0 + ES_PER)
+  int c[ES_PER], sum = 0;
+#pragma unroll
+  for (int i = 0; i < ES_PER; ++i) c[i] = 0;
+  if (b0 >= 0)
+    for (int k = 0; k < copies; ++k)
+#pragma unroll
+      for (int i = 0; i < ES_PER; i += 4) {
+        const int4 x = *reinterpret_cast<const int4 *>(&hist[k * ES_PITCH + b0 + i]);
+        c[i] += x.x;
+        c[i + 1] += x.y;
+        c[i + 2] += x.z;
+        c[i + 3] += x.w;
+      }
+#pragma unroll
+  for (int i = 0; i < ES_PER; ++i) sum += c[i];
+  int incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int up = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += up;
   }
   if (lane == 31) warp_sums[warp] = incl;
-  __syncthreads();
-  int w = warp_sums[lane];
+  asm volatile("bar.sync 1, %0;" ::"n"(ES_SCAN) : "memory");
+  int above = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sums[lane] : 0) + incl - sum;
+  if (above < left && left <= above + sum) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int up = __shfl_up_sync(0xffffffffu, w, o);
-    if (lane >= o) w += up;
+    for (int i = ES_PER - 1; i >= 0; --i) {
+      if (above < left && left <= above + c[i]) {
+        found[0] = b0 + i;
+        found[1] = above;
+        found[2] = c[i];
+      }
+      above += c[i];
+    }
   }
-  const int before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
-  return (warp ? before : 0) + incl - v;
 }
 
 // grid (parts, n_kv_heads, n_seqs).  idx[s, g]: the kept rows by slot; vecs: 16-byte pieces per row.
@@ -52,11 +74,11 @@ evict_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long
              int max_len, int budget, int n_recent, int32_t *__restrict__ idx, uint4 *__restrict__ kc,
              uint4 *__restrict__ vc, float *__restrict__ cmass, int32_t *__restrict__ cpos, int32_t *__restrict__ clen, int cap,
              DevStatus *status) {
-  extern __shared__ uint32_t es_smem[];
+  extern __shared__ __align__(16) uint32_t es_smem[];
   int *hist = reinterpret_cast<int *>(es_smem);
   uint32_t *keys = es_smem + ES_HIST;
   __shared__ int warp_sums[2][ES_WARPS];
-  __shared__ int s_bin, s_above;
+  __shared__ int found[3];  // by find_bin
   const int g = blockIdx.y, s = blockIdx.z, Hkv = gridDim.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const size_t sg = (size_t)s * Hkv + g;
@@ -89,71 +111,70 @@ evict_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long
   int left = need;
   for (int pass = 0; pass < 3; ++pass) {  // digits of 11, 11 and 10 bits from the top
     const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : ES_BINS;
-    for (int i = threadIdx.x; i < ES_HIST; i += ES_THREADS) hist[i] = 0;
+    const int copies = pass == 0 ? ES_COPIES : 1;  // later passes count the few rows of one bin
+    for (int i = threadIdx.x; i < copies * ES_PITCH; i += ES_THREADS) hist[i] = 0;
     __syncthreads();
 #pragma unroll 4
     for (int i = threadIdx.x; i < old; i += ES_THREADS) {
       const uint32_t key = key_of(i);
-      if ((key & mask) == prefix) atomicAdd(&hist[(lane & (ES_COPIES - 1)) * ES_PITCH + ((key >> shift) & (bins - 1))], 1);
+      if ((key & mask) == prefix) atomicAdd(&hist[(lane & (copies - 1)) * ES_PITCH + ((key >> shift) & (bins - 1))], 1);
     }
     __syncthreads();
-    // counts from the top: thread t owns the two bins at 2 t and 2 t + 1 counted downwards
-    const int b0 = bins - 1 - 2 * (int)threadIdx.x, b1 = b0 - 1;
-    int c0 = 0, c1 = 0;
-    if (b0 >= 0) {
-#pragma unroll
-      for (int k = 0; k < ES_COPIES; ++k) {
-        c0 += hist[k * ES_PITCH + b0];
-        c1 += hist[k * ES_PITCH + b1];
-      }
-    }
-    const int above = block_exclusive(c0 + c1, warp_sums[pass & 1]);
-    if (c0 && above < left && left <= above + c0) {
-      s_bin = b0;
-      s_above = above;
-    } else if (c1 && above + c0 < left && left <= above + c0 + c1) {
-      s_bin = b1;
-      s_above = above + c0;
-    }
+    if (threadIdx.x < ES_SCAN) find_bin(hist, copies, bins, left, warp_sums[0], found);
     __syncthreads();
-    left -= s_above;
-    prefix |= (uint32_t)s_bin << shift;
+    left -= found[1];
+    prefix |= (uint32_t)found[0] << shift;
     mask |= (uint32_t)(bins - 1) << shift;
   }
-  // ---- keys above `prefix` stay, and of those equal to it the first `left`; warp w walks rows [w part, (w + 1) part)
+  // ---- keys above `prefix` stay, and of those equal to it the first `left`; warp w walks rows [w part, (w + 1) part).
+  // Where all equal ones stay (no tie is cut) "above" takes them in, and one vote per 32 rows is enough.
+  const bool cut = found[2] != left;
   const int part = ((old + ES_WARPS - 1) / ES_WARPS + 31) / 32 * 32;
   const int begin = min(warp * part, old), end = min(begin + part, old);
   int n_above = 0, n_equal = 0;
-  for (int i0 = begin; i0 < end; i0 += 32) {
-    const int i = i0 + lane;
-    const uint32_t key = i < end ? key_of(i) : 0u;
-    n_above += __popc(__ballot_sync(0xffffffffu, i < end && key > prefix));
-    n_equal += __popc(__ballot_sync(0xffffffffu, i < end && key == prefix));
+#pragma unroll 4
+  for (int i = begin + lane; i < end; i += 32) {
+    const uint32_t key = key_of(i);
+    n_above += cut ? key > prefix : key >= prefix;
+    n_equal += key == prefix;
   }
+  n_above = __reduce_add_sync(0xffffffffu, n_above);
+  n_equal = cut ? __reduce_add_sync(0xffffffffu, n_equal) : 0;
   __syncthreads();  // warp_sums may still be read from the last pass
   if (lane == 0) {
     warp_sums[0][warp] = n_above;
     warp_sums[1][warp] = n_equal;
   }
   __syncthreads();
-  int at = 0, ties = 0;  // rows above, and equal ones, before this warp's
-  {
-    int a = lane < warp ? warp_sums[0][lane] : 0, e = lane < warp ? warp_sums[1][lane] : 0;
-    at = __reduce_add_sync(0xffffffffu, a);
-    ties = __reduce_add_sync(0xffffffffu, e);
-  }
+  // rows above, and equal ones, before this warp's
+  int at = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sums[0][lane] : 0);
+  int ties = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sums[1][lane] : 0);
   const uint32_t below = (1u << lane) - 1u;
-  for (int i0 = begin; i0 < end; i0 += 32) {
-    const int i = i0 + lane;
-    const uint32_t key = i < end ? key_of(i) : 0u;
-    const uint32_t above = __ballot_sync(0xffffffffu, i < end && key > prefix);
-    const uint32_t equal = __ballot_sync(0xffffffffu, i < end && key == prefix);
-    const int my_ties = ties + __popc(equal & below);
-    const int slot = at + __popc(above & below) + min(my_ties, left);
-    if (((above >> lane & 1u) || ((equal >> lane & 1u) && my_ties < left)) && slot >= first && slot < last)
-      list[slot] = start + i;
-    at += __popc(above);
-    ties += __popc(equal);
+  if (!cut) {
+    if (at < last && at + n_above > first) {
+#pragma unroll 4
+      for (int i0 = begin; i0 < end; i0 += 32) {
+        const int i = i0 + lane;
+        const bool stays = i < end && key_of(i) >= prefix;
+        const uint32_t all = __ballot_sync(0xffffffffu, stays);
+        const int slot = at + __popc(all & below);
+        if (stays && slot >= first && slot < last) list[slot] = start + i;
+        at += __popc(all);
+      }
+    }
+  } else {
+    for (int i0 = begin; i0 < end; i0 += 32) {
+      const int i = i0 + lane;
+      const uint32_t key = i < end ? key_of(i) : 0u;
+      const uint32_t above = __ballot_sync(0xffffffffu, i < end && key > prefix);
+      const uint32_t equal = __ballot_sync(0xffffffffu, i < end && key == prefix);
+      const int my_ties = ties + __popc(equal & below);
+      const int slot = at + __popc(above & below) + min(my_ties, left);
+      if (((above >> lane & 1u) || ((equal >> lane & 1u) && my_ties < left)) && slot >= first && slot < last)
+        list[slot] = start + i;
+      at += __popc(above);
+      ties += __popc(equal);
+    }
   }
   }
   __syncthreads();  // the share's list is complete
