@@ -14,78 +14,105 @@ namespace lazy {
 namespace {
 
 // ---- general form: CUDA cores, any storage type and head width -------------------------------------------------
-// 64 x 64 tiles of logits, 256 threads with 4 x 4 each, the head taken 32 columns at a time through shared memory.
-constexpr int MG_T = 64, MG_K = 32, MG_THREADS = 256;
+// 32 rows of one side stay in shared memory, 64-row tiles of the other stream past them through two buffers; 256
+// threads hold 2 x 4 logits each and read both sides 16 bytes at a time (rows are padded by 16 bytes: no conflicts).
+// Small tiles and a cluster that shares the streamed tiles keep a short prompt from running on a few SMs: three prompts of
+// 278 rows in all, 4 heads of 64 in fp32, took 48.7 us with 64 x 64 tiles and one CTA per tile.
+constexpr int MG_A = 32, MG_B = 64, MG_THREADS = 256, MG_MAX_CLUSTER = 8;
 
-template <typename T>
-__device__ __forceinline__ void mg_load(const T *row, int c0, int head_dim, float *dst) {
-  // eight threads per row, four columns each; a row that does not exist reads as zeros
-  const int c = (threadIdx.x & 7) * 4;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) dst[c + i] = row && c0 + c + i < head_dim ? Elem<T>::to_f(row[c0 + c + i]) : 0.f;
+struct MassGeneralShared {
+  float m[MG_A], l[MG_A];  // this CTA's part, read by the cluster
+};
+
+// Rows [r0, r0 + ROWS) of one side into shared memory; row_of(r) gives a row or NULL (reads as zeros).
+template <typename T, int ROWS, typename RowOf>
+__device__ __forceinline__ void mg_load(T *dst, int head_dim, RowOf row_of) {
+  constexpr int V = Elem<T>::kPerVec;
+  const int pieces = head_dim / V, pitch = head_dim + V;
+  for (int i = threadIdx.x; i < ROWS * pieces; i += MG_THREADS) {
+    const int r = i / pieces, c = i - r * pieces;
+    const T *row = row_of(r);
+    const uint32_t to = smem_u32(dst + r * pitch + c * V);
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row ? row + c * V : dst), "r"(row ? 16 : 0)
+                 : "memory");
+  }
 }
 
-// grid (tiles of the stationary side, n_kv_heads, n_seqs).  PASS 1: stationary lanes, streamed keys.  PASS 2:
+// grid (n_kv_heads * cluster, tiles of the stationary side, n_seqs).  PASS 1: stationary lanes, streamed keys.  PASS 2:
 // stationary keys, streamed lanes.
 template <typename T, int PASS>
 __global__ void __launch_bounds__(MG_THREADS)
 mass_general_kernel(const T *__restrict__ q, int ldq, const T *__restrict__ k, int ldkv,
                     const int32_t *__restrict__ cu, int max_len, int n_total, int group, int head_dim, int window,
                     float *lse, float *__restrict__ mass, DevStatus *status) {
-  __shared__ float sa[MG_T][MG_K + 1], sb[MG_T][MG_K + 1];
-  const int g = blockIdx.y, s = blockIdx.z;
+  constexpr int V = Elem<T>::kPerVec;
+  extern __shared__ __align__(128) uint8_t mg_smem[];
+  __shared__ MassGeneralShared sh;
+  const int rank = (int)co_cluster_rank(), csize = (int)co_cluster_size();
+  const int g = blockIdx.x / csize, s = blockIdx.z, pitch = head_dim + V;
+  if (PASS == 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int start, n;
-  if (!co_span(cu, s, n_total, max_len, status, W_MASS, start, n)) return;
+  if (!co_span(cu, s, n_total, max_len, status, W_MASS, start, n)) return;  // the whole cluster alike
   const int first = window > 0 ? max(n - window, 0) : 0;  // rows [first, n) accumulate
   const int n_lanes = (n - first) * group;
-  const int n_a = PASS == 1 ? n_lanes : n, a0 = blockIdx.x * MG_T;
+  const int n_a = PASS == 1 ? n_lanes : n, a0 = blockIdx.y * MG_A;
   if (a0 >= n_a) return;
-  float *lse_g = lse + ((size_t)g * n_total + start + first) * group;  // lane f of this sequence at lse_g[f]
+  const float *lse_g = lse + ((size_t)g * n_total + start + first) * group;  // lane f of this sequence at lse_g[f]
   const float scale = rsqrtf((float)head_dim) * CO_LOG2E;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  // keys [b_begin, b_end) or lanes [b_begin, b_end) that matter to this tile
-  int b_begin = 0, b_end;
-  if (PASS == 1) b_end = min(n, first + (min(a0 + MG_T, n_a) - 1) / group + 1);
+  // streamed rows [all0, all1) that matter to this tile, and this CTA's share of them in whole tiles
+  int all0 = 0, all1;
+  if (PASS == 1) all1 = min(n, first + (min(a0 + MG_A, n_a) - 1) / group + 1);
   else {
-    b_begin = max(a0 - first, 0) * group;  // the first lane whose row sees key a0
-    b_end = n_lanes;
+    all0 = max(a0 - first, 0) * group;  // the first lane whose row sees key a0
+    all1 = n_lanes;
   }
+  const int tiles = (all1 - all0 + MG_B - 1) / MG_B, per = (tiles + csize - 1) / csize;
+  const int b_begin = min(all0 + rank * per * MG_B, all1), b_end = min(b_begin + per * MG_B, all1);
   auto lane_row = [&](int f) -> const T * {
     return f < n_lanes ? q + (size_t)(start + first + f / group) * ldq + (size_t)(g * group + f % group) * head_dim : nullptr;
   };
   auto key_row = [&](int j) -> const T * { return j < n ? k + (size_t)(start + j) * ldkv + (size_t)g * head_dim : nullptr; };
-  float m[4], l[4];
+  T *sa = reinterpret_cast<T *>(mg_smem), *sb = sa + MG_A * pitch;
+  auto load_b = [&](int b0, int buf) {
+    if (b0 < b_end)
+      mg_load<T, MG_B>(sb + buf * MG_B * pitch, head_dim, [&](int r) { return PASS == 1 ? key_row(b0 + r) : lane_row(b0 + r); });
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  mg_load<T, MG_A>(sa, head_dim, [&](int r) { return PASS == 1 ? lane_row(a0 + r) : key_row(a0 + r); });
+  load_b(b_begin, 0);
+  if (PASS == 2) asm volatile("griddepcontrol.wait;" ::: "memory");  // the log-sum-exps of pass 1
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  int buf = 0;
+  for (int b0 = b_begin; b0 < b_end; b0 += MG_B, buf ^= 1) {
+    load_b(b0 + MG_B, buf ^ 1);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncthreads();
+    const T *pa = sa + ty * 2 * pitch, *pb = sb + (buf * MG_B + tx) * pitch;
+    float x[2][4] = {};
+    for (int c = 0; c < head_dim; c += V) {
+      float av[2][V], bv[4][V];
+      Vec16<T> t;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    m[i] = -INFINITY;
-    l[i] = 0.f;
-  }
-  for (int b0 = b_begin; b0 < b_end; b0 += MG_T) {
-    float x[4][4] = {};
-    for (int c0 = 0; c0 < head_dim; c0 += MG_K) {
-      __syncthreads();
-      for (int r = threadIdx.x >> 3; r < MG_T; r += MG_THREADS / 8) {
-        mg_load<T>(PASS == 1 ? lane_row(a0 + r) : key_row(a0 + r), c0, head_dim, sa[r]);
-        mg_load<T>(PASS == 1 ? key_row(b0 + r) : lane_row(b0 + r), c0, head_dim, sb[r]);
+      for (int i = 0; i < 2; ++i) {
+        t.load(pa + i * pitch + c);
+        t.unpack(av[i]);
       }
-      __syncthreads();
-#pragma unroll 8
-      for (int c = 0; c < MG_K; ++c) {
-        float av[4], bv[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          av[i] = sa[ty * 4 + i][c];
-          bv[i] = sb[tx + i * 16][c];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[i][j] = fmaf(av[i], bv[j], x[i][j]);
+      for (int j = 0; j < 4; ++j) {
+        t.load(pb + j * 16 * pitch + c);
+        t.unpack(bv[j]);
       }
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[i][j] = fmaf(av[i][e], bv[j][e], x[i][j]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int a = a0 + ty * 4 + i;
+    for (int i = 0; i < 2; ++i) {
+      const int a = a0 + ty * 2 + i;
       if (PASS == 1) {
         const int row = first + a / group;
         float mt = m[i];
@@ -109,10 +136,11 @@ mass_general_kernel(const T *__restrict__ q, int ldq, const T *__restrict__ k, i
         }
       }
     }
+    __syncthreads();  // the buffer may be filled again
   }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int a = a0 + ty * 4 + i;
+  for (int i = 0; i < 2; ++i) {
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) {
       const float lo = __shfl_xor_sync(0xffffffffu, l[i], o);
@@ -125,11 +153,45 @@ mass_general_kernel(const T *__restrict__ q, int ldq, const T *__restrict__ k, i
         l[i] += lo;
       }
     }
-    if (tx == 0 && a < n_a) {
-      if (PASS == 1) lse_g[a] = m[i] + log2f(l[i]);
-      else mass[(size_t)g * n_total + start + a] = l[i];
+    if (tx == 0) {
+      sh.m[ty * 2 + i] = m[i];
+      sh.l[ty * 2 + i] = l[i];
     }
   }
+  if (csize > 1) co_cluster_sync();
+  else __syncthreads();
+  if (rank == 0 && threadIdx.x < MG_A && a0 + (int)threadIdx.x < n_a) {
+    float mm = -INFINITY, ll = 0.f;
+    for (int r = 0; r < csize; ++r) {
+      const float lr = *co_map_shared(&sh.l[threadIdx.x], r);
+      if (PASS == 1) {
+        const float mr = *co_map_shared(&sh.m[threadIdx.x], r);
+        const float mt = fmaxf(mm, mr), ref = mt == -INFINITY ? 0.f : mt;
+        ll = ll * exp2f(mm - ref) + lr * exp2f(mr - ref);
+        mm = mt;
+      } else {
+        ll += lr;
+      }
+    }
+    const size_t a = a0 + threadIdx.x;
+    if (PASS == 1) lse[((size_t)g * n_total + start + first) * group + a] = mm + log2f(ll);
+    else mass[(size_t)g * n_total + start + a] = ll;
+  }
+  if (csize > 1) co_cluster_sync();  // nobody leaves while its part is being read
+}
+
+// CTAs per stationary tile: the next power of two that still finds room for every CTA at once (`per_sm` on an SM), while
+// each keeps at least `least` streamed tiles.
+int mass_cluster(long long tiles, int streamed, int per_sm, int least, int most) {
+  int c = 1;
+  while (c < most && tiles * c * 2 <= (long long)per_sm * sm_count() && streamed >= 2 * least * c) c *= 2;
+  return c;
+}
+
+// Tiles of `rows` that a batch can hold at most: `longest` per sequence, but no more than all rows make up.
+long long mass_tiles(long long longest, int rows, int n_seqs, long long all_rows) {
+  const long long a = longest * n_seqs, b = all_rows / rows + n_seqs;
+  return a < b ? a : b;
 }
 
 template <typename T>
@@ -138,17 +200,23 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
                  DevStatus *status) {
   const int group = n_heads / n_kv_heads;
   const int rows = window > 0 && window < max_len ? window : max_len;
-  const long long tiles = ((long long)rows * group + MG_T - 1) / MG_T;
-  if (tiles > 0x7fffffffLL) return LAZY_E_CAPACITY;
-  mass_general_kernel<T, 1><<<dim3((unsigned)tiles, n_kv_heads, n_seqs), MG_THREADS, 0, st>>>(
-      q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, lse, mass, status);
-  LAZY_COUNT_LAUNCH();
-  mass_general_kernel<T, 2><<<dim3(cdiv(max_len, MG_T), n_kv_heads, n_seqs), MG_THREADS, 0, st>>>(
-      q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, lse, mass, status);
-  LAZY_COUNT_LAUNCH();
-  return launch_ok();
+  const long long lanes = (long long)rows * group;
+  const int smem = (MG_A + 2 * MG_B) * (head_dim + Elem<T>::kPerVec) * (int)sizeof(T);
+  constexpr int MOST = (MG_A + 2 * MG_B) * (256 + Elem<T>::kPerVec) * (int)sizeof(T);
+  LAZY_TRY((co_allow_smem<mass_general_kernel<T, 1>>(MOST)));
+  LAZY_TRY((co_allow_smem<mass_general_kernel<T, 2>>(MOST)));
+  const long long lane_tiles = (lanes + MG_A - 1) / MG_A, key_tiles = cdiv(max_len, MG_A);
+  if (lane_tiles > 65535 || key_tiles > 65535) return LAZY_E_CAPACITY;
+  const int per_sm = smem <= 100 * 1024 ? 2 : 1;
+  const int c1 = mass_cluster(mass_tiles(lane_tiles, MG_A, n_seqs, n_total * (long long)group) * n_kv_heads, cdiv(max_len, MG_B),
+                              per_sm, 1, MG_MAX_CLUSTER);
+  const int c2 = mass_cluster(mass_tiles(key_tiles, MG_A, n_seqs, n_total) * n_kv_heads, (int)((lanes + MG_B - 1) / MG_B), per_sm, 1,
+                              MG_MAX_CLUSTER);
+  LAZY_TRY(co_launch(mass_general_kernel<T, 1>, dim3(n_kv_heads * c1, (unsigned)lane_tiles, n_seqs), dim3(MG_THREADS), smem,
+                     st, c1, false, q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, lse, mass, status));
+  return co_launch(mass_general_kernel<T, 2>, dim3(n_kv_heads * c2, (unsigned)key_tiles, n_seqs), dim3(MG_THREADS), smem, st,
+                   c2, true, q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, lse, mass, status);
 }
-
 
 // ---- tensor-core form: bf16, head width 64 or 128 -----------------------------------------------------------------
 // One CTA holds 128 rows of one side (pass 1: lanes, pass 2: keys) in shared memory as the M side of the product and
@@ -428,14 +496,6 @@ bool mass_tc_eligible(int dtype, int head_dim, int group) {
 }
 int mass_seq_tiles(int n_seqs, int n_total, int group) { return n_total / (MT / group) + n_seqs + 1; }
 
-// CTAs per stationary tile: the next power of two that still finds room for every CTA at once (two per SM), while each
-// keeps at least two streamed tiles.
-int mass_cluster(long long tiles, int streamed) {
-  int c = 1;
-  while (c < MT_MAX_CLUSTER && tiles * c * 2 <= 2LL * sm_count() && streamed >= 4 * c) c *= 2;
-  return c;
-}
-
 template <int HD>
 int mass_tc(cudaStream_t st, const void *q, int ldq, const void *k, int ldkv, const int32_t *cu, int n_seqs, int max_len,
             int n_total, int n_heads, int n_kv_heads, int window, float *lse, float *mass, DevStatus *status) {
@@ -448,8 +508,8 @@ int mass_tc(cudaStream_t st, const void *q, int ldq, const void *k, int ldkv, co
   const int rows = window > 0 && window < max_len ? window : max_len;
   const int lane_tiles = cdiv(rows, R), key_tiles = cdiv(max_len, MT), seq_tiles = mass_seq_tiles(n_seqs, n_total, group);
   if (lane_tiles > 65535 || key_tiles > 65535) return LAZY_E_CAPACITY;
-  const long long per_tile = (long long)n_kv_heads * n_seqs;
-  const int c1 = mass_cluster(lane_tiles * per_tile, key_tiles), c2 = mass_cluster(key_tiles * per_tile, lane_tiles);
+  const int c1 = mass_cluster(mass_tiles(lane_tiles, R, n_seqs, n_total) * n_kv_heads, key_tiles, 2, 2, MT_MAX_CLUSTER);
+  const int c2 = mass_cluster(mass_tiles(key_tiles, MT, n_seqs, n_total) * n_kv_heads, lane_tiles, 2, 2, MT_MAX_CLUSTER);
   LAZY_TRY(co_launch(mass_tc_kernel<1, HD>, dim3(n_kv_heads * c1, lane_tiles, n_seqs), dim3(MT_THREADS),
                      mass_smem_bytes<HD>(), st, c1, false, mq, mk, cu, max_len, n_total, group, R, window, lse, seq_tiles,
                      mass, status));
