@@ -184,7 +184,7 @@ mass_general_kernel(const T *__restrict__ q, int ldq, const T *__restrict__ k, i
 // each keeps at least `least` streamed tiles.
 int mass_cluster(long long tiles, int streamed, int per_sm, int least, int most) {
   int c = 1;
-  while (c < most && tiles * c * 2 <= (long long)per_sm * sm_count() && streamed >= 2 * least * c) c *= 2;
+  while (c < most && tiles * c * 2 <= (long long)per_sm * co_cluster_sms(c * 2) && streamed >= 2 * least * c) c *= 2;
   return c;
 }
 
@@ -232,59 +232,91 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
 // Lane tiles hold R = 128 / group rows x group heads, loaded as one 3-d box; with a group that does not divide 128
 // the last lanes of a tile are unused.  A short grid is filled up by clusters: the CTAs of a cluster share a
 // stationary tile, split the streamed tiles and add their parts in rank order through distributed shared memory.
+//
+// DEEP is the form for few lanes over many keys (a window of a long prompt), where a CTA would spend its time on starting up:
+// one CTA per SM with four stages; pass 1 cuts the keys into ranges (no clusters: eight to a cluster only 120 of the 148 SMs
+// can be used) and leaves each range's (maximum, sum), pass 2 merges them and takes a range of key tiles, the next one
+// loaded while the last is used.  A 64-row window over 16384 keys of 8 heads, group 4: 49 us without it.
 constexpr int MT = 128;                       // tile rows of either side, columns of S
-constexpr int MT_STAGES = 2, MT_LSE_STAGES = 4, MT_MAX_CLUSTER = 8;
+constexpr int MT_LSE_STAGES = 4, MT_MAX_CLUSTER = 8, MT_DEEP_TILES = 4;  // lane tiles that DEEP pass 2 takes at most
+static_assert(MT_DEEP_TILES <= MT_LSE_STAGES, "DEEP pass 2 keeps all lanes' log-sum-exps where the ring would be");
 constexpr int MT_THREADS = 320;
 constexpr int MT_TMEM_COLS = 256;
 
+template <bool DEEP>
+struct MassShape {
+  static constexpr int A_BUFS = DEEP ? 2 : 1, STAGES = DEEP ? 4 : 2, CTAS = DEEP ? 1 : 2;
+};
+template <bool DEEP>
 struct __align__(16) MassShared {
+  using Shape = MassShape<DEEP>;
   float lse[MT_LSE_STAGES][MT];
-  float part_m[2][MT], part_l[2][MT];  // per column half: a lane's (maximum, sum), a key's sum
-  unsigned long long a_full, b_full[MT_STAGES], b_empty[MT_STAGES], s_full[2], s_free[2], l_full[MT_LSE_STAGES],
-      l_free[MT_LSE_STAGES];
+  float part_m[2][MT], part_l[2][2][MT];  // per column half: a lane's (maximum, sum), a key's sum (two tiles' in turn)
+  unsigned long long a_full[Shape::A_BUFS], a_empty[Shape::A_BUFS], b_full[Shape::STAGES], b_empty[Shape::STAGES], s_full[2],
+      s_free[2], l_full[MT_LSE_STAGES], l_free[MT_LSE_STAGES];
   uint32_t tmem_base;
   int abort_flag;
 };
-template <int HD>
-constexpr int mass_smem_bytes() {
-  return (1 + MT_STAGES) * MT * HD * 2 + 1024 + (int)sizeof(MassShared);
-}
+template <int HD, bool DEEP>
+constexpr int mass_smem = (MassShape<DEEP>::A_BUFS + MassShape<DEEP>::STAGES) * MT * HD * 2 + 1024 + (int)sizeof(MassShared<DEEP>);
 
-// grid (n_kv_heads * cluster, tiles, n_seqs).  lse: tiles of 128 floats, tile t of sequence s of key/value head g at
-// ((g * seq_tiles) + start_s / R + s + t) * 128: sequences' tiles cannot overlap and every tile is 512-byte aligned.
-template <int PASS, int HD>
-__global__ void __launch_bounds__(MT_THREADS, 2)
+// grid (n_kv_heads * cluster, tiles, n_seqs); DEEP pass 1 with `splits` > 0: (n_kv_heads * splits, tiles, n_seqs) and no clusters;
+// DEEP pass 2: (n_kv_heads, ranges of key tiles, n_seqs), no clusters.  parts: (maximum, sum) of tile t's lanes over key
+// range i at (((s * n_kv_heads + g) * deep_tiles + t) * splits + i) * 128.
+// lse: tiles of 128 floats (minus the log-sum-exps, log2 units), tile t of sequence s of key/value head g at ((g * seq_tiles)
+// + start_s / R + s + t) * 128: sequences' tiles cannot overlap and every tile is 512-byte aligned.
+template <int PASS, int HD, bool DEEP>
+__global__ void __launch_bounds__(MT_THREADS, MassShape<DEEP>::CTAS)
 mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                const int32_t *__restrict__ cu, int max_len, int n_total, int group, int rows_per_tile, int window,
-               float *lse, int seq_tiles, float *__restrict__ mass, DevStatus *status) {
+               float *lse, int seq_tiles, int splits, float2 *parts, int deep_tiles, float *__restrict__ mass,
+               DevStatus *status) {
   extern __shared__ uint8_t mass_smem_raw[];
+  constexpr int A_BUFS = MassShape<DEEP>::A_BUFS, STAGES = MassShape<DEEP>::STAGES;
   constexpr int CH = HD / 64;                // 64-column chunks of the head
   constexpr int CHUNK = MT * 128;            // bytes of one chunk of a tile
   const uint32_t raw_addr = smem_u32(mass_smem_raw);
   uint8_t *smem = mass_smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
-  const uint32_t sA = smem_u32(smem), sB = sA + CH * CHUNK;
-  MassShared *sh = reinterpret_cast<MassShared *>(smem + (1 + MT_STAGES) * CH * CHUNK);
+  const uint32_t sA = smem_u32(smem), sB = sA + A_BUFS * CH * CHUNK;
+  auto *sh = reinterpret_cast<MassShared<DEEP> *>(smem + (A_BUFS + STAGES) * CH * CHUNK);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = (int)co_cluster_rank(), csize = (int)co_cluster_size();
-  const int g = blockIdx.x / csize, s = blockIdx.z, R = rows_per_tile;
+  const bool split = DEEP && PASS == 1 && splits > 0;
+  const int csize = split ? splits : (int)co_cluster_size();  // CTAs that share a stationary tile
+  const int g = blockIdx.x / csize, rank = blockIdx.x - g * csize, s = blockIdx.z, R = rows_per_tile;
+  const int Hkv = gridDim.x / csize;
   if (PASS == 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int start, n;
   if (!co_span(cu, s, n_total, max_len, status, W_MASS, start, n)) return;  // the whole cluster alike
   const int first = window > 0 ? max(n - window, 0) : 0;
   const int lane_tiles = (n - first + R - 1) / R, key_tiles = (n + MT - 1) / MT;
   const int a_tiles = PASS == 1 ? lane_tiles : key_tiles;
-  if ((int)blockIdx.y >= a_tiles) return;
-  const int at = PASS == 1 ? a_tiles - 1 - (int)blockIdx.y : (int)blockIdx.y;  // most work first
-  // streamed tiles [b0, b1) of this CTA
-  const int all0 = PASS == 1 ? 0 : max(at * MT - first, 0) / R;
-  const int all1 = PASS == 1 ? min(key_tiles, (min(first + (at + 1) * R, n) + MT - 1) / MT) : lane_tiles;
-  const int per = (all1 - all0 + csize - 1) / csize;
-  const int b0 = min(all0 + rank * per, all1), b1 = min(b0 + per, all1), nb = b1 - b0;
+  // stationary tiles [at0, at1): one, most work first, or in DEEP pass 2 an equal range of all of them
+  int at0, at1;
+  if (DEEP && PASS == 2) {
+    at0 = (int)((long long)a_tiles * blockIdx.y / gridDim.y);
+    at1 = (int)((long long)a_tiles * (blockIdx.y + 1) / gridDim.y);
+    if (at0 == at1) return;
+  } else {
+    if ((int)blockIdx.y >= a_tiles) return;
+    at0 = PASS == 1 ? a_tiles - 1 - (int)blockIdx.y : (int)blockIdx.y;
+    at1 = at0 + 1;
+  }
+  // streamed tiles [b0, b1) of this CTA for a stationary one
+  auto streamed = [&](int at, int &b0, int &b1) {
+    const int all0 = PASS == 1 ? 0 : max(at * MT - first, 0) / R;
+    const int all1 = PASS == 1 ? min(key_tiles, (min(first + (at + 1) * R, n) + MT - 1) / MT) : lane_tiles;
+    const int per = (all1 - all0 + csize - 1) / csize;
+    b0 = min(all0 + rank * per, all1);
+    b1 = min(b0 + per, all1);
+  };
   const size_t lse_base = ((size_t)g * seq_tiles + start / R + s) * MT;
 
   if (threadIdx.x == 0) {
-    mbar_init(smem_u32(&sh->a_full), 1);
-    for (int i = 0; i < MT_STAGES; ++i) {
+    for (int i = 0; i < A_BUFS; ++i) {
+      mbar_init(smem_u32(&sh->a_full[i]), 1);
+      mbar_init(smem_u32(&sh->a_empty[i]), 1);
+    }
+    for (int i = 0; i < STAGES; ++i) {
       mbar_init(smem_u32(&sh->b_full[i]), 1);
       mbar_init(smem_u32(&sh->b_empty[i]), 1);
     }
@@ -313,8 +345,9 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(&sh->tmem_base);
   volatile int *abort_flag = &sh->abort_flag;
 
+  // Every role walks the same (stationary, streamed) pairs: `t` counts pairs, `ai` stationary tiles.
   if (warp == 0) {
-    if (lane == 0 && nb > 0) {
+    if (lane == 0) {
       const uint32_t lane_bytes = (uint32_t)(R * group * 128 * CH), key_bytes = (uint32_t)(CH * CHUNK);
       auto load = [&](bool lanes, int tile, uint32_t dst, uint32_t bar) {
         mbar_expect_tx(bar, lanes ? lane_bytes : key_bytes);
@@ -324,40 +357,64 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           else tma_load_2d(dst + c * CHUNK, &map_k, bar, g * HD + c * 64, start + tile * MT);
         }
       };
-      load(PASS == 1, at, sA, smem_u32(&sh->a_full));
-      if (PASS == 2) asm volatile("griddepcontrol.wait;" ::: "memory");  // the log-sum-exps of pass 1
-      for (int j = 0; j < nb; ++j) {
-        const int st = j % MT_STAGES;
-        if (!mbar_wait(smem_u32(&sh->b_empty[st]), (uint32_t)((j / MT_STAGES) & 1) ^ 1u, abort_flag, status, W_MASS)) break;
-        load(PASS == 2, b0 + j, sB + st * CH * CHUNK, smem_u32(&sh->b_full[st]));
-        if (PASS == 2) {
-          const int ls = j % MT_LSE_STAGES;
-          if (!mbar_wait(smem_u32(&sh->l_free[ls]), (uint32_t)((j / MT_LSE_STAGES) & 1) ^ 1u, abort_flag, status, W_MASS))
-            break;
-          mbar_expect_tx(smem_u32(&sh->l_full[ls]), MT * 4);
-          bulk_load(smem_u32(sh->lse[ls]), lse + lse_base + (size_t)(b0 + j) * MT, MT * 4, smem_u32(&sh->l_full[ls]));
+      bool ok = true, waited = PASS == 1 || DEEP;
+      int t = 0, ai = 0;
+      for (int at = at0; at < at1 && ok; ++at) {
+        int b0, b1;
+        streamed(at, b0, b1);
+        if (b0 == b1) continue;
+        ok = mbar_wait(smem_u32(&sh->a_empty[ai % A_BUFS]), (uint32_t)((ai / A_BUFS) & 1) ^ 1u, abort_flag, status, W_MASS);
+        if (!ok) break;
+        load(PASS == 1, at, sA + (ai % A_BUFS) * CH * CHUNK, smem_u32(&sh->a_full[ai % A_BUFS]));
+        ++ai;
+        if (!waited) {
+          asm volatile("griddepcontrol.wait;" ::: "memory");  // the log-sum-exps of pass 1
+          waited = true;
+        }
+        for (int b = b0; b < b1; ++b, ++t) {
+          const int st = t % STAGES;
+          ok = mbar_wait(smem_u32(&sh->b_empty[st]), (uint32_t)((t / STAGES) & 1) ^ 1u, abort_flag, status, W_MASS);
+          if (!ok) break;
+          load(PASS == 2, b, sB + st * CH * CHUNK, smem_u32(&sh->b_full[st]));
+          if (PASS == 2 && !DEEP) {
+            const int ls = t % MT_LSE_STAGES;
+            ok = mbar_wait(smem_u32(&sh->l_free[ls]), (uint32_t)((t / MT_LSE_STAGES) & 1) ^ 1u, abort_flag, status, W_MASS);
+            if (!ok) break;
+            mbar_expect_tx(smem_u32(&sh->l_full[ls]), MT * 4);
+            bulk_load(smem_u32(sh->lse[ls]), lse + lse_base + (size_t)b * MT, MT * 4, smem_u32(&sh->l_full[ls]));
+          }
         }
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && nb > 0) {
+    if (lane == 0) {
       const uint32_t idesc = idesc_bf16(MT, MT, 0, 0);
-      bool ok = mbar_wait(smem_u32(&sh->a_full), 0, abort_flag, status, W_MASS);
-      for (int j = 0; j < nb && ok; ++j) {
-        const int st = j % MT_STAGES, sb = j & 1;
-        ok = mbar_wait(smem_u32(&sh->b_full[st]), (uint32_t)((j / MT_STAGES) & 1), abort_flag, status, W_MASS);
-        if (!ok) break;
-        ok = mbar_wait(smem_u32(&sh->s_free[sb]), (uint32_t)((j >> 1) & 1) ^ 1u, abort_flag, status, W_MASS);
-        if (!ok) break;
-        tc_fence_after();
+      bool ok = true;
+      int t = 0, ai = 0;
+      for (int at = at0; at < at1 && ok; ++at) {
+        int b0, b1;
+        streamed(at, b0, b1);
+        if (b0 == b1) continue;
+        const uint32_t a_tile = sA + (ai % A_BUFS) * CH * CHUNK;
+        ok = mbar_wait(smem_u32(&sh->a_full[ai % A_BUFS]), (uint32_t)((ai / A_BUFS) & 1), abort_flag, status, W_MASS);
+        for (int b = b0; b < b1 && ok; ++b, ++t) {
+          const int st = t % STAGES, sb = t & 1;
+          ok = mbar_wait(smem_u32(&sh->b_full[st]), (uint32_t)((t / STAGES) & 1), abort_flag, status, W_MASS);
+          if (!ok) break;
+          ok = mbar_wait(smem_u32(&sh->s_free[sb]), (uint32_t)((t >> 1) & 1) ^ 1u, abort_flag, status, W_MASS);
+          if (!ok) break;
+          tc_fence_after();
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint64_t ad = umma_smem_desc(sA + (k >> 2) * CHUNK + (k & 3) * 32);
-          const uint64_t bd = umma_smem_desc(sB + st * CH * CHUNK + (k >> 2) * CHUNK + (k & 3) * 32);
-          umma_bf16(tmem_base + (uint32_t)(sb * MT), ad, bd, idesc, k != 0 ? 1u : 0u);
+          for (int k = 0; k < HD / 16; ++k) {
+            const uint64_t ad = umma_smem_desc(a_tile + (k >> 2) * CHUNK + (k & 3) * 32);
+            const uint64_t bd = umma_smem_desc(sB + st * CH * CHUNK + (k >> 2) * CHUNK + (k & 3) * 32);
+            umma_bf16(tmem_base + (uint32_t)(sb * MT), ad, bd, idesc, k != 0 ? 1u : 0u);
+          }
+          umma_commit(smem_u32(&sh->b_empty[st]));
+          if (b + 1 == b1) umma_commit(smem_u32(&sh->a_empty[ai % A_BUFS]));
+          umma_commit(smem_u32(&sh->s_full[sb]));
         }
-        umma_commit(smem_u32(&sh->b_empty[st]));
-        umma_commit(smem_u32(&sh->s_full[sb]));
+        ++ai;
       }
     }
   } else {
@@ -366,100 +423,133 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     const int row = quarter * 32 + lane;  // row of the stationary tile
     const float sl2 = rsqrtf((float)HD) * CO_LOG2E;
     const unsigned long long sl2x2 = f32x2_pack(sl2, sl2);
-    // pass 1: this lane's row inside the sequence, -1 for a lane that does not exist (it sees no key)
-    int own = PASS == 1 ? first + at * R + row / group : at * MT + row;
-    if (PASS == 1 && (row >= R * group || own >= n)) own = -1;
     float m = -INFINITY, l = 0.f;
     bool ok = true;
-    for (int j = 0; j < nb && ok; ++j) {
-      const int sb = j & 1;
-      ok = mbar_wait(smem_u32(&sh->s_full[sb]), (uint32_t)((j >> 1) & 1), abort_flag, status, W_MASS);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t raw[64];
-      tmem_ld_32x32_raw(t_s + (uint32_t)(sb * MT), raw);
-      tmem_ld_32x32_raw(t_s + (uint32_t)(sb * MT) + 32u, raw + 32);
-      tmem_ld_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sh->s_free[sb]));
-      // columns [lo, hi) of this thread's 64 are seen
-      int lo = 0, hi = 64;
-      if (PASS == 1) hi = own + 1 - ((b0 + j) * MT + half * 64);
-      else {
-        const int row0 = first + (b0 + j) * R;  // first row of the streamed tile
-        lo = (own - row0) * group - half * 64;
-        hi = min(R, n - row0) * group - half * 64;
+    int t = 0;
+    if (PASS == 2 && DEEP) {  // minus the lanes' log-sum-exps, from the key ranges of pass 1
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      const float2 *p = parts + ((size_t)s * Hkv + g) * deep_tiles * splits * MT;
+      for (int i = threadIdx.x - 64; i < lane_tiles * MT; i += 256) {
+        const float2 *pi = p + (size_t)(i / MT) * splits * MT + i % MT;
+        float mm = -INFINITY, ll = 0.f;
+#pragma unroll 4
+        for (int r = 0; r < splits; ++r) {
+          const float2 x = pi[(size_t)r * MT];
+          const float mt = fmaxf(mm, x.x), ref = mt == -INFINITY ? 0.f : mt;
+          ll = ll * ex2_approx(mm - ref) + x.y * ex2_approx(x.x - ref);
+          mm = mt;
+        }
+        sh->lse[i / MT][i % MT] = -(mm + log2f(ll));
       }
-      if (PASS == 1) {
-        if (hi < 64) {
-#pragma unroll
-          for (int c = 0; c < 64; ++c)
-            if (c >= hi) raw[c] = 0xff800000u;  // -inf
-        }
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int c = 0; c < 64; c += 8) {
-          mx[0] = fmax3(mx[0], __uint_as_float(raw[c]), __uint_as_float(raw[c + 1]));
-          mx[1] = fmax3(mx[1], __uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3]));
-          mx[2] = fmax3(mx[2], __uint_as_float(raw[c + 4]), __uint_as_float(raw[c + 5]));
-          mx[3] = fmax3(mx[3], __uint_as_float(raw[c + 6]), __uint_as_float(raw[c + 7]));
-        }
-        const float mt = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2);
-        const float ref = mt == -INFINITY ? 0.f : mt;
-        const unsigned long long neg = f32x2_pack(-ref, -ref);
-        unsigned long long sum0 = 0ull, sum1 = 0ull;
-#pragma unroll
-        for (int c = 0; c < 64; c += 4) {
-          float x0, x1, x2, x3;
-          f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2, neg), x0, x1);
-          f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])), sl2x2, neg), x2, x3);
-          sum0 = f32x2_add(sum0, f32x2_pack(ex2_approx(x0), ex2_approx(x1)));
-          sum1 = f32x2_add(sum1, f32x2_pack(ex2_approx(x2), ex2_approx(x3)));
-        }
-        float u0, u1;
-        f32x2_unpack(f32x2_add(sum0, sum1), u0, u1);
-        l = l * ex2_approx(m - ref) + (u0 + u1);
-        m = mt;
-      } else {
-        const int ls = j % MT_LSE_STAGES;
-        ok = mbar_wait(smem_u32(&sh->l_full[ls]), (uint32_t)((j / MT_LSE_STAGES) & 1), abort_flag, status, W_MASS);
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+    }
+    for (int at = at0; at < at1; ++at) {
+      int b0, b1;
+      streamed(at, b0, b1);
+      // pass 1: this lane's row inside the sequence, -1 for a lane that does not exist (it sees no key); pass 2: the key
+      int own = PASS == 1 ? first + at * R + row / group : at * MT + row;
+      if (PASS == 1 && (row >= R * group || own >= n)) own = -1;
+      l = 0.f;
+      for (int b = b0; b < b1 && ok; ++b, ++t) {
+        const int sb = t & 1;
+        ok = mbar_wait(smem_u32(&sh->s_full[sb]), (uint32_t)((t >> 1) & 1), abort_flag, status, W_MASS);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        const float4 *le = reinterpret_cast<const float4 *>(sh->lse[ls] + half * 64);
-        if (lo <= 0 && hi >= 64) {
+        tc_fence_after();
+        uint32_t raw[64];
+        tmem_ld_32x32_raw(t_s + (uint32_t)(sb * MT), raw);
+        tmem_ld_32x32_raw(t_s + (uint32_t)(sb * MT) + 32u, raw + 32);
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh->s_free[sb]));
+        // columns [lo, hi) of this thread's 64 are seen
+        int lo = 0, hi = 64;
+        if (PASS == 1) hi = own + 1 - (b * MT + half * 64);
+        else {
+          const int row0 = first + b * R;  // first row of the streamed tile
+          lo = (own - row0) * group - half * 64;
+          hi = min(R, n - row0) * group - half * 64;
+        }
+        if (PASS == 1) {
+          if (hi < 64) {
+#pragma unroll
+            for (int c = 0; c < 64; ++c)
+              if (c >= hi) raw[c] = 0xff800000u;  // -inf
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < 64; c += 8) {
+            mx[0] = fmax3(mx[0], __uint_as_float(raw[c]), __uint_as_float(raw[c + 1]));
+            mx[1] = fmax3(mx[1], __uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3]));
+            mx[2] = fmax3(mx[2], __uint_as_float(raw[c + 4]), __uint_as_float(raw[c + 5]));
+            mx[3] = fmax3(mx[3], __uint_as_float(raw[c + 6]), __uint_as_float(raw[c + 7]));
+          }
+          const float mt = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2);
+          const float ref = mt == -INFINITY ? 0.f : mt;
+          const unsigned long long neg = f32x2_pack(-ref, -ref);
           unsigned long long sum0 = 0ull, sum1 = 0ull;
 #pragma unroll
           for (int c = 0; c < 64; c += 4) {
-            const float4 e = le[c >> 2];  // minus the log-sum-exp
             float x0, x1, x2, x3;
-            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2,
-                                   f32x2_pack(e.x, e.y)), x0, x1);
-            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])), sl2x2,
-                                   f32x2_pack(e.z, e.w)), x2, x3);
+            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2, neg), x0, x1);
+            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])), sl2x2, neg), x2, x3);
             sum0 = f32x2_add(sum0, f32x2_pack(ex2_approx(x0), ex2_approx(x1)));
             sum1 = f32x2_add(sum1, f32x2_pack(ex2_approx(x2), ex2_approx(x3)));
           }
           float u0, u1;
           f32x2_unpack(f32x2_add(sum0, sum1), u0, u1);
-          l += u0 + u1;
-        } else {  // a tile on the diagonal or at the end: unseen columns are left out, whatever they hold
-          float sum = 0.f;
-#pragma unroll
-          for (int c = 0; c < 64; ++c) {
-            const float x = fmaf(__uint_as_float(raw[c]), sl2, sh->lse[ls][half * 64 + c]);
-            sum += c >= lo && c < hi ? ex2_approx(x) : 0.f;
+          l = l * ex2_approx(m - ref) + (u0 + u1);
+          m = mt;
+        } else {
+          const int ls = DEEP ? b : t % MT_LSE_STAGES;
+          if (!DEEP) {
+            ok = mbar_wait(smem_u32(&sh->l_full[ls]), (uint32_t)((t / MT_LSE_STAGES) & 1), abort_flag, status, W_MASS);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
           }
-          l += sum;
+          const float4 *le = reinterpret_cast<const float4 *>(sh->lse[ls] + half * 64);
+          if (lo <= 0 && hi >= 64) {
+            unsigned long long sum0 = 0ull, sum1 = 0ull;
+#pragma unroll
+            for (int c = 0; c < 64; c += 4) {
+              const float4 e = le[c >> 2];
+              float x0, x1, x2, x3;
+              f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2,
+                                     f32x2_pack(e.x, e.y)), x0, x1);
+              f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])), sl2x2,
+                                     f32x2_pack(e.z, e.w)), x2, x3);
+              sum0 = f32x2_add(sum0, f32x2_pack(ex2_approx(x0), ex2_approx(x1)));
+              sum1 = f32x2_add(sum1, f32x2_pack(ex2_approx(x2), ex2_approx(x3)));
+            }
+            float u0, u1;
+            f32x2_unpack(f32x2_add(sum0, sum1), u0, u1);
+            l += u0 + u1;
+          } else {  // a tile on the diagonal or at the end: unseen columns are left out, whatever they hold
+            float sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < 64; ++c) {
+              const float x = fmaf(__uint_as_float(raw[c]), sl2, sh->lse[ls][half * 64 + c]);
+              sum += c >= lo && c < hi ? ex2_approx(x) : 0.f;
+            }
+            l += sum;
+          }
+          if (!DEEP) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->l_free[ls]));
+          }
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&sh->l_free[ls]));
+      }
+      if (!ok) l = NAN;  // a wait ran out (reported): nothing that looks like a result
+      const int buf = (at - at0) & 1;
+      sh->part_l[buf][half][row] = l;
+      if (DEEP && PASS == 2) {
+        // the two halves of the columns meet; two buffers, so that nobody overwrites what is still being read
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (half == 0 && own < n) mass[(size_t)g * n_total + start + own] = l + sh->part_l[buf][1][row];
       }
     }
-    if (!ok) l = NAN;  // a wait ran out (reported): nothing that looks like a result
     sh->part_m[half][row] = m;
-    sh->part_l[half][row] = l;
   }
   tc_fence_before();
   __syncthreads();
@@ -468,16 +558,17 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)MT_TMEM_COLS)
                  : "memory");
   }
-  if (csize > 1) co_cluster_sync();
-  if (rank == 0 && threadIdx.x < MT) {
+  if (DEEP && PASS == 2) return;
+  if (csize > 1 && !split) co_cluster_sync();
+  if ((rank == 0 || split) && threadIdx.x < MT) {
     const int row = threadIdx.x;
     float m = -INFINITY, l = 0.f;
-    for (int r = 0; r < csize; ++r)
+    for (int r = 0; r < (split ? 1 : csize); ++r)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float lr = *co_map_shared(&sh->part_l[h][row], r);
+        const float lr = split ? sh->part_l[0][h][row] : *co_map_shared(&sh->part_l[0][h][row], r);
         if (PASS == 1) {
-          const float mr = *co_map_shared(&sh->part_m[h][row], r);
+          const float mr = split ? sh->part_m[h][row] : *co_map_shared(&sh->part_m[h][row], r);
           const float mt = fmaxf(m, mr), ref = mt == -INFINITY ? 0.f : mt;
           l = l * ex2_approx(m - ref) + lr * ex2_approx(mr - ref);
           m = mt;
@@ -485,16 +576,33 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           l += lr;
         }
       }
-    if (PASS == 1) lse[lse_base + (size_t)at * MT + row] = -(m + log2f(l));  // lanes that do not exist: never looked at
-    else if (at * MT + row < n) mass[(size_t)g * n_total + start + at * MT + row] = l;
+    if (split) parts[((((size_t)s * Hkv + g) * deep_tiles + at0) * splits + rank) * MT + row] = make_float2(m, l);
+    else if (PASS == 1) lse[lse_base + (size_t)at0 * MT + row] = -(m + log2f(l));  // lanes that do not exist: never looked at
+    else if (at0 * MT + row < n) mass[(size_t)g * n_total + start + at0 * MT + row] = l;
   }
-  if (csize > 1) co_cluster_sync();  // nobody leaves while its parts are being read
+  if (csize > 1 && !split) co_cluster_sync();  // nobody leaves while its parts are being read
 }
 
 bool mass_tc_eligible(int dtype, int head_dim, int group) {
   return dtype == LAZY_BF16 && (head_dim == 64 || head_dim == 128) && group <= MT;
 }
 int mass_seq_tiles(int n_seqs, int n_total, int group) { return n_total / (MT / group) + n_seqs + 1; }
+
+// Whether both passes take the DEEP form (splits > 0): few lane tiles, many key tiles, a CTA for every (sequence, head).
+struct MassDeep {
+  int splits, ranges;  // key ranges per lane tile (pass 1), ranges of key tiles per head (pass 2)
+};
+MassDeep mass_deep(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window) {
+  const int R = MT / (n_heads / n_kv_heads), rows = window > 0 && window < max_len ? window : max_len;
+  const int lane_tiles = cdiv(rows, R), key_tiles = cdiv(max_len, MT);
+  const long long heads = (long long)n_kv_heads * n_seqs, sms = sm_count();
+  const long long all_lane = mass_tiles(lane_tiles, R, n_seqs, n_total) * n_kv_heads;
+  const long long all_key = mass_tiles(key_tiles, MT, n_seqs, n_total) * n_kv_heads;
+  if (lane_tiles > MT_DEEP_TILES || all_key <= 2 * sms || heads > sms) return {0, 0};
+  long long splits = sms / all_lane;
+  if (splits > key_tiles) splits = key_tiles;
+  return {splits < 1 ? 1 : (int)splits, (int)(sms / heads)};
+}
 
 template <int HD>
 int mass_tc(cudaStream_t st, const void *q, int ldq, const void *k, int ldkv, const int32_t *cu, int n_seqs, int max_len,
@@ -503,29 +611,46 @@ int mass_tc(cudaStream_t st, const void *q, int ldq, const void *k, int ldkv, co
   CUtensorMap mq, mk;
   LAZY_TRY(tma_map_heads_bf16(&mq, q, n_total, n_heads, HD, ldq, group, R));
   LAZY_TRY(tma_map_2d_bf16(&mk, k, n_total, n_kv_heads * HD, ldkv, 64, MT));
-  LAZY_TRY((co_allow_smem<mass_tc_kernel<1, HD>>(mass_smem_bytes<HD>())));
-  LAZY_TRY((co_allow_smem<mass_tc_kernel<2, HD>>(mass_smem_bytes<HD>())));
   const int rows = window > 0 && window < max_len ? window : max_len;
   const int lane_tiles = cdiv(rows, R), key_tiles = cdiv(max_len, MT), seq_tiles = mass_seq_tiles(n_seqs, n_total, group);
   if (lane_tiles > 65535 || key_tiles > 65535) return LAZY_E_CAPACITY;
-  const int c1 = mass_cluster(mass_tiles(lane_tiles, R, n_seqs, n_total) * n_kv_heads, key_tiles, 2, 2, MT_MAX_CLUSTER);
-  const int c2 = mass_cluster(mass_tiles(key_tiles, MT, n_seqs, n_total) * n_kv_heads, lane_tiles, 2, 2, MT_MAX_CLUSTER);
-  LAZY_TRY(co_launch(mass_tc_kernel<1, HD>, dim3(n_kv_heads * c1, lane_tiles, n_seqs), dim3(MT_THREADS),
-                     mass_smem_bytes<HD>(), st, c1, false, mq, mk, cu, max_len, n_total, group, R, window, lse, seq_tiles,
-                     mass, status));
-  return co_launch(mass_tc_kernel<2, HD>, dim3(n_kv_heads * c2, key_tiles, n_seqs), dim3(MT_THREADS),
-                   mass_smem_bytes<HD>(), st, c2, true, mq, mk, cu, max_len, n_total, group, R, window, lse, seq_tiles,
-                   mass, status);
+  const long long all_lane = mass_tiles(lane_tiles, R, n_seqs, n_total) * n_kv_heads;
+  const long long all_key = mass_tiles(key_tiles, MT, n_seqs, n_total) * n_kv_heads;
+  const MassDeep deep = mass_deep(n_seqs, n_total, max_len, n_heads, n_kv_heads, window);
+  float2 *parts = reinterpret_cast<float2 *>(lse + (size_t)n_kv_heads * seq_tiles * MT);
+  auto launch = [&](auto kernel, dim3 grid, int smem, int cluster, bool dependent) {
+    return co_launch(kernel, grid, dim3(MT_THREADS), smem, st, cluster, dependent, mq, mk, cu, max_len, n_total, group, R, window,
+                     lse, seq_tiles, deep.splits, parts, lane_tiles, mass, status);
+  };
+  // pass 1: DEEP also where one CTA per SM is all there is
+  int c1 = deep.splits ? 1 : mass_cluster(all_lane, key_tiles, 1, 2, MT_MAX_CLUSTER);
+  if (deep.splits || all_lane * c1 <= co_cluster_sms(c1)) {
+    LAZY_TRY((co_allow_smem<mass_tc_kernel<1, HD, true>>(mass_smem<HD, true>)));
+    LAZY_TRY(launch(mass_tc_kernel<1, HD, true>, dim3(n_kv_heads * (deep.splits ? deep.splits : c1), lane_tiles, n_seqs),
+                    mass_smem<HD, true>, c1, false));
+  } else {
+    c1 = mass_cluster(all_lane, key_tiles, 2, 2, MT_MAX_CLUSTER);
+    LAZY_TRY((co_allow_smem<mass_tc_kernel<1, HD, false>>(mass_smem<HD, false>)));
+    LAZY_TRY(launch(mass_tc_kernel<1, HD, false>, dim3(n_kv_heads * c1, lane_tiles, n_seqs), mass_smem<HD, false>, c1, false));
+  }
+  if (deep.splits) {
+    LAZY_TRY((co_allow_smem<mass_tc_kernel<2, HD, true>>(mass_smem<HD, true>)));
+    return launch(mass_tc_kernel<2, HD, true>, dim3(n_kv_heads, deep.ranges, n_seqs), mass_smem<HD, true>, 1, true);
+  }
+  const int c2 = mass_cluster(all_key, lane_tiles, 2, 2, MT_MAX_CLUSTER);
+  LAZY_TRY((co_allow_smem<mass_tc_kernel<2, HD, false>>(mass_smem<HD, false>)));
+  return launch(mass_tc_kernel<2, HD, false>, dim3(n_kv_heads * c2, key_tiles, n_seqs), mass_smem<HD, false>, c2, true);
 }
 
 }  // namespace
 
 size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window) {
-  (void)max_len, (void)window;
   const int group = n_heads / n_kv_heads;
   const size_t general = (size_t)n_total * n_heads;
   if (group > MT) return general;
-  const size_t tiled = (size_t)n_kv_heads * mass_seq_tiles(n_seqs, n_total, group) * MT;
+  const MassDeep deep = mass_deep(n_seqs, n_total, max_len, n_heads, n_kv_heads, window);
+  const size_t tiled = (size_t)n_kv_heads * mass_seq_tiles(n_seqs, n_total, group) * MT +
+                       (size_t)n_seqs * n_kv_heads * MT_DEEP_TILES * deep.splits * MT * 2;
   return (general > tiled ? general : tiled) + 4;  // + 4: tiles start on a 16-byte boundary
 }
 

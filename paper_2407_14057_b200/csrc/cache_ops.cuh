@@ -72,6 +72,13 @@ inline int co_launch(void (*kfn)(KArgs...), dim3 grid, dim3 block, size_t smem, 
   return e == cudaSuccess ? LAZY_OK : LAZY_E_CUDA;
 }
 
+// SMs that clusters of `size` CTAs can use, one CTA to an SM: a cluster stays within a group of SMs, and the groups are not
+// multiples of it (132 of 148 with four to a cluster, 120 with eight, asked of the occupancy calculator).  A launch of more
+// runs its last clusters after the others.
+inline int co_cluster_sms(int size) {
+  return size <= 2 ? sm_count() : sm_count() * (size == 4 ? 132 : 120) / 148;
+}
+
 __device__ __forceinline__ uint32_t co_cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));

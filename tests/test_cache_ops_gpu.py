@@ -140,6 +140,19 @@ def test_attention_mass_long_prompt_sums_to_its_rows():
     assert np.all(np.abs(got - want) <= weight_error(qn, kn, dh) * want)
 
 
+@pytest.mark.parametrize("heads", [(8, 8, 64), (32, 8, 128), (24, 8, 64)], ids=["8on8x64", "32on8x128", "24on8x64"])
+@pytest.mark.parametrize("lens,window", [([5000], 33), ([300, 4500, 1], 100), ([4700], 1)])
+def test_attention_mass_window_over_long_prompts(heads, lens, window):
+    """Few rows over many keys: the form that cuts the keys into ranges."""
+    H, Hkv, dh = heads
+    q, k, dq, dk = mass_case(8, lens, H, Hkv, dh, BF16, fused=True)
+    got = f64(B.lazy_k_attention_mass(dq, dk, cu(lens), max(lens), H, Hkv, dh, window))
+    B.lazy_device_status()
+    qn, kn = f64(q).reshape(-1, H, dh), f64(k).reshape(-1, Hkv, dh)
+    want = R.attention_mass(qn, kn, lens, H, Hkv, dh, window)
+    assert np.all(np.abs(got - want) <= weight_error(qn, kn, dh) * want)
+
+
 # ------------------------------------------------------------------------------------------- compaction
 def new_cache(n_seqs, cap, Hkv, dh, dtype):
     return dict(kc=torch.full((n_seqs, cap, Hkv, dh), 99.0, dtype=dtype, device="cuda"),
