@@ -228,7 +228,8 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
 //   warp 1     owns TMEM and issues S_j = A B_j^T (M128 N128 K16) from one lane into two buffers of 128 columns;
 //   warps 2-9  two threads per TMEM lane, 64 columns each: tcgen05.ld, then one exponential per logit.
 // Two CTAs share an SM.  The bound is the special-function unit: one exponential per (row, key, head) and pass is 1024 clocks
-// per tile against 512 of the tensor cores (head width 128).
+// per tile against 512 of the tensor cores (head width 128), so a quarter of them is taken on the FMA pipe (a 3376-row
+// prompt of 32 heads: 131 us with none, 122 with a quarter, 142 with half).
 // Lane tiles hold R = 128 / group rows x group heads, loaded as one 3-d box; with a group that does not divide 128
 // the last lanes of a tile are unused.  A short grid is filled up by clusters: the CTAs of a cluster share a
 // stationary tile, split the streamed tiles and add their parts in rank order through distributed shared memory.
@@ -240,6 +241,7 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
 constexpr int MT = 128;                       // tile rows of either side, columns of S
 constexpr int MT_LSE_STAGES = 4, MT_MAX_CLUSTER = 8, MT_DEEP_TILES = 4;  // lane tiles that DEEP pass 2 takes at most
 static_assert(MT_DEEP_TILES <= MT_LSE_STAGES, "DEEP pass 2 keeps all lanes' log-sum-exps where the ring would be");
+constexpr int MT_POLY = 8;  // of as many columns, two exponentials are taken on the FMA pipe (a quarter): see ex2_poly_x2
 constexpr int MT_THREADS = 320;
 constexpr int MT_TMEM_COLS = 256;
 
@@ -491,11 +493,10 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           unsigned long long sum0 = 0ull, sum1 = 0ull;
 #pragma unroll
           for (int c = 0; c < 64; c += 4) {
-            float x0, x1, x2, x3;
-            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2, neg), x0, x1);
-            f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])), sl2x2, neg), x2, x3);
-            sum0 = f32x2_add(sum0, f32x2_pack(ex2_approx(x0), ex2_approx(x1)));
-            sum1 = f32x2_add(sum1, f32x2_pack(ex2_approx(x2), ex2_approx(x3)));
+            const unsigned long long x0 = f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2, neg);
+            const unsigned long long x1 = f32x2_fma(f32x2_pack(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])), sl2x2, neg);
+            sum0 = f32x2_add(sum0, ex2_approx_x2(x0));
+            sum1 = f32x2_add(sum1, c % MT_POLY == MT_POLY - 4 ? ex2_poly_x2(x1) : ex2_approx_x2(x1));
           }
           float u0, u1;
           f32x2_unpack(f32x2_add(sum0, sum1), u0, u1);
@@ -514,13 +515,12 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 #pragma unroll
             for (int c = 0; c < 64; c += 4) {
               const float4 e = le[c >> 2];
-              float x0, x1, x2, x3;
-              f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2,
-                                     f32x2_pack(e.x, e.y)), x0, x1);
-              f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])), sl2x2,
-                                     f32x2_pack(e.z, e.w)), x2, x3);
-              sum0 = f32x2_add(sum0, f32x2_pack(ex2_approx(x0), ex2_approx(x1)));
-              sum1 = f32x2_add(sum1, f32x2_pack(ex2_approx(x2), ex2_approx(x3)));
+              const unsigned long long x0 = f32x2_fma(f32x2_pack(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), sl2x2,
+                                                      f32x2_pack(e.x, e.y));
+              const unsigned long long x1 = f32x2_fma(f32x2_pack(__uint_as_float(raw[c + 2]), __uint_as_float(raw[c + 3])), sl2x2,
+                                                      f32x2_pack(e.z, e.w));
+              sum0 = f32x2_add(sum0, ex2_approx_x2(x0));
+              sum1 = f32x2_add(sum1, c % MT_POLY == MT_POLY - 4 ? ex2_poly_x2(x1) : ex2_approx_x2(x1));
             }
             float u0, u1;
             f32x2_unpack(f32x2_add(sum0, sum1), u0, u1);

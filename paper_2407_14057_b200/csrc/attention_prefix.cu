@@ -24,10 +24,23 @@ __device__ __forceinline__ int px_seq_of_row(const int32_t *cu, int n_seqs, int 
   return lo;
 }
 
+// The same by a warp: 32 entries are looked at in one round.
+__device__ __forceinline__ int px_seq_of_row_warp(const int32_t *cu, int n_seqs, int r) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = n_seqs;  // the sequence is one of [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 31) / 32, i = lo + lane * step;
+    const uint32_t le = __ballot_sync(0xffffffffu, lane == 0 || (lane * step < n && cu[i] <= r));
+    const int k = 31 - __clz(le);
+    n = min(step, n - k * step);
+    lo += k * step;
+  }
+  return lo;
+}
+
 // Own keys that row r sees, as a range of the key list: [*first, *first + return value).  Tables that do not fit
 // their declared sizes are reported and give no keys.
-__device__ __forceinline__ int px_own_keys(const PrefixArgs &a, int r, int *first, DevStatus *status) {
-  const int s = px_seq_of_row(a.cu_q, a.n_seqs, r);
+__device__ __forceinline__ int px_own_keys(const PrefixArgs &a, int r, int s, int *first, DevStatus *status) {
   const int q0 = a.cu_q[s], q1 = a.cu_q[s + 1], c0 = a.cu_kv[s], c1 = a.cu_kv[s + 1];
   *first = c0;
   if (q0 < 0 || q1 > a.n_rows || r < q0 || r >= q1 || q1 - q0 > a.max_q || c0 < 0 || c1 < c0 || c1 > a.n_kv || c1 - c0 > a.max_kv) {
@@ -46,7 +59,7 @@ prefix_partial_kernel(const PrefixArgs a, int per_split, float *__restrict__ par
   __shared__ AttnSplitSmem sm;
   __shared__ int s_first, s_own;
   const int r = blockIdx.z, h = blockIdx.y, H = gridDim.y, g = h / (H / a.n_kv_heads);
-  if (threadIdx.x == 0) s_own = px_own_keys(a, r, &s_first, status);
+  if (threadIdx.x == 0) s_own = px_own_keys(a, r, px_seq_of_row(a.cu_q, a.n_seqs, r), &s_first, status);
   __syncthreads();
   const int first = s_first, n = a.n_pre + s_own;
   const int k0 = blockIdx.x * per_split;
@@ -299,20 +312,23 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         mx[3] = fmax3(mx[3], __uint_as_float(raw[c + 6]), __uint_as_float(raw[c + 7]));
       }
       const float mj = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
+      // The reference exponent is settled before the exponentials; P_{j-1} V_{j-1} has to be done only where O is rescaled
+      // and, below, where P_j takes the place of P_{j-1}: the exponentials run while it does.
       float alpha = 1.f;
+      bool waited = j == 0;
       if (j == 0) m = mj;
       else {
-        // P_{j-1} V_{j-1} has to be done before P is overwritten, and before O is rescaled
-        ok = mbar_wait(smem_u32(&bars->pv_done[t]), (uint32_t)((j - 1) & 1), abort_flag, status, W_PREFIX);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        tc_fence_after();
         const bool need = mj - m > PT_RESCALE;
         if (need) {
           alpha = ex2_approx(m - mj);
           m = mj;
         }
         if (__any_sync(0xffffffffu, need)) {
+          ok = mbar_wait(smem_u32(&bars->pv_done[t]), (uint32_t)((j - 1) & 1), abort_flag, status, W_PREFIX);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          waited = true;
 #pragma unroll 1
           for (int c = 0; c < HD; c += 32) {
             uint32_t ov[32];
@@ -341,6 +357,12 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         raw[c >> 1] = bf16x2_pack(p0 - h0, p1 - h1);  // entry c / 2 has been used by now
       }
       l = l * alpha + (sm[0] + sm[1]);
+      if (!waited) {
+        ok = mbar_wait(smem_u32(&bars->pv_done[t]), (uint32_t)((j - 1) & 1), abort_flag, status, W_PREFIX);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+      }
       tmem_st_32x32(tile + 64u, hi);
       tmem_st_32x32(tile + 96u, raw);
       tmem_st_wait();
@@ -382,7 +404,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 // ---- (2) the requests' own keys -----------------------------------------------------------------------------------
 // One CTA: 8 NT columns (row, head) of one (request, key/value head) over one range of its list; warps take every fourth group of
 // 16 keys, and their parts are added in shared memory.
-constexpr int PO_WARPS = 4, PO_THREADS = PO_WARPS * 32, PO_STAGES = 3;
+constexpr int PO_WARPS = 4, PO_THREADS = PO_WARPS * 32, PO_STAGES = 2;
 
 template <int HD, int NT>
 struct PrefixOwnShared {
@@ -391,7 +413,7 @@ struct PrefixOwnShared {
 
 // grid (n_kv_heads * column blocks, splits, n_seqs)
 template <int HD, int NT>
-__global__ void __launch_bounds__(PO_THREADS)
+__global__ void __launch_bounds__(PO_THREADS, NT == 1 ? 3 : 2)
 prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, float *__restrict__ part_o,
                   float2 *__restrict__ part_ml, DevStatus *status) {
   using Rows = RowsMma<HD, NT>;
@@ -442,12 +464,11 @@ prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, 
       }
       return e;
     };
-    uint32_t there[PO_STAGES];  // by stage, kept in registers: every index below is a compile-time one
     auto request = [&](int i, int e, uint32_t &mask) {
       const int j0 = lo + (warp + i * PO_WARPS) * RM_KEYS;
       mask = __ballot_sync(0xffffffffu, e >= 0) & 0xffffu;
       if (j0 < end)
-        rows.load(stages + (i % PO_STAGES) * Rows::STAGE, [&](int r, const bf16 *&kr, const bf16 *&vr) {
+        rows.load(stages + (i & 1) * Rows::STAGE, [&](int r, const bf16 *&kr, const bf16 *&vr) {
           const int row = __shfl_sync(0xffffffffu, e, r);
           const size_t at = (size_t)max(row, 0) * a.ldkv;
           kr = kb + at;
@@ -456,14 +477,14 @@ prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, 
         });
       rm_cp_commit();
     };
-    static_assert(PO_STAGES == 3, "the loop below is unrolled by hand over three stages");
-    request(0, entry(0), there[0]);
-    request(1, entry(1), there[1]);
-    int e_next = entry(2);
-    auto step = [&](int i, uint32_t mask, uint32_t &mask_next) {
-      request(i + 2, e_next, mask_next);
-      e_next = entry(i + 3);
-      rm_cp_wait<PO_STAGES - 1>();
+    static_assert(PO_STAGES == 2, "one group is requested while another is used");
+    uint32_t there, there_next;
+    request(0, entry(0), there);
+    int e_next = entry(1);
+    for (int i = 0; lo + (warp + i * PO_WARPS) * RM_KEYS < end; ++i) {
+      request(i + 1, e_next, there_next);
+      e_next = entry(i + 2);
+      rm_cp_wait<1>();
       __syncwarp();
       const int j0 = lo + (warp + i * PO_WARPS) * RM_KEYS;
       int seen[NT][2];
@@ -471,18 +492,12 @@ prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, 
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int k = 0; k < 2; ++k) seen[t][k] = min(vis[t][k], hi) - j0;
-      const uint32_t stage = stages + (i % PO_STAGES) * Rows::STAGE;
+      const uint32_t stage = stages + (i & 1) * Rows::STAGE;
       auto none = [](int, int, float, float) {};
-      if (least >= min(j0 + RM_KEYS, end)) rows.template process<false>(stage, seen, mask, none);
-      else rows.template process<true>(stage, seen, mask, none);
+      if (least >= min(j0 + RM_KEYS, end)) rows.template process<false>(stage, seen, there, none);
+      else rows.template process<true>(stage, seen, there, none);
+      there = there_next;
       __syncwarp();
-    };
-    for (int i = 0; lo + (warp + i * PO_WARPS) * RM_KEYS < end; i += 3) {
-      step(i, there[0], there[2]);
-      if (lo + (warp + (i + 1) * PO_WARPS) * RM_KEYS >= end) break;
-      step(i + 1, there[1], there[0]);
-      if (lo + (warp + (i + 2) * PO_WARPS) * RM_KEYS >= end) break;
-      step(i + 2, there[2], there[1]);
     }
     rm_cp_wait<0>();
     rows.finish();
@@ -541,12 +556,13 @@ __global__ void __launch_bounds__(128)
 prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, const float2 *__restrict__ part_ml, int n_pre_parts,
                        int n_parts, int own_split, DevStatus *status) {
   constexpr int V = HD / 32;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31;
   const long long pairs = (long long)a.n_rows * a.n_heads, pair = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
   if (pair >= pairs) return;
   int first;
-  const int own = px_own_keys(a, (int)(pair / a.n_heads), &first, status);
+  const int row = (int)(pair / a.n_heads);  // the tables are inputs: they are read before the parts are there
+  const int own = px_own_keys(a, row, px_seq_of_row_warp(a.cu_q, a.n_seqs, row), &first, status);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   // parts of own keys that hold any for this row (the others may not have been written)
   const int n = n_pre_parts + (own > 0 ? min((own + own_split - 1) / own_split, n_parts - n_pre_parts) : 0);
   float m = -INFINITY, l = 0.f;
@@ -571,7 +587,7 @@ prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, con
       }
     }
     const int cnt = min(32, n - i0);
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < cnt; ++i) {
       const float wi = __shfl_sync(0xffffffffu, w, i);
       const float *p = part_o + ((i0 + i) * pairs + pair) * HD + lane * V;
