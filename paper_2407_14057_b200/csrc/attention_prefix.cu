@@ -109,20 +109,22 @@ int prefix_general(cudaStream_t st, const PrefixArgs &a, float *scratch, DevStat
 //   warp 0      TMA: the queries as one 3-d box per tile, then K and V tiles through a ring each (lanes 0 and 1);
 //   warp 1      owns TMEM, issues S = Q K^T (M128 N64) of every tile as soon as its logits have been taken to registers;
 //   warp 2      issues O += P V (M128 N = head width, P from TMEM);
-//   warps 4..   softmax, one thread per lane; running maximum raised only when it grows by more than 2^8.
+//   warps 3..   softmax, one thread per lane; running maximum raised only when it grows by more than 2^8.
 // TMEM columns of a tile: S (64) | P high (32) | P low (32) | O (head width).  P enters as the sum of two bf16 numbers, so
 // that the output's only rounding is its own: the part is bound by reading K and V up to 256 lanes, where the third
 // product's time is free.  Two lane tiles in one CTA share the K and V tiles in shared memory.
 constexpr int PT_Q = 128, PT_K = 64;
 constexpr float PT_RESCALE = 8.f;
+constexpr int PT_REGS = 120;  // of 352 threads, which leaves the registers of a CTA of the own keys (168 x 128)
 
 template <int HD, int TILES>
 struct PrefixShape {
   static constexpr int CH = HD / 64;
   static constexpr int Q_CHUNK = PT_Q * 128, Q_BYTES = CH * Q_CHUNK;
   static constexpr int KV_CHUNK = PT_K * 128, KV_BYTES = CH * KV_CHUNK;
-  static constexpr int STAGES = TILES == 1 ? 2 : 4;     // 96 KiB of two CTAs per SM, 192 KiB of one (head width 128)
-  static constexpr int THREADS = 128 + TILES * 128;
+  // 96 KiB of two CTAs per SM, or 160 KiB of one, which leave room for a CTA of the own keys (head width 128)
+  static constexpr int STAGES = TILES == 1 ? 2 : 3;
+  static constexpr int THREADS = 96 + TILES * 128;
   static constexpr int TMEM_COLS = 256 * TILES;
   static constexpr int RING = TILES * Q_BYTES;          // offset of the K ring, the V ring behind it
   static constexpr int BARRIERS = RING + 2 * STAGES * KV_BYTES;
@@ -141,7 +143,7 @@ constexpr int prefix_smem = PrefixShape<HD, TILES>::BARRIERS + 1024 +
 // grid (n_kv_heads, lane groups of TILES tiles, splits).  Parts: part_o [split][n_rows * n_heads][HD], part_ml
 // [split][n_rows * n_heads] (maximum in log2 units, sum); pair (row, head) at row * n_heads + head.
 template <int HD, int TILES>
-__global__ void __launch_bounds__(PrefixShape<HD, TILES>::THREADS, TILES == 1 ? 2 : 1)
+__global__ void __maxnreg__(PT_REGS)
 prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                  const __grid_constant__ CUtensorMap map_v, int n_rows, int group, int rows_per_tile, int n_pre,
                  int tiles_per_split, float *__restrict__ part_o, float2 *__restrict__ part_ml, DevStatus *status) {
@@ -259,8 +261,8 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (ok) umma_commit(smem_u32(&bars->v_empty[st]));
       }
     }
-  } else if (warp >= 4) {
-    const int t = (warp - 4) >> 2, quarter = warp & 3;
+  } else {
+    const int t = (warp - 3) >> 2, quarter = warp & 3;
     const uint32_t tile = tmem_base + (uint32_t)(t * 256) + ((uint32_t)(quarter * 32) << 16);
     const int f = quarter * 32 + lane;  // lane of the tile
     const int row = row0 + t * R + f / group;
@@ -376,17 +378,34 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     }
     if (warp_used) {
       tc_fence_after();
-      const size_t pair = (size_t)blockIdx.z * n_rows * H + (size_t)row * H + g * group + f % group;
-      if (used) part_ml[pair] = make_float2(m, ok ? l : NAN);  // a wait ran out (reported): nothing like a result
+      const size_t part0 = (size_t)blockIdx.z * n_rows * H;
+      const int pair = used ? row * H + g * group + f % group : -1;
+      if (used) part_ml[part0 + pair] = make_float2(m, ok ? l : NAN);  // a wait ran out: nothing like a result
+      // O leaves in whole 128-byte lines: 32 lanes x 32 columns at a time are turned around in the tile's query rows, which
+      // no product reads any more (16-byte pieces swizzled: no conflicts either way)
+      const uint32_t turn = sQ + t * Shape::Q_BYTES + quarter * 4096;
       if (ok) {
 #pragma unroll 1
         for (int c = 0; c < HD; c += 32) {
           float v[32];
           tmem_ld_32x32(tile + 128u + (uint32_t)c, v);
-          if (used) {
-            float4 *dst = reinterpret_cast<float4 *>(part_o + pair * HD + c);
+          __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dst[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          for (int i = 0; i < 8; ++i)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(turn + lane * 128 + ((i ^ (lane & 7)) << 4)),
+                         "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]), "f"(v[4 * i + 3])
+                         : "memory");
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int fl = i * 4 + (lane >> 3);  // the lane whose line this is
+            const int to = __shfl_sync(0xffffffffu, pair, fl);
+            float4 x;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
+                         : "r"(turn + fl * 128 + (((lane & 7) ^ (fl & 7)) << 4))
+                         : "memory");
+            if (to >= 0) *reinterpret_cast<float4 *>(part_o + (part0 + to) * HD + c + (lane & 7) * 4) = x;
           }
         }
       }
@@ -409,6 +428,7 @@ constexpr int PO_WARPS = 4, PO_THREADS = PO_WARPS * 32, PO_STAGES = 2;
 template <int HD, int NT>
 struct PrefixOwnShared {
   float wm[PO_WARPS][NT * 8], wl[PO_WARPS][NT * 8];
+  size_t pair[NT * 8];  // where a column's part goes
 };
 
 // grid (n_kv_heads * column blocks, splits, n_seqs)
@@ -533,16 +553,17 @@ prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, 
           float sum = 0.f;
 #pragma unroll
           for (int w = 0; w < PO_WARPS; ++w) sum += sh.wl[w][c] * ex2_approx(sh.wm[w][c] - ref);
-          part_ml[base + (size_t)(q0 + f / group) * a.n_heads + g * group + f % group] = make_float2(mx, sum);
+          const size_t pair = base + (size_t)(q0 + f / group) * a.n_heads + g * group + f % group;
+          part_ml[pair] = make_float2(mx, sum);
+          sh.pair[c] = pair;
         }
       }
     __syncthreads();
     for (int i = threadIdx.x; i < min(NT * 8, n_cols - col0) * HD; i += PO_THREADS) {
-      const int f = col0 + i / HD;
       float sum = 0.f;
 #pragma unroll
       for (int w = 0; w < PO_WARPS; ++w) sum += wo[(size_t)w * NT * 8 * HD + i];
-      part_o[(base + (size_t)(q0 + f / group) * a.n_heads + g * group + f % group) * HD + i % HD] = sum;
+      part_o[sh.pair[i / HD] * HD + i % HD] = sum;
     }
   }
   // the merge waits for this kernel alone: its end has to mean the end of the one before it.  One CTA sees to that; the
@@ -594,10 +615,8 @@ prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, con
       float x[V];
       if (V == 4) *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(p);
       else *reinterpret_cast<float2 *>(x) = *reinterpret_cast<const float2 *>(p);
-      if (wi != 0.f) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) acc[k] = fmaf(x[k], wi, acc[k]);
-      }
+      for (int k = 0; k < V; ++k) acc[k] = fmaf(x[k], wi, acc[k]);  // no branch: it would put the loads in a row
     }
   }
   l = warp_sum(l);
