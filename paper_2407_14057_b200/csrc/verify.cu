@@ -27,30 +27,86 @@ __device__ __forceinline__ float vf_weight(float p, float q, int j, int zeroed) 
   return j == zeroed ? 0.f : fmaxf(p - q, 0.f);
 }
 
-// Four consecutive weights from id j on (j a multiple of 4); ids past `end` weigh nothing.
-__device__ __forceinline__ void vf_load4(const float *row_p, const float *row_q, int j, int end, bool vec, int zeroed,
-                                         float *w) {
-  if (vec && j + 4 <= end) {
-    const float4 a = *reinterpret_cast<const float4 *>(row_p + j);
-    float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row_q) b = *reinterpret_cast<const float4 *>(row_q + j);
-    w[0] = vf_weight(a.x, b.x, j, zeroed);
-    w[1] = vf_weight(a.y, b.y, j + 1, zeroed);
-    w[2] = vf_weight(a.z, b.z, j + 2, zeroed);
-    w[3] = vf_weight(a.w, b.w, j + 3, zeroed);
-  } else {
+// The weights of one row.  VEC: rows and vocabulary are multiples of four ids and 16-byte aligned.
+template <bool VEC>
+struct VfRow {
+  const float *p, *q;  // q NULL: nothing is taken off
+  int zeroed;          // id without weight, or -1
+  __device__ __forceinline__ float at(int j) const { return vf_weight(p[j], q ? q[j] : 0.f, j, zeroed); }
+  // Sum over ids first, first + stride, ... < end (four consecutive ones each with VEC), UNROLL loads of a row in flight.
+  __device__ __forceinline__ double sum(int first, int end, int stride) const {
+    constexpr int UNROLL = 8, W = VEC ? 4 : 1;
+    double total = 0.0;
+    for (int j0 = first; j0 < end; j0 += UNROLL * stride) {
+      float x[UNROLL][W], y[UNROLL][W];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = j + i < end ? vf_weight(row_p[j + i], row_q ? row_q[j + i] : 0.f, j + i, zeroed) : 0.f;
+      for (int u = 0; u < UNROLL; ++u) {
+        const int j = j0 + u * stride;
+        if (VEC) {
+          float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+          *reinterpret_cast<float4 *>(x[u]) = j < end ? *reinterpret_cast<const float4 *>(p + j) : z;
+          *reinterpret_cast<float4 *>(y[u]) = j < end && q ? *reinterpret_cast<const float4 *>(q + j) : z;
+        } else {
+          x[u][0] = j < end ? p[j] : 0.f;
+          y[u][0] = j < end && q ? q[j] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) {
+        const int j = j0 + u * stride;
+        float w[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = vf_weight(x[u][i], y[u][i], j + i, zeroed);
+        if (VEC) total += ((double)w[0] + (double)w[1]) + ((double)w[2] + (double)w[3]);
+        else total += (double)w[0];
+      }
+    }
+    return total;
   }
+};
+
+__device__ __forceinline__ double warp_inclusive_f64(double v) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const double up = __shfl_up_sync(0xffffffffu, v, o);
+    if ((int)(threadIdx.x & 31) >= o) v += up;
+  }
+  return v;
+}
+
+// First id of [begin, end) whose running sum, from `run` on, exceeds the bar; if rounding leaves none, the last one with any
+// weight (-1: none has).  By a warp: every lane sums a contiguous piece, one scan finds the piece, then its ids 32 at a time.
+template <bool VEC>
+__device__ __forceinline__ int vf_crossing(const VfRow<VEC> &row, int begin, int end, double run, double bar) {
+  const int lane = threadIdx.x & 31;
+  const int piece = ((end - begin + 31) / 32 + 3) / 4 * 4;
+  const int b = min(begin + lane * piece, end), e = min(b + piece, end);
+  const double mine = row.sum(b, e, VEC ? 4 : 1), incl = warp_inclusive_f64(mine);
+  const uint32_t over = __ballot_sync(0xffffffffu, mine > 0.0 && run + incl > bar), any = __ballot_sync(0xffffffffu, mine > 0.0);
+  if (!any) return -1;
+  const int who = over ? __ffs(over) - 1 : 31 - __clz(any);
+  run += __shfl_sync(0xffffffffu, incl - mine, who);
+  const int b0 = begin + who * piece, e0 = min(b0 + piece, end);
+  int last = -1;
+  for (int j0 = b0; j0 < e0; j0 += 32) {
+    const int j = j0 + lane;
+    const float w = j < e0 ? row.at(j) : 0.f;
+    const double at = run + warp_inclusive_f64((double)w);
+    const uint32_t hit = __ballot_sync(0xffffffffu, w > 0.f && at > bar), some = __ballot_sync(0xffffffffu, w > 0.f);
+    if (hit) return j0 + __ffs(hit) - 1;
+    if (some) last = j0 + 31 - __clz(some);
+    run = __shfl_sync(0xffffffffu, at, 31);
+  }
+  return last;
 }
 
 // One cluster per sequence.
+template <bool VEC>
 __global__ void __launch_bounds__(VF_THREADS)
 verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q, int ldq,
               const int32_t *__restrict__ draft, const int32_t *__restrict__ cu, int n_draft, int max_draft, int vocab,
               const float *__restrict__ u_accept, const float *__restrict__ u_sample, int32_t *__restrict__ n_accept,
-              int32_t *__restrict__ tokens, int vec, DevStatus *status) {
+              int32_t *__restrict__ tokens, DevStatus *status) {
   __shared__ double warp_total[VF_WARPS];
   __shared__ double cta_total;
   __shared__ int s_acc;
@@ -85,21 +141,14 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
   }
   __syncthreads();
   const int acc = s_acc;
-  const float *row_p = p + (size_t)(d0 + s + acc) * ldp;
-  const float *row_q = acc < T && q ? q + (size_t)(d0 + acc) * ldq : nullptr;
-  int zeroed = acc < T && !q ? draft[d0 + acc] : -1;
+  VfRow<VEC> row = {p + (size_t)(d0 + s + acc) * ldp, acc < T && q ? q + (size_t)(d0 + acc) * ldq : nullptr,
+                    acc < T && !q ? draft[d0 + acc] : -1};
   // ---- this warp's contiguous part of the row, in multiples of 128 ids
   const int parts = size * VF_WARPS, part = rank * VF_WARPS + warp;
   const int len = ((vocab + parts - 1) / parts + 127) / 128 * 128;
   const int begin = (int)min((long long)part * len, (long long)vocab), end = min(vocab - begin, len) + begin;
   for (int pass = 0;; ++pass) {
-    double sum = 0.0;
-    for (int j0 = begin; j0 < end; j0 += 128) {
-      float w[4];
-      vf_load4(row_p, row_q, j0 + lane * 4, end, vec != 0, zeroed, w);
-      sum += ((double)w[0] + (double)w[1]) + ((double)w[2] + (double)w[3]);
-    }
-    sum = warp_sum_f64(sum);
+    const double sum = warp_sum_f64(row.sum(begin + lane * (VEC ? 4 : 1), end, VEC ? 128 : 32));
     if (lane == 0) warp_total[warp] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -115,9 +164,9 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
       total += cta[r];
     }
     co_cluster_sync();  // every total has been read: a second pass may write again, a CTA may leave
-    if (!(total > 0.0) && (row_q || zeroed >= 0) && pass == 0) {
-      row_q = nullptr;  // the draft's distribution covers the target's (equal but for rounding): the target's itself
-      zeroed = -1;
+    if (!(total > 0.0) && (row.q || row.zeroed >= 0) && pass == 0) {
+      row.q = nullptr;  // the draft's distribution covers the target's (equal but for rounding): the target's itself
+      row.zeroed = -1;
       continue;
     }
     // ---- the crossing lies in the first CTA, and there in the first warp's part, whose running sum exceeds the
@@ -150,37 +199,8 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
       }
     }
     if (owner == warp) {
-      double run = base;
-      int found = -1, last_pos = -1;
-      for (int j0 = begin; j0 < end && found < 0; j0 += 128) {
-        const int j = j0 + lane * 4;
-        float w[4];
-        vf_load4(row_p, row_q, j, end, vec != 0, zeroed, w);
-        const double mine = ((double)w[0] + (double)w[1]) + ((double)w[2] + (double)w[3]);
-        double incl = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const double up = __shfl_up_sync(0xffffffffu, incl, o);
-          if (lane >= o) incl += up;
-        }
-        double at = run + (incl - mine);
-        int hit = -1;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          at += (double)w[i];
-          if (hit < 0 && w[i] > 0.f && at > bar) hit = j + i;
-          if (w[i] > 0.f) last_pos = j + i;
-        }
-        const uint32_t hits = __ballot_sync(0xffffffffu, hit >= 0);
-        if (hits) found = __shfl_sync(0xffffffffu, hit, __ffs(hits) - 1);
-        run += __shfl_sync(0xffffffffu, incl, 31);
-      }
-      if (found < 0) {  // the two orders of summation round apart at the part's very end
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) last_pos = max(last_pos, __shfl_xor_sync(0xffffffffu, last_pos, o));
-        found = last_pos;
-      }
-      if (lane == 0) tokens[(size_t)s * (max_draft + 1) + acc] = found;
+      const int token = vf_crossing<VEC>(row, begin, end, base, bar);
+      if (lane == 0) tokens[(size_t)s * (max_draft + 1) + acc] = token;
     }
     if (rank == 0) {
       if (threadIdx.x == 0) {
@@ -205,9 +225,10 @@ int launch_verify(cudaStream_t st, const float *p, int ldp, const float *q, int 
   if (n_seqs == 0) return LAZY_OK;
   int cluster = 1;
   while (cluster < VF_MAX_CLUSTER && (long long)n_seqs * cluster < sm_count() && vocab > cluster * VF_WARPS * 128) cluster *= 2;
-  const int vec = !((uintptr_t)p & 15) && ldp % 4 == 0 && (!q || (!((uintptr_t)q & 15) && ldq % 4 == 0));
-  return co_launch(verify_kernel, dim3((unsigned)n_seqs * cluster), dim3(VF_THREADS), 0, st, cluster, false, p, ldp, q,
-                   ldq, draft, cu_draft, n_draft, max_draft, vocab, u_accept, u_sample, n_accept, tokens, vec, status);
+  const bool vec = vocab % 4 == 0 && !((uintptr_t)p & 15) && ldp % 4 == 0 && (!q || (!((uintptr_t)q & 15) && ldq % 4 == 0));
+  return co_launch(vec ? verify_kernel<true> : verify_kernel<false>, dim3((unsigned)n_seqs * cluster), dim3(VF_THREADS), 0, st,
+                   cluster, false, p, ldp, q, ldq, draft, cu_draft, n_draft, max_draft, vocab, u_accept, u_sample, n_accept,
+                   tokens, status);
 }
 
 }  // namespace lazy
