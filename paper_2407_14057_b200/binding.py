@@ -582,40 +582,38 @@ def lazy_prune_op(x: torch.Tensor, pos: torch.Tensor, w_qkv: torch.Tensor, w_o: 
 
 
 # ------------------------------------------------------------------------------- bounded and shared caches
-def _stream_of(dev: int) -> int:
-    """The current stream's handle on device `dev`, without building a stream object (3 us less per call)."""
-    return torch._C._cuda_getCurrentRawStream(dev)
+# These go through lazycall (csrc/lazycall.cpp), which checks types, sizes and devices and raises ValueError for what does not
+# fit; as everywhere, a refusal by the library raises LazyError.
+CALL_PATH = os.path.join(_HERE, "lazycall.so")
+_call = None
 
 
-def _dense(dev: int, dtype: torch.dtype, names: str, *tensors: torch.Tensor) -> List[int]:
-    """Addresses of contiguous tensors of the current device and the given type."""
-    out = []
-    for t in tensors:
-        if t.get_device() != dev or t.dtype is not dtype or not t.is_contiguous():
-            raise ValueError(f"{names.split()[len(out)]}: a contiguous {dtype} tensor on the current CUDA device is wanted")
-        out.append(t.data_ptr())
-    return out
+def _native():
+    """The marshaller, bound to the loaded library's entry points."""
+    global _call
+    if _call is None:
+        if not os.path.exists(CALL_PATH):
+            raise RuntimeError(f"{CALL_PATH} is missing: run `python -m paper_2407_14057_b200.build` "
+                               "(there is no fallback path)")
+        import importlib.util
+        spec = importlib.util.spec_from_file_location("lazycall", CALL_PATH)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        L = lib()
+        m.bind(*[C.cast(getattr(L, f), C.c_void_p).value for f in (
+            "lazy_k_attention_mass", "lazy_k_evict", "lazy_k_evict_step", "lazy_k_attention_prefix", "lazy_k_verify")])
+        _call = m
+    return _call
 
 
-def _rows(t: torch.Tensor, dev: int, dtype: torch.dtype, width: int, name: str) -> Tuple[int, int]:
-    """(address, pitch) of a matrix whose rows lie `pitch` elements apart, each of them contiguous."""
-    shape, stride = t.shape, t.stride()
-    if t.get_device() != dev or t.dtype is not dtype or len(shape) != 2 or shape[1] != width or \
-            (stride[1] != 1 and shape[0] > 0 and width > 1):
-        raise ValueError(f"{name}: {dtype} rows of {width} elements on the current CUDA device are wanted")
-    pitch = stride[0] if shape[0] > 1 else width
-    if pitch < width or pitch > 0x7fffffff:
-        raise ValueError(f"{name}: rows overlap or lie too far apart")
-    return t.data_ptr(), pitch
+def _here() -> Tuple[int, int]:
+    """(current device, handle of its current stream), without building a stream object (3 us)."""
+    dev = torch.cuda.current_device()
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _same(a: int, b: int, what: str) -> None:
-    if a != b:
-        raise ValueError(f"{what}: {a} and {b} do not agree")
-
-
-def _scratch(n: int, dtype: torch.dtype, device="cuda") -> torch.Tensor:
-    return torch.empty(max(int(n), 1), dtype=dtype, device=device)
+def _scratch(n: int, dtype: torch.dtype) -> torch.Tensor:
+    return torch.empty(max(int(n), 1), dtype=dtype, device="cuda")
 
 
 def lazy_k_attention_mass_scratch(n_seqs: int, n_total: int, max_len: int, n_heads: int, n_kv_heads: int,
@@ -630,21 +628,13 @@ def lazy_k_attention_mass(q: torch.Tensor, k: torch.Tensor, cu_seqlens: torch.Te
                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """mass fp32 [n_kv_heads, n_total]; q [n_total, n_heads * head_dim], k [n_total, n_kv_heads * head_dim], any row
     pitch (parts of a fused projection's rows)."""
-    dev, n_total, n_seqs = torch.cuda.current_device(), q.shape[0], cu_seqlens.numel() - 1
     n_kv_heads = n_kv_heads or n_heads
-    pq, ldq = _rows(q, dev, q.dtype, n_heads * head_dim, "q")
-    pk, ldk = _rows(k, dev, q.dtype, n_kv_heads * head_dim, "k")
-    _same(k.shape[0], n_total, "rows of q and k")
     if out is None:
-        out = torch.empty((n_kv_heads, n_total), dtype=torch.float32, device=q.device)
-    _same(out.numel(), n_kv_heads * n_total, "size of out")
+        out = torch.empty((n_kv_heads, q.shape[0]), dtype=torch.float32, device=q.device)
     if scratch is None:
-        scratch = lazy_k_attention_mass_scratch(n_seqs, n_total, max_len, n_heads, n_kv_heads, window)
-    pcu, = _dense(dev, torch.int32, "cu_seqlens", cu_seqlens)
-    pscr, pout = _dense(dev, torch.float32, "scratch out", scratch, out)
-    _check("lazy_k_attention_mass", lib().lazy_k_attention_mass(
-        _stream_of(dev), dtype_code(q.dtype), pq, ldq, pk, ldk, pcu, n_seqs, max_len, n_total, n_heads, n_kv_heads,
-        head_dim, window, pscr, scratch.numel(), pout))
+        scratch = lazy_k_attention_mass_scratch(cu_seqlens.numel() - 1, q.shape[0], max_len, n_heads, n_kv_heads, window)
+    _check("lazy_k_attention_mass", _native().attention_mass(*_here(), q, k, cu_seqlens, scratch, out, max_len, n_heads,
+                                                             n_kv_heads, head_dim, window))
     return out
 
 
@@ -653,37 +643,15 @@ def lazy_k_evict_scratch(n_seqs: int, n_kv_heads: int, budget: int) -> torch.Ten
     return _scratch(lib().lazy_k_evict_scratch_ints(n_seqs, n_kv_heads, budget), torch.int32)
 
 
-def _cache_ptrs(dev: int, kc, vc, dtype):
-    if kc.dim() != 4 or kc.shape != vc.shape:
-        raise ValueError("kc, vc: [n_seqs, cap, n_kv_heads, head_dim] are wanted")
-    return _dense(dev, dtype, "kc vc", kc, vc)
-
-
 def lazy_k_evict(k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, mass: torch.Tensor, cu_seqlens: torch.Tensor,
                  max_len: int, budget: int, n_recent: int, kc: torch.Tensor, vc: torch.Tensor, cmass: torch.Tensor,
                  cpos: torch.Tensor, clen: torch.Tensor, scratch: Optional[torch.Tensor] = None) -> None:
-    """Fills the bounded cache (kc, vc, cmass, cpos, clen) from packed prompt rows k, v and their weights."""
-    dev, n_total, n_seqs = torch.cuda.current_device(), k.shape[0], cu_seqlens.numel() - 1
-    pkc, pvc = _cache_ptrs(dev, kc, vc, k.dtype)
-    _, cap, n_kv_heads, head_dim = kc.shape
-    pk, ldk = _rows(k, dev, k.dtype, n_kv_heads * head_dim, "k")
-    pv, ldv = _rows(v, dev, k.dtype, n_kv_heads * head_dim, "v")
-    _same(ldk, ldv, "row pitches of k and v")
-    _same(v.shape[0], n_total, "rows of k and v")
-    _same(kc.shape[0], n_seqs, "sequences")
-    _same(pos.numel(), n_total, "size of pos")
-    _same(mass.numel(), n_kv_heads * n_total, "size of mass")
-    _same(cmass.numel(), n_seqs * n_kv_heads * cap, "size of cmass")
-    _same(cpos.numel(), n_seqs * n_kv_heads * cap, "size of cpos")
-    _same(clen.numel(), n_seqs * n_kv_heads, "size of clen")
+    """Fills the bounded cache (kc, vc [n_seqs, cap, n_kv_heads, head_dim], cmass, cpos [n_seqs, n_kv_heads, cap], clen
+    [n_seqs, n_kv_heads]) from packed prompt rows k, v, their positions and their weights mass [n_kv_heads, n_total]."""
     if scratch is None:
-        scratch = lazy_k_evict_scratch(n_seqs, n_kv_heads, budget)
-    ppos, pcu, pscr, pcpos, pclen = _dense(dev, torch.int32, "pos cu_seqlens scratch cpos clen", pos, cu_seqlens, scratch,
-                                           cpos, clen)
-    pmass, pcmass = _dense(dev, torch.float32, "mass cmass", mass, cmass)
-    _check("lazy_k_evict", lib().lazy_k_evict(
-        _stream_of(dev), dtype_code(k.dtype), pk, pv, ldk, ppos, pmass, pcu, n_seqs, max_len, n_total, n_kv_heads, head_dim,
-        budget, n_recent, pscr, scratch.numel(), pkc, pvc, pcmass, pcpos, pclen, cap))
+        scratch = lazy_k_evict_scratch(cu_seqlens.numel() - 1, kc.shape[2], budget)
+    _check("lazy_k_evict", _native().evict(*_here(), k, v, pos, mass, cu_seqlens, scratch, kc, vc, cmass, cpos, clen, max_len,
+                                           budget, n_recent))
 
 
 def lazy_k_evict_step_scratch(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, budget: int) -> torch.Tensor:
@@ -700,37 +668,17 @@ def lazy_k_evict_step(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
                       out: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None):
     """(o [n_seqs, n_heads * head_dim], slot, gone int32 [n_seqs, n_kv_heads]).  Without mass_out / pos_out / len_out
     the cache's own cmass / cpos / clen are updated in place, as kc and vc always are."""
-    dev, dt = torch.cuda.current_device(), q.dtype
-    pkc, pvc = _cache_ptrs(dev, kc, vc, dt)
-    n_seqs, cap, n_kv_heads, head_dim = kc.shape
-    pq, ldq = _rows(q, dev, dt, n_heads * head_dim, "q")
-    pkn, ldn = _rows(k_new, dev, dt, n_kv_heads * head_dim, "k_new")
-    pvn, ldv = _rows(v_new, dev, dt, n_kv_heads * head_dim, "v_new")
-    _same(ldn, ldv, "row pitches of k_new and v_new")
-    mass_out = cmass if mass_out is None else mass_out
-    pos_out = cpos if pos_out is None else pos_out
-    len_out = clen if len_out is None else len_out
-    heads = n_seqs * n_kv_heads
-    if not (q.shape[0] == k_new.shape[0] == v_new.shape[0] == pos_new.numel() == n_seqs and
-            cmass.numel() == mass_out.numel() == cpos.numel() == pos_out.numel() == heads * cap and
-            clen.numel() == len_out.numel() == heads):
-        raise ValueError("q, k_new, v_new, pos_new and the cache's arrays: sizes do not agree")
     if out is None:
-        out = (torch.empty((n_seqs, n_heads * head_dim), dtype=dt, device=q.device),
+        n_seqs, _, n_kv_heads, head_dim = kc.shape
+        out = (torch.empty((n_seqs, n_heads * head_dim), dtype=q.dtype, device=q.device),
                torch.empty((n_seqs, n_kv_heads), dtype=torch.int32, device=q.device),
                torch.empty((n_seqs, n_kv_heads), dtype=torch.int32, device=q.device))
-    o, slot, gone = out
-    if o.numel() != n_seqs * n_heads * head_dim or slot.numel() != heads or gone.numel() != heads:
-        raise ValueError("out: sizes do not agree")
     if scratch is None:
-        scratch = lazy_k_evict_step_scratch(n_seqs, n_heads, n_kv_heads, head_dim, budget)
-    pposn, ppos, pposo, plen, pleno, pslot, pgone = _dense(
-        dev, torch.int32, "pos_new cpos pos_out clen len_out slot gone", pos_new, cpos, pos_out, clen, len_out, slot, gone)
-    pmass, pmasso, pscr = _dense(dev, torch.float32, "cmass mass_out scratch", cmass, mass_out, scratch)
-    po, = _dense(dev, dt, "o", o)
-    _check("lazy_k_evict_step", lib().lazy_k_evict_step(
-        _stream_of(dev), dtype_code(dt), pq, ldq, pkn, pvn, ldn, pposn, pkc, pvc, cap, pmass, pmasso, ppos, pposo, plen,
-        pleno, n_seqs, n_heads, n_kv_heads, head_dim, budget, n_recent, pscr, scratch.numel(), po, pslot, pgone))
+        scratch = lazy_k_evict_step_scratch(kc.shape[0], n_heads, kc.shape[2], kc.shape[3], budget)
+    _check("lazy_k_evict_step", _native().evict_step(
+        *_here(), kc, vc, q, k_new, v_new, pos_new, cmass, cmass if mass_out is None else mass_out, cpos,
+        cpos if pos_out is None else pos_out, clen, clen if len_out is None else len_out, scratch, *out, n_heads, budget,
+        n_recent))
     return out
 
 
@@ -748,29 +696,14 @@ def lazy_k_attention_prefix(q: torch.Tensor, cu_q: torch.Tensor, max_q: int, k_p
                             out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """o [n_rows, n_heads * head_dim]; k_pre, v_pre [n_pre, n_kv_heads * head_dim] shared by the batch; k, v buffers of
     rows, of which sequence s owns kv_idx[cu_kv[s]:cu_kv[s + 1]]."""
-    dev, dt, n_rows, n_seqs = torch.cuda.current_device(), q.dtype, q.shape[0], cu_q.numel() - 1
     n_kv_heads = n_kv_heads or n_heads
-    width = n_kv_heads * head_dim
-    pq, ldq = _rows(q, dev, dt, n_heads * head_dim, "q")
-    pkp, ldp = _rows(k_pre, dev, dt, width, "k_pre")
-    pvp, ldvp = _rows(v_pre, dev, dt, width, "v_pre")
-    pk, ldk = _rows(k, dev, dt, width, "k")
-    pv, ldv = _rows(v, dev, dt, width, "v")
-    if ldp != ldvp or ldk != ldv or k_pre.shape[0] != v_pre.shape[0] or k.shape[0] != v.shape[0]:
-        raise ValueError("keys and values: numbers of rows or pitches do not agree")
-    _same(cu_kv.numel(), n_seqs + 1, "sizes of cu_q and cu_kv")
     if out is None:
-        out = torch.empty((n_rows, n_heads * head_dim), dtype=dt, device=q.device)
-    _same(out.numel(), n_rows * n_heads * head_dim, "size of out")
-    n_pre = k_pre.shape[0]
+        out = torch.empty((q.shape[0], n_heads * head_dim), dtype=q.dtype, device=q.device)
     if scratch is None:
-        scratch = lazy_k_attention_prefix_scratch(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads, n_kv_heads, head_dim)
-    pcq, pidx, pckv = _dense(dev, torch.int32, "cu_q kv_idx cu_kv", cu_q, kv_idx, cu_kv)
-    pscr, = _dense(dev, torch.float32, "scratch", scratch)
-    pout, = _dense(dev, dt, "out", out)
-    _check("lazy_k_attention_prefix", lib().lazy_k_attention_prefix(
-        _stream_of(dev), dtype_code(dt), pq, ldq, pcq, n_rows, n_seqs, max_q, pkp, pvp, ldp, n_pre, pk, pv, ldk, k.shape[0],
-        pidx, pckv, kv_idx.numel(), max_kv, n_heads, n_kv_heads, head_dim, pscr, scratch.numel(), pout))
+        scratch = lazy_k_attention_prefix_scratch(q.shape[0], cu_q.numel() - 1, max_q, k_pre.shape[0], max_kv, n_heads,
+                                                  n_kv_heads, head_dim)
+    _check("lazy_k_attention_prefix", _native().attention_prefix(*_here(), q, cu_q, k_pre, v_pre, k, v, kv_idx, cu_kv, scratch,
+                                                                 out, max_q, max_kv, n_heads, n_kv_heads, head_dim))
     return out
 
 
@@ -779,21 +712,9 @@ def lazy_k_verify(p: torch.Tensor, draft: torch.Tensor, cu_draft: torch.Tensor, 
                   out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
     """(n_accept int32 [n_seqs], tokens int32 [n_seqs, max_draft + 1]); p [n_draft + n_seqs, vocab], q [n_draft, vocab]
     or None for drafts chosen outright."""
-    dev, f32, i32 = torch.cuda.current_device(), torch.float32, torch.int32
-    n_seqs, n_draft, vocab = cu_draft.numel() - 1, draft.numel(), p.shape[-1]
-    pp, ldp = _rows(p, dev, f32, vocab, "p")
-    pq, ldq = (None, 0) if q is None or n_draft == 0 else _rows(q, dev, f32, vocab, "q")
-    if p.shape[0] != n_draft + n_seqs or u_accept.numel() != n_draft or u_sample.numel() != n_seqs or \
-            (q is not None and q.shape[0] != n_draft):
-        raise ValueError("p, q, draft, u_accept, u_sample: sizes do not agree")
     if out is None:
-        out = (torch.empty(n_seqs, dtype=i32, device=p.device),
-               torch.empty((n_seqs, max_draft + 1), dtype=i32, device=p.device))
-    n_accept, tokens = out
-    if n_accept.numel() != n_seqs or tokens.numel() != n_seqs * (max_draft + 1):
-        raise ValueError("out: sizes do not agree")
-    pdraft, pcu, pacc, ptok = _dense(dev, i32, "draft cu_draft n_accept tokens", draft, cu_draft, n_accept, tokens)
-    pua, pus = _dense(dev, f32, "u_accept u_sample", u_accept, u_sample)
-    _check("lazy_k_verify", lib().lazy_k_verify(
-        _stream_of(dev), pp, ldp, pq, ldq, pdraft, pcu, n_seqs, n_draft, max_draft, vocab, pua, pus, pacc, ptok))
+        n_seqs = cu_draft.numel() - 1
+        out = (torch.empty(n_seqs, dtype=torch.int32, device=p.device),
+               torch.empty((n_seqs, max_draft + 1), dtype=torch.int32, device=p.device))
+    _check("lazy_k_verify", _native().verify(*_here(), p, q, draft, cu_draft, u_accept, u_sample, *out, max_draft))
     return out

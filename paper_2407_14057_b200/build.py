@@ -1,4 +1,4 @@
-"""Builds the CUDA library in-tree: nvcc, sm_100a only, one shared object."""
+"""Builds the CUDA library in-tree (nvcc, sm_100a only, one shared object) and the argument marshaller beside it."""
 from __future__ import annotations
 
 import hashlib
@@ -11,6 +11,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblazyllm.so")
 STAMP = os.path.join(HERE, "_build", "stamp.txt")
+CALL_SRC = os.path.join(CSRC, "lazycall.cpp")
+CALL_LIB = os.path.join(HERE, "lazycall.so")
+CALL_STAMP = os.path.join(HERE, "_build", "lazycall.txt")
 
 # No --use_fast_math: it would turn expf and division into approximations everywhere; the kernels
 # call the fast intrinsics explicitly where that is wanted.
@@ -37,8 +40,35 @@ def _digest() -> str:
     return h.hexdigest()
 
 
+def build_call(force: bool = False) -> str:
+    """Compiles csrc/lazycall.cpp, the Python module that marshals tensors, against the installed torch."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-o", CALL_LIB, CALL_SRC,
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"],
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd += [f"-I{p}" for p in include_paths()]
+    cmd += ["-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    h = hashlib.sha256(" ".join(cmd + [torch.__version__]).encode())
+    for f in (CALL_SRC, os.path.join(ROOT, "include", "lazyllm.h")):
+        with open(f, "rb") as fh:
+            h.update(fh.read())
+    if not force and os.path.exists(CALL_LIB) and os.path.exists(CALL_STAMP):
+        with open(CALL_STAMP) as f:
+            if f.read().strip() == h.hexdigest():
+                return CALL_LIB
+    os.makedirs(os.path.dirname(CALL_STAMP), exist_ok=True)
+    subprocess.run(cmd, check=True)
+    with open(CALL_STAMP, "w") as f:
+        f.write(h.hexdigest())
+    return CALL_LIB
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compiles every .cu under csrc/ and links liblazyllm.so; returns its path."""
+    """Compiles every .cu under csrc/ and links liblazyllm.so, and the marshaller; returns the library's path."""
+    build_call(force)
     dig = _digest()
     if not force and os.path.exists(LIB) and os.path.exists(STAMP):
         with open(STAMP) as f:
