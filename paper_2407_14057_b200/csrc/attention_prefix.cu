@@ -122,8 +122,7 @@ struct PrefixShape {
   static constexpr int CH = HD / 64;
   static constexpr int Q_CHUNK = PT_Q * 128, Q_BYTES = CH * Q_CHUNK;
   static constexpr int KV_CHUNK = PT_K * 128, KV_BYTES = CH * KV_CHUNK;
-  // 96 KiB of two CTAs per SM, or 160 KiB of one, which leave room for a CTA of the own keys (head width 128)
-  static constexpr int STAGES = TILES == 1 ? 2 : 3;
+  static constexpr int STAGES = TILES == 1 ? 4 : 3;     // 160 KiB, beside which a CTA of the own keys fits (head width 128)
   static constexpr int THREADS = 96 + TILES * 128;
   static constexpr int TMEM_COLS = 256 * TILES;
   static constexpr int RING = TILES * Q_BYTES;          // offset of the K ring, the V ring behind it
@@ -424,6 +423,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 // One CTA: 8 NT columns (row, head) of one (request, key/value head) over one range of its list; warps take every fourth group of
 // 16 keys, and their parts are added in shared memory.
 constexpr int PO_WARPS = 4, PO_THREADS = PO_WARPS * 32, PO_STAGES = 2;
+constexpr int PO_KEYS = 256;  // of a part; 64 requests with 1 to 500 keys of their own: 69 us with 64, 55 with 128, 50 with 256, 51 with 512
 
 template <int HD, int NT>
 struct PrefixOwnShared {
@@ -433,7 +433,7 @@ struct PrefixOwnShared {
 
 // grid (n_kv_heads * column blocks, splits, n_seqs)
 template <int HD, int NT>
-__global__ void __launch_bounds__(PO_THREADS, NT == 1 ? 3 : 2)
+__global__ void __launch_bounds__(PO_THREADS, NT == 1 ? 4 : 2)
 prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, float *__restrict__ part_o,
                   float2 *__restrict__ part_ml, DevStatus *status) {
   using Rows = RowsMma<HD, NT>;
@@ -488,7 +488,7 @@ prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, 
       const int j0 = lo + (warp + i * PO_WARPS) * RM_KEYS;
       mask = __ballot_sync(0xffffffffu, e >= 0) & 0xffffu;
       if (j0 < end)
-        rows.load(stages + (i & 1) * Rows::STAGE, [&](int r, const bf16 *&kr, const bf16 *&vr) {
+        rows_load<HD>(stages + (i & 1) * Rows::STAGE, [&](int r, const bf16 *&kr, const bf16 *&vr) {
           const int row = __shfl_sync(0xffffffffu, e, r);
           const size_t at = (size_t)max(row, 0) * a.ldkv;
           kr = kb + at;
@@ -586,12 +586,28 @@ prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, con
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // parts of own keys that hold any for this row (the others may not have been written)
   const int n = n_pre_parts + (own > 0 ? min((own + own_split - 1) / own_split, n_parts - n_pre_parts) : 0);
+  // The outputs' loads do not wait for the weights: a batch is in flight while the (maximum, sum) pairs arrive, and the next
+  // one while a batch is added up.
+  constexpr int BATCH = 8;
+  const float *first_o = part_o + pair * HD + lane * V;
+  auto fetch = [&](int i0, float (&x)[BATCH][V]) {
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const float *p = first_o + (size_t)min(i0 + i, n - 1) * pairs * HD;
+      if (V == 4) *reinterpret_cast<float4 *>(x[i]) = *reinterpret_cast<const float4 *>(p);
+      else *reinterpret_cast<float2 *>(x[i]) = *reinterpret_cast<const float2 *>(p);
+    }
+  };
+  float x[BATCH][V], next[BATCH][V];
   float m = -INFINITY, l = 0.f;
   bool bad = false;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < n) ml = part_ml[lane * pairs + pair];
+  if (n > 0) fetch(0, x);
   for (int i = lane; i < n; i += 32) {
-    const float2 ml = part_ml[i * pairs + pair];
-    bad |= ml.y != ml.y;
-    if (ml.y > 0.f) m = fmaxf(m, ml.x);
+    const float2 y = i == lane ? ml : part_ml[i * pairs + pair];
+    bad |= y.y != y.y;
+    if (y.y > 0.f) m = fmaxf(m, y.x);
   }
   m = warp_max(m);
   bad = __any_sync(0xffffffffu, bad);
@@ -599,24 +615,24 @@ prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, con
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.f;
   for (int i0 = 0; i0 < n; i0 += 32) {
+    if (i0 > 0) ml = i0 + lane < n ? part_ml[(i0 + lane) * pairs + pair] : make_float2(-INFINITY, 0.f);
     float w = 0.f;
-    if (i0 + lane < n) {
-      const float2 ml = part_ml[(i0 + lane) * pairs + pair];
-      if (ml.y > 0.f) {
-        w = ex2_approx(ml.x - m);
-        l = fmaf(ml.y, w, l);
-      }
+    if (ml.y > 0.f) {
+      w = ex2_approx(ml.x - m);
+      l = fmaf(ml.y, w, l);
     }
-    const int cnt = min(32, n - i0);
-#pragma unroll 8
-    for (int i = 0; i < cnt; ++i) {
-      const float wi = __shfl_sync(0xffffffffu, w, i);
-      const float *p = part_o + ((i0 + i) * pairs + pair) * HD + lane * V;
-      float x[V];
-      if (V == 4) *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(p);
-      else *reinterpret_cast<float2 *>(x) = *reinterpret_cast<const float2 *>(p);
+    for (int k = 0; k < min(32, n - i0); k += BATCH) {
+      fetch(i0 + k + BATCH, next);  // past the end: the last part again, not used
 #pragma unroll
-      for (int k = 0; k < V; ++k) acc[k] = fmaf(x[k], wi, acc[k]);  // no branch: it would put the loads in a row
+      for (int i = 0; i < BATCH; ++i) {
+        const float wi = __shfl_sync(0xffffffffu, w, k + i);  // 0 past the end
+        if (i0 + k + i < n) {
+#pragma unroll
+          for (int c = 0; c < V; ++c) acc[c] = fmaf(x[i][c], wi, acc[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < V; ++c) x[i][c] = next[i][c];
+      }
     }
   }
   l = warp_sum(l);
@@ -643,7 +659,7 @@ PrefixPlan prefix_plan(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv,
   p.lane_groups = cdiv(lane_tiles, p.tiles);
   p.pre_parts = p.tiles_per_split = 0;
   if (key_tiles > 0) {
-    const long long ctas = (long long)n_kv_heads * p.lane_groups, slots = (p.tiles == 1 ? 2LL : 1LL) * sm_count();
+    const long long ctas = (long long)n_kv_heads * p.lane_groups, slots = sm_count();
     long long want = slots / ctas;
     if (want < 1) want = 1;
     if (want > key_tiles) want = key_tiles;
@@ -656,7 +672,9 @@ PrefixPlan prefix_plan(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv,
   if (max_kv > 0) {
     const long long ctas = (long long)n_kv_heads * p.col_blocks * n_seqs;
     long long want = (2LL * sm_count() + ctas - 1) / ctas;
-    const int most = cdiv(max_kv, PO_WARPS * RM_KEYS * 2);  // two groups of keys per warp at least
+    if (want < cdiv(max_kv, PO_KEYS)) want = cdiv(max_kv, PO_KEYS);
+    if (want > 64) want = 64;
+    const int most = cdiv(max_kv, PO_WARPS * RM_KEYS);  // a group of keys per warp at least
     if (want > most) want = most;
     p.own_split = cdiv(cdiv(max_kv, (int)want), RM_KEYS) * RM_KEYS;
     p.own_parts = cdiv(max_kv, p.own_split);
@@ -674,7 +692,7 @@ int prefix_tc_launch(cudaStream_t st, const PrefixArgs &a, const PrefixPlan &p, 
   LAZY_TRY(tma_map_heads_bf16(&mq, a.q, a.n_rows, a.n_heads, HD, a.ldq, group, R));
   LAZY_TRY(tma_map_2d_bf16(&mk, a.k_pre, a.n_pre, a.n_kv_heads * HD, a.ld_pre, 64, PT_K));
   LAZY_TRY(tma_map_2d_bf16(&mv, a.v_pre, a.n_pre, a.n_kv_heads * HD, a.ld_pre, 64, PT_K));
-  LAZY_TRY((co_allow_smem<prefix_tc_kernel<HD, TILES>>(prefix_smem<HD, TILES>)));
+  LAZY_TRY((co_allow_smem<prefix_tc_kernel<HD, TILES>>(prefix_smem<HD, TILES>, true)));
   return co_launch(prefix_tc_kernel<HD, TILES>, dim3(a.n_kv_heads, p.lane_groups, p.pre_parts),
                    dim3(PrefixShape<HD, TILES>::THREADS), prefix_smem<HD, TILES>, st, 1, false, mq, mk, mv, a.n_rows, group, R,
                    a.n_pre, p.tiles_per_split, part_o, part_ml, status);
@@ -683,7 +701,7 @@ template <int HD, int NT>
 int prefix_own_launch(cudaStream_t st, const PrefixArgs &a, const PrefixPlan &p, int group, float *part_o, float2 *part_ml,
                       DevStatus *status) {
   constexpr int SMEM = PO_WARPS * PO_STAGES * RowsMma<HD, NT>::STAGE;
-  LAZY_TRY((co_allow_smem<prefix_own_kernel<HD, NT>>(SMEM)));
+  LAZY_TRY((co_allow_smem<prefix_own_kernel<HD, NT>>(SMEM, true)));
   return co_launch(prefix_own_kernel<HD, NT>, dim3(a.n_kv_heads * p.col_blocks, p.own_parts, a.n_seqs), dim3(PO_THREADS), SMEM,
                    st, 1, p.pre_parts > 0, a, group, p.col_blocks, p.own_split, part_o, part_ml, status);
 }

@@ -30,14 +30,18 @@ __device__ __forceinline__ uint32_t co_weight_key(float w) {
 
 // Opts a kernel in to `bytes` of dynamic shared memory, once per device (the attribute belongs to the device's
 // context).  More than 64 devices simply set it again each time.
+// `beside`: asks for the largest split of the SM's memory in favour of shared memory, so that a CTA of another kernel finds
+// room beside this one's (both have to ask; it takes L1 from kernels that want it).
 template <auto Kernel>
-inline int co_allow_smem(int bytes) {
+inline int co_allow_smem(int bytes, bool beside = false) {
   static std::atomic<unsigned long long> done{0};
   int dev = 0;
   LAZY_CUDA_OK(cudaGetDevice(&dev));
   const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
   if (done.load(std::memory_order_acquire) & bit) return LAZY_OK;
   LAZY_CUDA_OK(cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  if (beside)
+    LAZY_CUDA_OK(cudaFuncSetAttribute(Kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
   done.fetch_or(bit, std::memory_order_release);
   return LAZY_OK;
 }

@@ -235,7 +235,7 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
   auto request = [&](int i) {  // group warp + 4 i of this CTA
     const int j0 = lo + (warp + i * SF_WARPS) * RM_KEYS;
     if (j0 < hi)
-      rows.load(stages + (i % SF_STAGES) * Rows::STAGE, [&](int r, const bf16 *&kr, const bf16 *&vr) {
+      rows_load<HD>(stages + (i % SF_STAGES) * Rows::STAGE, [&](int r, const bf16 *&kr, const bf16 *&vr) {
         const int j = min(j0 + r, max(len - 1, 0));
         kr = kc + j * ld;
         vr = vc + j * ld;

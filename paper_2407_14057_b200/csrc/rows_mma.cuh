@@ -53,6 +53,26 @@ __device__ __forceinline__ void rm_mma(float *c, const uint32_t *a, uint32_t b0,
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// 16-byte piece c of row r of a stage's half (K, then V).
+template <int HD>
+__device__ __forceinline__ uint32_t rows_at(int r, int c) {
+  return (uint32_t)(r * HD * 2 + ((c ^ (r & 7)) << 4));
+}
+// Requests one stage: rows(r) gives (K row, V row, exists) of key r; call with the whole warp, then rm_cp_commit().
+template <int HD, typename Rows>
+__device__ __forceinline__ void rows_load(uint32_t stage, Rows rows) {
+  const int lane = threadIdx.x & 31;
+  constexpr int CHUNKS = HD / 8, PER = 32 / CHUNKS;  // rows per round of the warp: 2 (HD 128) or 4 (HD 64)
+#pragma unroll
+  for (int i = 0; i < RM_KEYS / PER; ++i) {
+    const int r = i * PER + lane / CHUNKS, c = lane % CHUNKS;
+    const bf16 *kr, *vr;
+    const bool there = rows(r, kr, vr);
+    rm_cp_async16(stage + rows_at<HD>(r, c), kr + c * 8, there);
+    rm_cp_async16(stage + RM_KEYS * HD * 2 + rows_at<HD>(r, c), vr + c * 8, there);
+  }
+}
+
 template <int HD, int NT>
 struct RowsMma {
   static constexpr int CHUNKS = HD / 8;              // 16-byte pieces per row
@@ -62,8 +82,7 @@ struct RowsMma {
   float m[NT][2], l[NT][2];   // of columns (lane % 4) * 2 + {0, 1} of each block of 8; l is this lane's keys' only
   float o[NT][HD / 16][4];
 
-  // 16-byte piece c of row r of a stage's half
-  __device__ static __forceinline__ uint32_t at(int r, int c) { return (uint32_t)(r * HD * 2 + ((c ^ (r & 7)) << 4)); }
+  __device__ static __forceinline__ uint32_t at(int r, int c) { return rows_at<HD>(r, c); }
 
   // q_of(column): the column's query, or NULL for a column that is not used (reads as zeros)
   template <typename QOf>
@@ -86,21 +105,6 @@ struct RowsMma {
       for (int k = 0; k < HD / 16; ++k)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[t][k][i] = 0.f;
-    }
-  }
-
-  // Requests one stage: rows(r) gives (K row, V row, exists) of key r; call with the whole warp, then rm_cp_commit().
-  template <typename Rows>
-  __device__ __forceinline__ void load(uint32_t stage, Rows rows) const {
-    const int lane = threadIdx.x & 31;
-    constexpr int PER = 32 / CHUNKS;  // rows per round of the warp: 2 (HD 128) or 4 (HD 64)
-#pragma unroll
-    for (int i = 0; i < RM_KEYS / PER; ++i) {
-      const int r = i * PER + lane / CHUNKS, c = lane % CHUNKS;
-      const bf16 *kr, *vr;
-      const bool there = rows(r, kr, vr);
-      rm_cp_async16(stage + at(r, c), kr + c * 8, there);
-      rm_cp_async16(stage + HALF + at(r, c), vr + c * 8, there);
     }
   }
 
