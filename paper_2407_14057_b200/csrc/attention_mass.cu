@@ -227,9 +227,12 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
 //              lanes' log-sum-exps through a four-stage ring);
 //   warp 1     owns TMEM and issues S_j = A B_j^T (M128 N128 K16) from one lane into two buffers of 128 columns;
 //   warps 2-9  two threads per TMEM lane, 64 columns each: tcgen05.ld, then one exponential per logit.
-// Two CTAs share an SM.  The bound is the special-function unit: one exponential per (row, key, head) and pass is 1024 clocks
-// per tile against 512 of the tensor cores (head width 128), so a quarter of them is taken on the FMA pipe (a 3376-row
-// prompt of 32 heads: 131 us with none, 122 with a quarter, 142 with half).
+// Two CTAs share an SM.  The bound is what the softmax threads issue: one exponential per (row, key, head) and pass is 1024
+// clocks of the special-function unit per tile against 514 of the tensor cores (head width 128), so a quarter of them is
+// taken on the FMA pipe (a 3376-row prompt of 32 heads: 131 us with none, 122 with a quarter, 142 with half), which
+// leaves 768 clocks of that unit and about as many of instruction issue; a tile takes some 1350.  What does not change that:
+// persistent CTAs (128 us), 256 stationary rows with one streamed tile for both and rings for both sides (128 to 135 us, the
+// stationary side in shared or tensor memory, one or two issuing warps).
 // Lane tiles hold R = 128 / group rows x group heads, loaded as one 3-d box; with a group that does not divide 128
 // the last lanes of a tile are unused.  A short grid is filled up by clusters: the CTAs of a cluster share a
 // stationary tile, split the streamed tiles and add their parts in rank order through distributed shared memory.

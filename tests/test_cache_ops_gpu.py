@@ -153,6 +153,28 @@ def test_attention_mass_window_over_long_prompts(heads, lens, window):
     assert np.all(np.abs(got - want) <= weight_error(qn, kn, dh) * want)
 
 
+@pytest.mark.parametrize("heads", [(8, 8, 64), (32, 8, 128), (10, 2, 128), (24, 24, 64)],
+                         ids=["8on8x64", "32on8x128", "10on2x128", "24on24x64"])
+@pytest.mark.parametrize("lens,window", [([4900], 0), ([2500, 1, 2700], 0), ([129, 4097, 640], 3000)])
+def test_attention_mass_many_tiles(heads, lens, window):
+    """Full prompts with more tiles than the machine takes at once, odd numbers of them among them."""
+    H, Hkv, dh = heads
+    q, k, dq, dk = mass_case(9, lens, H, Hkv, dh, BF16, fused=True)
+    got = B.lazy_k_attention_mass(dq, dk, cu(lens), max(lens), H, Hkv, dh, window).double()
+    B.lazy_device_status()
+    want, a = torch.zeros_like(got), 0
+    for n in lens:
+        first = max(n - window, 0) if window else 0
+        hide = torch.ones((n - first, n), dtype=torch.bool, device="cuda").triu(first + 1)
+        for h in range(H):
+            g = h // (H // Hkv)
+            x = dq[a + first:a + n, h * dh:(h + 1) * dh].double() @ dk[a:a + n, g * dh:(g + 1) * dh].double().t() * dh ** -0.5
+            want[g, a:a + n] += torch.softmax(x.masked_fill(hide, -float("inf")), -1).sum(0)
+        a += n
+    e = weight_error(f64(q).reshape(-1, H, dh), f64(k).reshape(-1, Hkv, dh), dh)
+    assert torch.all((got - want).abs() <= (e + 2.0 ** -18) * want)   # and up to 2^14 positive terms, in chains of 2^8
+
+
 # ------------------------------------------------------------------------------------------- compaction
 def new_cache(n_seqs, cap, Hkv, dh, dtype):
     return dict(kc=torch.full((n_seqs, cap, Hkv, dh), 99.0, dtype=dtype, device="cuda"),
