@@ -218,7 +218,7 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
                    c2, true, q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, lse, mass, status);
 }
 
-// ---- tensor-core form: bf16, head width 64 or 128 -----------------------------------------------------------------
+// ---- tensor-core form: bf16, head width up to 128 ----------------------------------------------------------------
 // One CTA holds 128 rows of one side (pass 1: lanes, pass 2: keys) in shared memory as the M side of the product and
 // streams 128-row tiles of the other side past them; a logit tile S (128 x 128, fp32) lands in TMEM and is consumed from
 // there, so every row's reduction stays inside one thread: pass 1 keeps a lane's running maximum and sum, pass 2 a
@@ -263,7 +263,7 @@ struct __align__(16) MassShared {
   int abort_flag;
 };
 template <int HD, bool DEEP>
-constexpr int mass_smem = (MassShape<DEEP>::A_BUFS + MassShape<DEEP>::STAGES) * MT * HD * 2 + 1024 + (int)sizeof(MassShared<DEEP>);
+constexpr int mass_smem = (MassShape<DEEP>::A_BUFS + MassShape<DEEP>::STAGES) * MT * ((HD + 63) / 64) * 128 + 1024 + (int)sizeof(MassShared<DEEP>);
 
 // grid (n_kv_heads * cluster, tiles, n_seqs); DEEP pass 1 with `splits` > 0: (n_kv_heads * splits, tiles, n_seqs) and no clusters;
 // DEEP pass 2: (n_kv_heads, ranges of key tiles, n_seqs), no clusters.  parts: (maximum, sum) of tile t's lanes over key
@@ -278,7 +278,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                DevStatus *status) {
   extern __shared__ uint8_t mass_smem_raw[];
   constexpr int A_BUFS = MassShape<DEEP>::A_BUFS, STAGES = MassShape<DEEP>::STAGES;
-  constexpr int CH = HD / 64;                // 64-column chunks of the head
+  constexpr int CH = (HD + 63) / 64;         // 64-column chunks of the head, the last one filled up with zeros
   constexpr int CHUNK = MT * 128;            // bytes of one chunk of a tile
   const uint32_t raw_addr = smem_u32(mass_smem_raw);
   uint8_t *smem = mass_smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
@@ -359,7 +359,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
           if (lanes) tma_load_3d(dst + c * CHUNK, &map_q, bar, c * 64, g * group, start + first + tile * R);
-          else tma_load_2d(dst + c * CHUNK, &map_k, bar, g * HD + c * 64, start + tile * MT);
+          else tma_load_3d(dst + c * CHUNK, &map_k, bar, c * 64, g, start + tile * MT);
         }
       };
       bool ok = true, waited = PASS == 1 || DEEP;
@@ -587,7 +587,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 }
 
 bool mass_tc_eligible(int dtype, int head_dim, int group) {
-  return dtype == LAZY_BF16 && (head_dim == 64 || head_dim == 128) && group <= MT;
+  return dtype == LAZY_BF16 && head_dim <= 128 && group <= MT;
 }
 int mass_seq_tiles(int n_seqs, int n_total, int group) { return n_total / (MT / group) + n_seqs + 1; }
 
@@ -613,7 +613,7 @@ int mass_tc(cudaStream_t st, const void *q, int ldq, const void *k, int ldkv, co
   const int group = n_heads / n_kv_heads, R = MT / group;
   CUtensorMap mq, mk;
   LAZY_TRY(tma_map_heads_bf16(&mq, q, n_total, n_heads, HD, ldq, group, R));
-  LAZY_TRY(tma_map_2d_bf16(&mk, k, n_total, n_kv_heads * HD, ldkv, 64, MT));
+  LAZY_TRY(tma_map_heads_bf16(&mk, k, n_total, n_kv_heads, HD, ldkv, 1, MT));
   const int rows = window > 0 && window < max_len ? window : max_len;
   const int lane_tiles = cdiv(rows, R), key_tiles = cdiv(max_len, MT), seq_tiles = mass_seq_tiles(n_seqs, n_total, group);
   if (lane_tiles > 65535 || key_tiles > 65535) return LAZY_E_CAPACITY;
@@ -663,10 +663,9 @@ int launch_attention_mass(cudaStream_t st, int dtype, const void *q, int ldq, co
   if (n_seqs == 0 || max_len == 0) return LAZY_OK;
   if (mass_tc_eligible(dtype, head_dim, n_heads / n_kv_heads)) {
     float *lse = reinterpret_cast<float *>(align_up((uintptr_t)scratch, 16));
-    return head_dim == 64 ? mass_tc<64>(st, q, ldq, k, ldkv, cu, n_seqs, max_len, n_total, n_heads, n_kv_heads, window, lse,
-                                        mass, status)
-                          : mass_tc<128>(st, q, ldq, k, ldkv, cu, n_seqs, max_len, n_total, n_heads, n_kv_heads, window,
-                                         lse, mass, status);
+    return co_head_dim(head_dim, [&](auto hd) {
+      return mass_tc<hd.value>(st, q, ldq, k, ldkv, cu, n_seqs, max_len, n_total, n_heads, n_kv_heads, window, lse, mass, status);
+    });
   }
   if (dtype == LAZY_F32)
     return mass_general<float>(st, (const float *)q, ldq, (const float *)k, ldkv, cu, n_seqs, max_len, n_total, n_heads,

@@ -2,7 +2,7 @@
 // its request's own key list (row i of T rows: keys j <= C - T + i of C), so the prefix part is one product of all
 // rows with the prefix's keys: it is computed for the batch together and read once, not once per request.
 //
-// bf16, head width 64 or 128: three launches.  (1) The prefix on tcgen05: the batch's (row, head) pairs of one
+// bf16, head width up to 128: three launches.  (1) The prefix on tcgen05: the batch's (row, head) pairs of one
 // key/value head are the lanes of 128-lane tiles, the prefix's keys are cut into ranges, every CTA leaves the partial
 // softmax of its lanes over its range.  (2) The requests' own keys on the warp-level path of rows_mma.cuh, launched as a
 // dependent that does not wait for (1), so that its CTAs fill the SMs as the first ones leave.  (3) A merge of
@@ -56,7 +56,7 @@ template <typename T>
 __global__ void __launch_bounds__(AS_THREADS)
 prefix_partial_kernel(const PrefixArgs a, int per_split, float *__restrict__ part_o, float *__restrict__ part_ml,
                       DevStatus *status) {
-  __shared__ AttnSplitSmem sm;
+  __shared__ AttnSplitSmem<T> sm;
   __shared__ int s_first, s_own;
   const int r = blockIdx.z, h = blockIdx.y, H = gridDim.y, g = h / (H / a.n_kv_heads);
   if (threadIdx.x == 0) s_own = px_own_keys(a, r, px_seq_of_row(a.cu_q, a.n_seqs, r), &s_first, status);
@@ -119,7 +119,7 @@ constexpr int PT_REGS = 120;  // of 352 threads, which leaves the registers of a
 
 template <int HD, int TILES>
 struct PrefixShape {
-  static constexpr int CH = HD / 64;
+  static constexpr int CH = (HD + 63) / 64;  // 64-column chunks of the head, the last one filled up with zeros
   static constexpr int Q_CHUNK = PT_Q * 128, Q_BYTES = CH * Q_CHUNK;
   static constexpr int KV_CHUNK = PT_K * 128, KV_BYTES = CH * KV_CHUNK;
   static constexpr int STAGES = TILES == 1 ? 4 : 3;     // 160 KiB, beside which a CTA of the own keys fits (head width 128)
@@ -211,7 +211,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         mbar_expect_tx(full, Shape::KV_BYTES);
 #pragma unroll
         for (int c = 0; c < Shape::CH; ++c)
-          tma_load_2d(ring + st * Shape::KV_BYTES + c * Shape::KV_CHUNK, map, full, g * HD + c * 64, (t0 + j) * PT_K);
+          tma_load_3d(ring + st * Shape::KV_BYTES + c * Shape::KV_CHUNK, map, full, c * 64, g, (t0 + j) * PT_K);
       }
     }
   } else if (warp == 1) {
@@ -577,6 +577,7 @@ __global__ void __launch_bounds__(128)
 prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, const float2 *__restrict__ part_ml, int n_pre_parts,
                        int n_parts, int own_split, DevStatus *status) {
   constexpr int V = HD / 32;
+  constexpr bool WIDE = V % 2 == 0;  // a lane's columns: V in a row, or every 32nd where V is odd
   const int lane = threadIdx.x & 31;
   const long long pairs = (long long)a.n_rows * a.n_heads, pair = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
   if (pair >= pairs) return;
@@ -589,13 +590,17 @@ prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, con
   // The outputs' loads do not wait for the weights: a batch is in flight while the (maximum, sum) pairs arrive, and the next
   // one while a batch is added up.
   constexpr int BATCH = 8;
-  const float *first_o = part_o + pair * HD + lane * V;
+  const float *first_o = part_o + pair * HD + (WIDE ? lane * V : lane);
   auto fetch = [&](int i0, float (&x)[BATCH][V]) {
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
       const float *p = first_o + (size_t)min(i0 + i, n - 1) * pairs * HD;
       if (V == 4) *reinterpret_cast<float4 *>(x[i]) = *reinterpret_cast<const float4 *>(p);
-      else *reinterpret_cast<float2 *>(x[i]) = *reinterpret_cast<const float2 *>(p);
+      else if (V == 2) *reinterpret_cast<float2 *>(x[i]) = *reinterpret_cast<const float2 *>(p);
+      else {
+#pragma unroll
+        for (int c = 0; c < V; ++c) x[i][c] = p[c * 32];
+      }
     }
   };
   float x[BATCH][V], next[BATCH][V];
@@ -637,13 +642,17 @@ prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, con
   }
   l = warp_sum(l);
   const float inv = bad ? NAN : (l > 0.f ? 1.f / l : 0.f);
-  bf16 *o = (bf16 *)a.o + pair * HD + lane * V;
+  bf16 *o = (bf16 *)a.o + pair * HD + (WIDE ? lane * V : lane);
   if (V == 4) *reinterpret_cast<uint2 *>(o) = make_uint2(bf16x2_pack(acc[0] * inv, acc[1] * inv), bf16x2_pack(acc[2] * inv, acc[3] * inv));
-  else *reinterpret_cast<uint32_t *>(o) = bf16x2_pack(acc[0] * inv, acc[1] * inv);
+  else if (V == 2) *reinterpret_cast<uint32_t *>(o) = bf16x2_pack(acc[0] * inv, acc[1] * inv);
+  else {
+#pragma unroll
+    for (int c = 0; c < V; ++c) o[c * 32] = __float2bfloat16_rn(acc[c] * inv);
+  }
 }
 
 bool prefix_tc_eligible(int dtype, int head_dim, int group) {
-  return dtype == LAZY_BF16 && (head_dim == 64 || head_dim == 128) && group <= PT_Q;
+  return dtype == LAZY_BF16 && head_dim <= 128 && group <= PT_Q;
 }
 
 // How the work is cut: key ranges of the prefix and of the own lists, so that every launch fills the machine once.
@@ -690,8 +699,8 @@ int prefix_tc_launch(cudaStream_t st, const PrefixArgs &a, const PrefixPlan &p, 
   const int R = PT_Q / group;
   CUtensorMap mq, mk, mv;
   LAZY_TRY(tma_map_heads_bf16(&mq, a.q, a.n_rows, a.n_heads, HD, a.ldq, group, R));
-  LAZY_TRY(tma_map_2d_bf16(&mk, a.k_pre, a.n_pre, a.n_kv_heads * HD, a.ld_pre, 64, PT_K));
-  LAZY_TRY(tma_map_2d_bf16(&mv, a.v_pre, a.n_pre, a.n_kv_heads * HD, a.ld_pre, 64, PT_K));
+  LAZY_TRY(tma_map_heads_bf16(&mk, a.k_pre, a.n_pre, a.n_kv_heads, HD, a.ld_pre, 1, PT_K));
+  LAZY_TRY(tma_map_heads_bf16(&mv, a.v_pre, a.n_pre, a.n_kv_heads, HD, a.ld_pre, 1, PT_K));
   LAZY_TRY((co_allow_smem<prefix_tc_kernel<HD, TILES>>(prefix_smem<HD, TILES>, true)));
   return co_launch(prefix_tc_kernel<HD, TILES>, dim3(a.n_kv_heads, p.lane_groups, p.pre_parts),
                    dim3(PrefixShape<HD, TILES>::THREADS), prefix_smem<HD, TILES>, st, 1, false, mq, mk, mv, a.n_rows, group, R,
@@ -742,7 +751,7 @@ size_t attention_prefix_scratch_floats(int n_rows, int n_seqs, int max_q, int n_
 int launch_attention_prefix(cudaStream_t st, int dtype, const PrefixArgs &a, float *scratch, DevStatus *status) {
   if (a.n_rows == 0) return LAZY_OK;
   if (prefix_tc_eligible(dtype, a.head_dim, a.n_heads / a.n_kv_heads))
-    return a.head_dim == 64 ? prefix_tc<64>(st, a, scratch, status) : prefix_tc<128>(st, a, scratch, status);
+    return co_head_dim(a.head_dim, [&](auto hd) { return prefix_tc<hd.value>(st, a, scratch, status); });
   return dtype == LAZY_F32 ? prefix_general<float>(st, a, scratch, status) : prefix_general<bf16>(st, a, scratch, status);
 }
 

@@ -1,45 +1,81 @@
 // Attention of single query rows over split key ranges on CUDA cores, for every storage type and head width: the
 // form behind the tensor-core kernels of the bounded-cache step and of the shared prefix.  One CTA takes a range of
-// keys of one (row, head), 128 at a time: a warp per key for the logits (lanes along the head), a thread per column for the weighted
-// sum; the partial softmaxes (maximum in log2 units, sum, unnormalised output) are merged by a second kernel.
+// keys of one (row, head), 128 at a time: a warp per eight keys for the logits (lanes along the head), a thread per four columns and
+// every few keys for the weighted sum, eight rows in flight in either; the partial softmaxes (maximum in log2 units, sum, unnormalised output) are merged by a second kernel.
 #pragma once
 #include "cache_ops.cuh"
 
 namespace lazy {
 
 constexpr int AS_TILE = 128, AS_THREADS = 128, AS_MAX_HD = 256;
+constexpr int AS_KEYS = 8;  // key rows that a warp (logits) or a thread (weighted sum) has in flight
 
+template <typename T>
 struct AttnSplitSmem {
   float q[AS_MAX_HD];
-  float logit[AS_TILE];
+  float logit[AS_TILE];                // then the weights
+  const T *k_row[AS_TILE], *v_row[AS_TILE];
+  float4 sum[AS_THREADS];
+  float l[AS_THREADS / 32];
 };
+
+__device__ __forceinline__ float4 as_load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+__device__ __forceinline__ float4 as_load4(const bf16 *p) {
+  const uint2 u = *reinterpret_cast<const uint2 *>(p);
+  float4 x;
+  bf16x2_unpack(u.x, x.x, x.y);
+  bf16x2_unpack(u.y, x.z, x.w);
+  return x;
+}
 
 // Key rows are given by key_k(j) / key_v(j): pointers to the head's part of key j's K and V row, or NULL for a
 // key that is skipped.  Keys [k0, k1), AS_TILE at a time with a running maximum; logits (may be NULL) receives
 // their logits in log2 units.  Call with all AS_THREADS threads.
 template <typename T, typename KeyK, typename KeyV>
-__device__ __forceinline__ void attn_split_partial(AttnSplitSmem &sm, const T *q, int head_dim, int k0, int k1,
+__device__ __forceinline__ void attn_split_partial(AttnSplitSmem<T> &sm, const T *q, int head_dim, int k0, int k1,
                                                    KeyK key_k, KeyV key_v, float *part_o, float *part_ml,
                                                    float *logits) {
-  constexpr int COLS = AS_MAX_HD / AS_THREADS;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float scale = rsqrtf((float)head_dim) * CO_LOG2E;
   for (int c = threadIdx.x; c < head_dim; c += AS_THREADS) sm.q[c] = Elem<T>::to_f(q[c]) * scale;
-  float m = -INFINITY, l = 0.f, acc[COLS];
-#pragma unroll
-  for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
+  // weighted sum: a thread has four columns of every `key_lanes`-th key
+  const int quads = head_dim / 4, key_lanes = AS_THREADS / quads, quad = threadIdx.x % quads, key_lane = threadIdx.x / quads;
+  float m = -INFINITY, l = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int t0 = k0; t0 < k1; t0 += AS_TILE) {
     const int cnt = min(AS_TILE, k1 - t0);
-    __syncthreads();  // q is there; the logits of the tile before have been read
-    for (int j = warp; j < cnt; j += AS_THREADS / 32) {
-      const T *row = key_k(t0 + j);
-      float dot = 0.f;
-      if (row)
-        for (int c = lane; c < head_dim; c += 32) dot = fmaf(sm.q[c], Elem<T>::to_f(row[c]), dot);
-      dot = warp_sum(dot);
-      if (lane == 0) {
-        sm.logit[j] = row ? dot : -INFINITY;
-        if (logits) logits[t0 + j] = sm.logit[j];
+    if (t0 > k0) __syncthreads();  // the weights of the tile before have been used
+    if ((int)threadIdx.x < cnt) {
+      sm.k_row[threadIdx.x] = key_k(t0 + threadIdx.x);
+      sm.v_row[threadIdx.x] = key_v(t0 + threadIdx.x);
+    }
+    __syncthreads();  // and q is there
+    for (int j0 = warp * AS_KEYS; j0 < cnt; j0 += AS_THREADS / 32 * AS_KEYS) {
+      float dot[AS_KEYS];
+      const T *row[AS_KEYS];
+#pragma unroll
+      for (int i = 0; i < AS_KEYS; ++i) {
+        row[i] = j0 + i < cnt ? sm.k_row[j0 + i] : nullptr;
+        dot[i] = 0.f;
+      }
+      for (int c = lane * 4; c < head_dim; c += 128) {
+        const float4 a = *reinterpret_cast<const float4 *>(sm.q + c);
+        float4 x[AS_KEYS];
+#pragma unroll
+        for (int i = 0; i < AS_KEYS; ++i) x[i] = row[i] ? as_load4(row[i] + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < AS_KEYS; ++i)
+          dot[i] = fmaf(a.x, x[i].x, fmaf(a.y, x[i].y, fmaf(a.z, x[i].z, fmaf(a.w, x[i].w, dot[i]))));
+      }
+      float mine = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < AS_KEYS; ++i) {
+        const float d = warp_sum(dot[i]);
+        if (lane == i && row[i]) mine = d;
+      }
+      if (lane < AS_KEYS && j0 + lane < cnt) {
+        sm.logit[j0 + lane] = mine;
+        if (logits) logits[t0 + j0 + lane] = mine;
       }
     }
     __syncthreads();
@@ -49,27 +85,50 @@ __device__ __forceinline__ void attn_split_partial(AttnSplitSmem &sm, const T *q
     const float ref = mt == -INFINITY ? 0.f : mt;  // nothing seen so far: every weight is 2^-inf = 0
     const float alpha = exp2f(m - ref);
     m = mt;
-    float lt = 0.f;
-    for (int j = lane; j < cnt; j += 32) lt += exp2f(sm.logit[j] - ref);
-    l = l * alpha + warp_sum(lt);
+    l *= alpha;
+    __syncthreads();  // every warp has the maximum: the logits become weights
+    if ((int)threadIdx.x < cnt) {
+      const float p = exp2f(sm.logit[threadIdx.x] - ref);
+      sm.logit[threadIdx.x] = p;
+      l += p;
+    }
+    __syncthreads();
+    acc = make_float4(acc.x * alpha, acc.y * alpha, acc.z * alpha, acc.w * alpha);
+    if (key_lane < key_lanes) {
+      for (int j0 = key_lane; j0 < cnt; j0 += AS_KEYS * key_lanes) {
+        float4 x[AS_KEYS];
+        float p[AS_KEYS];
 #pragma unroll
-    for (int i = 0; i < COLS; ++i) {
-      const int c = threadIdx.x + i * AS_THREADS;
-      if (c >= head_dim) continue;
-      float a = acc[i] * alpha;
-      for (int j = 0; j < cnt; ++j) {
-        const T *row = key_v(t0 + j);
-        if (row) a = fmaf(exp2f(sm.logit[j] - ref), Elem<T>::to_f(row[c]), a);
+        for (int i = 0; i < AS_KEYS; ++i) {
+          const int j = j0 + i * key_lanes;
+          const T *row = j < cnt ? sm.v_row[j] : nullptr;
+          x[i] = row ? as_load4(row + quad * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+          p[i] = row ? sm.logit[j] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < AS_KEYS; ++i)
+          acc = make_float4(fmaf(p[i], x[i].x, acc.x), fmaf(p[i], x[i].y, acc.y), fmaf(p[i], x[i].z, acc.z), fmaf(p[i], x[i].w, acc.w));
       }
-      acc[i] = a;
     }
   }
-#pragma unroll
-  for (int i = 0; i < COLS; ++i)
-    if (threadIdx.x + i * AS_THREADS < head_dim) part_o[threadIdx.x + i * AS_THREADS] = acc[i];
+  sm.sum[threadIdx.x] = acc;
+  l = warp_sum(l);
+  if (lane == 0) sm.l[warp] = l;
+  __syncthreads();
+  if ((int)threadIdx.x < quads) {
+    float4 o = sm.sum[threadIdx.x];
+    for (int i = 1; i < key_lanes; ++i) {
+      const float4 x = sm.sum[i * quads + threadIdx.x];
+      o = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
+    }
+    part_o[threadIdx.x * 4] = o.x;  // parts may start anywhere in the scratch
+    part_o[threadIdx.x * 4 + 1] = o.y;
+    part_o[threadIdx.x * 4 + 2] = o.z;
+    part_o[threadIdx.x * 4 + 3] = o.w;
+  }
   if (threadIdx.x == 0) {
     part_ml[0] = m;
-    part_ml[1] = l;
+    part_ml[1] = sm.l[0] + sm.l[1] + sm.l[2] + sm.l[3];
   }
 }
 

@@ -2,6 +2,7 @@
 // order of accumulated weights, per-device kernel attributes, launch shapes with clusters.
 #pragma once
 #include <atomic>
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -44,6 +45,18 @@ inline int co_allow_smem(int bytes, bool beside = false) {
     LAZY_CUDA_OK(cudaFuncSetAttribute(Kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
   done.fetch_or(bit, std::memory_order_release);
   return LAZY_OK;
+}
+
+// Calls f(std::integral_constant<int, HD>) for a head width of 32, 64, 96 or 128.
+template <typename F>
+inline int co_head_dim(int head_dim, F f) {
+  switch (head_dim) {
+    case 32: return f(std::integral_constant<int, 32>{});
+    case 64: return f(std::integral_constant<int, 64>{});
+    case 96: return f(std::integral_constant<int, 96>{});
+    case 128: return f(std::integral_constant<int, 128>{});
+  }
+  return LAZY_E_BADARG;
 }
 
 // Launch with a cluster of `cluster` CTAs along x and, on request, as a programmatic dependent.

@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(AS_THREADS)
 step_partial_kernel(const T *__restrict__ q, int ldq, const T *__restrict__ kc, const T *__restrict__ vc, int cap,
                     int head_dim, int group, const int32_t *__restrict__ held, int budget, int per_split,
                     float *__restrict__ part_o, float *__restrict__ part_ml, float *__restrict__ logits) {
-  __shared__ AttnSplitSmem sm;
+  __shared__ AttnSplitSmem<T> sm;
   const int h = blockIdx.y, s = blockIdx.z, H = gridDim.y, g = h / group, Hkv = H / group;
   const int n = held[(size_t)s * Hkv + g], k0 = blockIdx.x * per_split;
   const size_t sh = (size_t)s * H + h, part = sh * gridDim.x + blockIdx.x;
@@ -160,7 +160,7 @@ int step_general(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevSta
 }
 
 
-// ---- one launch: bf16, head width 64 or 128, up to 16 query heads per key/value head ------------------------------
+// ---- one launch: bf16, head width up to 128, up to 16 query heads per key/value head ------------------------------
 // A cluster of CTAs holds one (sequence, key/value head), each CTA a contiguous part of the slots, each warp every
 // fourth group of 16 of them.  The first groups' rows are requested before anything else, the choice of the slot
 // (a minimum over the part's weights, then over the cluster) runs underneath; the new token's row replaces the chosen slot's in
@@ -448,7 +448,7 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
 }
 
 bool step_fused_eligible(int dtype, int head_dim, int group) {
-  return dtype == LAZY_BF16 && (head_dim == 64 || head_dim == 128) && group <= 16;
+  return dtype == LAZY_BF16 && head_dim <= 128 && group <= 16;
 }
 
 // CTAs per (sequence, head): the next power of two that still leaves every warp a group of 16 slots and room for
@@ -488,9 +488,9 @@ int launch_evict_step(cudaStream_t st, int dtype, const EvictStepArgs &a, float 
   if (a.n_seqs == 0) return LAZY_OK;
   const int group = a.n_heads / a.n_kv_heads;
   if (step_fused_eligible(dtype, a.head_dim, group)) {
-    if (a.head_dim == 64)
-      return group <= 8 ? step_fused<64, 1>(st, a, scratch, status) : step_fused<64, 2>(st, a, scratch, status);
-    return group <= 8 ? step_fused<128, 1>(st, a, scratch, status) : step_fused<128, 2>(st, a, scratch, status);
+    return co_head_dim(a.head_dim, [&](auto hd) {
+      return group <= 8 ? step_fused<hd.value, 1>(st, a, scratch, status) : step_fused<hd.value, 2>(st, a, scratch, status);
+    });
   }
   return dtype == LAZY_F32 ? step_general<float>(st, a, scratch, status) : step_general<bf16>(st, a, scratch, status);
 }

@@ -53,30 +53,33 @@ __device__ __forceinline__ void rm_mma(float *c, const uint32_t *a, uint32_t b0,
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// 16-byte piece c of row r of a stage's half (K, then V).
+// 16-byte piece c of row r of a stage's half (K, then V).  Rows lie 128 or 256 bytes apart: the swizzle moves a piece by up
+// to eight places, which a head width of 32 or 96 has no room for by itself.
+template <int HD>
+constexpr int rows_pitch = HD <= 64 ? 128 : 256;
 template <int HD>
 __device__ __forceinline__ uint32_t rows_at(int r, int c) {
-  return (uint32_t)(r * HD * 2 + ((c ^ (r & 7)) << 4));
+  return (uint32_t)(r * rows_pitch<HD> + ((c ^ (r & 7)) << 4));
 }
 // Requests one stage: rows(r) gives (K row, V row, exists) of key r; call with the whole warp, then rm_cp_commit().
 template <int HD, typename Rows>
 __device__ __forceinline__ void rows_load(uint32_t stage, Rows rows) {
   const int lane = threadIdx.x & 31;
-  constexpr int CHUNKS = HD / 8, PER = 32 / CHUNKS;  // rows per round of the warp: 2 (HD 128) or 4 (HD 64)
+  constexpr int CHUNKS = HD / 8;
 #pragma unroll
-  for (int i = 0; i < RM_KEYS / PER; ++i) {
-    const int r = i * PER + lane / CHUNKS, c = lane % CHUNKS;
+  for (int i = 0; i < RM_KEYS * CHUNKS / 32; ++i) {
+    const int r = (i * 32 + lane) / CHUNKS, c = (i * 32 + lane) % CHUNKS;
     const bf16 *kr, *vr;
     const bool there = rows(r, kr, vr);
     rm_cp_async16(stage + rows_at<HD>(r, c), kr + c * 8, there);
-    rm_cp_async16(stage + RM_KEYS * HD * 2 + rows_at<HD>(r, c), vr + c * 8, there);
+    rm_cp_async16(stage + RM_KEYS * rows_pitch<HD> + rows_at<HD>(r, c), vr + c * 8, there);
   }
 }
 
 template <int HD, int NT>
 struct RowsMma {
   static constexpr int CHUNKS = HD / 8;              // 16-byte pieces per row
-  static constexpr int HALF = RM_KEYS * HD * 2;      // bytes of a stage's K (or V)
+  static constexpr int HALF = RM_KEYS * rows_pitch<HD>;  // bytes of a stage's K (or V)
   static constexpr int STAGE = 2 * HALF;
   uint32_t qf[NT][HD / 16][2];
   float m[NT][2], l[NT][2];   // of columns (lane % 4) * 2 + {0, 1} of each block of 8; l is this lane's keys' only
@@ -190,7 +193,7 @@ struct RowsMma {
     uint32_t wild = 0u;
 #pragma unroll
     for (int i = 0; i < RM_KEYS / PER; ++i) {
-      const int r = i * PER + lane / CHUNKS, c = lane % CHUNKS;
+      const int k0 = lane / CHUNKS, r = i * PER + min(k0, PER - 1), c = lane % CHUNKS;  // head width 96: eight lanes are left over
       const uint32_t addr = stage + HALF + at(r, c);
       uint32_t x[4];
       asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
@@ -200,9 +203,9 @@ struct RowsMma {
       const uint32_t lanes = __ballot_sync(0xffffffffu, bad);
 #pragma unroll
       for (int k = 0; k < PER; ++k)
-        if (lanes >> (k * CHUNKS) & (CHUNKS == 32 ? 0xffffffffu : (1u << CHUNKS) - 1u)) {
+        if (lanes >> (k * CHUNKS) & ((1u << CHUNKS) - 1u)) {
           wild |= 1u << (i * PER + k);
-          if (lane / CHUNKS == k) {
+          if (k0 == k) {
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + at(r, c)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(addr), "r"(0u) : "memory");
           }

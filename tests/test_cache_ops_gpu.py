@@ -21,7 +21,7 @@ BF16, F32 = torch.bfloat16, torch.float32
 # (n_heads, n_kv_heads, head_dim, dtype): tensor-core widths, grouped and not, groups that do not divide a tile, other
 # widths, fp32
 HEADS = [(4, 4, 128, BF16), (8, 2, 128, BF16), (8, 1, 64, BF16), (6, 2, 64, BF16), (5, 1, 128, BF16), (2, 2, 96, BF16),
-         (4, 2, 256, BF16), (4, 4, 64, F32), (6, 2, 32, F32)]
+         (4, 2, 256, BF16), (4, 4, 64, F32), (6, 2, 32, F32), (8, 2, 32, BF16), (12, 2, 96, BF16), (4, 1, 160, F32)]
 IDS = [f"{h}on{k}x{d}{'' if t == BF16 else 'f32'}" for h, k, d, t in HEADS]
 
 
@@ -508,6 +508,52 @@ def test_attention_prefix_large_logits_and_infinities():
     got = f64(run_prefix(d, rows, own, H, Hkv, dh)).reshape(want.shape)
     keep = [0, 2, 3]
     assert np.all(np.abs(got[keep] - want[keep]) <= tol[keep]) and np.all(np.isnan(got[1]))
+
+
+@pytest.mark.parametrize("dh", [32, 64, 96, 128, 160])
+@pytest.mark.parametrize("column", [0, 31, -1])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_attention_prefix_hidden_values_at_every_width(dh, column, value):
+    """One odd number in one column of keys that only later rows see: the rows before are as without it."""
+    H, Hkv, rows, own, n_pre = 4, 2, [3, 5], [37, 18], 70
+    d = prefix_case(24, n_pre, rows, own, H, Hkv, dh, BF16)
+    want, tol = prefix_expected(d, rows, own, H, Hkv, dh)
+    clean = run_prefix(d, rows, own, H, Hkv, dh)
+    for j in (36, 37 + 15, 37 + 16):  # the first request's last key, the second's last but two and last but one
+        d["v"][int(d["kv_idx"][j])].view(Hkv, dh)[:, column] = value
+    got = f64(run_prefix(d, rows, own, H, Hkv, dh)).reshape(want.shape)
+    clean = f64(clean).reshape(want.shape)
+    assert np.all(np.abs(clean - want) <= tol)
+    sees = [2, 5, 6, 7]
+    hidden = [r for r in range(8) if r not in sees]
+    assert np.array_equal(got[hidden], clean[hidden])
+    odd = np.zeros(dh, bool)
+    odd[column] = True
+    assert np.all(~np.isfinite(got[sees][..., odd])) and np.all(np.isfinite(got[sees][..., ~odd]))
+
+
+@pytest.mark.parametrize("dh", [32, 96, 160])
+def test_other_widths_do_not_reach_beyond_their_heads(dh):
+    """Rows and heads beside the ones in use hold NaN; nothing of it arrives, in products that fill a width up."""
+    H, Hkv, n, rows, own, n_pre = 4, 2, 150, [2, 1], [20, 33], 90
+    _, _, q, k = mass_case(25, [n], H, Hkv, dh, BF16, fused=False)
+    want = B.lazy_k_attention_mass(q, k, cu([n]), n, H, Hkv, dh)
+    wide_q = torch.full((n + 3, H * dh + 64), float("nan"), dtype=BF16, device="cuda")
+    wide_k = torch.full((n + 3, Hkv * dh + 64), float("nan"), dtype=BF16, device="cuda")
+    wide_q[:n, :H * dh], wide_k[:n, :Hkv * dh] = q, k
+    got = B.lazy_k_attention_mass(wide_q[:n, :H * dh], wide_k[:n, :Hkv * dh], cu([n]), n, H, Hkv, dh)
+    assert torch.equal(got, want)
+    d = prefix_case(26, n_pre, rows, own, H, Hkv, dh, BF16)
+    clean = run_prefix(d, rows, own, H, Hkv, dh)
+    for name in ("k_pre", "v_pre"):
+        x = torch.full((n_pre + 70, Hkv * dh + 64), float("nan"), dtype=BF16)
+        x[:n_pre, :Hkv * dh] = d[name]
+        d[name] = x
+    dev = {key: v.cuda() for key, v in d.items()}
+    got = B.lazy_k_attention_prefix(dev["q"], cu(rows), 2, dev["k_pre"][:n_pre, :Hkv * dh], dev["v_pre"][:n_pre, :Hkv * dh],
+                                    dev["k"], dev["v"], dev["kv_idx"], cu(own), 33, H, Hkv, dh)
+    assert torch.equal(got, clean)
+    B.lazy_device_status()
 
 
 @pytest.mark.parametrize("heads", [HEADS[1], HEADS[5]], ids=[IDS[1], IDS[5]])
