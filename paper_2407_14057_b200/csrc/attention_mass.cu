@@ -18,8 +18,26 @@ namespace {
 // threads hold 2 x 4 logits each and read both sides 16 bytes at a time (rows are padded by 16 bytes: no conflicts).
 // Small tiles and a cluster that shares the streamed tiles keep a short prompt from running on a few SMs: three prompts of
 // 278 rows in all, 4 heads of 64 in fp32, took 48.7 us with 64 x 64 tiles and one CTA per tile.
-constexpr int MG_A = 32, MG_B = 64, MG_THREADS = 256, MG_MAX_CLUSTER = 8;
+constexpr int MG_A = 32, MG_B = 64, MG_THREADS = 256;
+constexpr double MG_START = 0.5, MG_JOIN = 0.25;  // see mass_cluster; 700 rows of 8 heads in groups of 4: 63 us, 80 with a start of 5
+constexpr int MT_MAX_CLUSTER = 8;
 
+// Tile blockIdx.y of sequence blockIdx.z, or the other way round (by_tile): tiles then start in the order of their work over all
+// sequences, so that none of the longest starts late because of the sequence it belongs to (3309, 1968, 4079 and 2232 rows:
+// 415 us one sequence after the other, 391 so).  CTAs without a tile then lie between the others, though, which
+// costs more than it gives where the lengths differ much (3402 and 85 rows: 131 us and 143).
+struct MassGrid {
+  bool by_tile;
+  MassGrid(int n_seqs, int max_len, long long n_total) : by_tile(3 * n_total >= 2LL * n_seqs * max_len) {}
+  dim3 grid(int x, int n_seqs, long long tiles) const {
+    return by_tile ? dim3((unsigned)x, n_seqs, (unsigned)tiles) : dim3((unsigned)x, (unsigned)tiles, n_seqs);
+  }
+};
+// Tiles of `rows` that a batch can hold at most: `longest` per sequence, but no more than all rows make up.
+long long mass_tiles(long long longest, int rows, int n_seqs, long long all_rows) {
+  const long long a = longest * n_seqs, b = all_rows / rows + n_seqs;
+  return a < b ? a : b;
+}
 struct MassGeneralShared {
   float m[MG_A], l[MG_A];  // this CTA's part, read by the cluster
 };
@@ -38,25 +56,28 @@ __device__ __forceinline__ void mg_load(T *dst, int head_dim, RowOf row_of) {
   }
 }
 
-// grid (n_kv_heads * cluster, tiles of the stationary side, n_seqs).  PASS 1: stationary lanes, streamed keys.  PASS 2:
+// grid (n_kv_heads * cluster, tiles of the stationary side and sequences).  PASS 1: stationary lanes, streamed keys.  PASS 2:
 // stationary keys, streamed lanes.
 template <typename T, int PASS>
 __global__ void __launch_bounds__(MG_THREADS)
 mass_general_kernel(const T *__restrict__ q, int ldq, const T *__restrict__ k, int ldkv,
                     const int32_t *__restrict__ cu, int max_len, int n_total, int group, int head_dim, int window,
-                    float *lse, float *__restrict__ mass, DevStatus *status) {
+                    bool by_tile, float *lse, float *__restrict__ mass, DevStatus *status) {
   constexpr int V = Elem<T>::kPerVec;
   extern __shared__ __align__(128) uint8_t mg_smem[];
   __shared__ MassGeneralShared sh;
   const int rank = (int)co_cluster_rank(), csize = (int)co_cluster_size();
-  const int g = blockIdx.x / csize, s = blockIdx.z, pitch = head_dim + V;
+  const int g = blockIdx.x / csize, pitch = head_dim + V;
+  const int s = by_tile ? blockIdx.y : blockIdx.z, z = by_tile ? blockIdx.z : blockIdx.y;
   if (PASS == 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  auto rows_of = [&](int n) { return window > 0 ? min(n, window) : n; };  // the last ones accumulate
+  auto tiles_of = [&](int n) { return ((PASS == 1 ? rows_of(n) * group : n) + MG_A - 1) / MG_A; };
   int start, n;
-  if (!co_span(cu, s, n_total, max_len, status, W_MASS, start, n)) return;  // the whole cluster alike
-  const int first = window > 0 ? max(n - window, 0) : 0;  // rows [first, n) accumulate
-  const int n_lanes = (n - first) * group;
-  const int n_a = PASS == 1 ? n_lanes : n, a0 = blockIdx.y * MG_A;
-  if (a0 >= n_a) return;
+  if (!co_span(cu, s, n_total, max_len, status, W_MASS, start, n) ) return;  // the whole cluster alike
+  const int at = PASS == 1 ? (by_tile ? (int)gridDim.z : tiles_of(n)) - 1 - z : z;  // most work first
+  if (at < 0 || at >= tiles_of(n)) return;
+  const int first = n - rows_of(n), n_lanes = rows_of(n) * group;
+  const int n_a = PASS == 1 ? n_lanes : n, a0 = at * MG_A;
   const float *lse_g = lse + ((size_t)g * n_total + start + first) * group;  // lane f of this sequence at lse_g[f]
   const float scale = rsqrtf((float)head_dim) * CO_LOG2E;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
@@ -180,19 +201,31 @@ mass_general_kernel(const T *__restrict__ q, int ldq, const T *__restrict__ k, i
   if (csize > 1) co_cluster_sync();  // nobody leaves while its part is being read
 }
 
-// CTAs per stationary tile: the next power of two that still finds room for every CTA at once (`per_sm` on an SM), while
-// each keeps at least `least` streamed tiles.
-int mass_cluster(long long tiles, int streamed, int per_sm, int least, int most) {
-  int c = 1;
-  while (c < most && tiles * c * 2 <= (long long)per_sm * co_cluster_sms(c * 2) && streamed >= 2 * least * c) c *= 2;
-  return c;
+// CTAs per stationary tile, for `tiles` of them that stream up to `streamed` tiles each and `seen` of that on average, the
+// longest first: the number whose estimated time is the least.  The unit is a streamed tile; `start` is what starting and leaving a
+// CTA costs, `join` what every doubling of the cluster adds.  A launch takes its longest CTA, or the CTAs' time shared out,
+// or, when a part of the CTAs starts after the others, the shortest of the first with the longest of the second.  Longest CTAs that
+// all run at once are not the best choice for triangles (us, clusters filling the machine once | by this rule): 3402 + 85 rows of
+// 32 heads in groups of 4 171 | 131, 4100 rows of 12 in groups of 3 109 | 87, 2328 rows of 8 in groups of 4 50 | 32.
+int mass_cluster(long long tiles, int streamed, double seen, int per_sm, double start, double join) {
+  int best = 1;
+  double least = 0.;
+  for (int c = 1, log2c = 0; c <= MT_MAX_CLUSTER; c *= 2, ++log2c) {
+    const double over = start + join * log2c, longest = (streamed + c - 1) / c, waves = (double)tiles * c / co_cluster_ctas(c, per_sm);
+    double t = longest + over;
+    if (waves > 1.) {
+      t = fmax(t, waves * (streamed * seen / c + over));
+      t = fmax(t, 2. * (over + longest * (1. - 2. * (1. - seen) / waves)));
+    }
+    if (c == 1 || t < least) {
+      best = c;
+      least = t;
+    }
+  }
+  return best;
 }
-
-// Tiles of `rows` that a batch can hold at most: `longest` per sequence, but no more than all rows make up.
-long long mass_tiles(long long longest, int rows, int n_seqs, long long all_rows) {
-  const long long a = longest * n_seqs, b = all_rows / rows + n_seqs;
-  return a < b ? a : b;
-}
+// The part of a rectangle of `rows` last rows and n keys that is seen.
+double mass_seen(int rows, int n) { return 1. - rows / (2. * n); }
 
 template <typename T>
 int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, const int32_t *cu, int n_seqs, int max_len,
@@ -208,14 +241,16 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
   const long long lane_tiles = (lanes + MG_A - 1) / MG_A, key_tiles = cdiv(max_len, MG_A);
   if (lane_tiles > 65535 || key_tiles > 65535) return LAZY_E_CAPACITY;
   const int per_sm = smem <= 100 * 1024 ? 2 : 1;
-  const int c1 = mass_cluster(mass_tiles(lane_tiles, MG_A, n_seqs, n_total * (long long)group) * n_kv_heads, cdiv(max_len, MG_B),
-                              per_sm, 1, MG_MAX_CLUSTER);
-  const int c2 = mass_cluster(mass_tiles(key_tiles, MG_A, n_seqs, n_total) * n_kv_heads, (int)((lanes + MG_B - 1) / MG_B), per_sm, 1,
-                              MG_MAX_CLUSTER);
-  LAZY_TRY(co_launch(mass_general_kernel<T, 1>, dim3(n_kv_heads * c1, (unsigned)lane_tiles, n_seqs), dim3(MG_THREADS), smem,
-                     st, c1, false, q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, lse, mass, status));
-  return co_launch(mass_general_kernel<T, 2>, dim3(n_kv_heads * c2, (unsigned)key_tiles, n_seqs), dim3(MG_THREADS), smem, st,
-                   c2, true, q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, lse, mass, status);
+  const double seen = mass_seen(rows, max_len);
+  const long long all_lane = mass_tiles(lane_tiles, MG_A, n_seqs, n_total * (long long)group);
+  const long long all_key = mass_tiles(key_tiles, MG_A, n_seqs, n_total);
+  const int c1 = mass_cluster(all_lane * n_kv_heads, cdiv(max_len, MG_B), seen, per_sm, MG_START, MG_JOIN);
+  const int c2 = mass_cluster(all_key * n_kv_heads, (int)((lanes + MG_B - 1) / MG_B), seen, per_sm, MG_START, MG_JOIN);
+  const MassGrid grid(n_seqs, max_len, n_total);
+  LAZY_TRY(co_launch(mass_general_kernel<T, 1>, grid.grid(n_kv_heads * c1, n_seqs, lane_tiles), dim3(MG_THREADS), smem, st, c1, false,
+                     q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, grid.by_tile, lse, mass, status));
+  return co_launch(mass_general_kernel<T, 2>, grid.grid(n_kv_heads * c2, n_seqs, key_tiles), dim3(MG_THREADS), smem, st, c2, true, q,
+                   ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, grid.by_tile, lse, mass, status);
 }
 
 // ---- tensor-core form: bf16, head width up to 128 ----------------------------------------------------------------
@@ -240,14 +275,19 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
 // DEEP is the form for few lanes over many keys (a window of a long prompt), where a CTA would spend its time on starting up:
 // one CTA per SM with four stages; pass 1 cuts the keys into ranges (no clusters: eight to a cluster only 120 of the 148 SMs
 // can be used) and leaves each range's (maximum, sum), pass 2 merges them and takes a range of key tiles, the next one
-// loaded while the last is used.  A 64-row window over 16384 keys of 8 heads, group 4: 49 us without it.
+// loaded while the last is used.  Ranges are of one length for all sequences, so that long and short ones share the SMs.  A 64-row window over 16384 keys of 8 heads, group 4: 49 us without it.
 constexpr int MT = 128;                       // tile rows of either side, columns of S
-constexpr int MT_LSE_STAGES = 4, MT_MAX_CLUSTER = 8, MT_DEEP_TILES = 4;  // lane tiles that DEEP pass 2 takes at most
+constexpr int MT_LSE_STAGES = 4, MT_DEEP_TILES = 4, MT_DEEP_SPLITS = 32;  // lane tiles that DEEP pass 2 takes at most
 static_assert(MT_DEEP_TILES <= MT_LSE_STAGES, "DEEP pass 2 keeps all lanes' log-sum-exps where the ring would be");
 constexpr int MT_POLY = 8;  // of as many columns, two exponentials are taken on the FMA pipe (a quarter): see ex2_poly_x2
+constexpr double MT_START = 7., MT_JOIN = 1.;  // see mass_cluster
 constexpr int MT_THREADS = 320;
 constexpr int MT_TMEM_COLS = 256;
 
+struct MassDeep {
+  int splits, split_tiles;   // pass 1: key ranges per lane tile, key tiles in each
+  int ranges, range_tiles;   // pass 2: ranges of key tiles per head
+};
 template <bool DEEP>
 struct MassShape {
   static constexpr int A_BUFS = DEEP ? 2 : 1, STAGES = DEEP ? 4 : 2, CTAS = DEEP ? 1 : 2;
@@ -265,17 +305,17 @@ struct __align__(16) MassShared {
 template <int HD, bool DEEP>
 constexpr int mass_smem = (MassShape<DEEP>::A_BUFS + MassShape<DEEP>::STAGES) * MT * ((HD + 63) / 64) * 128 + 1024 + (int)sizeof(MassShared<DEEP>);
 
-// grid (n_kv_heads * cluster, tiles, n_seqs); DEEP pass 1 with `splits` > 0: (n_kv_heads * splits, tiles, n_seqs) and no clusters;
-// DEEP pass 2: (n_kv_heads, ranges of key tiles, n_seqs), no clusters.  parts: (maximum, sum) of tile t's lanes over key
-// range i at (((s * n_kv_heads + g) * deep_tiles + t) * splits + i) * 128.
+// grid (n_kv_heads * cluster, tiles and sequences); DEEP, no clusters: pass 1 (n_kv_heads * splits, the same), pass 2 (n_kv_heads,
+// ranges of key tiles and sequences).  parts: (maximum, sum) of tile t's lanes over key range i at (((s * n_kv_heads + g) *
+// deep_tiles + t) * splits + i) * 128; a range that holds none of a sequence's tiles is not written.
 // lse: tiles of 128 floats (minus the log-sum-exps, log2 units), tile t of sequence s of key/value head g at ((g * seq_tiles)
 // + start_s / R + s + t) * 128: sequences' tiles cannot overlap and every tile is 512-byte aligned.
 template <int PASS, int HD, bool DEEP>
 __global__ void __launch_bounds__(MT_THREADS, MassShape<DEEP>::CTAS)
 mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                const int32_t *__restrict__ cu, int max_len, int n_total, int group, int rows_per_tile, int window,
-               float *lse, int seq_tiles, int splits, float2 *parts, int deep_tiles, float *__restrict__ mass,
-               DevStatus *status) {
+               bool by_tile, float *lse, int seq_tiles, const MassDeep deep, float2 *parts, int deep_tiles,
+               float *__restrict__ mass, DevStatus *status) {
   extern __shared__ uint8_t mass_smem_raw[];
   constexpr int A_BUFS = MassShape<DEEP>::A_BUFS, STAGES = MassShape<DEEP>::STAGES;
   constexpr int CH = (HD + 63) / 64;         // 64-column chunks of the head, the last one filled up with zeros
@@ -285,35 +325,35 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   const uint32_t sA = smem_u32(smem), sB = sA + A_BUFS * CH * CHUNK;
   auto *sh = reinterpret_cast<MassShared<DEEP> *>(smem + (A_BUFS + STAGES) * CH * CHUNK);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool split = DEEP && PASS == 1 && splits > 0;
-  const int csize = split ? splits : (int)co_cluster_size();  // CTAs that share a stationary tile
-  const int g = blockIdx.x / csize, rank = blockIdx.x - g * csize, s = blockIdx.z, R = rows_per_tile;
-  const int Hkv = gridDim.x / csize;
+  constexpr bool SPLIT = DEEP && PASS == 1;
+  const int csize = SPLIT ? deep.splits : (int)co_cluster_size();  // CTAs that share a stationary tile
+  const int g = blockIdx.x / csize, rank = blockIdx.x - g * csize, R = rows_per_tile, Hkv = gridDim.x / csize;
+  const int s = by_tile ? blockIdx.y : blockIdx.z, z = by_tile ? blockIdx.z : blockIdx.y;
   if (PASS == 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  auto rows_of = [&](int n) { return window > 0 ? min(n, window) : n; };  // the last ones accumulate
+  auto tiles_of = [&](int n) { return PASS == 1 ? (rows_of(n) + R - 1) / R : (n + MT - 1) / MT; };
+  const int range = DEEP && PASS == 2 ? deep.range_tiles : 1;  // stationary tiles of a CTA
   int start, n;
-  if (!co_span(cu, s, n_total, max_len, status, W_MASS, start, n)) return;  // the whole cluster alike
-  const int first = window > 0 ? max(n - window, 0) : 0;
+  if (!co_span(cu, s, n_total, max_len, status, W_MASS, start, n) ) return;  // the whole cluster alike
+  const int first = n - rows_of(n), a_tiles = tiles_of(n);
   const int lane_tiles = (n - first + R - 1) / R, key_tiles = (n + MT - 1) / MT;
-  const int a_tiles = PASS == 1 ? lane_tiles : key_tiles;
-  // stationary tiles [at0, at1): one, most work first, or in DEEP pass 2 an equal range of all of them
-  int at0, at1;
-  if (DEEP && PASS == 2) {
-    at0 = (int)((long long)a_tiles * blockIdx.y / gridDim.y);
-    at1 = (int)((long long)a_tiles * (blockIdx.y + 1) / gridDim.y);
-    if (at0 == at1) return;
-  } else {
-    if ((int)blockIdx.y >= a_tiles) return;
-    at0 = PASS == 1 ? a_tiles - 1 - (int)blockIdx.y : (int)blockIdx.y;
-    at1 = at0 + 1;
-  }
-  // streamed tiles [b0, b1) of this CTA for a stationary one
+  // stationary tiles [at0, at1): one, most work first, or in DEEP pass 2 a range of them
+  const int at0 = PASS == 1 ? (by_tile ? (int)gridDim.z : a_tiles) - 1 - z : z * range, at1 = DEEP && PASS == 2 ? min(at0 + range, a_tiles) : at0 + 1;
+  if (at0 < 0 || at0 >= a_tiles) return;
+  // key tiles that some lane of a lane tile sees; streamed tiles [b0, b1) of this CTA for a stationary one
+  auto keys_of = [&](int lane_tile) { return min(key_tiles, (min(first + (lane_tile + 1) * R, n) + MT - 1) / MT); };
   auto streamed = [&](int at, int &b0, int &b1) {
     const int all0 = PASS == 1 ? 0 : max(at * MT - first, 0) / R;
-    const int all1 = PASS == 1 ? min(key_tiles, (min(first + (at + 1) * R, n) + MT - 1) / MT) : lane_tiles;
-    const int per = (all1 - all0 + csize - 1) / csize;
+    const int all1 = PASS == 1 ? keys_of(at) : lane_tiles;
+    const int per = SPLIT ? deep.split_tiles : (all1 - all0 + csize - 1) / csize;
     b0 = min(all0 + rank * per, all1);
     b1 = min(b0 + per, all1);
   };
+  if (SPLIT) {
+    int b0, b1;
+    streamed(at0, b0, b1);
+    if (b0 == b1) return;
+  }
   const size_t lse_base = ((size_t)g * seq_tiles + start / R + s) * MT;
 
   if (threadIdx.x == 0) {
@@ -433,12 +473,13 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     int t = 0;
     if (PASS == 2 && DEEP) {  // minus the lanes' log-sum-exps, from the key ranges of pass 1
       asm volatile("griddepcontrol.wait;" ::: "memory");
-      const float2 *p = parts + ((size_t)s * Hkv + g) * deep_tiles * splits * MT;
+      const float2 *p = parts + ((size_t)s * Hkv + g) * deep_tiles * deep.splits * MT;
       for (int i = threadIdx.x - 64; i < lane_tiles * MT; i += 256) {
-        const float2 *pi = p + (size_t)(i / MT) * splits * MT + i % MT;
+        const float2 *pi = p + (size_t)(i / MT) * deep.splits * MT + i % MT;
+        const int written = (keys_of(i / MT) + deep.split_tiles - 1) / deep.split_tiles;
         float mm = -INFINITY, ll = 0.f;
-#pragma unroll 4
-        for (int r = 0; r < splits; ++r) {
+#pragma unroll 8
+        for (int r = 0; r < written; ++r) {
           const float2 x = pi[(size_t)r * MT];
           const float mt = fmaxf(mm, x.x), ref = mt == -INFINITY ? 0.f : mt;
           ll = ll * ex2_approx(mm - ref) + x.y * ex2_approx(x.x - ref);
@@ -461,13 +502,6 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
-        uint32_t raw[64];
-        tmem_ld_32x32_raw(t_s + (uint32_t)(sb * MT), raw);
-        tmem_ld_32x32_raw(t_s + (uint32_t)(sb * MT) + 32u, raw + 32);
-        tmem_ld_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&sh->s_free[sb]));
         // columns [lo, hi) of this thread's 64 are seen
         int lo = 0, hi = 64;
         if (PASS == 1) hi = own + 1 - (b * MT + half * 64);
@@ -476,7 +510,19 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           lo = (own - row0) * group - half * 64;
           hi = min(R, n - row0) * group - half * 64;
         }
+        // a warp that sees nothing has nothing to do: in DEEP, whose lanes can be few (elsewhere the test costs more than it saves)
+        const bool any = !DEEP || __any_sync(0xffffffffu, hi > max(lo, 0) && lo < 64);
+        uint32_t raw[64];
+        if (any) {
+          tmem_ld_32x32_raw(t_s + (uint32_t)(sb * MT), raw);
+          tmem_ld_32x32_raw(t_s + (uint32_t)(sb * MT) + 32u, raw + 32);
+          tmem_ld_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh->s_free[sb]));
         if (PASS == 1) {
+          if (!any) continue;
           if (hi < 64) {
 #pragma unroll
             for (int c = 0; c < 64; ++c)
@@ -513,7 +559,8 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             if (!ok) break;
           }
           const float4 *le = reinterpret_cast<const float4 *>(sh->lse[ls] + half * 64);
-          if (lo <= 0 && hi >= 64) {
+          if (!any) {
+          } else if (lo <= 0 && hi >= 64) {
             unsigned long long sum0 = 0ull, sum1 = 0ull;
 #pragma unroll
             for (int c = 0; c < 64; c += 4) {
@@ -531,9 +578,13 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           } else {  // a tile on the diagonal or at the end: unseen columns are left out, whatever they hold
             float sum = 0.f;
 #pragma unroll
-            for (int c = 0; c < 64; ++c) {
-              const float x = fmaf(__uint_as_float(raw[c]), sl2, sh->lse[ls][half * 64 + c]);
-              sum += c >= lo && c < hi ? ex2_approx(x) : 0.f;
+            for (int c0 = 0; c0 < 64; c0 += 16) {
+              if (c0 >= hi || c0 + 16 <= lo) continue;
+#pragma unroll
+              for (int c = c0; c < c0 + 16; ++c) {
+                const float x = fmaf(__uint_as_float(raw[c]), sl2, sh->lse[ls][half * 64 + c]);
+                sum += c >= lo && c < hi ? ex2_approx(x) : 0.f;
+              }
             }
             l += sum;
           }
@@ -562,16 +613,16 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                  : "memory");
   }
   if (DEEP && PASS == 2) return;
-  if (csize > 1 && !split) co_cluster_sync();
-  if ((rank == 0 || split) && threadIdx.x < MT) {
+  if (csize > 1 && !SPLIT) co_cluster_sync();
+  if ((rank == 0 || SPLIT) && threadIdx.x < MT) {
     const int row = threadIdx.x;
     float m = -INFINITY, l = 0.f;
-    for (int r = 0; r < (split ? 1 : csize); ++r)
+    for (int r = 0; r < (SPLIT ? 1 : csize); ++r)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float lr = split ? sh->part_l[0][h][row] : *co_map_shared(&sh->part_l[0][h][row], r);
+        const float lr = SPLIT ? sh->part_l[0][h][row] : *co_map_shared(&sh->part_l[0][h][row], r);
         if (PASS == 1) {
-          const float mr = split ? sh->part_m[h][row] : *co_map_shared(&sh->part_m[h][row], r);
+          const float mr = SPLIT ? sh->part_m[h][row] : *co_map_shared(&sh->part_m[h][row], r);
           const float mt = fmaxf(m, mr), ref = mt == -INFINITY ? 0.f : mt;
           l = l * ex2_approx(m - ref) + lr * ex2_approx(mr - ref);
           m = mt;
@@ -579,11 +630,11 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           l += lr;
         }
       }
-    if (split) parts[((((size_t)s * Hkv + g) * deep_tiles + at0) * splits + rank) * MT + row] = make_float2(m, l);
+    if (SPLIT) parts[((((size_t)s * Hkv + g) * deep_tiles + at0) * deep.splits + rank) * MT + row] = make_float2(m, l);
     else if (PASS == 1) lse[lse_base + (size_t)at0 * MT + row] = -(m + log2f(l));  // lanes that do not exist: never looked at
     else if (at0 * MT + row < n) mass[(size_t)g * n_total + start + at0 * MT + row] = l;
   }
-  if (csize > 1 && !split) co_cluster_sync();  // nobody leaves while its parts are being read
+  if (csize > 1 && !SPLIT) co_cluster_sync();  // nobody leaves while its parts are being read
 }
 
 bool mass_tc_eligible(int dtype, int head_dim, int group) {
@@ -591,20 +642,31 @@ bool mass_tc_eligible(int dtype, int head_dim, int group) {
 }
 int mass_seq_tiles(int n_seqs, int n_total, int group) { return n_total / (MT / group) + n_seqs + 1; }
 
+// Key tiles per CTA so that all of them run at once: `most` to a sequence and `all` in all, `ctas` CTAs if none is cut.
+int mass_range(int most, long long all, long long ctas) {
+  const long long sms = sm_count();
+  long long per = ctas < sms ? cdiv(most, (int)(sms / ctas)) : most;  // every sequence with as many ranges as the longest
+  if (ctas < sms) {  // or as many as its length fills, one more for what is left over
+    const long long b = (all + (sms - ctas) - 1) / (sms - ctas);
+    if (b < per) per = b;
+  }
+  return (int)(per < 1 ? 1 : per);
+}
 // Whether both passes take the DEEP form (splits > 0): few lane tiles, many key tiles, a CTA for every (sequence, head).
-struct MassDeep {
-  int splits, ranges;  // key ranges per lane tile (pass 1), ranges of key tiles per head (pass 2)
-};
 MassDeep mass_deep(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window) {
   const int R = MT / (n_heads / n_kv_heads), rows = window > 0 && window < max_len ? window : max_len;
   const int lane_tiles = cdiv(rows, R), key_tiles = cdiv(max_len, MT);
   const long long heads = (long long)n_kv_heads * n_seqs, sms = sm_count();
   const long long all_lane = mass_tiles(lane_tiles, R, n_seqs, n_total) * n_kv_heads;
   const long long all_key = mass_tiles(key_tiles, MT, n_seqs, n_total) * n_kv_heads;
-  if (lane_tiles > MT_DEEP_TILES || all_key <= 2 * sms || heads > sms) return {0, 0};
-  long long splits = sms / all_lane;
-  if (splits > key_tiles) splits = key_tiles;
-  return {splits < 1 ? 1 : (int)splits, (int)(sms / heads)};
+  if (lane_tiles > MT_DEEP_TILES || all_key <= 2 * sms || heads > sms) return {0, 0, 0, 0};
+  MassDeep d;
+  d.split_tiles = mass_range(key_tiles, all_key * lane_tiles, all_lane);
+  if (d.split_tiles < cdiv(key_tiles, MT_DEEP_SPLITS)) d.split_tiles = cdiv(key_tiles, MT_DEEP_SPLITS);
+  d.splits = cdiv(key_tiles, d.split_tiles);
+  d.range_tiles = mass_range(key_tiles, all_key, heads);
+  d.ranges = cdiv(key_tiles, d.range_tiles);
+  return d;
 }
 
 template <int HD>
@@ -616,33 +678,28 @@ int mass_tc(cudaStream_t st, const void *q, int ldq, const void *k, int ldkv, co
   LAZY_TRY(tma_map_heads_bf16(&mk, k, n_total, n_kv_heads, HD, ldkv, 1, MT));
   const int rows = window > 0 && window < max_len ? window : max_len;
   const int lane_tiles = cdiv(rows, R), key_tiles = cdiv(max_len, MT), seq_tiles = mass_seq_tiles(n_seqs, n_total, group);
+  const long long all_lane = mass_tiles(lane_tiles, R, n_seqs, n_total), all_key = mass_tiles(key_tiles, MT, n_seqs, n_total);
   if (lane_tiles > 65535 || key_tiles > 65535) return LAZY_E_CAPACITY;
-  const long long all_lane = mass_tiles(lane_tiles, R, n_seqs, n_total) * n_kv_heads;
-  const long long all_key = mass_tiles(key_tiles, MT, n_seqs, n_total) * n_kv_heads;
   const MassDeep deep = mass_deep(n_seqs, n_total, max_len, n_heads, n_kv_heads, window);
   float2 *parts = reinterpret_cast<float2 *>(lse + (size_t)n_kv_heads * seq_tiles * MT);
-  auto launch = [&](auto kernel, dim3 grid, int smem, int cluster, bool dependent) {
-    return co_launch(kernel, grid, dim3(MT_THREADS), smem, st, cluster, dependent, mq, mk, cu, max_len, n_total, group, R, window,
-                     lse, seq_tiles, deep.splits, parts, lane_tiles, mass, status);
+  const MassGrid grid(n_seqs, max_len, n_total);
+  auto launch = [&](auto kernel, int x, int tiles, int smem, int cluster, bool dependent) {
+    return co_launch(kernel, grid.grid(x, n_seqs, tiles), dim3(MT_THREADS), smem, st, cluster, dependent, mq, mk, cu, max_len, n_total,
+                     group, R, window, grid.by_tile, lse, seq_tiles, deep, parts, lane_tiles, mass, status);
   };
-  // pass 1: DEEP also where one CTA per SM is all there is
-  int c1 = deep.splits ? 1 : mass_cluster(all_lane, key_tiles, 1, 2, MT_MAX_CLUSTER);
-  if (deep.splits || all_lane * c1 <= co_cluster_sms(c1)) {
-    LAZY_TRY((co_allow_smem<mass_tc_kernel<1, HD, true>>(mass_smem<HD, true>)));
-    LAZY_TRY(launch(mass_tc_kernel<1, HD, true>, dim3(n_kv_heads * (deep.splits ? deep.splits : c1), lane_tiles, n_seqs),
-                    mass_smem<HD, true>, c1, false));
-  } else {
-    c1 = mass_cluster(all_lane, key_tiles, 2, 2, MT_MAX_CLUSTER);
-    LAZY_TRY((co_allow_smem<mass_tc_kernel<1, HD, false>>(mass_smem<HD, false>)));
-    LAZY_TRY(launch(mass_tc_kernel<1, HD, false>, dim3(n_kv_heads * c1, lane_tiles, n_seqs), mass_smem<HD, false>, c1, false));
-  }
   if (deep.splits) {
+    LAZY_TRY((co_allow_smem<mass_tc_kernel<1, HD, true>>(mass_smem<HD, true>)));
     LAZY_TRY((co_allow_smem<mass_tc_kernel<2, HD, true>>(mass_smem<HD, true>)));
-    return launch(mass_tc_kernel<2, HD, true>, dim3(n_kv_heads, deep.ranges, n_seqs), mass_smem<HD, true>, 1, true);
+    LAZY_TRY(launch(mass_tc_kernel<1, HD, true>, n_kv_heads * deep.splits, lane_tiles, mass_smem<HD, true>, 1, false));
+    return launch(mass_tc_kernel<2, HD, true>, n_kv_heads, deep.ranges, mass_smem<HD, true>, 1, true);
   }
-  const int c2 = mass_cluster(all_key, lane_tiles, 2, 2, MT_MAX_CLUSTER);
+  const double seen = mass_seen(rows, max_len);
+  const int c1 = mass_cluster(all_lane * n_kv_heads, key_tiles, seen, 2, MT_START, MT_JOIN);
+  const int c2 = mass_cluster(all_key * n_kv_heads, lane_tiles, seen, 2, MT_START, MT_JOIN);
+  LAZY_TRY((co_allow_smem<mass_tc_kernel<1, HD, false>>(mass_smem<HD, false>)));
   LAZY_TRY((co_allow_smem<mass_tc_kernel<2, HD, false>>(mass_smem<HD, false>)));
-  return launch(mass_tc_kernel<2, HD, false>, dim3(n_kv_heads * c2, key_tiles, n_seqs), mass_smem<HD, false>, c2, true);
+  LAZY_TRY(launch(mass_tc_kernel<1, HD, false>, n_kv_heads * c1, lane_tiles, mass_smem<HD, false>, c1, false));
+  return launch(mass_tc_kernel<2, HD, false>, n_kv_heads * c2, key_tiles, mass_smem<HD, false>, c2, true);
 }
 
 }  // namespace
@@ -653,7 +710,7 @@ size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n
   if (group > MT) return general;
   const MassDeep deep = mass_deep(n_seqs, n_total, max_len, n_heads, n_kv_heads, window);
   const size_t tiled = (size_t)n_kv_heads * mass_seq_tiles(n_seqs, n_total, group) * MT +
-                       (size_t)n_seqs * n_kv_heads * MT_DEEP_TILES * deep.splits * MT * 2;
+                       (size_t)n_seqs * n_kv_heads * deep.splits * MT * 2 * cdiv(window > 0 && window < max_len ? window : max_len, MT / group);
   return (general > tiled ? general : tiled) + 4;  // + 4: tiles start on a 16-byte boundary
 }
 

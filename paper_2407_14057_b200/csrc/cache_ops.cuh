@@ -89,11 +89,13 @@ inline int co_launch(void (*kfn)(KArgs...), dim3 grid, dim3 block, size_t smem, 
   return e == cudaSuccess ? LAZY_OK : LAZY_E_CUDA;
 }
 
-// SMs that clusters of `size` CTAs can use, one CTA to an SM: a cluster stays within a group of SMs, and the groups are not
-// multiples of it (132 of 148 with four to a cluster, 120 with eight, asked of the occupancy calculator).  A launch of more
-// runs its last clusters after the others.
-inline int co_cluster_sms(int size) {
-  return size <= 2 ? sm_count() : sm_count() * (size == 4 ? 132 : 120) / 148;
+// CTAs that run at once in clusters of `size` (1, 2, 4 or 8), up to three to an SM: a cluster stays within a group of SMs, and
+// the groups are not multiples of it (as the occupancy calculator has it for 148 SMs).  A launch of more runs its last
+// clusters after the others.
+inline int co_cluster_ctas(int size, int per_sm) {
+  constexpr int FOUR[3] = {132, 284, 416}, EIGHT[3] = {120, 264, 384};
+  if (size <= 2) return sm_count() * per_sm;
+  return sm_count() * (size == 4 ? FOUR : EIGHT)[per_sm - 1] / 148;
 }
 
 __device__ __forceinline__ uint32_t co_cluster_rank() {

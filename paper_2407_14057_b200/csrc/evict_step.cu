@@ -456,7 +456,7 @@ bool step_fused_eligible(int dtype, int head_dim, int group) {
 // take 47 us with one CTA each, 61 us with two, 63 us with four.
 int step_cluster(long long heads, int budget) {
   int c = 1;
-  while (c < SF_MAX_CLUSTER && heads * c * 2 <= (long long)SF_CTAS * co_cluster_sms(c * 2) && budget > c * SF_WARPS * RM_KEYS) c *= 2;
+  while (c < SF_MAX_CLUSTER && heads * c * 2 <= co_cluster_ctas(c * 2, SF_CTAS) && budget > c * SF_WARPS * RM_KEYS) c *= 2;
   return c;
 }
 int step_part_slots(int budget, int cluster) { return cdiv(cdiv(budget, RM_KEYS), cluster) * RM_KEYS; }
