@@ -19,7 +19,8 @@ namespace {
 // Small tiles and a cluster that shares the streamed tiles keep a short prompt from running on a few SMs: three prompts of
 // 278 rows in all, 4 heads of 64 in fp32, took 48.7 us with 64 x 64 tiles and one CTA per tile.
 constexpr int MG_A = 32, MG_B = 64, MG_THREADS = 256;
-constexpr double MG_START = 0.5, MG_JOIN = 0.25;  // see mass_cluster; 700 rows of 8 heads in groups of 4: 63 us, 80 with a start of 5
+// See mass_cluster; 700 rows of 8 heads in groups of 4: 63 us, 80 with a start of 5
+constexpr double MG_START = 0.5, MG_JOIN = 0.25;
 constexpr int MT_MAX_CLUSTER = 8;
 
 // Tile blockIdx.y of sequence blockIdx.z, or the other way round (by_tile): tiles then start in the order of their work over all
@@ -211,7 +212,8 @@ int mass_cluster(long long tiles, int streamed, double seen, int per_sm, double 
   int best = 1;
   double least = 0.;
   for (int c = 1, log2c = 0; c <= MT_MAX_CLUSTER; c *= 2, ++log2c) {
-    const double over = start + join * log2c, longest = (streamed + c - 1) / c, waves = (double)tiles * c / co_cluster_ctas(c, per_sm);
+    const double over = start + join * log2c, longest = (streamed + c - 1) / c;
+    const double waves = (double)tiles * c / co_cluster_ctas(c, per_sm);
     double t = longest + over;
     if (waves > 1.) {
       t = fmax(t, waves * (streamed * seen / c + over));
@@ -247,10 +249,10 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
   const int c1 = mass_cluster(all_lane * n_kv_heads, cdiv(max_len, MG_B), seen, per_sm, MG_START, MG_JOIN);
   const int c2 = mass_cluster(all_key * n_kv_heads, (int)((lanes + MG_B - 1) / MG_B), seen, per_sm, MG_START, MG_JOIN);
   const MassGrid grid(n_seqs, max_len, n_total);
-  LAZY_TRY(co_launch(mass_general_kernel<T, 1>, grid.grid(n_kv_heads * c1, n_seqs, lane_tiles), dim3(MG_THREADS), smem, st, c1, false,
-                     q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, grid.by_tile, lse, mass, status));
-  return co_launch(mass_general_kernel<T, 2>, grid.grid(n_kv_heads * c2, n_seqs, key_tiles), dim3(MG_THREADS), smem, st, c2, true, q,
-                   ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, grid.by_tile, lse, mass, status);
+  LAZY_TRY(co_launch(mass_general_kernel<T, 1>, grid.grid(n_kv_heads * c1, n_seqs, lane_tiles), dim3(MG_THREADS), smem, st, c1,
+                     false, q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, grid.by_tile, lse, mass, status));
+  return co_launch(mass_general_kernel<T, 2>, grid.grid(n_kv_heads * c2, n_seqs, key_tiles), dim3(MG_THREADS), smem, st, c2,
+                   true, q, ldq, k, ldkv, cu, max_len, n_total, group, head_dim, window, grid.by_tile, lse, mass, status);
 }
 
 // ---- tensor-core form: bf16, head width up to 128 ----------------------------------------------------------------
@@ -275,7 +277,9 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
 // DEEP is the form for few lanes over many keys (a window of a long prompt), where a CTA would spend its time on starting up:
 // one CTA per SM with four stages; pass 1 cuts the keys into ranges (no clusters: eight to a cluster only 120 of the 148 SMs
 // can be used) and leaves each range's (maximum, sum), pass 2 merges them and takes a range of key tiles, the next one
-// loaded while the last is used.  Ranges are of one length for all sequences, so that long and short ones share the SMs.  A 64-row window over 16384 keys of 8 heads, group 4: 49 us without it.
+// loaded while the last is used.  Ranges are of one length for all sequences, so that long and short ones share the SMs (a one-row
+// window of five sequences of 16169 to 9 rows: 46 us with as many ranges to each, 28 so).  A 64-row window over 16384 keys of 8
+// heads, group 4: 35 us, 49 without this form.
 constexpr int MT = 128;                       // tile rows of either side, columns of S
 constexpr int MT_LSE_STAGES = 4, MT_DEEP_TILES = 4, MT_DEEP_SPLITS = 32;  // lane tiles that DEEP pass 2 takes at most
 static_assert(MT_DEEP_TILES <= MT_LSE_STAGES, "DEEP pass 2 keeps all lanes' log-sum-exps where the ring would be");
@@ -303,7 +307,8 @@ struct __align__(16) MassShared {
   int abort_flag;
 };
 template <int HD, bool DEEP>
-constexpr int mass_smem = (MassShape<DEEP>::A_BUFS + MassShape<DEEP>::STAGES) * MT * ((HD + 63) / 64) * 128 + 1024 + (int)sizeof(MassShared<DEEP>);
+constexpr int mass_smem =
+    (MassShape<DEEP>::A_BUFS + MassShape<DEEP>::STAGES) * MT * ((HD + 63) / 64) * 128 + 1024 + (int)sizeof(MassShared<DEEP>);
 
 // grid (n_kv_heads * cluster, tiles and sequences); DEEP, no clusters: pass 1 (n_kv_heads * splits, the same), pass 2 (n_kv_heads,
 // ranges of key tiles and sequences).  parts: (maximum, sum) of tile t's lanes over key range i at (((s * n_kv_heads + g) *
@@ -338,7 +343,8 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   const int first = n - rows_of(n), a_tiles = tiles_of(n);
   const int lane_tiles = (n - first + R - 1) / R, key_tiles = (n + MT - 1) / MT;
   // stationary tiles [at0, at1): one, most work first, or in DEEP pass 2 a range of them
-  const int at0 = PASS == 1 ? (by_tile ? (int)gridDim.z : a_tiles) - 1 - z : z * range, at1 = DEEP && PASS == 2 ? min(at0 + range, a_tiles) : at0 + 1;
+  const int at0 = PASS == 1 ? (by_tile ? (int)gridDim.z : a_tiles) - 1 - z : z * range;
+  const int at1 = DEEP && PASS == 2 ? min(at0 + range, a_tiles) : at0 + 1;
   if (at0 < 0 || at0 >= a_tiles) return;
   // key tiles that some lane of a lane tile sees; streamed tiles [b0, b1) of this CTA for a stationary one
   auto keys_of = [&](int lane_tile) { return min(key_tiles, (min(first + (lane_tile + 1) * R, n) + MT - 1) / MT); };
@@ -684,8 +690,8 @@ int mass_tc(cudaStream_t st, const void *q, int ldq, const void *k, int ldkv, co
   float2 *parts = reinterpret_cast<float2 *>(lse + (size_t)n_kv_heads * seq_tiles * MT);
   const MassGrid grid(n_seqs, max_len, n_total);
   auto launch = [&](auto kernel, int x, int tiles, int smem, int cluster, bool dependent) {
-    return co_launch(kernel, grid.grid(x, n_seqs, tiles), dim3(MT_THREADS), smem, st, cluster, dependent, mq, mk, cu, max_len, n_total,
-                     group, R, window, grid.by_tile, lse, seq_tiles, deep, parts, lane_tiles, mass, status);
+    return co_launch(kernel, grid.grid(x, n_seqs, tiles), dim3(MT_THREADS), smem, st, cluster, dependent, mq, mk, cu, max_len,
+                     n_total, group, R, window, grid.by_tile, lse, seq_tiles, deep, parts, lane_tiles, mass, status);
   };
   if (deep.splits) {
     LAZY_TRY((co_allow_smem<mass_tc_kernel<1, HD, true>>(mass_smem<HD, true>)));
@@ -709,8 +715,9 @@ size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n
   const size_t general = (size_t)n_total * n_heads;
   if (group > MT) return general;
   const MassDeep deep = mass_deep(n_seqs, n_total, max_len, n_heads, n_kv_heads, window);
+  const int lane_tiles = cdiv(window > 0 && window < max_len ? window : max_len, MT / group);
   const size_t tiled = (size_t)n_kv_heads * mass_seq_tiles(n_seqs, n_total, group) * MT +
-                       (size_t)n_seqs * n_kv_heads * deep.splits * MT * 2 * cdiv(window > 0 && window < max_len ? window : max_len, MT / group);
+                       (size_t)n_seqs * n_kv_heads * lane_tiles * deep.splits * MT * 2;
   return (general > tiled ? general : tiled) + 4;  // + 4: tiles start on a 16-byte boundary
 }
 

@@ -664,6 +664,7 @@ PrefixPlan prefix_plan(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv,
   PrefixPlan p;
   const int group = n_heads / n_kv_heads, R = PT_Q / group;
   const int lane_tiles = cdiv(n_rows, R), key_tiles = cdiv(n_pre, PT_K);
+  if (max_q > n_rows) max_q = n_rows;  // a bound may be any number
   p.tiles = lane_tiles > 1 ? 2 : 1;
   p.lane_groups = cdiv(lane_tiles, p.tiles);
   p.pre_parts = p.tiles_per_split = 0;
@@ -742,7 +743,7 @@ size_t attention_prefix_scratch_floats(int n_rows, int n_seqs, int max_q, int n_
                                        int n_kv_heads, int head_dim) {
   const size_t general =
       (size_t)n_rows * n_heads * attn_split_count((long long)n_rows * n_heads, n_pre + max_kv) * (head_dim + 2);
-  if (n_heads / n_kv_heads > PT_Q || max_q < 1 || n_seqs < 1) return general;
+  if (n_heads / n_kv_heads > PT_Q || max_q < 1 || n_seqs < 1 || n_rows < 1) return general;
   const PrefixPlan p = prefix_plan(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads, n_kv_heads);
   const size_t tiled = p.parts * p.pairs * (head_dim + 2) + 4;  // + 4: parts start on a 16-byte boundary
   return general > tiled ? general : tiled;

@@ -96,86 +96,86 @@ evict_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long
   // the newest rows, and all rows where all stay: slot t holds row t + (n - keep)
   for (int t = max(first, need == old ? 0 : need) + threadIdx.x; t < last; t += ES_THREADS) list[t] = start + n - keep + t;
   if (need > 0 && need < old && first < need) {
-  const bool held = old <= ES_KEYS;
-  if (held)
-    for (int i0 = threadIdx.x; i0 < old; i0 += ES_THREADS * ES_BATCH) {
-      float w[ES_BATCH];
-#pragma unroll
-      for (int i = 0; i < ES_BATCH; ++i) w[i] = i0 + i * ES_THREADS < old ? m[i0 + i * ES_THREADS] : 0.f;
-#pragma unroll
-      for (int i = 0; i < ES_BATCH; ++i)
-        if (i0 + i * ES_THREADS < old) keys[i0 + i * ES_THREADS] = co_weight_key(w[i]);
+    const bool held = old <= ES_KEYS;
+    if (held)
+      for (int i0 = threadIdx.x; i0 < old; i0 += ES_THREADS * ES_BATCH) {
+        float w[ES_BATCH];
+  #pragma unroll
+        for (int i = 0; i < ES_BATCH; ++i) w[i] = i0 + i * ES_THREADS < old ? m[i0 + i * ES_THREADS] : 0.f;
+  #pragma unroll
+        for (int i = 0; i < ES_BATCH; ++i)
+          if (i0 + i * ES_THREADS < old) keys[i0 + i * ES_THREADS] = co_weight_key(w[i]);
+      }
+    auto key_of = [&](int i) { return held ? keys[i] : co_weight_key(m[i]); };
+    uint32_t prefix = 0u, mask = 0u;
+    int left = need;
+    for (int pass = 0; pass < 3; ++pass) {  // digits of 11, 11 and 10 bits from the top
+      const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : ES_BINS;
+      const int copies = pass == 0 ? ES_COPIES : 1;  // later passes count the few rows of one bin
+      for (int i = threadIdx.x; i < copies * ES_PITCH; i += ES_THREADS) hist[i] = 0;
+      __syncthreads();
+  #pragma unroll 4
+      for (int i = threadIdx.x; i < old; i += ES_THREADS) {
+        const uint32_t key = key_of(i);
+        if ((key & mask) == prefix) atomicAdd(&hist[(lane & (copies - 1)) * ES_PITCH + ((key >> shift) & (bins - 1))], 1);
+      }
+      __syncthreads();
+      if (threadIdx.x < ES_SCAN) find_bin(hist, copies, bins, left, warp_sums[0], found);
+      __syncthreads();
+      left -= found[1];
+      prefix |= (uint32_t)found[0] << shift;
+      mask |= (uint32_t)(bins - 1) << shift;
     }
-  auto key_of = [&](int i) { return held ? keys[i] : co_weight_key(m[i]); };
-  uint32_t prefix = 0u, mask = 0u;
-  int left = need;
-  for (int pass = 0; pass < 3; ++pass) {  // digits of 11, 11 and 10 bits from the top
-    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : ES_BINS;
-    const int copies = pass == 0 ? ES_COPIES : 1;  // later passes count the few rows of one bin
-    for (int i = threadIdx.x; i < copies * ES_PITCH; i += ES_THREADS) hist[i] = 0;
-    __syncthreads();
-#pragma unroll 4
-    for (int i = threadIdx.x; i < old; i += ES_THREADS) {
+    // ---- keys above `prefix` stay, and of those equal to it the first `left`; warp w walks rows [w part, (w + 1) part).
+    // Where all equal ones stay (no tie is cut) "above" takes them in, and one vote per 32 rows is enough.
+    const bool cut = found[2] != left;
+    const int part = ((old + ES_WARPS - 1) / ES_WARPS + 31) / 32 * 32;
+    const int begin = min(warp * part, old), end = min(begin + part, old);
+    int n_above = 0, n_equal = 0;
+  #pragma unroll 4
+    for (int i = begin + lane; i < end; i += 32) {
       const uint32_t key = key_of(i);
-      if ((key & mask) == prefix) atomicAdd(&hist[(lane & (copies - 1)) * ES_PITCH + ((key >> shift) & (bins - 1))], 1);
+      n_above += cut ? key > prefix : key >= prefix;
+      n_equal += key == prefix;
+    }
+    n_above = __reduce_add_sync(0xffffffffu, n_above);
+    n_equal = cut ? __reduce_add_sync(0xffffffffu, n_equal) : 0;
+    __syncthreads();  // warp_sums may still be read from the last pass
+    if (lane == 0) {
+      warp_sums[0][warp] = n_above;
+      warp_sums[1][warp] = n_equal;
     }
     __syncthreads();
-    if (threadIdx.x < ES_SCAN) find_bin(hist, copies, bins, left, warp_sums[0], found);
-    __syncthreads();
-    left -= found[1];
-    prefix |= (uint32_t)found[0] << shift;
-    mask |= (uint32_t)(bins - 1) << shift;
-  }
-  // ---- keys above `prefix` stay, and of those equal to it the first `left`; warp w walks rows [w part, (w + 1) part).
-  // Where all equal ones stay (no tie is cut) "above" takes them in, and one vote per 32 rows is enough.
-  const bool cut = found[2] != left;
-  const int part = ((old + ES_WARPS - 1) / ES_WARPS + 31) / 32 * 32;
-  const int begin = min(warp * part, old), end = min(begin + part, old);
-  int n_above = 0, n_equal = 0;
-#pragma unroll 4
-  for (int i = begin + lane; i < end; i += 32) {
-    const uint32_t key = key_of(i);
-    n_above += cut ? key > prefix : key >= prefix;
-    n_equal += key == prefix;
-  }
-  n_above = __reduce_add_sync(0xffffffffu, n_above);
-  n_equal = cut ? __reduce_add_sync(0xffffffffu, n_equal) : 0;
-  __syncthreads();  // warp_sums may still be read from the last pass
-  if (lane == 0) {
-    warp_sums[0][warp] = n_above;
-    warp_sums[1][warp] = n_equal;
-  }
-  __syncthreads();
-  // rows above, and equal ones, before this warp's
-  int at = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sums[0][lane] : 0);
-  int ties = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sums[1][lane] : 0);
-  const uint32_t below = (1u << lane) - 1u;
-  if (!cut) {
-    if (at < last && at + n_above > first) {
-#pragma unroll 4
+    // rows above, and equal ones, before this warp's
+    int at = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sums[0][lane] : 0);
+    int ties = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sums[1][lane] : 0);
+    const uint32_t below = (1u << lane) - 1u;
+    if (!cut) {
+      if (at < last && at + n_above > first) {
+  #pragma unroll 4
+        for (int i0 = begin; i0 < end; i0 += 32) {
+          const int i = i0 + lane;
+          const bool stays = i < end && key_of(i) >= prefix;
+          const uint32_t all = __ballot_sync(0xffffffffu, stays);
+          const int slot = at + __popc(all & below);
+          if (stays && slot >= first && slot < last) list[slot] = start + i;
+          at += __popc(all);
+        }
+      }
+    } else {
       for (int i0 = begin; i0 < end; i0 += 32) {
         const int i = i0 + lane;
-        const bool stays = i < end && key_of(i) >= prefix;
-        const uint32_t all = __ballot_sync(0xffffffffu, stays);
-        const int slot = at + __popc(all & below);
-        if (stays && slot >= first && slot < last) list[slot] = start + i;
-        at += __popc(all);
+        const uint32_t key = i < end ? key_of(i) : 0u;
+        const uint32_t above = __ballot_sync(0xffffffffu, i < end && key > prefix);
+        const uint32_t equal = __ballot_sync(0xffffffffu, i < end && key == prefix);
+        const int my_ties = ties + __popc(equal & below);
+        const int slot = at + __popc(above & below) + min(my_ties, left);
+        if (((above >> lane & 1u) || ((equal >> lane & 1u) && my_ties < left)) && slot >= first && slot < last)
+          list[slot] = start + i;
+        at += __popc(above);
+        ties += __popc(equal);
       }
     }
-  } else {
-    for (int i0 = begin; i0 < end; i0 += 32) {
-      const int i = i0 + lane;
-      const uint32_t key = i < end ? key_of(i) : 0u;
-      const uint32_t above = __ballot_sync(0xffffffffu, i < end && key > prefix);
-      const uint32_t equal = __ballot_sync(0xffffffffu, i < end && key == prefix);
-      const int my_ties = ties + __popc(equal & below);
-      const int slot = at + __popc(above & below) + min(my_ties, left);
-      if (((above >> lane & 1u) || ((equal >> lane & 1u) && my_ties < left)) && slot >= first && slot < last)
-        list[slot] = start + i;
-      at += __popc(above);
-      ties += __popc(equal);
-    }
-  }
   }
   __syncthreads();  // the share's list is complete
   const int pieces = (last - first) * vecs;

@@ -556,6 +556,21 @@ def test_other_widths_do_not_reach_beyond_their_heads(dh):
     B.lazy_device_status()
 
 
+@pytest.mark.parametrize("heads", [HEADS[1], HEADS[7]], ids=[IDS[1], IDS[7]])
+def test_attention_prefix_takes_any_bounds(heads):
+    """max_q and max_kv are bounds, not lengths: the largest number is one."""
+    H, Hkv, dh, dtype = heads
+    n_pre, rows, own = 65, [2, 1, 3], [5, 0, 70]
+    d = prefix_case(27, n_pre, rows, own, H, Hkv, dh, dtype)
+    want, tol = prefix_expected(d, rows, own, H, Hkv, dh)
+    dev = {k: v.cuda() for k, v in d.items()}
+    for max_q, max_kv in ((2 ** 31 - 1, 70), (3, 20000), (2 ** 31 - 1, 20000)):
+        got = B.lazy_k_attention_prefix(dev["q"], cu(rows), max_q, dev["k_pre"], dev["v_pre"], dev["k"], dev["v"],
+                                        dev["kv_idx"], cu(own), max_kv, H, Hkv, dh)
+        assert np.all(np.abs(f64(got).reshape(want.shape) - want) <= tol)
+    B.lazy_device_status()
+
+
 @pytest.mark.parametrize("heads", [HEADS[1], HEADS[5]], ids=[IDS[1], IDS[5]])
 def test_attention_prefix_reports_bad_rows_and_tables(heads):
     H, Hkv, dh, dtype = heads
