@@ -32,9 +32,10 @@ __device__ __forceinline__ uint32_t co_weight_key(float w) {
 // Opts a kernel in to `bytes` of dynamic shared memory, once per device (the attribute belongs to the device's
 // context).  More than 64 devices simply set it again each time.
 // `beside`: asks for the largest split of the SM's memory in favour of shared memory, so that a CTA of another kernel finds
-// room beside this one's (both have to ask; it takes L1 from kernels that want it).
+// room beside this one's (both have to ask; it takes L1 from kernels that want it).  `large_clusters`: lets it run in clusters of
+// more than eight.
 template <auto Kernel>
-inline int co_allow_smem(int bytes, bool beside = false) {
+inline int co_allow_smem(int bytes, bool beside = false, bool large_clusters = false) {
   static std::atomic<unsigned long long> done{0};
   int dev = 0;
   LAZY_CUDA_OK(cudaGetDevice(&dev));
@@ -43,6 +44,7 @@ inline int co_allow_smem(int bytes, bool beside = false) {
   LAZY_CUDA_OK(cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
   if (beside)
     LAZY_CUDA_OK(cudaFuncSetAttribute(Kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
+  if (large_clusters) LAZY_CUDA_OK(cudaFuncSetAttribute(Kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   done.fetch_or(bit, std::memory_order_release);
   return LAZY_OK;
 }
@@ -89,13 +91,13 @@ inline int co_launch(void (*kfn)(KArgs...), dim3 grid, dim3 block, size_t smem, 
   return e == cudaSuccess ? LAZY_OK : LAZY_E_CUDA;
 }
 
-// CTAs that run at once in clusters of `size` (1, 2, 4 or 8), up to three to an SM: a cluster stays within a group of SMs, and
+// CTAs that run at once in clusters of `size` (1, 2, 4, 8 or 16), up to three to an SM: a cluster stays within a group of SMs, and
 // the groups are not multiples of it (as the occupancy calculator has it for 148 SMs).  A launch of more runs its last
 // clusters after the others.
 inline int co_cluster_ctas(int size, int per_sm) {
-  constexpr int FOUR[3] = {132, 284, 416}, EIGHT[3] = {120, 264, 384};
+  constexpr int TABLE[3][3] = {{132, 284, 416}, {120, 264, 384}, {112, 224, 336}};
   if (size <= 2) return sm_count() * per_sm;
-  return sm_count() * (size == 4 ? FOUR : EIGHT)[per_sm - 1] / 148;
+  return sm_count() * TABLE[size == 4 ? 0 : (size == 8 ? 1 : 2)][per_sm - 1] / 148;
 }
 
 __device__ __forceinline__ uint32_t co_cluster_rank() {

@@ -167,7 +167,8 @@ int step_general(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevSta
 // shared memory when its group comes up.  The parts' maxima, sums and outputs meet in distributed shared memory, and
 // every CTA adds the final weights of its own slots to their masses from the logits it kept (in shared memory, or in
 // the scratch when a part is too long).
-constexpr int SF_WARPS = 4, SF_THREADS = SF_WARPS * 32, SF_STAGES = 2, SF_CTAS = 3, SF_MAX_CLUSTER = 8;
+constexpr int SF_WARPS = 4, SF_THREADS = SF_WARPS * 32, SF_STAGES = 2, SF_CTAS = 3;
+constexpr int SF_MAX_CLUSTER = 8, SF_LARGE_CLUSTER = 16;  // the second is beyond what every device has to offer: see step_cluster
 // A part's logits stay in shared memory up to this size: with three CTAs on an SM, with two or one
 constexpr int SF_LOGIT_BYTES = 8192, SF_LOGIT_BYTES_2 = 40960;
 constexpr int SF_BATCH = 8;           // slots a thread has in flight in the loops over weights
@@ -183,7 +184,7 @@ struct StepShared {
 template <int HD, int NT>
 constexpr int step_stage_bytes = SF_WARPS * SF_STAGES * RowsMma<HD, NT>::STAGE;
 
-template <int HD, int NT>
+template <int HD, int NT, int MAX_CLUSTER>
 __global__ void __launch_bounds__(SF_THREADS, SF_CTAS)
 step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_in_smem, float *__restrict__ scratch,
                   DevStatus *status) {
@@ -282,7 +283,7 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
         co_cluster_sync();
         best = *co_map_shared(&sh.best, lane & (csize - 1));  // csize is a power of two
 #pragma unroll
-        for (int k = SF_MAX_CLUSTER / 2; k > 0; k >>= 1) best = min_u64(best, __shfl_xor_sync(0xffffffffu, best, k));
+        for (int k = MAX_CLUSTER / 2; k > 0; k >>= 1) best = min_u64(best, __shfl_xor_sync(0xffffffffu, best, k));
       } else {
         __syncthreads();
         best = sh.best;
@@ -387,33 +388,33 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
   // ---- the final maxima and sums, the same in every thread that needs them; this CTA's share of the outputs.  All
   // reads of the other CTAs' memory are in flight together.
   auto gather = [&](int c, float &ref, float &inv, float *scale) {
-    float rm[SF_MAX_CLUSTER], rl[SF_MAX_CLUSTER], mx = -INFINITY, sum = 0.f;
+    float rm[MAX_CLUSTER], rl[MAX_CLUSTER], mx = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int r = 0; r < SF_MAX_CLUSTER; ++r) {
+    for (int r = 0; r < MAX_CLUSTER; ++r) {
       rm[r] = r < csize ? *co_map_shared(&sh.m[c], r) : -INFINITY;
       rl[r] = r < csize ? *co_map_shared(&sh.l[c], r) : 0.f;
     }
 #pragma unroll
-    for (int r = 0; r < SF_MAX_CLUSTER; ++r) mx = fmaxf(mx, rm[r]);
+    for (int r = 0; r < MAX_CLUSTER; ++r) mx = fmaxf(mx, rm[r]);
     ref = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
-    for (int r = 0; r < SF_MAX_CLUSTER; ++r) {
+    for (int r = 0; r < MAX_CLUSTER; ++r) {
       scale[r] = ex2_approx(rm[r] - ref);
       sum += rl[r] * scale[r];
     }
     inv = 1.f / sum;
   };
   for (int i = rank * SF_THREADS + threadIdx.x; i < group * HD; i += csize * SF_THREADS) {
-    float part[SF_MAX_CLUSTER], scale[SF_MAX_CLUSTER], ref, inv, sum = 0.f;
+    float part[MAX_CLUSTER], scale[MAX_CLUSTER], ref, inv, sum = 0.f;
 #pragma unroll
-    for (int r = 0; r < SF_MAX_CLUSTER; ++r) part[r] = r < csize ? *co_map_shared(co + i, r) : 0.f;
+    for (int r = 0; r < MAX_CLUSTER; ++r) part[r] = r < csize ? *co_map_shared(co + i, r) : 0.f;
     gather(i / HD, ref, inv, scale);
 #pragma unroll
-    for (int r = 0; r < SF_MAX_CLUSTER; ++r) sum += part[r] * scale[r];  // ranks that do not exist: 0 x 0
+    for (int r = 0; r < MAX_CLUSTER; ++r) sum += part[r] * scale[r];  // ranks that do not exist: 0 x 0
     o[i] = __float2bfloat16_rn(sum * inv);
   }
   if (threadIdx.x < group) {
-    float scale[SF_MAX_CLUSTER], ref, inv;
+    float scale[MAX_CLUSTER], ref, inv;
     gather(threadIdx.x, ref, inv, scale);
     sh.fm[threadIdx.x] = ref;
     sh.finv[threadIdx.x] = inv;
@@ -453,25 +454,34 @@ bool step_fused_eligible(int dtype, int head_dim, int group) {
 
 // CTAs per (sequence, head): the next power of two that still leaves every warp a group of 16 slots and room for
 // all CTAs at once at three per SM.  A second wave costs more than it spreads: 32 sequences of 2048 slots on 8 heads
-// take 47 us with one CTA each, 61 us with two, 63 us with four.
+// take 47 us with one CTA each, 61 us with two, 63 us with four.  Sixteen to a cluster, where the heads are few and the lists
+// long: a CTA's four warps get through 1000 slots in some 14 us, whatever is left idle beside it (8000 slots on 8 heads: 19.6 us
+// with eight, 16.3 with sixteen; 16000 on one: 30.8 and 18.6; 2000 on eight: 9.5 and 9.6; 4000 on 16: 15.9 and 15.7).
 int step_cluster(long long heads, int budget) {
+  if (heads * SF_LARGE_CLUSTER <= co_cluster_ctas(SF_LARGE_CLUSTER, 2) && budget > SF_LARGE_CLUSTER * 2 * SF_WARPS * RM_KEYS)
+    return SF_LARGE_CLUSTER;
   int c = 1;
   while (c < SF_MAX_CLUSTER && heads * c * 2 <= co_cluster_ctas(c * 2, SF_CTAS) && budget > c * SF_WARPS * RM_KEYS) c *= 2;
   return c;
 }
 int step_part_slots(int budget, int cluster) { return cdiv(cdiv(budget, RM_KEYS), cluster) * RM_KEYS; }
 
-template <int HD, int NT>
-int step_fused(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevStatus *status) {
-  const int group = a.n_heads / a.n_kv_heads;
-  const long long heads = (long long)a.n_seqs * a.n_kv_heads;
-  const int cluster = step_cluster(heads, a.budget), part = step_part_slots(a.budget, cluster);
-  const long long logit_bytes = (long long)part * ((group + 1) & ~1) * 4;
+template <int HD, int NT, int MAX_CLUSTER>
+int step_fused_launch(cudaStream_t st, const EvictStepArgs &a, int cluster, float *scratch, DevStatus *status) {
+  const int group = a.n_heads / a.n_kv_heads, part = step_part_slots(a.budget, cluster);
+  const long long heads = (long long)a.n_seqs * a.n_kv_heads, logit_bytes = (long long)part * ((group + 1) & ~1) * 4;
   const int in_smem = logit_bytes <= (heads * cluster <= 2LL * sm_count() ? SF_LOGIT_BYTES_2 : SF_LOGIT_BYTES);
   const int smem = step_stage_bytes<HD, NT> + (in_smem ? (int)logit_bytes : 0);
-  LAZY_TRY((co_allow_smem<step_fused_kernel<HD, NT>>(step_stage_bytes<HD, NT> + SF_LOGIT_BYTES_2)));
-  return co_launch(step_fused_kernel<HD, NT>, dim3((unsigned)(heads * cluster)), dim3(SF_THREADS), smem, st, cluster, false,
-                   a, group, part, in_smem, scratch, status);
+  LAZY_TRY((co_allow_smem<step_fused_kernel<HD, NT, MAX_CLUSTER>>(step_stage_bytes<HD, NT> + SF_LOGIT_BYTES_2, false,
+                                                                 MAX_CLUSTER > SF_MAX_CLUSTER)));
+  return co_launch(step_fused_kernel<HD, NT, MAX_CLUSTER>, dim3((unsigned)(heads * cluster)), dim3(SF_THREADS), smem, st, cluster,
+                   false, a, group, part, in_smem, scratch, status);
+}
+template <int HD, int NT>
+int step_fused(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevStatus *status) {
+  const int cluster = step_cluster((long long)a.n_seqs * a.n_kv_heads, a.budget);
+  return cluster > SF_MAX_CLUSTER ? step_fused_launch<HD, NT, SF_LARGE_CLUSTER>(st, a, cluster, scratch, status)
+                                  : step_fused_launch<HD, NT, SF_MAX_CLUSTER>(st, a, cluster, scratch, status);
 }
 
 }  // namespace
@@ -480,7 +490,7 @@ size_t evict_step_scratch_floats(int n_seqs, int n_heads, int n_kv_heads, int he
   const size_t general = step_scratch(n_seqs, n_heads, n_kv_heads, head_dim, budget).total;
   // the one-launch form keeps at most every slot's logits, an even number of columns, parts rounded up to 16 slots
   const size_t heads = (size_t)n_seqs * n_kv_heads, group = n_heads / n_kv_heads;
-  const size_t fused = heads * ((size_t)budget + SF_MAX_CLUSTER * RM_KEYS) * ((group + 1) & ~(size_t)1);
+  const size_t fused = heads * ((size_t)budget + SF_LARGE_CLUSTER * RM_KEYS) * ((group + 1) & ~(size_t)1);
   return general > fused ? general : fused;
 }
 

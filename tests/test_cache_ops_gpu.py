@@ -381,6 +381,15 @@ def test_evict_step_long_cache():
     check_step(c, new, H, 9000, 1000)
 
 
+@pytest.mark.parametrize("heads", [HEADS[2], HEADS[9], HEADS[10], (16, 1, 128, BF16)], ids=[IDS[2], IDS[9], IDS[10], "16on1x128"])
+@pytest.mark.parametrize("lens", [[2100, 0], [2600, 2599, 17], [2049]])
+def test_evict_step_long_caches_of_few_heads(heads, lens):
+    """Many CTAs to a head, most of them without a slot where the cache is nearly empty."""
+    H, Hkv, dh, dtype = heads
+    c, new = step_case(28 + len(lens), lens, max(lens), H, Hkv, dh, dtype)
+    check_step(c, new, H, max(lens), 100)
+
+
 def test_evict_steps_in_a_row_and_replayed():
     """Forty steps in place from an almost empty cache, the same forty from one captured graph: the same state."""
     H, Hkv, dh, dtype, budget, S = 8, 2, 128, BF16, 24, 3
