@@ -2,7 +2,7 @@
 // its request's own key list (row i of T rows: keys j <= C - T + i of C), so the prefix part is one product of all
 // rows with the prefix's keys: it is computed for the batch together and read once, not once per request.
 //
-// bf16, head width up to 128: three launches.  (1) The prefix on tcgen05: the batch's (row, head) pairs of one
+// bf16, head width up to 128: three launches, one for a few requests without a prefix.  (1) The prefix on tcgen05: the batch's (row, head) pairs of one
 // key/value head are the lanes of 128-lane tiles, the prefix's keys are cut into ranges, every CTA leaves the partial
 // softmax of its lanes over its range.  (2) The requests' own keys on the warp-level path of rows_mma.cuh, launched as a
 // dependent that does not wait for (1): a CTA of it fits beside one of (1).  (3) A merge of the parts, one warp per
@@ -428,17 +428,21 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 // ---- (2) the requests' own keys -----------------------------------------------------------------------------------
 // One CTA: 8 NT columns (row, head) of one (request, key/value head) over one range of its list; warps take every fourth group of
 // 16 keys, and their parts are added in shared memory.
-constexpr int PO_WARPS = 4, PO_THREADS = PO_WARPS * 32, PO_STAGES = 2;
+constexpr int PO_WARPS = 4, PO_THREADS = PO_WARPS * 32, PO_STAGES = 2, PO_CLUSTER = 8;
 constexpr int PO_KEYS = 256;  // of a part; 64 requests with 1 to 500 keys of their own: 69 us with 64, 55 with 128, 50 with 256, 51 with 512
 
 template <int HD, int NT>
 struct PrefixOwnShared {
   float wm[PO_WARPS][NT * 8], wl[PO_WARPS][NT * 8];
-  size_t pair[NT * 8];  // where a column's part goes
+  float m[NT * 8], l[NT * 8];  // of the CTA, read by the cluster
+  size_t pair[NT * 8];         // where a column's part goes
 };
 
-// grid (n_kv_heads * column blocks, splits, n_seqs)
-template <int HD, int NT>
+// grid (n_kv_heads * column blocks, splits, n_seqs).  DIRECT, without a prefix and with lists of few parts: the parts are the
+// CTAs of a cluster, grid (n_kv_heads * column blocks * parts, 1, n_seqs), which leave the outputs themselves and no merge is
+// needed: one row with 20 keys, 8 heads of 64, 3.7 us, 4.4 with a merge (among calls from Python 4.7 and 6.7); with 300 keys, 8
+// heads of 128, 4.9 and 5.7.  More CTAs than run at once lose by it: 32 requests of five rows, 200 keys 34.4 us, with a merge 27.8.
+template <int HD, int NT, bool DIRECT>
 __global__ void __launch_bounds__(PO_THREADS, NT == 1 ? 4 : 2)
 prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, float *__restrict__ part_o,
                   float2 *__restrict__ part_ml, DevStatus *status) {
@@ -446,14 +450,25 @@ prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, 
   extern __shared__ __align__(128) uint8_t own_smem[];
   __shared__ PrefixOwnShared<HD, NT> sh;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int g = blockIdx.x / col_blocks, cb = blockIdx.x - g * col_blocks, s = blockIdx.z;
+  const int csize = DIRECT ? (int)co_cluster_size() : 1, split = DIRECT ? (int)co_cluster_rank() : (int)blockIdx.y;
+  const int unit = blockIdx.x / csize, g = unit / col_blocks, cb = unit - g * col_blocks, s = blockIdx.z;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int q0 = a.cu_q[s], T = a.cu_q[s + 1] - q0, c0 = a.cu_kv[s], C = a.cu_kv[s + 1] - c0;
   const bool fits = q0 >= 0 && T >= 0 && q0 + T <= a.n_rows && T <= a.max_q && c0 >= 0 && C >= 0 && c0 + C <= a.n_kv &&
                     C <= a.max_kv;
   if (!fits && threadIdx.x == 0) dev_fail(status, LAZY_E_BADARG, W_PREFIX, s, -1);
   const int n_cols = T * group, col0 = cb * NT * 8;
-  const int lo = blockIdx.y * per_split, hi = min(lo + per_split, C);
+  const int lo = split * per_split, hi = min(lo + per_split, C);
+  bf16 *o = (bf16 *)a.o;
+  if (DIRECT && blockIdx.x == 0) {  // rows that belong to nobody, or to a list that does not fit, are zero
+    const int before = s == 0 ? min(max(q0, 0), a.n_rows) : 0, behind = s == a.n_seqs - 1 ? max(q0 + T, 0) : a.n_rows;
+    const int bad0 = fits ? 0 : max(q0, 0), bad1 = fits ? 0 : min(q0 + T, a.n_rows);
+    if ((before > 0 || behind < a.n_rows) && threadIdx.x == 0) dev_fail(status, LAZY_E_BADARG, W_PREFIX, s, behind);
+    const size_t width = (size_t)a.n_heads * HD;
+    for (size_t i = threadIdx.x; i < before * width; i += PO_THREADS) o[i] = __float2bfloat16_rn(0.f);
+    for (size_t i = behind * width + threadIdx.x; i < a.n_rows * width; i += PO_THREADS) o[i] = __float2bfloat16_rn(0.f);
+    for (size_t i = bad0 * width + threadIdx.x; bad1 > bad0 && i < bad1 * width; i += PO_THREADS) o[i] = __float2bfloat16_rn(0.f);
+  }
   if (fits && col0 < n_cols) {
     const uint32_t stages = smem_u32(own_smem) + warp * PO_STAGES * Rows::STAGE;
     Rows rows;
@@ -538,7 +553,7 @@ prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, 
     }
     __syncthreads();  // also: no warp reads its stages any more
     float *wo = reinterpret_cast<float *>(own_smem);  // [warp][column][HD]
-    const size_t base = (size_t)blockIdx.y * a.n_rows * a.n_heads;
+    const size_t base = DIRECT ? 0 : (size_t)split * a.n_rows * a.n_heads;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -560,21 +575,51 @@ prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, 
 #pragma unroll
           for (int w = 0; w < PO_WARPS; ++w) sum += sh.wl[w][c] * ex2_approx(sh.wm[w][c] - ref);
           const size_t pair = base + (size_t)(q0 + f / group) * a.n_heads + g * group + f % group;
-          part_ml[pair] = make_float2(mx, sum);
+          if (!DIRECT) part_ml[pair] = make_float2(mx, sum);
           sh.pair[c] = pair;
+          sh.m[c] = mx;
+          sh.l[c] = sum;
         }
       }
     __syncthreads();
-    for (int i = threadIdx.x; i < min(NT * 8, n_cols - col0) * HD; i += PO_THREADS) {
+    const int outputs = min(NT * 8, n_cols - col0) * HD;
+    float *co = wo + PO_WARPS * NT * 8 * HD;  // [column][HD]: the CTA's part, read by the cluster
+    static_assert((PO_WARPS + 1) * NT * 8 * HD * 4 <= PO_WARPS * PO_STAGES * Rows::STAGE, "the stages hold the outputs in the end");
+    for (int i = threadIdx.x; i < outputs; i += PO_THREADS) {
       float sum = 0.f;
 #pragma unroll
       for (int w = 0; w < PO_WARPS; ++w) sum += wo[(size_t)w * NT * 8 * HD + i];
-      part_o[sh.pair[i / HD] * HD + i % HD] = sum;
+      if (DIRECT) co[i] = sum;
+      else part_o[sh.pair[i / HD] * HD + i % HD] = sum;
+    }
+    if (DIRECT) {
+      co_cluster_sync();
+      for (int i = split * PO_THREADS + threadIdx.x; i < outputs; i += csize * PO_THREADS) {
+        float part[PO_CLUSTER], m[PO_CLUSTER], l[PO_CLUSTER], mx = -INFINITY, sum = 0.f, total = 0.f;
+#pragma unroll
+        for (int r = 0; r < PO_CLUSTER; ++r) {
+          part[r] = r < csize ? *co_map_shared(co + i, r) : 0.f;
+          m[r] = r < csize ? *co_map_shared(&sh.m[i / HD], r) : -INFINITY;
+          l[r] = r < csize ? *co_map_shared(&sh.l[i / HD], r) : 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < PO_CLUSTER; ++r) mx = fmaxf(mx, m[r]);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+        for (int r = 0; r < PO_CLUSTER; ++r) {
+          const float scale = ex2_approx(m[r] - ref);
+          sum += part[r] * scale;
+          total += l[r] * scale;
+        }
+        const float inv = total > 0.f ? 1.f / total : (total != total ? NAN : 0.f);
+        o[sh.pair[i / HD] * HD + i % HD] = __float2bfloat16_rn(sum * inv);
+      }
+      co_cluster_sync();  // nobody leaves while its part is being read
     }
   }
   // the merge waits for this kernel alone: its end has to mean the end of the one before it.  One CTA sees to that; the
   // others leave their SMs to the next ones.
-  if (blockIdx.x + blockIdx.y + blockIdx.z == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (!DIRECT && blockIdx.x + blockIdx.y + blockIdx.z == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // ---- (3) the merge: one warp per (row, head) ------------------------------------------------------------------------
@@ -664,6 +709,7 @@ bool prefix_tc_eligible(int dtype, int head_dim, int group) {
 // How the work is cut: key ranges of the prefix and of the own lists, so that every launch fills the machine once.
 struct PrefixPlan {
   int tiles, lane_groups, pre_parts, tiles_per_split, nt, col_blocks, own_parts, own_split;
+  bool direct;  // no prefix, and clusters of the own keys' parts all run at once: one launch
   size_t pairs, parts;
 };
 PrefixPlan prefix_plan(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv, int n_heads, int n_kv_heads) {
@@ -685,6 +731,7 @@ PrefixPlan prefix_plan(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv,
   p.nt = max_q * group <= 8 ? 1 : 2;
   p.col_blocks = cdiv(max_q * group, p.nt * 8);
   p.own_parts = p.own_split = 0;
+  p.direct = false;
   if (max_kv > 0) {
     const long long ctas = (long long)n_kv_heads * p.col_blocks * n_seqs;
     long long want = (2LL * sm_count() + ctas - 1) / ctas;
@@ -692,8 +739,14 @@ PrefixPlan prefix_plan(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv,
     if (want > 64) want = 64;
     const int most = cdiv(max_kv, PO_WARPS * RM_KEYS);  // a group of keys per warp at least
     if (want > most) want = most;
+    if (key_tiles == 0) {
+      long long c = 1;
+      while (c < PO_CLUSTER && c < want && ctas * c * 2 <= co_cluster_ctas((int)c * 2, 3)) c *= 2;
+      p.direct = c * PO_KEYS * 2 >= max_kv && ctas * c <= co_cluster_ctas((int)c, 3);
+      if (p.direct) want = c;
+    }
     p.own_split = cdiv(cdiv(max_kv, (int)want), RM_KEYS) * RM_KEYS;
-    p.own_parts = cdiv(max_kv, p.own_split);
+    p.own_parts = p.direct ? (int)want : cdiv(max_kv, p.own_split);
   }
   p.pairs = (size_t)n_rows * n_heads;
   p.parts = (size_t)p.pre_parts + p.own_parts;
@@ -713,13 +766,15 @@ int prefix_tc_launch(cudaStream_t st, const PrefixArgs &a, const PrefixPlan &p, 
                    dim3(PrefixShape<HD, TILES>::THREADS), prefix_smem<HD, TILES>, st, 1, false, mq, mk, mv, a.n_rows, group, R,
                    a.n_pre, p.tiles_per_split, part_o, part_ml, status);
 }
-template <int HD, int NT>
+template <int HD, int NT, bool DIRECT>
 int prefix_own_launch(cudaStream_t st, const PrefixArgs &a, const PrefixPlan &p, int group, float *part_o, float2 *part_ml,
                       DevStatus *status) {
   constexpr int SMEM = PO_WARPS * PO_STAGES * RowsMma<HD, NT>::STAGE;
-  LAZY_TRY((co_allow_smem<prefix_own_kernel<HD, NT>>(SMEM, true)));
-  return co_launch(prefix_own_kernel<HD, NT>, dim3(a.n_kv_heads * p.col_blocks, p.own_parts, a.n_seqs), dim3(PO_THREADS), SMEM,
-                   st, 1, p.pre_parts > 0, a, group, p.col_blocks, p.own_split, part_o, part_ml, status);
+  const int units = a.n_kv_heads * p.col_blocks;
+  LAZY_TRY((co_allow_smem<prefix_own_kernel<HD, NT, DIRECT>>(SMEM, true)));
+  return co_launch(prefix_own_kernel<HD, NT, DIRECT>, DIRECT ? dim3(units * p.own_parts, 1, a.n_seqs) : dim3(units, p.own_parts, a.n_seqs),
+                   dim3(PO_THREADS), SMEM, st, DIRECT ? p.own_parts : 1, p.pre_parts > 0, a, group, p.col_blocks, p.own_split,
+                   part_o, part_ml, status);
 }
 
 template <int HD>
@@ -731,11 +786,14 @@ int prefix_tc(cudaStream_t st, const PrefixArgs &a, float *scratch, DevStatus *s
   if (p.pre_parts > 0)
     LAZY_TRY((p.tiles == 1 ? prefix_tc_launch<HD, 1>(st, a, p, group, part_o, part_ml, status)
                            : prefix_tc_launch<HD, 2>(st, a, p, group, part_o, part_ml, status)));
+  if (p.direct)
+    return p.nt == 1 ? prefix_own_launch<HD, 1, true>(st, a, p, group, nullptr, nullptr, status)
+                     : prefix_own_launch<HD, 2, true>(st, a, p, group, nullptr, nullptr, status);
   if (p.own_parts > 0) {
     float *own_o = part_o + (size_t)p.pre_parts * p.pairs * HD;
     float2 *own_ml = part_ml + (size_t)p.pre_parts * p.pairs;
-    LAZY_TRY((p.nt == 1 ? prefix_own_launch<HD, 1>(st, a, p, group, own_o, own_ml, status)
-                        : prefix_own_launch<HD, 2>(st, a, p, group, own_o, own_ml, status)));
+    LAZY_TRY((p.nt == 1 ? prefix_own_launch<HD, 1, false>(st, a, p, group, own_o, own_ml, status)
+                        : prefix_own_launch<HD, 2, false>(st, a, p, group, own_o, own_ml, status)));
   }
   const long long warps = (long long)p.pairs;
   return co_launch(prefix_tc_merge_kernel<HD>, dim3((unsigned)((warps + 3) / 4)), dim3(128), 0, st, 1, p.parts > 0, a,

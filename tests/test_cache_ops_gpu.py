@@ -467,7 +467,8 @@ def run_prefix(d, rows, own, H, Hkv, dh, **kw):
 
 PREFIX_SHAPES = [(0, [1], [1]), (0, [1, 2], [0, 1]), (1, [1], [0]), (63, [1, 1, 1], [5, 64, 65]), (64, [5, 3], [5, 200]),
                  (65, [2], [1]), (300, [1] * 40, [1 + 3 * i for i in range(40)]), (129, [8, 1, 4], [129, 0, 128]),
-                 (1000, [33], [40]), (200, [1, 0, 2], [3, 7, 2])]
+                 (1000, [33], [40]), (200, [1, 0, 2], [3, 7, 2]), (0, [1, 1], [300, 20]), (0, [3, 5], [200, 4]),
+                 (0, [4, 0, 8], [600, 9, 599])]
 
 
 @pytest.mark.parametrize("heads", HEADS, ids=IDS)
@@ -522,9 +523,10 @@ def test_attention_prefix_large_logits_and_infinities():
 @pytest.mark.parametrize("dh", [32, 64, 96, 128, 160])
 @pytest.mark.parametrize("column", [0, 31, -1])
 @pytest.mark.parametrize("value", [float("inf"), float("nan")])
-def test_attention_prefix_hidden_values_at_every_width(dh, column, value):
+@pytest.mark.parametrize("n_pre", [0, 70])
+def test_attention_prefix_hidden_values_at_every_width(dh, column, value, n_pre):
     """One odd number in one column of keys that only later rows see: the rows before are as without it."""
-    H, Hkv, rows, own, n_pre = 4, 2, [3, 5], [37, 18], 70
+    H, Hkv, rows, own = 4, 2, [3, 5], [37, 18]
     d = prefix_case(24, n_pre, rows, own, H, Hkv, dh, BF16)
     want, tol = prefix_expected(d, rows, own, H, Hkv, dh)
     clean = run_prefix(d, rows, own, H, Hkv, dh)
@@ -563,6 +565,25 @@ def test_other_widths_do_not_reach_beyond_their_heads(dh):
                                     dev["k"], dev["v"], dev["kv_idx"], cu(own), 33, H, Hkv, dh)
     assert torch.equal(got, clean)
     B.lazy_device_status()
+
+
+@pytest.mark.parametrize("heads", [HEADS[1], HEADS[6], HEADS[10]], ids=[IDS[1], IDS[6], IDS[10]])
+def test_attention_prefix_rows_of_nobody(heads):
+    """Without a prefix, rows before the first request's and behind the last one's are reported and zero."""
+    H, Hkv, dh, dtype = heads
+    rows, own = [2, 3], [40, 90]
+    d = prefix_case(29, 0, [1] + rows + [2], [1] + own + [2], H, Hkv, dh, dtype)
+    dev = {k: v.cuda() for k, v in d.items()}
+    cu_q = torch.tensor([1, 3, 6], dtype=torch.int32).cuda()
+    cu_kv = torch.tensor([1, 41, 131], dtype=torch.int32).cuda()
+    out = torch.full((8, H * dh), 7.0, dtype=dtype, device="cuda")
+    got = B.lazy_k_attention_prefix(dev["q"], cu_q, 3, dev["k_pre"], dev["v_pre"], dev["k"], dev["v"], dev["kv_idx"], cu_kv,
+                                    90, H, Hkv, dh, out=out)
+    with pytest.raises(B.LazyError, match="BADARG"):
+        B.lazy_device_status()
+    want, tol = prefix_expected(d, [1] + rows + [2], [1] + own + [2], H, Hkv, dh)
+    assert np.all(np.abs(f64(got).reshape(want.shape)[1:6] - want[1:6]) <= tol[1:6])
+    assert not torch.any(got[0]) and not torch.any(got[6:])
 
 
 @pytest.mark.parametrize("heads", [HEADS[1], HEADS[7]], ids=[IDS[1], IDS[7]])
