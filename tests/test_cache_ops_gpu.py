@@ -747,6 +747,195 @@ def test_binding_refuses_what_does_not_fit():
         B.lazy_k_attention_mass(q, k, c, 4, 4, 2, 64, scratch=torch.zeros(1, device="cuda"))
 
 
+# ------------------------------------------------------------------------------------------- graphs and streams
+def _mass_call(H, Hkv, dh, dtype, lens, window):
+    def inputs(seed):
+        _, _, q, k = mass_case(seed, lens, H, Hkv, dh, dtype, fused=False)
+        return dict(q=q, k=k, cu=cu(lens))
+
+    def call(x):
+        return (B.lazy_k_attention_mass(x["q"], x["k"], x["cu"], max(lens), H, Hkv, dh, window),)
+    return inputs, call
+
+
+def _evict_call(Hkv, dh, dtype, lens, budget, recent):
+    def inputs(seed):
+        g, n = gen(seed), sum(lens)
+        return dict(k=randn(g, n, Hkv * dh, dtype=dtype).cuda(), v=randn(g, n, Hkv * dh, dtype=dtype).cuda(),
+                    pos=torch.arange(n, dtype=torch.int32).cuda(), mass=torch.rand((Hkv, n), generator=g).cuda(), cu=cu(lens),
+                    **new_cache(len(lens), budget + 2, Hkv, dh, dtype))
+
+    def call(x):
+        c = {name: x[name] for name in ("kc", "vc", "cmass", "cpos", "clen")}
+        B.lazy_k_evict(x["k"], x["v"], x["pos"], x["mass"], x["cu"], max(lens), budget, recent, **c)
+        return tuple(c.values())
+    return inputs, call
+
+
+def _step_call(H, Hkv, dh, dtype, lens, budget):
+    def inputs(seed):
+        c, new = step_case(seed, lens, budget, H, Hkv, dh, dtype)
+        return {name: t.cuda() for name, t in {**c, **new}.items()}
+
+    def call(x):
+        out = B.lazy_k_evict_step(**x, n_heads=H, budget=budget, n_recent=1)
+        return (*out, x["cpos"], x["clen"], *(x["kc"][s, :n] for s, n in enumerate(lens)),
+                *(x["cmass"][s, :, :min(n + 1, budget)] for s, n in enumerate(lens)))
+    return inputs, call
+
+
+def _prefix_call(H, Hkv, dh, dtype, n_pre, rows, own):
+    def inputs(seed):
+        d = prefix_case(seed, n_pre, rows, own, H, Hkv, dh, dtype)
+        return {**{name: t.cuda() for name, t in d.items()}, "cu_q": cu(rows), "cu_kv": cu(own)}
+
+    def call(x):
+        return (B.lazy_k_attention_prefix(x["q"], x["cu_q"], max(rows), x["k_pre"], x["v_pre"], x["k"], x["v"], x["kv_idx"],
+                                          x["cu_kv"], max(own), H, Hkv, dh),)
+    return inputs, call
+
+
+def _verify_call(V, drafts):
+    def inputs(seed):
+        return {**{name: t.cuda() for name, t in verify_case(seed, drafts, V).items()}, "cu": cu(drafts)}
+
+    def call(x):
+        return B.lazy_k_verify(x["p"], x["draft"], x["cu"], max(drafts), x["u_accept"], x["u_sample"], q=x["q"])
+    return inputs, call
+
+
+CALLS = {
+    "mass": _mass_call(8, 2, 128, BF16, [700, 1, 333], 0), "mass_split_keys": _mass_call(8, 8, 64, BF16, [5000, 40], 33),
+    "mass_f32": _mass_call(4, 2, 64, F32, [150, 20], 0), "evict": _evict_call(2, 64, BF16, [500, 30], 100, 10),
+    "step": _step_call(8, 2, 128, BF16, [300, 40, 0], 300), "step_long": _step_call(8, 1, 64, BF16, [2200], 2200),
+    "step_f32": _step_call(4, 4, 64, F32, [60, 3], 60), "prefix": _prefix_call(8, 2, 128, BF16, 700, [2, 1, 3], [9, 150, 40]),
+    "prefix_none": _prefix_call(8, 2, 64, BF16, 0, [1, 2], [200, 30]), "prefix_f32": _prefix_call(6, 2, 32, F32, 100, [2, 1], [9, 15]),
+    "verify": _verify_call(5000, [3, 0, 5]),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_captured_calls_take_new_inputs(name):
+    """A captured call, replayed on other inputs in the same buffers, gives what the call itself gives."""
+    inputs, call = CALLS[name]
+    x = inputs(50)
+    want = [t.clone() for t in call(inputs(51))]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = call(x)
+    for seed in (52, 51):
+        for key, t in inputs(seed).items():
+            x[key].copy_(t)
+        graph.replay()
+    torch.cuda.synchronize()
+    B.lazy_device_status()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and len(got) == len(want)
+
+
+def test_calls_at_once_on_two_streams():
+    """Every operator on two streams at once, several times over, each with its own scratch: the same bits as alone."""
+    for name, (inputs, call) in CALLS.items():
+        want = [[t.clone() for t in call(inputs(seed))] for seed in (60, 61)]
+        sets = [[inputs(seed) for _ in range(6)] for seed in (60, 61)]
+        torch.cuda.synchronize()
+        streams, got = (torch.cuda.Stream(), torch.cuda.Stream()), ([], [])
+        for i in range(6):
+            for k in range(2):
+                with torch.cuda.stream(streams[k]):
+                    got[k].append(call(sets[k][i]))
+        torch.cuda.synchronize()
+        B.lazy_device_status()
+        for k in range(2):
+            for out in got[k]:
+                assert all(torch.equal(a, b) for a, b in zip(out, want[k])), name
+
+
+# ------------------------------------------------------------------------------------------- far offsets
+FAR = 2 ** 31 + 2 ** 24   # elements: rows at the end of such a buffer lie behind what 32 bits reach
+
+
+def far_rows(t, pitch):
+    """The rows of t at the end of a buffer of FAR elements, `pitch` apart; the first row lies at its start."""
+    rows = FAR // pitch
+    far = torch.zeros((rows, pitch), dtype=t.dtype, device="cuda")
+    far[rows - t.shape[0]:, :t.shape[1]] = t.cuda()
+    return far, rows - t.shape[0]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_mass_and_evict_of_far_rows(dtype):
+    H, Hkv, dh, n = 4, 2, 64, 90
+    _, _, q, k = mass_case(70, [n], H, Hkv, dh, dtype, fused=False)
+    v = randn(gen(71), n, Hkv * dh, dtype=dtype).cuda()
+    want = B.lazy_k_attention_mass(q, k, cu([n]), n, H, Hkv, dh)
+    wide = torch.cat([q, k, v], 1)
+    far, first = far_rows(wide, 2 ** 21)
+    table = cu([first, n])
+    fq, fk, fv = far[:, :H * dh], far[:, H * dh:(H + Hkv) * dh], far[:, (H + Hkv) * dh:(H + 2 * Hkv) * dh]
+    got = B.lazy_k_attention_mass(fq, fk, table, far.shape[0], H, Hkv, dh)
+    e = weight_error(f64(q).reshape(n, H, dh), f64(k).reshape(n, Hkv, dh), dh) + n * H * 2.0 ** -24   # and of fp32 sums
+    assert torch.all((got[:, first:] - want).abs() <= 2 * e * want)
+    pos = torch.arange(far.shape[0], dtype=torch.int32).cuda()
+    c = new_cache(2, 20, Hkv, dh, dtype)
+    B.lazy_k_evict(fk, fv, pos, got, table, far.shape[0], 20, 5, **c)
+    B.lazy_device_status()
+    for h in range(Hkv):
+        kept = R.kept_rows(got[h, first:].cpu().numpy(), n, 20, 5)
+        assert (c["cpos"][1, h].cpu() - first).tolist() == kept
+        assert torch.equal(c["kc"][1, :, h], k.view(n, Hkv, dh)[kept, h]) and torch.equal(c["vc"][1, :, h], v.view(n, Hkv, dh)[kept, h])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_prefix_and_verify_of_far_rows(dtype):
+    H, Hkv, dh, rows, own = 4, 2, 64, [2, 1], [30, 70]
+    d = prefix_case(72, 130, rows, own, H, Hkv, dh, dtype)
+    clean = run_prefix(d, rows, own, H, Hkv, dh)
+    far_k, first = far_rows(torch.nan_to_num(d["k"], posinf=0.0), 2 ** 21)
+    far_v, _ = far_rows(torch.nan_to_num(d["v"], posinf=0.0), 2 ** 21)
+    w = Hkv * dh
+    got = B.lazy_k_attention_prefix(d["q"].cuda(), cu(rows), 2, d["k_pre"].cuda(), d["v_pre"].cuda(), far_k[:, :w], far_v[:, :w],
+                                    d["kv_idx"].cuda() + first, cu(own), 70, H, Hkv, dh)
+    assert torch.equal(got, clean)
+    del far_v
+    if dtype == F32:   # the last request's rows of the target lie far behind the first one's
+        V, n = 40, far_k.shape[0] - 2
+        x = verify_case(73, [1], V)
+        far_k[:, :V] = 0.0
+        far_k[-2:, :V] = x["p"].cuda()
+        far_k[:-2, 0] = 1.0
+        acc, tokens = B.lazy_k_verify(far_k[:, :V], x["draft"].cuda(), torch.tensor([0] * (n + 1) + [1], dtype=torch.int32).cuda(),
+                                      1, x["u_accept"].cuda(), torch.cat([torch.zeros(n), x["u_sample"]]).cuda(), q=x["q"].cuda())
+        assert (acc[-1].item(), tokens[-1, acc[-1].item()].item()) == R.verify(
+            x["p"].numpy(), x["q"].numpy(), x["draft"].numpy(), x["u_accept"].numpy(), x["u_sample"][0].item())
+        assert not torch.any(tokens[:-1, 0]) and not torch.any(acc[:-1])
+    B.lazy_device_status()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_step_on_far_caches(dtype):
+    """Many sequences, the last of which lies behind 2^31 elements."""
+    H, Hkv, dh, budget, cap = 4, 2, 64, 40, 270
+    c, new = step_case(74, [40], budget, H, Hkv, dh, dtype, cap=cap)
+    S = FAR // (cap * Hkv * dh)
+    many = {name: torch.zeros((S, *t.shape[1:]), dtype=t.dtype, device="cuda") for name, t in {**c, **new}.items()}
+    for name, t in {**c, **new}.items():
+        many[name][-1] = t[0].cuda()
+    one = {name: t.cuda() for name, t in {**c, **new}.items()}
+    want = B.lazy_k_evict_step(**one, n_heads=H, budget=budget, n_recent=3)
+    got = B.lazy_k_evict_step(**many, n_heads=H, budget=budget, n_recent=3)
+    B.lazy_device_status()
+    _, m64, o64, amount, slots, gones, e = step_expected(c, new, H, budget, 3)
+    for o, slot, gone in ((got[0][-1], got[1][-1], got[2][-1]), (want[0][0], want[1][0], want[2][0])):
+        assert np.all(np.abs(f64(o).reshape(o64[0].shape) - o64[0]) <= e * amount[0] + half_step(dtype) * np.abs(o64[0]) * (1 + e))
+        assert np.array_equal(slot.cpu().numpy(), slots[0]) and np.array_equal(gone.cpu().numpy(), gones[0])
+    for name in ("kc", "vc"):
+        assert torch.equal(many[name][-1, :40], one[name][0, :40])
+    assert torch.equal(many["cpos"][-1, :, :40], one["cpos"][0, :, :40])
+    assert same_weights(many["cmass"][-1:, :, :40].cpu().numpy().astype(np.float64), m64[:, :, :40], e)
+
+
 # ------------------------------------------------------------------------------------------- together
 def test_a_pruned_prompt_shared_by_requests_with_drafts():
     """As they are used: a prompt is weighed, cut to a budget, shared by three requests with drafted tokens, whose
