@@ -3,11 +3,11 @@
 // to the lower row.  Heads choose for themselves, so slot t of two heads may hold different tokens.
 //
 // One launch, a few CTAs per (sequence, head).  Each of them makes the whole selection for itself (which needs no word
-// between them): a radix select over order-preserving keys held in shared memory finds the weight at the last kept
-// rank, every warp counts the kept rows of its contiguous part, and after one scan over the warps the rows are listed
+// between them): a radix select over order-preserving keys held in shared memory (of few keys, a comparison of each with all)
+// finds the weight at the last kept rank, every warp counts the kept rows of its contiguous part, and after one scan over the warps the rows are listed
 // in row order without a barrier per chunk.  A CTA lists and then copies only its share of the slots.  The copy is what
-// is bound by memory: kept rows are read and written once.  A prompt of 3376 rows on 32 heads cut to 1024 slots: 15.5 us (34 MB,
-// about half of it the selection); eight prompts of 1 to 16384 rows on 8 heads cut to 2048: 31.5 us (119 MB, 3.8 TB/s).
+// is bound by memory: kept rows are read and written once.  A prompt of 3376 rows on 32 heads cut to 1024 slots: 14.4 us (34 MB,
+// 4.6 us of it the selection, 5.3 the copy); eight prompts of 1 to 16384 rows on 8 heads cut to 2048: 31 us (119 MB, 3.8 TB/s).
 #include "cache_ops.cuh"
 
 namespace lazy {
@@ -21,6 +21,9 @@ constexpr int ES_KEYS = 45056;     // keys held in shared memory (176 KiB); long
 constexpr int ES_PITCH = ES_BINS + 8;  // copies start 8 banks apart
 constexpr int ES_HIST = ES_COPIES * ES_PITCH;
 constexpr int ES_SMEM = (ES_HIST + ES_KEYS) * 4;
+// Keys that are compared one with another instead of by digits: a bin of a 3376-row prompt's weights holds a hundred, and two
+// more digits would take 2.1 us where comparing takes 1; comparing 250 takes as long as a digit.
+constexpr int ES_FEW = 192;
 constexpr int ES_BATCH = 8;        // weights in flight per thread
 constexpr int EG_PIECES = 4;       // 16-byte pieces of K and of V in flight per thread
 constexpr int ES_MAX_PARTS = 8;    // CTAs per (sequence, head)
@@ -68,6 +71,29 @@ __device__ __forceinline__ void find_bin(const int *hist, int copies, int bins, 
   }
 }
 
+// The key at rank `left` of m <= ES_FEW of them (zeros behind them), each compared with all; written to found as find_bin does.
+__device__ __forceinline__ void find_key(const uint32_t *few, int m, int left, int *found) {
+  if ((int)threadIdx.x >= m) return;
+  const uint32_t mine = few[threadIdx.x];
+  int above = 0, reach = 0;  // keys above, and above or equal
+#pragma unroll 2
+  for (int j = 0; j < m; j += 8) {
+    const uint4 a = *reinterpret_cast<const uint4 *>(few + j), b = *reinterpret_cast<const uint4 *>(few + j + 4);
+    const uint32_t key[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      above += key[i] > mine;
+      reach += key[i] >= mine;
+    }
+  }
+  if (mine == 0u) reach = m;  // without the zeros behind
+  if (above < left && left <= reach) {  // equal keys write the same
+    found[0] = (int)mine;
+    found[1] = above;
+    found[2] = reach - above;
+  }
+}
+
 // grid (parts, n_kv_heads, n_seqs).  idx[s, g]: the kept rows by slot; vecs: 16-byte pieces per row.
 __global__ void __launch_bounds__(ES_THREADS, 1)
 evict_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long ld, int vecs,
@@ -79,7 +105,9 @@ evict_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long
   int *hist = reinterpret_cast<int *>(es_smem);
   uint32_t *keys = es_smem + ES_HIST;
   __shared__ int warp_sums[2][ES_WARPS];
-  __shared__ int found[3];  // by find_bin
+  __shared__ int found[3];  // by find_bin, find_key
+  __shared__ __align__(16) uint32_t few[ES_FEW];
+  __shared__ int n_few;
   const int g = blockIdx.y, s = blockIdx.z, Hkv = gridDim.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const size_t sg = (size_t)s * Hkv + g;
@@ -110,22 +138,47 @@ evict_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long
     auto key_of = [&](int i) { return held ? keys[i] : co_weight_key(m[i]); };
     uint32_t prefix = 0u, mask = 0u;
     int left = need;
-    for (int pass = 0; pass < 3; ++pass) {  // digits of 11, 11 and 10 bits from the top
-      const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : ES_BINS;
-      const int copies = pass == 0 ? ES_COPIES : 1;  // later passes count the few rows of one bin
-      for (int i = threadIdx.x; i < copies * ES_PITCH; i += ES_THREADS) hist[i] = 0;
+    if (threadIdx.x < ES_FEW) few[threadIdx.x] = 0u;
+    if (old <= ES_FEW) {
       __syncthreads();
-  #pragma unroll 4
-      for (int i = threadIdx.x; i < old; i += ES_THREADS) {
-        const uint32_t key = key_of(i);
-        if ((key & mask) == prefix) atomicAdd(&hist[(lane & (copies - 1)) * ES_PITCH + ((key >> shift) & (bins - 1))], 1);
-      }
+      if ((int)threadIdx.x < old) few[threadIdx.x] = keys[threadIdx.x];
       __syncthreads();
-      if (threadIdx.x < ES_SCAN) find_bin(hist, copies, bins, left, warp_sums[0], found);
+      find_key(few, old, left, found);
       __syncthreads();
+      prefix = (uint32_t)found[0];
       left -= found[1];
-      prefix |= (uint32_t)found[0] << shift;
-      mask |= (uint32_t)(bins - 1) << shift;
+    } else {
+      for (int pass = 0; pass < 3; ++pass) {  // digits of 11, 11 and 10 bits from the top
+        const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : ES_BINS;
+        const int copies = pass == 0 ? ES_COPIES : 1;  // later passes count the few rows of one bin
+        for (int i = threadIdx.x; i < copies * ES_PITCH; i += ES_THREADS) hist[i] = 0;
+        if (threadIdx.x == 0) n_few = 0;
+        __syncthreads();
+#pragma unroll 4
+        for (int i = threadIdx.x; i < old; i += ES_THREADS) {
+          const uint32_t key = key_of(i);
+          if ((key & mask) == prefix) atomicAdd(&hist[(lane & (copies - 1)) * ES_PITCH + ((key >> shift) & (bins - 1))], 1);
+        }
+        __syncthreads();
+        if (threadIdx.x < ES_SCAN) find_bin(hist, copies, bins, left, warp_sums[0], found);
+        __syncthreads();
+        left -= found[1];
+        prefix |= (uint32_t)found[0] << shift;
+        mask |= (uint32_t)(bins - 1) << shift;
+        const int m = found[2];
+        if (pass < 2 && m <= ES_FEW) {  // in any order: only the key at the rank is looked for
+          for (int i = threadIdx.x; i < old; i += ES_THREADS) {
+            const uint32_t key = key_of(i);
+            if ((key & mask) == prefix) few[atomicAdd(&n_few, 1)] = key;
+          }
+          __syncthreads();
+          find_key(few, m, left, found);
+          __syncthreads();
+          prefix = (uint32_t)found[0];
+          left -= found[1];
+          break;
+        }
+      }
     }
     // ---- keys above `prefix` stay, and of those equal to it the first `left`; warp w walks rows [w part, (w + 1) part).
     // Where all equal ones stay (no tie is cut) "above" takes them in, and one vote per 32 rows is enough.

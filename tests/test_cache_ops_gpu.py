@@ -186,7 +186,8 @@ def new_cache(n_seqs, cap, Hkv, dh, dtype):
 
 @pytest.mark.parametrize("heads", [HEADS[1], HEADS[5], HEADS[8]], ids=[IDS[1], IDS[5], IDS[8]])
 @pytest.mark.parametrize("lens,budget,recent", [([1], 1, 0), ([5, 0, 40], 8, 3), ([64, 8, 9], 8, 8), ([3000, 1500], 700, 0),
-                                                ([2049], 2048, 100), ([70], 1, 1), ([1025, 33], 300, 299)])
+                                                ([2049], 2048, 100), ([70], 1, 1), ([1025, 33], 300, 299),
+                                                ([200, 199, 201, 300, 192], 60, 8)])
 @pytest.mark.parametrize("weights", ["distinct", "ties", "odd"])
 def test_evict(heads, lens, budget, recent, weights):
     _, Hkv, dh, dtype = heads
