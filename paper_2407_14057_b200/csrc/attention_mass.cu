@@ -269,7 +269,8 @@ int mass_general(cudaStream_t st, const T *q, int ldq, const T *k, int ldkv, con
 // taken on the FMA pipe (a 3376-row prompt of 32 heads: 131 us with none, 122 with a quarter, 142 with half), which
 // leaves 768 clocks of that unit and about as many of instruction issue; a tile takes some 1350.  What does not change that:
 // persistent CTAs (128 us), 256 stationary rows with one streamed tile for both and rings for both sides (128 to 135 us, the
-// stationary side in shared or tensor memory, one or two issuing warps).
+// stationary side in shared or tensor memory, one or two issuing warps), 32 or 128 columns to a thread (130 and 137), half
+// of a thread's columns loaded while the other half is used (141).
 // Lane tiles hold R = 128 / group rows x group heads, loaded as one 3-d box; with a group that does not divide 128
 // the last lanes of a tile are unused.  A short grid is filled up by clusters: the CTAs of a cluster share a
 // stationary tile, split the streamed tiles and add their parts in rank order through distributed shared memory.
