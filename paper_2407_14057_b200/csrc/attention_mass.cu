@@ -112,6 +112,7 @@ mass_general_kernel(const T *__restrict__ q, int ldq, const T *__restrict__ k, i
     __syncthreads();
     const T *pa = sa + ty * 2 * pitch, *pb = sb + (buf * MG_B + tx) * pitch;
     float x[2][4] = {};
+#pragma unroll 4
     for (int c = 0; c < head_dim; c += V) {
       float av[2][V], bv[4][V];
       Vec16<T> t;

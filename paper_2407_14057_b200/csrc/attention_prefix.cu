@@ -2,12 +2,13 @@
 // its request's own key list (row i of T rows: keys j <= C - T + i of C), so the prefix part is one product of all
 // rows with the prefix's keys: it is computed for the batch together and read once, not once per request.
 //
-// bf16, head width up to 128: three launches, one for a few requests without a prefix.  (1) The prefix on tcgen05: the batch's (row, head) pairs of one
-// key/value head are the lanes of 128-lane tiles, the prefix's keys are cut into ranges, every CTA leaves the partial
-// softmax of its lanes over its range.  (2) The requests' own keys on the warp-level path of rows_mma.cuh, launched as a
-// dependent that does not wait for (1): a CTA of it fits beside one of (1).  (3) A merge of the parts, one warp per
-// (row, head).  64 requests of one row behind 16384 keys, 8 heads of 128 in groups of 4, 1 to 500 own keys each: 47 us (139 MB;
-// 33 us without own keys, 24 without the prefix); four requests of five rows behind 1000 keys, 32 heads: 16.5 us (24 MB).
+// bf16, head width up to 128: three launches, one for a few requests without a prefix.  (1) The prefix on tcgen05: the
+// batch's (row, head) pairs of one key/value head are the lanes of 128-lane tiles, the prefix's keys are cut into ranges, every
+// CTA leaves the partial softmax of its lanes over its range.  (2) The requests' own keys on the warp-level path of
+// rows_mma.cuh, launched as a dependent that does not wait for (1): a CTA of it fits beside one of (1).  (3) A merge of the
+// parts, one warp per (row, head).  64 requests of one row behind 16384 keys, 8 heads of 128 in groups of 4, 1 to 500 own keys
+// each: 47 us (139 MB; 33 us without own keys, 24 without the prefix); four requests of five rows behind 1000 keys, 32 heads:
+// 16.5 us (24 MB).
 #include "attn_split.cuh"
 #include "rows_mma.cuh"
 
@@ -429,7 +430,8 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 // One CTA: 8 NT columns (row, head) of one (request, key/value head) over one range of its list; warps take every fourth group of
 // 16 keys, and their parts are added in shared memory.
 constexpr int PO_WARPS = 4, PO_THREADS = PO_WARPS * 32, PO_STAGES = 2, PO_CLUSTER = 8;
-constexpr int PO_KEYS = 256;  // of a part; 64 requests with 1 to 500 keys of their own: 69 us with 64, 55 with 128, 50 with 256, 51 with 512
+// Keys of a part; 64 requests with 1 to 500 keys of their own: 69 us with 64, 55 with 128, 50 with 256, 51 with 512
+constexpr int PO_KEYS = 256;
 
 template <int HD, int NT>
 struct PrefixOwnShared {
@@ -694,7 +696,8 @@ prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, con
   l = warp_sum(l);
   const float inv = bad ? NAN : (l > 0.f ? 1.f / l : 0.f);
   bf16 *o = (bf16 *)a.o + pair * HD + (WIDE ? lane * V : lane);
-  if (V == 4) *reinterpret_cast<uint2 *>(o) = make_uint2(bf16x2_pack(acc[0] * inv, acc[1] * inv), bf16x2_pack(acc[2] * inv, acc[3] * inv));
+  if (V == 4)
+    *reinterpret_cast<uint2 *>(o) = make_uint2(bf16x2_pack(acc[0] * inv, acc[1] * inv), bf16x2_pack(acc[2] * inv, acc[3] * inv));
   else if (V == 2) *reinterpret_cast<uint32_t *>(o) = bf16x2_pack(acc[0] * inv, acc[1] * inv);
   else {
 #pragma unroll
@@ -740,9 +743,10 @@ PrefixPlan prefix_plan(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv,
     const int most = cdiv(max_kv, PO_WARPS * RM_KEYS);  // a group of keys per warp at least
     if (want > most) want = most;
     if (key_tiles == 0) {
+      const int per_sm = p.nt == 1 ? 3 : 2;
       long long c = 1;
-      while (c < PO_CLUSTER && c < want && ctas * c * 2 <= co_cluster_ctas((int)c * 2, 3)) c *= 2;
-      p.direct = c * PO_KEYS * 2 >= max_kv && ctas * c <= co_cluster_ctas((int)c, 3);
+      while (c < PO_CLUSTER && c < want && ctas * c * 2 <= co_cluster_ctas((int)c * 2, per_sm)) c *= 2;
+      p.direct = c * PO_KEYS * 2 >= max_kv && ctas * c <= co_cluster_ctas((int)c, per_sm);
       if (p.direct) want = c;
     }
     p.own_split = cdiv(cdiv(max_kv, (int)want), RM_KEYS) * RM_KEYS;
@@ -772,9 +776,9 @@ int prefix_own_launch(cudaStream_t st, const PrefixArgs &a, const PrefixPlan &p,
   constexpr int SMEM = PO_WARPS * PO_STAGES * RowsMma<HD, NT>::STAGE;
   const int units = a.n_kv_heads * p.col_blocks;
   LAZY_TRY((co_allow_smem<prefix_own_kernel<HD, NT, DIRECT>>(SMEM, true)));
-  return co_launch(prefix_own_kernel<HD, NT, DIRECT>, DIRECT ? dim3(units * p.own_parts, 1, a.n_seqs) : dim3(units, p.own_parts, a.n_seqs),
-                   dim3(PO_THREADS), SMEM, st, DIRECT ? p.own_parts : 1, p.pre_parts > 0, a, group, p.col_blocks, p.own_split,
-                   part_o, part_ml, status);
+  const dim3 grid = DIRECT ? dim3(units * p.own_parts, 1, a.n_seqs) : dim3(units, p.own_parts, a.n_seqs);
+  return co_launch(prefix_own_kernel<HD, NT, DIRECT>, grid, dim3(PO_THREADS), SMEM, st, DIRECT ? p.own_parts : 1, p.pre_parts > 0,
+                   a, group, p.col_blocks, p.own_split, part_o, part_ml, status);
 }
 
 template <int HD>
