@@ -19,7 +19,8 @@ namespace {
 // Small tiles and a cluster that shares the streamed tiles keep a short prompt from running on a few SMs: three prompts of
 // 278 rows in all, 4 heads of 64 in fp32, took 48.7 us with 64 x 64 tiles and one CTA per tile.
 constexpr int MG_A = 32, MG_B = 64, MG_THREADS = 256;
-// See mass_cluster; 700 rows of 8 heads in groups of 4: 63 us, 80 with a start of 5
+// See mass_cluster.  Four prompts of 400 to 700 rows, 4 on 2 heads of 128: 103 us, 149 with a start of 5; one prompt of 700, 8 on
+// 2 heads of 64: 60 and 55.
 constexpr double MG_START = 0.5, MG_JOIN = 0.25;
 constexpr int MT_MAX_CLUSTER = 8;
 

@@ -114,6 +114,9 @@ __device__ __forceinline__ uint32_t co_cluster_size() {
 __device__ __forceinline__ void co_cluster_sync() {
   asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
+// The same in two steps, with work between them that needs no word from the others.
+__device__ __forceinline__ void co_cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
+__device__ __forceinline__ void co_cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 // Address of `p` (this CTA's shared memory) in CTA `rank` of the cluster.
 template <typename T>
 __device__ __forceinline__ T *co_map_shared(T *p, uint32_t rank) {

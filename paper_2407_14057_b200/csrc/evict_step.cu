@@ -422,6 +422,7 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
     sh.finv[threadIdx.x] = inv;
   }
   __syncthreads();
+  if (csize > 1) co_cluster_arrive();  // the other CTAs' parts have been read
   // ---- the slots' masses
   for (int j0 = lo + threadIdx.x; j0 < hi; j0 += SF_THREADS * SF_BATCH) {
     float w[SF_BATCH];
@@ -447,7 +448,8 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
       if (j0 + i * SF_THREADS < hi) mo[j[i]] = (j[i] == slot ? 0.f : bw[i]) + w[i];
   }
   if (rank == 0 && threadIdx.x == 0) a.len_out[sg] = n;  // the cluster has read the old length long ago
-  if (csize > 1) co_cluster_sync();                      // nobody leaves while its parts are being read
+  __syncwarp();
+  if (csize > 1) co_cluster_wait();                      // nobody leaves while its parts are being read
 }
 
 bool step_fused_eligible(int dtype, int head_dim, int group) {

@@ -7,8 +7,8 @@
 // other rows are touched at the drafted ids only.  A cluster of CTAs shares the row: each sums its contiguous
 // part, the totals meet in distributed shared memory, and the one warp whose part holds the crossing reads its
 // few hundred values again (from L2).  Sums run in 64 bits: with 32 the running sum's rounding would move the crossing to a
-// neighbouring id about once in a few hundred draws at a vocabulary of 32000.  One request, 32000 ids: 6.5 us, the latency of
-// three rounds of loads and two cluster barriers; 128 requests of up to 7 drafts: 12.5 us (31 MB).
+// neighbouring id about once in a few hundred draws at a vocabulary of 32000.  One request, 32000 ids: 6.2 us, the latency of
+// three rounds of loads and two scans; 128 requests of up to 7 drafts: 12.3 us (31 MB).
 #include "cache_ops.cuh"
 
 namespace lazy {
@@ -152,10 +152,10 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
     const double sum = warp_sum_f64(row.sum(begin + lane * (VEC ? 4 : 1), end, VEC ? 128 : 32));
     if (lane == 0) warp_total[warp] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
-      double t = 0.0;
-      for (int w = 0; w < VF_WARPS; ++w) t += warp_total[w];
-      cta_total = t;
+    const double mine = lane < VF_WARPS ? warp_total[lane] : 0.0;
+    if (warp == 0) {
+      const double t = warp_sum_f64(mine);
+      if (lane == 0) cta_total = t;
     }
     co_cluster_sync();
     double cta[VF_MAX_CLUSTER], total = 0.0;
@@ -164,8 +164,9 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
       cta[r] = r < size ? *co_map_shared(&cta_total, r) : 0.0;
       total += cta[r];
     }
-    co_cluster_sync();  // every total has been read: a second pass may write again, a CTA may leave
+    co_cluster_arrive();  // when all have, every total has been read: a second pass may write again, a CTA may leave
     if (!(total > 0.0) && (row.q || row.zeroed >= 0) && pass == 0) {
+      co_cluster_wait();
       row.q = nullptr;  // the draft's distribution covers the target's (equal but for rounding): the target's itself
       row.zeroed = -1;
       continue;
@@ -186,18 +187,11 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
       }
       run0 += cta[r];
     }
-    if (owner_cta == rank) {
-      double run = base;
-      crossed = false;
-      for (int w = 0; w < VF_WARPS && !crossed; ++w) {
-        const double t = warp_total[w];
-        if (t > 0.0) {
-          owner = w;
-          base = run;
-          crossed = run + t > bar;
-        }
-        run += t;
-      }
+    if (owner_cta == rank) {  // lane w: warp w
+      const double incl = warp_inclusive_f64(mine);
+      const uint32_t over = __ballot_sync(0xffffffffu, mine > 0.0 && base + incl > bar), any = __ballot_sync(0xffffffffu, mine > 0.0);
+      owner = over ? __ffs(over) - 1 : 31 - __clz(any);
+      base += __shfl_sync(0xffffffffu, incl - mine, owner & 31);
     }
     if (owner == warp) {
       const int token = vf_crossing<VEC>(row, begin, end, base, bar);
@@ -214,6 +208,8 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
       for (int t = threadIdx.x; t <= max_draft; t += VF_THREADS)
         if (t != acc) tokens[(size_t)s * (max_draft + 1) + t] = t < acc ? draft[d0 + t] : -1;
     }
+    __syncwarp();
+    co_cluster_wait();
     return;
   }
 }
