@@ -6,6 +6,7 @@ using namespace lazy;
 namespace {
 
 constexpr int MAX_GRID_YZ = 65535;
+constexpr long long MAX_KEYS = 0x7fffff00LL;  // that a row of the shared prefix's attention sees
 
 bool bad_dtype(int dtype) { return dtype != LAZY_BF16 && dtype != LAZY_F32; }
 
@@ -115,7 +116,7 @@ int lazy_k_evict_step(void *stream, int32_t dtype, const void *q, int32_t ldq, c
 
 size_t lazy_k_attention_prefix_scratch_floats(int32_t n_rows, int32_t n_seqs, int32_t max_q, int32_t n_pre,
                                               int32_t max_kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
-  if (n_rows < 0 || n_seqs < 0 || max_q < 0 || n_pre < 0 || max_kv < 0 ||
+  if (n_rows < 0 || n_seqs < 0 || max_q < 0 || n_pre < 0 || max_kv < 0 || (long long)n_pre + max_kv > MAX_KEYS ||
       check_heads(n_heads, n_kv_heads, head_dim) != LAZY_OK)
     return 0;
   return attention_prefix_scratch_floats(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads, n_kv_heads, head_dim);
@@ -130,7 +131,7 @@ int lazy_k_attention_prefix(void *stream, int32_t dtype, const void *q, int32_t 
   if (bad_dtype(dtype) || n_rows < 0 || n_seqs < 0 || max_q < 0 || n_pre < 0 || kv_rows < 0 || n_kv < 0 || max_kv < 0)
     return LAZY_E_BADARG;
   LAZY_TRY(check_heads(n_heads, n_kv_heads, head_dim));
-  if (n_rows > MAX_GRID_YZ || n_seqs > MAX_GRID_YZ || (long long)n_pre + max_kv > 0x7fffff00LL) return LAZY_E_CAPACITY;
+  if (n_rows > MAX_GRID_YZ || n_seqs > MAX_GRID_YZ || (long long)n_pre + max_kv > MAX_KEYS) return LAZY_E_CAPACITY;
   if (n_rows == 0) return LAZY_OK;
   if (n_seqs == 0 || max_q == 0) return LAZY_E_BADARG;
   const long long width = (long long)n_kv_heads * head_dim;

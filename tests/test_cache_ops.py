@@ -89,6 +89,8 @@ def test_attention_prefix_refuses(lib):
     refuse(f, PREFIX, CAPACITY, n_rows=65536)
     refuse(f, PREFIX, 0, n_rows=0)
     assert lib.lazy_k_attention_prefix_scratch_floats(2, 1, 2, 3, 2, 4, 3, 64) == 0
+    assert lib.lazy_k_attention_prefix_scratch_floats(2, 1, 2, 2 ** 31 - 1, 2 ** 31 - 1, 4, 2, 64) == 0
+    refuse(f, PREFIX, CAPACITY, n_pre=2 ** 31 - 1)
 
 
 def test_verify_refuses(lib):
