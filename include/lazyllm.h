@@ -401,8 +401,9 @@ int lazy_k_gather_rows(void *stream, const void *src, const int32_t *idx, void *
  * heads side by side start on 16-byte boundaries (base address and pitch); caches kc / vc are [n_seqs, cap, n_kv_heads,
  * head_dim], cmass / cpos [n_seqs, n_kv_heads, cap], clen [n_seqs, n_kv_heads]; device tables that do not fit the
  * sizes given are reported through the status word (LAZY_E_BADARG unless stated otherwise) and that sequence is
- * skipped.  Outputs must not overlap inputs except where stated.  Scratch need not be initialised, keeps nothing from
- * one call for the next, and must not be shared by calls that may run at the same time (two replayed graphs included). */
+ * skipped.  Outputs must not overlap inputs except where stated.  Scratch need not be initialised, may start at any address that
+ * its element type may have, keeps nothing from one call for the next, and must not be shared by calls that may run at the same
+ * time (two replayed graphs included). */
 
 /* Accumulated attention weight of prompts: mass[g][r] (fp32 [n_kv_heads, n_total]) = sum over the last `window` rows
  * i >= r of r's sequence (0 = all its rows) and over the query heads h of key/value head g of

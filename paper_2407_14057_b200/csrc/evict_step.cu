@@ -492,9 +492,10 @@ int step_fused(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevStatu
 
 size_t evict_step_scratch_floats(int n_seqs, int n_heads, int n_kv_heads, int head_dim, int budget) {
   const size_t general = step_scratch(n_seqs, n_heads, n_kv_heads, head_dim, budget).total;
-  // the one-launch form keeps at most every slot's logits, an even number of columns, parts rounded up to 16 slots
+  // the one-launch form keeps at most every slot's logits, an even number of columns, parts rounded up to 16 slots; + 4: they
+  // are read two at a time and start on a 16-byte boundary
   const size_t heads = (size_t)n_seqs * n_kv_heads, group = n_heads / n_kv_heads;
-  const size_t fused = heads * ((size_t)budget + SF_LARGE_CLUSTER * RM_KEYS) * ((group + 1) & ~(size_t)1);
+  const size_t fused = heads * ((size_t)budget + SF_LARGE_CLUSTER * RM_KEYS) * ((group + 1) & ~(size_t)1) + 4;
   return general > fused ? general : fused;
 }
 
@@ -502,8 +503,9 @@ int launch_evict_step(cudaStream_t st, int dtype, const EvictStepArgs &a, float 
   if (a.n_seqs == 0) return LAZY_OK;
   const int group = a.n_heads / a.n_kv_heads;
   if (step_fused_eligible(dtype, a.head_dim, group)) {
+    float *logits = reinterpret_cast<float *>(align_up((uintptr_t)scratch, 16));
     return co_head_dim(a.head_dim, [&](auto hd) {
-      return group <= 8 ? step_fused<hd.value, 1>(st, a, scratch, status) : step_fused<hd.value, 2>(st, a, scratch, status);
+      return group <= 8 ? step_fused<hd.value, 1>(st, a, logits, status) : step_fused<hd.value, 2>(st, a, logits, status);
     });
   }
   return dtype == LAZY_F32 ? step_general<float>(st, a, scratch, status) : step_general<bf16>(st, a, scratch, status);

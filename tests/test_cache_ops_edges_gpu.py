@@ -1,0 +1,65 @@
+"""Edges of the operators on bounded and shared caches: scratch anywhere in memory, infinite values, loose bounds, odd
+probabilities.  Statements in 64 bits and tolerances are those of test_cache_ops_gpu."""
+import numpy as np
+import pytest
+import torch
+
+import cache_reference as R
+from paper_2407_14057_b200 import binding as B
+from paper_2407_14057_b200 import build
+from test_cache_ops_gpu import (BF16, CALLS, F32, HEADS, IDS, check_step, cu, f64, gen, half_step, mass_case, prefix_case,
+                                prefix_expected, randn, run_prefix, step_case, step_expected, verify_case, weight_error)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build.build()
+    B.lib()
+
+
+# ------------------------------------------------------------------------------------------- scratch
+@pytest.fixture
+def late_scratch(monkeypatch):
+    """Makes every call's scratch a slice of just the size asked for, 4 bytes behind a 16-byte boundary, between guards."""
+    made = []
+
+    def scratch(n, dtype):
+        n = max(int(n), 1)
+        buf = torch.full((n + 65,), -7, dtype=dtype, device="cuda")
+        assert buf.data_ptr() % 16 == 0
+        buf[1:1 + n] = float("nan") if dtype.is_floating_point else 0
+        made.append((buf, n))
+        return buf[1:1 + n]
+
+    monkeypatch.setattr(B, "_scratch", scratch)
+    yield made
+    assert made
+    for buf, n in made:
+        assert buf[0].item() == -7 and torch.all(buf[1 + n:] == -7)
+
+
+@pytest.mark.parametrize("name", [n for n in CALLS if n != "verify"])
+def test_scratch_may_start_anywhere(name, late_scratch, monkeypatch):
+    inputs, call = CALLS[name]
+    got = [t.clone() for t in call(inputs(80))]
+    monkeypatch.undo()
+    want = call(inputs(80))
+    B.lazy_device_status()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# (sequences, heads, budget): a part's logits have no room in shared memory, because many CTAs share an SM (over 8 KiB, the
+# first ones) or at all (over 40 KiB); odd groups, two blocks of columns, parts cut by a cluster
+STEP_LOGITS = [(40, (32, 8, 128, BF16), 700), (40, (24, 8, 64, BF16), 650), (300, (16, 1, 32, BF16), 330), (75, (20, 4, 96, BF16), 560),
+               (15, (8, 1, 64, BF16), 10500), (20, (32, 8, 64, BF16), 1500)]
+
+
+@pytest.mark.parametrize("n_seqs,heads,budget", STEP_LOGITS, ids=[f"{s}x{h[0]}on{h[1]}x{h[2]}-{b}" for s, h, b in STEP_LOGITS])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_step_keeps_logits_in_the_scratch(n_seqs, heads, budget, in_place, late_scratch):
+    H, Hkv, dh, dtype = heads
+    lens = [budget if s % 3 else (0, 1, budget - 1, budget // 2)[s // 3 % 4] for s in range(n_seqs)]
+    c, new = step_case(81 + n_seqs, lens, budget, H, Hkv, dh, dtype)
+    check_step(c, new, H, budget, budget // 8, in_place=in_place)
