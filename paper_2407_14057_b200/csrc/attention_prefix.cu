@@ -112,8 +112,8 @@ int prefix_general(cudaStream_t st, const PrefixArgs &a, float *scratch, DevStat
 //   warp 1      owns TMEM, issues S = Q K^T (M128 N64) of every tile as soon as its logits have been taken to registers;
 //   warp 2      issues O += P V (M128 N = head width, P from TMEM);
 //   warps 3..   softmax, one thread per lane; running maximum raised only when it grows by more than 2^8.
-// TMEM columns of a tile: S (64) | P high (32) | P low (32) | O (head width).  P enters as the sum of two bf16 numbers, so
-// that the output's only rounding is its own; without the low part the 64 requests above would take 2.7 % less.  Two lane
+// TMEM columns of a tile: S (64) | P high (32) | P low (32) | O (head width).  P enters as the sum of two bf16 numbers (see
+// WEIGHT_REST), so that the only rounding of an output that counts is its own; without the low part the 64 requests above would take 2.7 % less.  Two lane
 // tiles in one CTA share the K and V tiles in shared memory.  64 keys take a CTA 1.17 us with two tiles, 0.9 with one: the products
 // alone would take 0.8 and 0.4, the softmax threads' instructions about as much, and neither hides all of the other.
 constexpr int PT_Q = 128, PT_K = 64;
@@ -348,7 +348,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       const float ref = m == -INFINITY ? 0.f : m;
       const unsigned long long neg = f32x2_pack(-ref, -ref);
       unsigned long long sum = 0ull;
-      const unsigned long long minus = f32x2_pack(-1.f, -1.f);
+      const unsigned long long rest = f32x2_pack(-WEIGHT_REST, -WEIGHT_REST);
       uint32_t hi[32];
 #pragma unroll
       for (int c = 0; c < 64; c += 2) {
@@ -357,9 +357,9 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         float p0, p1, h0, h1;
         sum = f32x2_add(sum, p);
         f32x2_unpack(p, p0, p1);
-        hi[c >> 1] = bf16x2_pack(p0, p1);
+        hi[c >> 1] = bf16x2_pack_rz(p0, p1);
         bf16x2_unpack(hi[c >> 1], h0, h1);
-        f32x2_unpack(f32x2_fma(f32x2_pack(h0, h1), minus, p), p0, p1);
+        f32x2_unpack(f32x2_fma(f32x2_pack(h0, h1), rest, p), p0, p1);
         raw[c >> 1] = bf16x2_pack(p0, p1);  // entry c / 2 has been used by now
       }
       float sm0, sm1;
@@ -395,6 +395,8 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         for (int c = 0; c < HD; c += 32) {
           float v[32];
           tmem_ld_32x32(tile + 128u + (uint32_t)c, v);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] *= WEIGHT_UNLIFT;
           __syncwarp();
 #pragma unroll
           for (int i = 0; i < 8; ++i)
@@ -565,7 +567,7 @@ prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, 
 #pragma unroll
         for (int w = 1; w < PO_WARPS; ++w) mx = fmaxf(mx, sh.wm[w][c]);
         const float ref = mx == -INFINITY ? 0.f : mx;
-        const float scale = ex2_approx(rows.m[t][i] - ref);
+        const float scale = ex2_approx(rows.m[t][i] - ref) * WEIGHT_UNLIFT;
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k) {
           wo[((size_t)warp * NT * 8 + c) * HD + k * 16 + (lane >> 2)] = rows.o[t][k][i] * scale;

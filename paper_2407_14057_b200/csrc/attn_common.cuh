@@ -26,6 +26,17 @@ __device__ __forceinline__ float ex2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Softmax weights enter a bf16 product as the sum of two bf16 numbers, P = hi + lo.  hi is cut off, not rounded, and lo = p - (1 -
+// 2^-20) hi, so that lo of a weight above zero is above zero too: times an infinite value both parts then give that infinity,
+// where a rounded hi would leave lo = 0 or below it and the sum NaN.  hi + lo is p (1 + 2^-20) up to 2^-16 of it (lo's
+// rounding), and the products' sums are multiplied by WEIGHT_UNLIFT.  A weight below 2^-100 may have lo = 0.
+constexpr float WEIGHT_REST = 1.f - 0x1p-20f, WEIGHT_LIFT = 1.f + 0x1p-20f, WEIGHT_UNLIFT = 1.f / WEIGHT_LIFT;
+__device__ __forceinline__ uint32_t bf16x2_pack_rz(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
 // Three-input maximum and two-wide fp32 arithmetic (one instruction each on this architecture): the
 // softmax threads are bound by instruction issue, so halving the count of the plain ALU work matters.
 __device__ __forceinline__ float fmax3(float a, float b, float c) {

@@ -364,7 +364,7 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
 #pragma unroll
       for (int w = 1; w < SF_WARPS; ++w) mx = fmaxf(mx, sh.wm[w][c]);
       const float ref = mx == -INFINITY ? 0.f : mx;
-      const float f = ex2_approx(rows.m[t][i] - ref);
+      const float f = ex2_approx(rows.m[t][i] - ref) * WEIGHT_UNLIFT;
 #pragma unroll
       for (int k = 0; k < HD / 16; ++k) {
         wo[((size_t)warp * NT * 8 + c) * HD + k * 16 + (lane >> 2)] = rows.o[t][k][i] * f;

@@ -5,8 +5,8 @@
 // key/value head.  Keys are the M side of both products, so few columns waste nothing of the instruction:
 //   S^T [16 keys x 8] = K [16 x HD] Q^T,   O^T [HD x 8] += V^T [HD x 16] P^T       (m16n8k16, bf16, fp32 accumulators)
 // The accumulator of S^T holds P with keys along the rows; one 8 x 8 transpose per half turns it into the second
-// product's operand without shared memory.  P enters as the sum of two bf16 numbers (its rounding and the rest), so
-// that the only rounding of an output is its own: the step is bound by reading K and V, and the second product's extra
+// product's operand without shared memory.  P enters as the sum of two bf16 numbers (see WEIGHT_REST), so that the only
+// rounding of an output that counts is its own: the step is bound by reading K and V, and the second product's extra
 // instructions (24 instead of 16 per 16 keys of a head width of 128, about 3 clocks per key of an SM against 22 that
 // the key's 512 bytes take) cost no time.  This is the warp-level tensor path, not tcgen05: with at most 16 columns a
 // 128-row instruction would be 7/8 padding, and keys named by lists cannot come through tensor maps.
@@ -83,7 +83,7 @@ struct RowsMma {
   static constexpr int STAGE = 2 * HALF;
   uint32_t qf[NT][HD / 16][2];
   float m[NT][2], l[NT][2];   // of columns (lane % 4) * 2 + {0, 1} of each block of 8; l is this lane's keys' only
-  float o[NT][HD / 16][4];
+  float o[NT][HD / 16][4];    // times WEIGHT_LIFT
 
   __device__ static __forceinline__ uint32_t at(int r, int c) { return rows_at<HD>(r, c); }
 
@@ -166,11 +166,11 @@ struct RowsMma {
       if (CUT && wild) add_wild(stage, wild, t, vis[t], there, p);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t h = bf16x2_pack(p[2 * i], p[2 * i + 1]);
+        const uint32_t h = bf16x2_pack_rz(p[2 * i], p[2 * i + 1]);
         float h0, h1;
         bf16x2_unpack(h, h0, h1);
         hi[t][i] = rm_transpose(h);
-        lo[t][i] = rm_transpose(bf16x2_pack(p[2 * i] - h0, p[2 * i + 1] - h1));
+        lo[t][i] = rm_transpose(bf16x2_pack(fmaf(h0, -WEIGHT_REST, p[2 * i]), fmaf(h1, -WEIGHT_REST, p[2 * i + 1])));
       }
     }
 #pragma unroll
@@ -221,7 +221,8 @@ struct RowsMma {
     for (int r = 0; r < RM_KEYS; ++r) {
       if (!(wild >> r & 1u)) continue;
       const int from = (r & 7) * 4 + (lane & 3);
-      const float p0 = __shfl_sync(0xffffffffu, r < 8 ? p[0] : p[2], from), p1 = __shfl_sync(0xffffffffu, r < 8 ? p[1] : p[3], from);
+      const float p0 = __shfl_sync(0xffffffffu, r < 8 ? p[0] : p[2], from) * WEIGHT_LIFT;
+      const float p1 = __shfl_sync(0xffffffffu, r < 8 ? p[1] : p[3], from) * WEIGHT_LIFT;
 #pragma unroll
       for (int k = 0; k < HD / 16; ++k)
 #pragma unroll

@@ -63,3 +63,56 @@ def test_evict_step_keeps_logits_in_the_scratch(n_seqs, heads, budget, in_place,
     lens = [budget if s % 3 else (0, 1, budget - 1, budget // 2)[s // 3 % 4] for s in range(n_seqs)]
     c, new = step_case(81 + n_seqs, lens, budget, H, Hkv, dh, dtype)
     check_step(c, new, H, budget, budget // 8, in_place=in_place)
+
+
+# ------------------------------------------------------------------------------------------- infinite values
+def with_infinities(v, g):
+    """Columns 1 and 2: every second row +inf, every second -inf; 3: one row +inf; 5: infinities of both signs."""
+    n, some = v.shape[0], torch.rand((2, v.shape[0]), generator=g) < 0.5
+    v[some[0], 1], v[some[1], 2] = float("inf"), -float("inf")
+    if n > 2:
+        v[n // 3, 3] = float("inf")
+        v[0, 5], v[n // 2, 5] = float("inf"), -float("inf")
+
+
+def same_with_infinities(got, want, tol):
+    odd = ~np.isfinite(want)
+    assert odd.any() and not odd.all()
+    assert np.array_equal(got[odd], want[odd], equal_nan=True)
+    assert np.all(np.abs(got[~odd] - want[~odd]) <= tol[~odd])
+
+
+@pytest.mark.parametrize("heads", HEADS, ids=IDS)
+@pytest.mark.parametrize("n_pre,rows,own", [(0, [1], [20]), (0, [3, 5], [200, 300]), (70, [2, 1], [3, 90]), (300, [1] * 40, [4] * 40),
+                                            (130, [2, 2], [2, 2]), (0, [1] * 30, [300] * 30)])
+def test_attention_prefix_infinite_values(heads, n_pre, rows, own):
+    """An infinite value gives every row that sees it the infinity that the formula has, wherever its key lies."""
+    H, Hkv, dh, dtype = heads
+    d = prefix_case(82, n_pre, rows, own, H, Hkv, dh, dtype)
+    for name, lines in (("v_pre", n_pre), ("v", d["v"].shape[0])):
+        for g in range(Hkv):
+            if lines:
+                with_infinities(d[name][:, g * dh:(g + 1) * dh], gen(83 + g))
+    with np.errstate(invalid="ignore"):
+        want, tol = prefix_expected(d, rows, own, H, Hkv, dh)
+    got = f64(run_prefix(d, rows, own, H, Hkv, dh)).reshape(want.shape)
+    B.lazy_device_status()
+    same_with_infinities(got, want, tol)
+
+
+@pytest.mark.parametrize("heads", HEADS + [(16, 1, 64, BF16)], ids=IDS + ["16on1x64"])
+@pytest.mark.parametrize("lens,budget", [([1, 2], 2), ([40, 39], 40), ([700], 700)])
+def test_evict_step_infinite_values(heads, lens, budget):
+    H, Hkv, dh, dtype = heads
+    c, new = step_case(84, lens, budget, H, Hkv, dh, dtype)
+    for s, n in enumerate(lens):
+        for g in range(Hkv):
+            with_infinities(c["vc"][s, :n, g], gen(85 + g))
+    new["v_new"].view(len(lens), Hkv, dh)[:, :, 7] = float("inf")
+    with np.errstate(invalid="ignore"):
+        _, _, o, amount, _, _, e = step_expected(c, new, H, budget, 1 if budget > 1 else 0)
+    dev = {k: v.cuda() for k, v in {**c, **new}.items()}
+    got, _, _ = B.lazy_k_evict_step(**dev, n_heads=H, budget=budget, n_recent=1)
+    B.lazy_device_status()
+    with np.errstate(invalid="ignore"):
+        same_with_infinities(f64(got).reshape(o.shape), o, e * amount + half_step(dtype) * np.abs(o) * (1 + e) + 1e-30)
