@@ -446,7 +446,7 @@ int lazy_k_evict_step(void *stream, int32_t dtype, const void *q, int32_t ldq, c
  * token and its drafted successors) of n_rows in all, and its own keys kv_idx[cu_kv[s] .. cu_kv[s+1]) (at most max_kv),
  * rows of the buffers k / v (kv_rows rows of pitch ldkv) in the order of their positions, its new rows' own keys last.  Row i of
  * T sees all n_pre rows of k_pre / v_pre (pitch ld_pre; the slots of one bounded cache serve too) and its own keys j
- * <= C - T + i of C; a row that sees nothing gives zeros.  The prefix is read once for the batch.  A row index outside
+ * <= C - T + i of C; a row that sees nothing gives zeros, and so does one that sees logits of -inf alone.  The prefix is read once for the batch.  A row index outside
  * [0, kv_rows) is reported and that key skipped.  n_rows <= 65535.  o [n_rows, n_heads * head_dim]. */
 size_t lazy_k_attention_prefix_scratch_floats(int32_t n_rows, int32_t n_seqs, int32_t max_q, int32_t n_pre,
                                               int32_t max_kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
@@ -465,7 +465,7 @@ int lazy_k_attention_prefix(void *stream, int32_t dtype, const void *q, int32_t 
  * if q is NULL; p if that leaves nothing), w = p behind the last draft: the sequence is then distributed as the target's.
  * tokens int32 [n_seqs, max_draft + 1]: accepted drafts, that token, then -1; n_accept int32 [n_seqs].  Sums in 64
  * bits.  A drafted id outside [0, vocab) is reported and rejected; a row without any positive probability is
- * reported and gives token -1.  p and q may be any rows; negative and NaN entries weigh nothing. */
+ * reported and gives token -1.  p and q may be any rows; negative and NaN entries count as 0 throughout. */
 int lazy_k_verify(void *stream, const float *p, int32_t ldp, const float *q, int32_t ldq, const int32_t *draft,
                   const int32_t *d_cu_draft, int32_t n_seqs, int32_t n_draft, int32_t max_draft, int32_t vocab,
                   const float *u_accept, const float *u_sample, int32_t *n_accept, int32_t *tokens);

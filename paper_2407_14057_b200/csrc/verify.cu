@@ -23,9 +23,13 @@ __device__ __forceinline__ double warp_sum_f64(double v) {
   return v;
 }
 
-// Weight of id j: p[j], less q[j] (row_q) or nothing at all for the one rejected id; never negative, NaN counts 0.
+// A probability as the caller has it: negative ones and NaN count as 0 (a negative one of the draft model's would give its id
+// a weight that the target does not).
+__device__ __forceinline__ float vf_prob(float x) { return fmaxf(x, 0.f); }
+
+// Weight of id j: p[j], less q[j] (row_q) or nothing at all for the one rejected id; never negative.
 __device__ __forceinline__ float vf_weight(float p, float q, int j, int zeroed) {
-  return j == zeroed ? 0.f : fmaxf(p - q, 0.f);
+  return j == zeroed ? 0.f : fmaxf(vf_prob(p) - vf_prob(q), 0.f);
 }
 
 // The weights of one row.  VEC: rows and vocabulary are multiples of four ids and 16-byte aligned.
@@ -124,8 +128,8 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
       if (t < T) {
         const int x = draft[d0 + t];
         if (x >= 0 && x < vocab) {
-          const double px = p[(size_t)(d0 + s + t) * ldp + x];
-          const double qx = q ? (double)q[(size_t)(d0 + t) * ldq + x] : 1.0;
+          const double px = vf_prob(p[(size_t)(d0 + s + t) * ldp + x]);
+          const double qx = q ? (double)vf_prob(q[(size_t)(d0 + t) * ldq + x]) : 1.0;
           ok = (double)u_accept[d0 + t] * qx < px;  // exact: 24 by 24 bits in 53
         } else if (rank == 0) {
           dev_fail(status, LAZY_E_BADARG, W_VERIFY, d0 + t, x);

@@ -116,3 +116,26 @@ def test_evict_step_infinite_values(heads, lens, budget):
     B.lazy_device_status()
     with np.errstate(invalid="ignore"):
         same_with_infinities(f64(got).reshape(o.shape), o, e * amount + half_step(dtype) * np.abs(o) * (1 + e) + 1e-30)
+
+
+# ------------------------------------------------------------------------------------------- verification
+@pytest.mark.parametrize("V", [299, 300, 4096])
+def test_verify_negative_and_nan_entries_count_as_zero(V):
+    """In both distributions, in the acceptance and in what is drawn from: no id is given weight by a negative one."""
+    g = gen(86)
+    drafts = [1] * 64
+    d = verify_case(87, drafts, V, near=2.0)
+    p, q = d["p"], d["q"]
+    odd = torch.tensor([-1.0, -0.25, float("nan"), -float("inf"), -1e-6])
+    q[:] = torch.where(torch.rand(q.shape, generator=g) < 0.3, odd[torch.randint(0, 5, q.shape, generator=g)], q)
+    p[:] = torch.where(torch.rand(p.shape, generator=g) < 0.5, odd[torch.randint(0, 5, p.shape, generator=g)], p)
+    p[0::2][torch.rand(q.shape, generator=g) < 0.3] = 0.0
+    acc, tokens = B.lazy_k_verify(p.cuda(), d["draft"].cuda(), cu(drafts), 1, d["u_accept"].cuda(), d["u_sample"].cuda(), q=q.cuda())
+    B.lazy_device_status()
+    acc, tokens = acc.cpu().tolist(), tokens.cpu().tolist()
+    zeroed = lambda t: np.where(t.numpy() > 0, t.numpy(), 0.0)  # noqa: E731
+    for s in range(64):
+        want, token = R.verify(zeroed(p[2 * s:2 * s + 2]), zeroed(q[s:s + 1]), d["draft"][s:s + 1].numpy(),
+                               d["u_accept"][s:s + 1].numpy(), d["u_sample"][s].item())
+        assert acc[s] == want and tokens[s][want] == token, s
+    assert 0 < sum(acc) < 64
