@@ -463,9 +463,10 @@ int lazy_k_attention_prefix(void *stream, int32_t dtype, const void *q, int32_t 
  * (u_accept fp32 [n_draft], u_sample fp32 [n_seqs], uniform in [0, 1)).  The token behind the accepted ones is the first id
  * whose running sum of w exceeds u_sample times their total, w = max(p - q, 0) after a rejection (p without the rejected id
  * if q is NULL; p if that leaves nothing), w = p behind the last draft: the sequence is then distributed as the target's.
- * tokens int32 [n_seqs, max_draft + 1]: accepted drafts, that token, then -1; n_accept int32 [n_seqs].  Sums in 64
- * bits.  A drafted id outside [0, vocab) is reported and rejected; a row without any positive probability is
- * reported and gives token -1.  p and q may be any rows; negative and NaN entries count as 0 throughout. */
+ * tokens int32 [n_seqs, max_draft + 1]: accepted drafts, that token, then -1; n_accept int32 [n_seqs].  Differences
+ * and sums in 64 bits.  A drafted id outside [0, vocab) is reported and rejected; a row without any positive probability is
+ * reported and gives token -1.  p and q may be any rows; negative and NaN entries count as 0 throughout,
+ * infinite ones as the largest number. */
 int lazy_k_verify(void *stream, const float *p, int32_t ldp, const float *q, int32_t ldq, const int32_t *draft,
                   const int32_t *d_cu_draft, int32_t n_seqs, int32_t n_draft, int32_t max_draft, int32_t vocab,
                   const float *u_accept, const float *u_sample, int32_t *n_accept, int32_t *tokens);

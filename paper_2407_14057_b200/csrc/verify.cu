@@ -6,9 +6,10 @@
 // What has to be read is one row of p (and one of q after a rejection) per sequence, wherever the scan ends; the
 // other rows are touched at the drafted ids only.  A cluster of CTAs shares the row: each sums its contiguous
 // part, the totals meet in distributed shared memory, and the one warp whose part holds the crossing reads its
-// few hundred values again (from L2).  Sums run in 64 bits: with 32 the running sum's rounding would move the crossing to a
+// few hundred values again (from L2).  Sums run in 64 bits, differences included: with 32 the running sum's rounding would move the crossing to a
 // neighbouring id about once in a few hundred draws at a vocabulary of 32000.  One request, 32000 ids: 6.2 us, the latency of
 // three rounds of loads and two scans; 128 requests of up to 7 drafts: 12.3 us (31 MB).
+#include "attn_common.cuh"
 #include "cache_ops.cuh"
 
 namespace lazy {
@@ -26,21 +27,44 @@ __device__ __forceinline__ double warp_sum_f64(double v) {
 // A probability as the caller has it: negative ones and NaN count as 0 (a negative one of the draft model's would give its id
 // a weight that the target does not).
 __device__ __forceinline__ float vf_prob(float x) { return fmaxf(x, 0.f); }
+// The same in 64 bits, an infinite one as the largest number.
+__device__ __forceinline__ double vf_prob_f64(float x) { return (double)fminf(vf_prob(x), 3.402823466e38f); }
 
-// Weight of id j: p[j], less q[j] (row_q) or nothing at all for the one rejected id; never negative.
-__device__ __forceinline__ float vf_weight(float p, float q, int j, int zeroed) {
-  return j == zeroed ? 0.f : fmaxf(vf_prob(p) - vf_prob(q), 0.f);
+// Weights max(p - q, 0) of two ids after a rejection, as the sum of the result and `rest`, what the subtraction in 32 bits
+// rounded off (exact, as the larger of p and q is subtracted from).  Infinities make one of them infinite or NaN.
+__device__ __forceinline__ unsigned long long vf_less_x2(float p0, float p1, float q0, float q1, unsigned long long &rest) {
+  const unsigned long long minus = f32x2_pack(-1.f, -1.f);
+  q0 = vf_prob(q0);
+  q1 = vf_prob(q1);
+  const unsigned long long q = f32x2_pack(q0, q1), most = f32x2_pack(fmaxf(p0, q0), fmaxf(p1, q1)), w = f32x2_fma(q, minus, most);
+  rest = f32x2_fma(q, minus, f32x2_fma(w, minus, most));
+  return w;
 }
 
 // The weights of one row.  VEC: rows and vocabulary are multiples of four ids and 16-byte aligned.
 template <bool VEC>
 struct VfRow {
   const float *p, *q;  // q NULL: nothing is taken off
-  int zeroed;          // id without weight, or -1
-  __device__ __forceinline__ float at(int j) const { return vf_weight(p[j], q ? q[j] : 0.f, j, zeroed); }
-  // Sum over ids first, first + stride, ... < end (four consecutive ones each with VEC), UNROLL loads of a row in flight.
+  int zeroed;          // id without weight, or -1 (always, where q is there)
+  bool wild;           // there are infinities among the weights
+  __device__ __forceinline__ double at(int j) const {
+    return j == zeroed ? 0.0 : fmax(vf_prob_f64(p[j]) - (q ? vf_prob_f64(q[j]) : 0.0), 0.0);
+  }
+  // Sum over ids first, first + stride, ... < end (four consecutive ones each with VEC).  What 32 bits lose of the
+  // differences is added up as well (2^-44 of the sum is left): without it a crossing would move to a neighbouring id now and
+  // then.  Subtracting in 64 bits throughout, with another conversion per id, takes 128 requests 12.5 us in a graph, 10.3 so.
   __device__ __forceinline__ double sum(int first, int end, int stride) const {
-    constexpr int UNROLL = 8, W = VEC ? 4 : 1;
+    if (wild) {
+      double total = 0.0;
+      for (int j0 = first; j0 < end; j0 += stride)
+        for (int j = j0; j < j0 + (VEC ? 4 : 1); ++j) total += at(j);
+      return total;
+    }
+    return q ? sum_of<true>(first, end, stride) : sum_of<false>(first, end, stride);
+  }
+  template <bool Q>
+  __device__ __forceinline__ double sum_of(int first, int end, int stride) const {
+    constexpr int UNROLL = 8, W = VEC ? 4 : 2;  // loads of a row in flight; of two ids the second is not there without VEC
     double total = 0.0;
     for (int j0 = first; j0 < end; j0 += UNROLL * stride) {
       float x[UNROLL][W], y[UNROLL][W];
@@ -50,20 +74,36 @@ struct VfRow {
         if (VEC) {
           float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
           *reinterpret_cast<float4 *>(x[u]) = j < end ? *reinterpret_cast<const float4 *>(p + j) : z;
-          *reinterpret_cast<float4 *>(y[u]) = j < end && q ? *reinterpret_cast<const float4 *>(q + j) : z;
+          if (Q) *reinterpret_cast<float4 *>(y[u]) = j < end ? *reinterpret_cast<const float4 *>(q + j) : z;
         } else {
           x[u][0] = j < end ? p[j] : 0.f;
-          y[u][0] = j < end && q ? q[j] : 0.f;
+          if (Q) y[u][0] = j < end ? q[j] : 0.f;
+          x[u][1] = y[u][1] = 0.f;
         }
       }
+      unsigned long long rests = 0ull;
 #pragma unroll
       for (int u = 0; u < UNROLL; ++u) {
         const int j = j0 + u * stride;
         float w[W];
 #pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = vf_weight(x[u][i], y[u][i], j + i, zeroed);
+        for (int i = 0; i < W; i += 2) {
+          if (Q) {
+            unsigned long long rest;
+            f32x2_unpack(vf_less_x2(x[u][i], x[u][i + 1], y[u][i], y[u][i + 1], rest), w[i], w[i + 1]);
+            rests = f32x2_add(rests, rest);
+          } else {
+            w[i] = j + i == zeroed ? 0.f : vf_prob(x[u][i]);
+            w[i + 1] = j + i + 1 == zeroed ? 0.f : vf_prob(x[u][i + 1]);
+          }
+        }
         if (VEC) total += ((double)w[0] + (double)w[1]) + ((double)w[2] + (double)w[3]);
         else total += (double)w[0];
+      }
+      if (Q) {
+        float r0, r1;
+        f32x2_unpack(rests, r0, r1);
+        total += (double)(r0 + r1);
       }
     }
     return total;
@@ -95,9 +135,9 @@ __device__ __forceinline__ int vf_crossing(const VfRow<VEC> &row, int begin, int
   int last = -1;
   for (int j0 = b0; j0 < e0; j0 += 32) {
     const int j = j0 + lane;
-    const float w = j < e0 ? row.at(j) : 0.f;
-    const double at = run + warp_inclusive_f64((double)w);
-    const uint32_t hit = __ballot_sync(0xffffffffu, w > 0.f && at > bar), some = __ballot_sync(0xffffffffu, w > 0.f);
+    const double w = j < e0 ? row.at(j) : 0.0;
+    const double at = run + warp_inclusive_f64(w);
+    const uint32_t hit = __ballot_sync(0xffffffffu, w > 0.0 && at > bar), some = __ballot_sync(0xffffffffu, w > 0.0);
     if (hit) return j0 + __ffs(hit) - 1;
     if (some) last = j0 + 31 - __clz(some);
     run = __shfl_sync(0xffffffffu, at, 31);
@@ -147,12 +187,12 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
   __syncthreads();
   const int acc = s_acc;
   VfRow<VEC> row = {p + (size_t)(d0 + s + acc) * ldp, acc < T && q ? q + (size_t)(d0 + acc) * ldq : nullptr,
-                    acc < T && !q ? draft[d0 + acc] : -1};
+                    acc < T && !q ? draft[d0 + acc] : -1, false};
   // ---- this warp's contiguous part of the row, in multiples of 128 ids
   const int parts = size * VF_WARPS, part = rank * VF_WARPS + warp;
   const int len = ((vocab + parts - 1) / parts + 127) / 128 * 128;
   const int begin = (int)min((long long)part * len, (long long)vocab), end = min(vocab - begin, len) + begin;
-  for (int pass = 0;; ++pass) {
+  while (true) {
     const double sum = warp_sum_f64(row.sum(begin + lane * (VEC ? 4 : 1), end, VEC ? 128 : 32));
     if (lane == 0) warp_total[warp] = sum;
     __syncthreads();
@@ -169,14 +209,19 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
       total += cta[r];
     }
     co_cluster_arrive();  // when all have, every total has been read: a second pass may write again, a CTA may leave
-    if (!(total > 0.0) && (row.q || row.zeroed >= 0) && pass == 0) {
+    if (!row.wild && !(total <= 1.7976931348623157e308)) {
+      co_cluster_wait();
+      row.wild = true;
+      continue;
+    }
+    if (!(total > 0.0) && (row.q || row.zeroed >= 0)) {
       co_cluster_wait();
       row.q = nullptr;  // the draft's distribution covers the target's (equal but for rounding): the target's itself
       row.zeroed = -1;
       continue;
     }
     // ---- the crossing lies in the first CTA, and there in the first warp's part, whose running sum exceeds the
-    // bar; where rounding (or an infinite total) leaves none, in the last with any weight.  All threads decide
+    // bar; where rounding leaves none, in the last with any weight.  All threads decide
     // alike from the same numbers.
     const double bar = (double)u_sample[s] * total;
     int owner_cta = -1, owner = -1;

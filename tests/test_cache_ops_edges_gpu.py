@@ -139,3 +139,38 @@ def test_verify_negative_and_nan_entries_count_as_zero(V):
                                d["u_accept"][s:s + 1].numpy(), d["u_sample"][s].item())
         assert acc[s] == want and tokens[s][want] == token, s
     assert 0 < sum(acc) < 64
+
+
+@pytest.mark.parametrize("V,first,second", [(3, 0, 1), (4, 0, 1), (4096, 5, 3001), (4095, 1000, 1001)])
+def test_verify_subtracts_in_64_bits(V, first, second):
+    """Weights 1 and 1 - 2^-30: half of their total lies just below the first one; in 32 bits both would be 1."""
+    p, q = torch.zeros((2, V)), torch.zeros((1, V))
+    p[0, first] = p[0, second] = 1.0
+    q[0, second] = 2.0 ** -30
+    q[0, V - 1] = 1.0                       # the draft, which the target never takes
+    half = torch.tensor([0.5]).cuda()
+    acc, tokens = B.lazy_k_verify(p.cuda(), torch.tensor([V - 1], dtype=torch.int32).cuda(), cu([1]), 1, half, half, q=q.cuda())
+    assert acc.item() == 0 and tokens[0].tolist() == [first, -1]
+    assert R.verify(p.numpy(), q.numpy(), [V - 1], [0.5], 0.5) == (0, first)
+
+
+@pytest.mark.parametrize("V", [3, 300, 4096, 32000])
+@pytest.mark.parametrize("with_q", [True, False])
+def test_verify_infinite_entries_count_as_the_largest_number(V, with_q):
+    """Behind the last draft, after a rejection, and where the draft model's own entry is infinite."""
+    g = gen(94)
+    big = torch.finfo(F32).max
+    drafts, at = [0, 1, 1], torch.randint(0, V - 1, (3,), generator=g)
+    p, q = torch.rand((5, V), generator=g), torch.rand((2, V), generator=g)
+    p[0, at[0]] = p[1, at[1]] = float("inf")
+    p[1::2, V - 1] = 0.0                     # both drafts are rejected
+    q[:, V - 1] = 1.0
+    q[1, at[2]] = float("inf")
+    half = torch.tensor([0.5] * 3).cuda()
+    acc, tokens = B.lazy_k_verify(p.cuda(), torch.tensor([V - 1] * 2, dtype=torch.int32).cuda(), cu(drafts), 1, half[:2], half,
+                                  q=q.cuda() if with_q else None)
+    B.lazy_device_status()
+    assert acc.tolist() == [0, 0, 0] and tokens[:, 1].tolist() == [-1, -1, -1]
+    assert tokens[:2, 0].tolist() == at[:2].tolist()
+    want = R.verify(p[3:].clamp(max=big).numpy(), q[1:].clamp(max=big).numpy() if with_q else None, [V - 1], [0.5], 0.5)
+    assert tokens[2, 0].item() == want[1] and (not with_q or want[1] != at[2])
