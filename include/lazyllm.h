@@ -408,8 +408,8 @@ int lazy_k_gather_rows(void *stream, const void *src, const int32_t *idx, void *
 
 /* Accumulated attention weight of prompts: mass[g][r] (fp32 [n_kv_heads, n_total]) = sum over the last `window` rows
  * i >= r of r's sequence (0 = all its rows) and over the query heads h of key/value head g of
- * softmax_r(q_i,h . k_r,g / sqrt(head_dim)), causal.  q rows of pitch ldq, k rows of pitch ldkv elements, packed sequences,
- * the longest of max_len rows.  Sums in fp32 in a fixed order (the same bits every call). */
+ * softmax_r(q_i,h . k_r,g / sqrt(head_dim)), causal.  q rows of pitch ldq, k rows of pitch ldkv elements, packed sequences
+ * of at most max_len rows (any number that no sequence exceeds).  Sums in fp32 in a fixed order (the same bits every call). */
 size_t lazy_k_attention_mass_scratch_floats(int32_t n_seqs, int32_t n_total, int32_t max_len, int32_t n_heads,
                                             int32_t n_kv_heads, int32_t window);
 int lazy_k_attention_mass(void *stream, int32_t dtype, const void *q, int32_t ldq, const void *k, int32_t ldkv,

@@ -715,6 +715,7 @@ int mass_tc(cudaStream_t st, const void *q, int ldq, const void *k, int ldkv, co
 
 size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window) {
   const int group = n_heads / n_kv_heads;
+  if (max_len > n_total) max_len = n_total;  // a bound may be any number
   const size_t general = (size_t)n_total * n_heads;
   if (group > MT) return general;
   const MassDeep deep = mass_deep(n_seqs, n_total, max_len, n_heads, n_kv_heads, window);
@@ -727,6 +728,7 @@ size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n
 int launch_attention_mass(cudaStream_t st, int dtype, const void *q, int ldq, const void *k, int ldkv,
                           const int32_t *cu, int n_seqs, int max_len, int n_total, int n_heads, int n_kv_heads,
                           int head_dim, int window, float *scratch, float *mass, DevStatus *status) {
+  if (max_len > n_total) max_len = n_total;  // a bound may be any number
   if (n_seqs == 0 || max_len == 0) return LAZY_OK;
   if (mass_tc_eligible(dtype, head_dim, n_heads / n_kv_heads)) {
     float *lse = reinterpret_cast<float *>(align_up((uintptr_t)scratch, 16));

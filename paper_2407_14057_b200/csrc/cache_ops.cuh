@@ -86,9 +86,12 @@ inline int co_launch(void (*kfn)(KArgs...), dim3 grid, dim3 block, size_t smem, 
   }
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kfn, static_cast<KArgs>(args)...);
+  if (cudaLaunchKernelEx(&cfg, kfn, static_cast<KArgs>(args)...) != cudaSuccess) {
+    cudaGetLastError();  // reported here and now: a later call must not find it
+    return LAZY_E_CUDA;
+  }
   LAZY_COUNT_LAUNCH();
-  return e == cudaSuccess ? LAZY_OK : LAZY_E_CUDA;
+  return LAZY_OK;
 }
 
 // CTAs that run at once in clusters of `size` (1, 2, 4, 8 or 16), up to three to an SM: a cluster stays within a group of SMs, and

@@ -101,3 +101,15 @@ def test_verify_refuses(lib):
         refuse(f, VERIFY, BADARG, **change)
     refuse(f, VERIFY, CAPACITY, n_seqs=(1 << 24) + 1)
     refuse(f, VERIFY, 0, n_seqs=0)
+
+
+def test_attention_mass_scratch_of_a_loose_bound(lib):
+    """max_len beyond all rows asks for no more than their number does."""
+    f = lib.lazy_k_attention_mass_scratch_floats
+    for window in (0, 1, 20):
+        for n_seqs, n_total in ((1, 8), (3, 5000), (2, 60000)):
+            for heads in ((4, 2), (32, 8), (8, 8)):
+                want = f(n_seqs, n_total, n_total, *heads, window)
+                assert want > 0
+                for bound in (n_total + 1, 10 ** 8, 2 ** 31 - 100, 2 ** 31 - 1):
+                    assert f(n_seqs, n_total, bound, *heads, window) == want

@@ -174,3 +174,20 @@ def test_verify_infinite_entries_count_as_the_largest_number(V, with_q):
     assert tokens[:2, 0].tolist() == at[:2].tolist()
     want = R.verify(p[3:].clamp(max=big).numpy(), q[1:].clamp(max=big).numpy() if with_q else None, [V - 1], [0.5], 0.5)
     assert tokens[2, 0].item() == want[1] and (not with_q or want[1] != at[2])
+
+
+# ------------------------------------------------------------------------------------------- loose bounds
+@pytest.mark.parametrize("heads", HEADS, ids=IDS)
+@pytest.mark.parametrize("lens,window", [([257, 31], 0), ([257, 31], 20), ([5], 1)])
+def test_attention_mass_takes_any_bound(heads, lens, window):
+    """max_len is a bound, not a length: the largest number is one, and no call after it finds an error left behind."""
+    H, Hkv, dh, dtype = heads
+    q, k, dq, dk = mass_case(88, lens, H, Hkv, dh, dtype, fused=True)
+    n = sum(lens)
+    want = R.attention_mass(f64(q).reshape(n, H, dh), f64(k).reshape(n, Hkv, dh), lens, H, Hkv, dh, window)
+    e = weight_error(f64(q).reshape(n, H, dh), f64(k).reshape(n, Hkv, dh), dh)
+    for bound in (2 ** 31 - 1, 2 ** 31 - 100, 10 ** 7):
+        got = B.lazy_k_attention_mass(dq, dk, cu(lens), bound, H, Hkv, dh, window)
+        assert np.all(np.abs(f64(got) - want) <= e * want + 1e-30), bound
+    c, new = step_case(89, [3], 5, 4, 2, 64, F32)
+    check_step(c, new, 4, 5, 1)
