@@ -627,10 +627,12 @@ prefix_own_kernel(const PrefixArgs a, int group, int col_blocks, int per_split, 
 }
 
 // ---- (3) the merge: one warp per (row, head) ------------------------------------------------------------------------
+// The parts are still being written when it starts: they must not be __restrict__, which with const says that nobody
+// writes them while it runs and lets their loads go ahead of the wait.
 template <int HD>
 __global__ void __launch_bounds__(128)
-prefix_tc_merge_kernel(const PrefixArgs a, const float *__restrict__ part_o, const float2 *__restrict__ part_ml, int n_pre_parts,
-                       int n_parts, int own_split, DevStatus *status) {
+prefix_tc_merge_kernel(const PrefixArgs a, const float *part_o, const float2 *part_ml, int n_pre_parts, int n_parts,
+                       int own_split, DevStatus *status) {
   constexpr int V = HD / 32;
   constexpr bool WIDE = V % 2 == 0;  // a lane's columns: V in a row, or every 32nd where V is odd
   const int lane = threadIdx.x & 31;

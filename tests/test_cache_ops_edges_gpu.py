@@ -191,3 +191,28 @@ def test_attention_mass_takes_any_bound(heads, lens, window):
         assert np.all(np.abs(f64(got) - want) <= e * want + 1e-30), bound
     c, new = step_case(89, [3], 5, 4, 2, 64, F32)
     check_step(c, new, 4, 5, 1)
+
+
+# ------------------------------------------------------------------------------------------- one scratch, call after call
+@pytest.mark.parametrize("name", [n for n in CALLS if n.startswith(("prefix", "mass"))])
+def test_a_captured_call_uses_nothing_that_its_scratch_held(name, monkeypatch):
+    """A call in a graph whose scratch is spoilt before every replay, on inputs that change between them."""
+    inputs, call = CALLS[name]
+    made = []
+    make = B._scratch
+    monkeypatch.setattr(B, "_scratch", lambda n, dtype: made.append(make(n, dtype)) or made[-1])
+    x = inputs(90)
+    want = {seed: [t.clone() for t in call(inputs(seed))] for seed in (91, 92)}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = call(x)
+    for i in range(40):
+        seed = 91 + i % 2
+        for key, t in inputs(seed).items():
+            x[key].copy_(t)
+        made[-1].fill_(float("nan"))
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, want[seed])), i
+    B.lazy_device_status()
