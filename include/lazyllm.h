@@ -402,7 +402,8 @@ int lazy_k_gather_rows(void *stream, const void *src, const int32_t *idx, void *
  * head_dim], cmass / cpos [n_seqs, n_kv_heads, cap], clen [n_seqs, n_kv_heads]; device tables that do not fit the
  * sizes given are reported through the status word (LAZY_E_BADARG unless stated otherwise) and that sequence is
  * skipped.  Outputs must not overlap inputs except where stated.  Scratch need not be initialised, may start at any address that
- * its element type may have, keeps nothing from one call for the next, and must not be shared by calls that may run at the same
+ * its element type may have, serves every call whose sizes are at most those that its own size was asked for (same heads; window
+ * 0 is the largest), keeps nothing from one call for the next, and must not be shared by calls that may run at the same
  * time (two replayed graphs included).  Infinities and NaN among what a row sees come out as the formulas have them, but
  * for weights below 2^-100, which may count as 0; what a row does not see changes nothing of its outputs. */
 

@@ -47,7 +47,7 @@ int lazy_k_attention_mass(void *stream, int32_t dtype, const void *q, int32_t ld
   if (bad_rows(q, ldq, (long long)n_heads * head_dim, dtype) || bad_rows(k, ldkv, (long long)n_kv_heads * head_dim, dtype) ||
       !d_cu_seqlens || !scratch || !mass)
     return LAZY_E_BADARG;
-  if (scratch_floats < attention_mass_scratch_floats(n_seqs, n_total, max_len, n_heads, n_kv_heads, window))
+  if (scratch_floats < attention_mass_scratch_need(n_seqs, n_total, max_len, n_heads, n_kv_heads, window))
     return LAZY_E_CAPACITY;
   DevStatus *status = dev_status_ptr();
   if (!status) return LAZY_E_CUDA;
@@ -106,7 +106,7 @@ int lazy_k_evict_step(void *stream, int32_t dtype, const void *q, int32_t ldq, c
       !pos_new || !mass_in || !mass_out || !pos_in || !pos_out || !len_in || !len_out || !scratch || !o ||
       ((uintptr_t)o & 15) || !slot || !gone)
     return LAZY_E_BADARG;
-  if (scratch_floats < evict_step_scratch_floats(n_seqs, n_heads, n_kv_heads, head_dim, budget)) return LAZY_E_CAPACITY;
+  if (scratch_floats < evict_step_scratch_need(n_seqs, n_heads, n_kv_heads, head_dim, budget)) return LAZY_E_CAPACITY;
   DevStatus *status = dev_status_ptr();
   if (!status) return LAZY_E_CUDA;
   const EvictStepArgs a = {q, k_new, v_new, ldq, ld_new, pos_new, kc, vc, cap, mass_in, mass_out, pos_in, pos_out, len_in,
@@ -142,7 +142,7 @@ int lazy_k_attention_prefix(void *stream, int32_t dtype, const void *q, int32_t 
   if (n_kv > 0 && max_kv > 0 &&
       (!kv_idx || kv_rows < 1 || bad_rows(k, ldkv, width, dtype) || bad_rows(v, ldkv, width, dtype)))
     return LAZY_E_BADARG;
-  if (scratch_floats < attention_prefix_scratch_floats(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads, n_kv_heads, head_dim))
+  if (scratch_floats < attention_prefix_scratch_need(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads, n_kv_heads, head_dim))
     return LAZY_E_CAPACITY;
   DevStatus *status = dev_status_ptr();
   if (!status) return LAZY_E_CUDA;

@@ -713,7 +713,7 @@ int mass_tc(cudaStream_t st, const void *q, int ldq, const void *k, int ldkv, co
 
 }  // namespace
 
-size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window) {
+size_t attention_mass_scratch_need(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window) {
   const int group = n_heads / n_kv_heads;
   if (max_len > n_total) max_len = n_total;  // a bound may be any number
   const size_t general = (size_t)n_total * n_heads;
@@ -723,6 +723,23 @@ size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n
   const size_t tiled = (size_t)n_kv_heads * mass_seq_tiles(n_seqs, n_total, group) * MT +
                        (size_t)n_seqs * n_kv_heads * lane_tiles * deep.splits * MT * 2;
   return (general > tiled ? general : tiled) + 4;  // + 4: tiles start on a 16-byte boundary
+}
+
+// As much as any batch no larger needs: of the DEEP form's parts, which a larger batch may do without, the most there can be.
+size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window) {
+  const int group = n_heads / n_kv_heads;
+  if (max_len > n_total) max_len = n_total;
+  const size_t general = (size_t)n_total * n_heads;
+  if (group > MT) return general;
+  size_t tiled = (size_t)n_kv_heads * mass_seq_tiles(n_seqs, n_total, group) * MT;
+  const int key_tiles = cdiv(max_len, MT), sms = sm_count();
+  if (mass_tiles(key_tiles, MT, n_seqs, n_total) * n_kv_heads > 2 * sms) {
+    const int lane_tiles = cdiv(window > 0 && window < max_len ? window : max_len, MT / group);
+    const size_t heads = (size_t)(n_seqs < sms / n_kv_heads ? n_seqs : sms / n_kv_heads) * n_kv_heads;
+    tiled += heads * (lane_tiles < MT_DEEP_TILES ? lane_tiles : MT_DEEP_TILES) *
+             (key_tiles < MT_DEEP_SPLITS ? key_tiles : MT_DEEP_SPLITS) * MT * 2;
+  }
+  return (general > tiled ? general : tiled) + 4;
 }
 
 int launch_attention_mass(cudaStream_t st, int dtype, const void *q, int ldq, const void *k, int ldkv,

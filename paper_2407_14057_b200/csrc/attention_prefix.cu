@@ -811,14 +811,39 @@ int prefix_tc(cudaStream_t st, const PrefixArgs &a, float *scratch, DevStatus *s
 
 }  // namespace
 
-size_t attention_prefix_scratch_floats(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv, int n_heads,
-                                       int n_kv_heads, int head_dim) {
+size_t attention_prefix_scratch_need(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv, int n_heads,
+                                     int n_kv_heads, int head_dim) {
   const size_t general =
       (size_t)n_rows * n_heads * attn_split_count((long long)n_rows * n_heads, n_pre + max_kv) * (head_dim + 2);
   if (n_heads / n_kv_heads > PT_Q || max_q < 1 || n_seqs < 1 || n_rows < 1) return general;
   const PrefixPlan p = prefix_plan(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads, n_kv_heads);
   const size_t tiled = p.parts * p.pairs * (head_dim + 2) + 4;  // + 4: parts start on a 16-byte boundary
   return general > tiled ? general : tiled;
+}
+
+// As much as any batch no larger needs (of n_rows <= n_seqs * max_q rows), although fewer rows are cut into more parts: parts
+// times (row, head) pairs of the prefix at the row counts that a number of lane groups ends with, and of the own keys, whose
+// parts fill the machine twice or hold PO_KEYS keys (prefix_plan; 16 or fewer pairs make a column block).
+size_t attention_prefix_scratch_floats(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv, int n_heads,
+                                       int n_kv_heads, int head_dim) {
+  const size_t need = attention_prefix_scratch_need(n_rows, n_seqs, max_q, n_pre, max_kv, n_heads, n_kv_heads, head_dim);
+  const size_t general = attn_split_parts((long long)n_rows * n_heads, n_pre + max_kv) * (head_dim + 2);
+  size_t tiled = 0;
+  if (n_heads / n_kv_heads <= PT_Q) {
+    const long long R = PT_Q / (n_heads / n_kv_heads), sms = sm_count(), key_tiles = cdiv(n_pre, PT_K), rows = n_rows;
+    auto least = [](long long a, long long b) { return a < b ? a : b; };
+    auto most = [](long long a, long long b) { return a > b ? a : b; };
+    long long pre = 0;
+    for (long long g = 1; g == 1 || ((g - 1) * 2 * R < rows && g <= sms / n_kv_heads); ++g)
+      pre = most(pre, least(rows, 2 * R * g) * least(key_tiles, most(sms / (n_kv_heads * g), 1)));
+    if (key_tiles > 0) pre = most(pre, rows);
+    const long long pairs = rows * n_heads, by_warps = least(64, cdiv(max_kv, PO_WARPS * RM_KEYS)),
+                    by_keys = least(64, cdiv(max_kv, PO_KEYS));
+    const long long own = least(pairs * by_warps, most(pairs + 2 * 16 * sms, pairs * by_keys));
+    tiled = (size_t)(pre * n_heads + own) * (head_dim + 2) + 4;
+  }
+  const size_t any = general > tiled ? general : tiled;
+  return any > need ? any : need;
 }
 
 int launch_attention_prefix(cudaStream_t st, int dtype, const PrefixArgs &a, float *scratch, DevStatus *status) {

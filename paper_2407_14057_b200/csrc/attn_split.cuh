@@ -170,6 +170,11 @@ inline int attn_split_count(long long rows_heads, int n_keys) {
   const long long per = (tiles + want - 1) / want;
   return (int)((tiles + per - 1) / per);
 }
+// The most ranges that any number of pairs up to rows_heads makes of up to n_keys, times the pairs.
+inline size_t attn_split_parts(long long rows_heads, int n_keys) {
+  const long long tiles = cdiv(n_keys > 0 ? n_keys : 1, AS_TILE), all = rows_heads * tiles, most = rows_heads + 4LL * 148 - 1;
+  return (size_t)(rows_heads < 1 ? 0 : (all < most ? all : most));
+}
 // Keys per range when n_keys are cut into `splits` ranges of whole tiles.
 inline int attn_split_keys(int n_keys, int splits) {
   return cdiv(cdiv(n_keys > 0 ? n_keys : 1, AS_TILE), splits) * AS_TILE;

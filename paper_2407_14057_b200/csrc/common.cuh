@@ -322,7 +322,10 @@ int launch_gather_i32(cudaStream_t st, const int32_t *src, const int32_t *idx, i
 int launch_lm_head(cudaStream_t st, int dtype, const void *h, const void *w, float *logits,
                    int n_rows, int d, int vocab, bool w_const = false);
 // ---- bounded and shared caches (evict.cu, evict_step.cu, attention_mass.cu, attention_prefix.cu, verify.cu) ----
-// Accumulated attention weight of prompts; scratch: attention_mass_scratch_floats().
+// Scratch: ..._need() is what a call of that shape has to have, ..._floats() as much as any smaller one needs too, which
+// callers are told.
+// Accumulated attention weight of prompts.
+size_t attention_mass_scratch_need(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window);
 size_t attention_mass_scratch_floats(int n_seqs, int n_total, int max_len, int n_heads, int n_kv_heads, int window);
 int launch_attention_mass(cudaStream_t st, int dtype, const void *q, int ldq, const void *k, int ldkv,
                           const int32_t *cu, int n_seqs, int max_len, int n_total, int n_heads, int n_kv_heads,
@@ -350,6 +353,7 @@ struct EvictStepArgs {
   void *o;
   int32_t *slot, *gone;
 };
+size_t evict_step_scratch_need(int n_seqs, int n_heads, int n_kv_heads, int head_dim, int budget);
 size_t evict_step_scratch_floats(int n_seqs, int n_heads, int n_kv_heads, int head_dim, int budget);
 int launch_evict_step(cudaStream_t st, int dtype, const EvictStepArgs &a, float *scratch, DevStatus *status);
 // Rows of a batch over one shared prefix and each sequence's own key list.
@@ -367,6 +371,8 @@ struct PrefixArgs {
   int n_heads, n_kv_heads, head_dim;
   void *o;
 };
+size_t attention_prefix_scratch_need(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv, int n_heads,
+                                     int n_kv_heads, int head_dim);
 size_t attention_prefix_scratch_floats(int n_rows, int n_seqs, int max_q, int n_pre, int max_kv, int n_heads,
                                        int n_kv_heads, int head_dim);
 int launch_attention_prefix(cudaStream_t st, int dtype, const PrefixArgs &a, float *scratch, DevStatus *status);

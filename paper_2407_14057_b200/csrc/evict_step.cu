@@ -490,13 +490,24 @@ int step_fused(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevStatu
 
 }  // namespace
 
-size_t evict_step_scratch_floats(int n_seqs, int n_heads, int n_kv_heads, int head_dim, int budget) {
-  const size_t general = step_scratch(n_seqs, n_heads, n_kv_heads, head_dim, budget).total;
+// What the call needs, or (`any`) as much as any smaller one does: of the general form's parts the most there can be.
+static size_t step_scratch_floats(int n_seqs, int n_heads, int n_kv_heads, int head_dim, int budget, bool any) {
+  size_t general = step_scratch(n_seqs, n_heads, n_kv_heads, head_dim, budget).total;
+  if (any) {
+    const size_t sh = (size_t)n_seqs * n_heads, splits = (size_t)attn_split_count((long long)sh, budget);
+    general += (attn_split_parts((long long)sh, budget) - sh * splits) * (head_dim + 2);
+  }
   // the one-launch form keeps at most every slot's logits, an even number of columns, parts rounded up to 16 slots; + 4: they
   // are read two at a time and start on a 16-byte boundary
   const size_t heads = (size_t)n_seqs * n_kv_heads, group = n_heads / n_kv_heads;
   const size_t fused = heads * ((size_t)budget + SF_LARGE_CLUSTER * RM_KEYS) * ((group + 1) & ~(size_t)1) + 4;
   return general > fused ? general : fused;
+}
+size_t evict_step_scratch_need(int n_seqs, int n_heads, int n_kv_heads, int head_dim, int budget) {
+  return step_scratch_floats(n_seqs, n_heads, n_kv_heads, head_dim, budget, false);
+}
+size_t evict_step_scratch_floats(int n_seqs, int n_heads, int n_kv_heads, int head_dim, int budget) {
+  return step_scratch_floats(n_seqs, n_heads, n_kv_heads, head_dim, budget, true);
 }
 
 int launch_evict_step(cudaStream_t st, int dtype, const EvictStepArgs &a, float *scratch, DevStatus *status) {

@@ -1,5 +1,7 @@
 """Refusals of the operators on bounded and shared caches: every check answers before the device is touched."""
 import ctypes as C
+import math
+import random
 
 import pytest
 
@@ -113,3 +115,42 @@ def test_attention_mass_scratch_of_a_loose_bound(lib):
                 assert want > 0
                 for bound in (n_total + 1, 10 ** 8, 2 ** 31 - 100, 2 ** 31 - 1):
                     assert f(n_seqs, n_total, bound, *heads, window) == want
+
+
+def _sizes(rng, top):
+    return max(1, min(top, int(round(2 ** rng.uniform(0, math.log2(top))))))
+
+
+SCRATCH_HEADS = [(32, 32, 128), (32, 8, 128), (8, 1, 128), (16, 4, 64), (12, 4, 128), (8, 2, 96), (4, 2, 256), (40, 1, 64),
+                 (6, 2, 32), (150, 1, 32), (200, 200, 64)]
+
+
+def test_scratch_for_the_largest_serves_every_smaller_call(lib):
+    """The size asked for a shape is at least that of every shape that is no larger in anything."""
+    rng = random.Random(3)
+    for _ in range(20000):
+        H, Hkv, dh = rng.choice(SCRATCH_HEADS)
+        n_seqs, longest, window = _sizes(rng, 300), _sizes(rng, 20000), rng.choice([0, 1, _sizes(rng, 400)])
+        total = rng.randint(longest, n_seqs * longest)
+        a = lib.lazy_k_attention_mass_scratch_floats(n_seqs, total, longest, H, Hkv, window)
+        less = (rng.randint(1, n_seqs), rng.randint(1, total), rng.randint(1, longest), H, Hkv,
+                rng.randint(1, window) if window else rng.choice([0, rng.randint(1, 400)]))
+        assert lib.lazy_k_attention_mass_scratch_floats(*less) <= a, (n_seqs, total, longest, window, less)
+        budget = _sizes(rng, 20000)
+        a = lib.lazy_k_evict_step_scratch_floats(n_seqs, H, Hkv, dh, budget)
+        less = (rng.randint(1, n_seqs), H, Hkv, dh, rng.randint(1, budget))
+        assert lib.lazy_k_evict_step_scratch_floats(*less) <= a, (n_seqs, budget, less)
+        assert lib.lazy_k_evict_scratch_ints(less[0], Hkv, less[4]) <= lib.lazy_k_evict_scratch_ints(n_seqs, Hkv, budget)
+        max_q, max_kv, n_pre = _sizes(rng, 20), rng.choice([0, _sizes(rng, 3000)]), rng.choice([0, _sizes(rng, 30000)])
+        rows = rng.randint(1, n_seqs * max_q)
+        a = lib.lazy_k_attention_prefix_scratch_floats(rows, n_seqs, max_q, n_pre, max_kv, H, Hkv, dh)
+        s, t = rng.randint(1, n_seqs), rng.randint(1, max_q)
+        less = (rng.randint(1, min(rows, s * t)), s, t, rng.randint(0, n_pre), rng.randint(0, max_kv), H, Hkv, dh)
+        assert lib.lazy_k_attention_prefix_scratch_floats(*less) <= a, (rows, n_seqs, max_q, n_pre, max_kv, less)
+
+
+def test_scratch_of_a_batch_that_shrinks(lib):
+    """One that fills a lane group of its own needs more parts than the next larger one: asked for either, it has room."""
+    f = lib.lazy_k_attention_prefix_scratch_floats
+    sizes = [f(n, n, 1, 16384, 500, 32, 8, 128) for n in range(1, 200)]
+    assert sizes == sorted(sizes) and sizes[-1] < 4 * sizes[63]

@@ -216,3 +216,25 @@ def test_a_captured_call_uses_nothing_that_its_scratch_held(name, monkeypatch):
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(got, want[seed])), i
     B.lazy_device_status()
+
+
+@pytest.mark.parametrize("heads", [HEADS[1], HEADS[7]], ids=[IDS[1], IDS[7]])
+def test_one_scratch_for_a_batch_that_shrinks(heads):
+    """Scratch sized once for the largest batch serves every smaller one, down to a single request."""
+    H, Hkv, dh, dtype = heads
+    d = prefix_case(95, 1500, [1] * 70, [9] * 70, H, Hkv, dh, dtype)
+    dev = {k: v.cuda() for k, v in d.items()}
+    scratch = B.lazy_k_attention_prefix_scratch(70, 70, 1, 1500, 9, H, Hkv, dh)
+    for n in (70, 65, 64, 33, 32, 31, 16, 5, 1):
+        args = (dev["q"][:n], cu([1] * n), 1, dev["k_pre"], dev["v_pre"], dev["k"], dev["v"], dev["kv_idx"][:9 * n], cu([9] * n), 9,
+                H, Hkv, dh)
+        got = B.lazy_k_attention_prefix(*args, scratch=scratch)
+        assert torch.equal(got, B.lazy_k_attention_prefix(*args)), n
+    lens = [5000, 4000, 30]
+    _, _, q, k = mass_case(96, lens, H, Hkv, dh, dtype, fused=False)
+    scratch = B.lazy_k_attention_mass_scratch(3, sum(lens), max(lens), H, Hkv)
+    for part, window in ((lens, 0), (lens, 40), (lens[:1], 1), (lens[:2], 33), ([2000], 0)):
+        n = sum(part)
+        got = B.lazy_k_attention_mass(q[:n], k[:n], cu(part), max(part), H, Hkv, dh, window, scratch=scratch)
+        assert torch.equal(got, B.lazy_k_attention_mass(q[:n], k[:n], cu(part), max(part), H, Hkv, dh, window))
+    B.lazy_device_status()
