@@ -60,15 +60,36 @@ def build_call(force: bool = False) -> str:
             if f.read().strip() == h.hexdigest():
                 return CALL_LIB
     os.makedirs(os.path.dirname(CALL_STAMP), exist_ok=True)
-    subprocess.run(cmd, check=True)
+    made = f"{CALL_LIB}.{os.getpid()}"
+    try:
+        subprocess.run([made if c == CALL_LIB else c for c in cmd], check=True)
+        os.replace(made, CALL_LIB)
+    except (OSError, subprocess.CalledProcessError):
+        for f in (made, CALL_LIB):  # no marshaller is better than an old one, which could expect other entry points
+            if os.path.exists(f):
+                os.remove(f)
+        raise
     with open(CALL_STAMP, "w") as f:
         f.write(h.hexdigest())
     return CALL_LIB
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compiles every .cu under csrc/ and links liblazyllm.so, and the marshaller; returns the library's path."""
-    build_call(force)
+    """Compiles every .cu under csrc/ and links liblazyllm.so, then the marshaller; returns the library's path.
+
+    The library needs nvcc alone.  The marshaller needs torch, Python's headers and a C++ compiler as well; where one of them is
+    missing this says so, and only the Python wrappers that go through it are then missing."""
+    path = build_library(force, verbose)
+    try:
+        build_call(force)
+    except (ImportError, OSError, subprocess.CalledProcessError) as e:
+        sys.stderr.write(f"{os.path.basename(CALL_LIB)} was not built ({e}): the Python wrappers of the operators on bounded "
+                         "and shared caches will raise\n")
+    return path
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
+    """Compiles every .cu under csrc/ and links liblazyllm.so; returns its path."""
     dig = _digest()
     if not force and os.path.exists(LIB) and os.path.exists(STAMP):
         with open(STAMP) as f:
