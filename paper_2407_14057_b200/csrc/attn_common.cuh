@@ -71,9 +71,10 @@ __device__ __forceinline__ unsigned long long f32x2_mul(unsigned long long a, un
 }
 // 2^x of two numbers on the FMA pipe, for loops that the special-function unit bounds: x = n + f with n the nearest
 // integer (found by adding 1.5 2^23, which leaves n + 127 in the low bits), 2^f by a polynomial of degree 5 on
-// [-1/2, 1/2], 2^n as a float with that exponent.  The coefficients minimise the largest relative error (weighted
-// least squares on Chebyshev nodes, weights raised where the error is largest): 7.5e-8, 2.4e-7 with the arithmetic's
-// rounding, which is what ex2.approx has.  x below -126 counts as -126; NaN stays NaN; x must be below 127.
+// [-1/2, 1/2], 2^n as a float with that exponent.  The constant term is 1, so that whole powers are exact; the others make
+// the largest relative error small (weighted least squares on Chebyshev nodes, weights raised where the error is largest, then
+// single steps of the rounded coefficients): 9.9e-8 by themselves, 1.5e-7 with the arithmetic's rounding (ex2.approx: 2.4e-7),
+// -1.8e-8 on average.  x below -126 counts as -126; NaN stays NaN; x must be below 127.
 __device__ __forceinline__ unsigned long long ex2_poly_x2(unsigned long long x) {
   float a, b, t0, t1;
   f32x2_unpack(x, a, b);
@@ -84,12 +85,12 @@ __device__ __forceinline__ unsigned long long ex2_poly_x2(unsigned long long x) 
   const unsigned long long t = f32x2_add(x, f32x2_pack(magic, magic));
   const unsigned long long n = f32x2_add(t, f32x2_pack(-magic, -magic));
   const unsigned long long f = f32x2_fma(n, f32x2_pack(-1.f, -1.f), x);
-  unsigned long long p = f32x2_pack(0x1.5c08e4p-10f, 0x1.5c08e4p-10f);
-  p = f32x2_fma(p, f, f32x2_pack(0x1.3d0c52p-7f, 0x1.3d0c52p-7f));
-  p = f32x2_fma(p, f, f32x2_pack(0x1.c6b6e4p-5f, 0x1.c6b6e4p-5f));
-  p = f32x2_fma(p, f, f32x2_pack(0x1.ebf918p-3f, 0x1.ebf918p-3f));
-  p = f32x2_fma(p, f, f32x2_pack(0x1.62e428p-1f, 0x1.62e428p-1f));
-  p = f32x2_fma(p, f, f32x2_pack(0x1.000002p+0f, 0x1.000002p+0f));
+  unsigned long long p = f32x2_pack(0x1.5bba1ep-10f, 0x1.5bba1ep-10f);
+  p = f32x2_fma(p, f, f32x2_pack(0x1.3cea94p-7f, 0x1.3cea94p-7f));
+  p = f32x2_fma(p, f, f32x2_pack(0x1.c6b72ep-5f, 0x1.c6b72ep-5f));
+  p = f32x2_fma(p, f, f32x2_pack(0x1.ebf9bep-3f, 0x1.ebf9bep-3f));
+  p = f32x2_fma(p, f, f32x2_pack(0x1.62e42ap-1f, 0x1.62e42ap-1f));
+  p = f32x2_fma(p, f, f32x2_pack(0x1.000000p+0f, 0x1.000000p+0f));
   f32x2_unpack(t, t0, t1);
   return f32x2_mul(p, f32x2_pack(__uint_as_float(__float_as_uint(t0) << 23), __uint_as_float(__float_as_uint(t1) << 23)));
 }
