@@ -305,9 +305,9 @@ struct __align__(16) MassShared {
   float lse[MT_LSE_STAGES][MT];
   float part_m[2][MT], part_l[2][2][MT];  // per column half: a lane's (maximum, sum), a key's sum (two tiles' in turn)
   unsigned long long a_full[Shape::A_BUFS], a_empty[Shape::A_BUFS], b_full[Shape::STAGES], b_empty[Shape::STAGES], s_full[2],
-      s_free[2], l_full[MT_LSE_STAGES], l_free[MT_LSE_STAGES];
+      s_free[2], l_full[MT_LSE_STAGES], l_free[MT_LSE_STAGES], done;
   uint32_t tmem_base;
-  int abort_flag;
+  int abort_flag, last_flag;  // last_flag: of the waits after an abort
 };
 template <int HD, bool DEEP>
 constexpr int mass_smem =
@@ -382,7 +382,8 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
       mbar_init(smem_u32(&sh->l_full[i]), 1);
       mbar_init(smem_u32(&sh->l_free[i]), 8);
     }
-    sh->abort_flag = 0;
+    mbar_init(smem_u32(&sh->done), 1);
+    sh->abort_flag = sh->last_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma_prefetch_desc(&map_q);
     tma_prefetch_desc(&map_k);
@@ -400,6 +401,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   volatile int *abort_flag = &sh->abort_flag;
 
   // Every role walks the same (stationary, streamed) pairs: `t` counts pairs, `ai` stationary tiles.
+  int a_loads = 0, b_loads = 0, l_loads = 0;  // by the loading thread
   if (warp == 0) {
     if (lane == 0) {
       const uint32_t lane_bytes = (uint32_t)(R * group * 128 * CH), key_bytes = (uint32_t)(CH * CHUNK);
@@ -420,7 +422,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         ok = mbar_wait(smem_u32(&sh->a_empty[ai % A_BUFS]), (uint32_t)((ai / A_BUFS) & 1) ^ 1u, abort_flag, status, W_MASS);
         if (!ok) break;
         load(PASS == 1, at, sA + (ai % A_BUFS) * CH * CHUNK, smem_u32(&sh->a_full[ai % A_BUFS]));
-        ++ai;
+        a_loads = ++ai;
         if (!waited) {
           asm volatile("griddepcontrol.wait;" ::: "memory");  // the log-sum-exps of pass 1
           waited = true;
@@ -430,12 +432,14 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
           ok = mbar_wait(smem_u32(&sh->b_empty[st]), (uint32_t)((t / STAGES) & 1) ^ 1u, abort_flag, status, W_MASS);
           if (!ok) break;
           load(PASS == 2, b, sB + st * CH * CHUNK, smem_u32(&sh->b_full[st]));
+          ++b_loads;
           if (PASS == 2 && !DEEP) {
             const int ls = t % MT_LSE_STAGES;
             ok = mbar_wait(smem_u32(&sh->l_free[ls]), (uint32_t)((t / MT_LSE_STAGES) & 1) ^ 1u, abort_flag, status, W_MASS);
             if (!ok) break;
             mbar_expect_tx(smem_u32(&sh->l_full[ls]), MT * 4);
             bulk_load(smem_u32(sh->lse[ls]), lse + lse_base + (size_t)b * MT, MT * 4, smem_u32(&sh->l_full[ls]));
+            ++l_loads;
           }
         }
       }
@@ -616,6 +620,17 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
   }
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {  // a wait ran out: what this CTA has in flight ends before it leaves
+    if (threadIdx.x == 0) {
+      ring_landed(sh->a_full, A_BUFS, a_loads, &sh->last_flag, status, W_MASS);
+      ring_landed(sh->b_full, STAGES, b_loads, &sh->last_flag, status, W_MASS);
+      ring_landed(sh->l_full, MT_LSE_STAGES, l_loads, &sh->last_flag, status, W_MASS);
+    } else if (threadIdx.x == 32) {
+      umma_commit(smem_u32(&sh->done));
+      mbar_wait(smem_u32(&sh->done), 0, &sh->last_flag, status, W_MASS);
+    }
+    __syncthreads();
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)MT_TMEM_COLS)

@@ -134,9 +134,9 @@ struct PrefixShape {
 template <int STAGES, int TILES>
 struct __align__(8) PrefixBarriers {
   unsigned long long q_full, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES];
-  unsigned long long s_full[TILES], s_free[TILES], p_full[TILES], pv_done[TILES];
+  unsigned long long s_full[TILES], s_free[TILES], p_full[TILES], pv_done[TILES], done[2];
   uint32_t tmem_base;
-  int abort_flag;
+  int abort_flag, last_flag;  // last_flag: of the waits after an abort
 };
 template <int HD, int TILES>
 constexpr int prefix_smem = PrefixShape<HD, TILES>::BARRIERS + 1024 +
@@ -176,7 +176,8 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       mbar_init(smem_u32(&bars->p_full[t]), 4);
       mbar_init(smem_u32(&bars->pv_done[t]), 1);
     }
-    bars->abort_flag = 0;
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars->done[i]), 1);
+    bars->abort_flag = bars->last_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma_prefetch_desc(&map_q);
     tma_prefetch_desc(&map_k);
@@ -193,6 +194,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   tc_fence_after();
   const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(&bars->tmem_base);
   volatile int *abort_flag = &bars->abort_flag;
+  int loads = 0;  // by a loading thread
 
   if (warp == 0) {
     if (lane < 2) {
@@ -215,6 +217,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 #pragma unroll
         for (int c = 0; c < Shape::CH; ++c)
           tma_load_3d(ring + st * Shape::KV_BYTES + c * Shape::KV_CHUNK, map, full, c * 64, g, (t0 + j) * PT_K);
+        ++loads;
       }
     }
   } else if (warp == 1) {
@@ -421,6 +424,18 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
   }
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {  // a wait ran out: what this CTA has in flight ends before it leaves
+    if (threadIdx.x == 0) {
+      ring_landed(&bars->q_full, 1, 1, &bars->last_flag, status, W_PREFIX);
+      ring_landed(bars->k_full, STAGES, loads, &bars->last_flag, status, W_PREFIX);
+    } else if (threadIdx.x == 1) {
+      ring_landed(bars->v_full, STAGES, loads, &bars->last_flag, status, W_PREFIX);
+    } else if (lane == 0 && (warp == 1 || warp == 2)) {
+      umma_commit(smem_u32(&bars->done[warp - 1]));
+      mbar_wait(smem_u32(&bars->done[warp - 1]), 0, &bars->last_flag, status, W_PREFIX);
+    }
+    __syncthreads();
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)Shape::TMEM_COLS)

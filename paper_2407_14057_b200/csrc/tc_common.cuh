@@ -59,6 +59,14 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return true;
 }
 
+// For a CTA that gives up after a wait ran out: until the last loads that went into a ring of `stages` buffers have landed, `n` of
+// them in all (bounded).  `flag`: an abort flag of its own, zero.
+__device__ __forceinline__ void ring_landed(unsigned long long *full, int stages, int n, volatile int *flag, DevStatus *status,
+                                            int where) {
+  for (int i = n > stages ? n - stages : 0; i < n; ++i)
+    mbar_wait(smem_u32(&full[i % stages]), (uint32_t)((i / stages) & 1), flag, status, where);
+}
+
 __device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const CUtensorMap *map, uint32_t bar,
                                             int x, int y) {
   asm volatile(
