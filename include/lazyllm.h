@@ -459,8 +459,8 @@ int lazy_k_attention_prefix(void *stream, int32_t dtype, const void *q, int32_t 
                             size_t scratch_floats, void *o);
 /* Verification of drafted tokens.  Sequence s drafted draft[d_cu_draft[s] .. d_cu_draft[s+1]) (T_s <= max_draft tokens; n_draft in
  * all); row t of q (pitch ldq) holds the draft model's probabilities that draft t was drawn from, NULL if the
- * drafts were chosen outright (probability 1); rows d_cu_draft[s] + s + t, t = 0..T_s, of p (pitch ldp) the target's at draft t
- * and, for t = T_s, behind the last one.  Draft t is accepted iff u_accept[t] q(x) < p(x) and all before it were
+ * drafts were chosen outright (probability 1); rows d_cu_draft[s] + s + t, t = 0..T_s, of p (pitch ldp; n_draft + n_seqs < 2^31
+ * rows) the target's at draft t and, for t = T_s, behind the last one.  Draft t is accepted iff u_accept[t] q(x) < p(x) and all before it were
  * (u_accept fp32 [n_draft], u_sample fp32 [n_seqs], uniform in [0, 1)).  The token behind the accepted ones is the first id
  * whose running sum of w exceeds u_sample times their total, w = max(p - q, 0) after a rejection (p without the rejected id
  * if q is NULL; p if that leaves nothing), w = p behind the last draft: the sequence is then distributed as the target's.

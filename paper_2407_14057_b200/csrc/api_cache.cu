@@ -156,7 +156,7 @@ int lazy_k_verify(void *stream, const float *p, int32_t ldp, const float *q, int
                   const float *u_accept, const float *u_sample, int32_t *n_accept, int32_t *tokens) {
   if (n_seqs < 0 || n_draft < 0 || max_draft < 0 || max_draft == 0x7fffffff || vocab < 1 || ldp < vocab || (q && ldq < vocab))
     return LAZY_E_BADARG;
-  if (n_seqs > (1 << 24) || vocab > (1 << 30)) return LAZY_E_CAPACITY;
+  if (n_seqs > (1 << 24) || vocab > (1 << 30) || (long long)n_draft + n_seqs > 0x7fffffff) return LAZY_E_CAPACITY;
   if (n_seqs == 0) return LAZY_OK;
   if (!p || !d_cu_draft || !u_sample || !n_accept || !tokens || (n_draft > 0 && (!draft || !u_accept))) return LAZY_E_BADARG;
   DevStatus *status = dev_status_ptr();

@@ -154,3 +154,10 @@ def test_scratch_of_a_batch_that_shrinks(lib):
     f = lib.lazy_k_attention_prefix_scratch_floats
     sizes = [f(n, n, 1, 16384, 500, 32, 8, 128) for n in range(1, 200)]
     assert sizes == sorted(sizes) and sizes[-1] < 4 * sizes[63]
+
+
+def test_verify_refuses_more_rows_than_an_index_reaches(lib):
+    """p has n_draft + n_seqs rows."""
+    f = lib.lazy_k_verify
+    for n_draft, n_seqs in ((2 ** 31 - 1, 1), (2 ** 31 - 1, 1 << 24), (2 ** 31 - 5, 6)):
+        refuse(f, VERIFY, CAPACITY, n_draft=n_draft, n_seqs=n_seqs)
