@@ -238,3 +238,63 @@ def test_one_scratch_for_a_batch_that_shrinks(heads):
         got = B.lazy_k_attention_mass(q[:n], k[:n], cu(part), max(part), H, Hkv, dh, window, scratch=scratch)
         assert torch.equal(got, B.lazy_k_attention_mass(q[:n], k[:n], cu(part), max(part), H, Hkv, dh, window))
     B.lazy_device_status()
+
+
+# ------------------------------------------------------------------------------------------- wide groups, rows of nobody
+WIDE = [(24, 1, 64, BF16), (100, 1, 64, BF16), (160, 1, 32, BF16), (34, 2, 128, BF16), (20, 1, 64, F32), (130, 1, 32, F32)]
+
+
+@pytest.mark.parametrize("heads", WIDE, ids=[f"{h}on{k}x{d}{'' if t == BF16 else 'f32'}" for h, k, d, t in WIDE])
+def test_wide_groups(heads):
+    """More query heads to a key/value head than a block of columns, or than a tile of lanes, holds."""
+    H, Hkv, dh, dtype = heads
+    for lens, window in (([70, 1, 130], 0), ([200], 3)):
+        n = sum(lens)
+        q, k, dq, dk = mass_case(97, lens, H, Hkv, dh, dtype, fused=True)
+        got = B.lazy_k_attention_mass(dq, dk, cu(lens), max(lens), H, Hkv, dh, window)
+        qn, kn = f64(q).reshape(n, H, dh), f64(k).reshape(n, Hkv, dh)
+        want = R.attention_mass(qn, kn, lens, H, Hkv, dh, window)
+        assert np.all(np.abs(f64(got) - want) <= weight_error(qn, kn, dh) * want + 1e-30)
+    c, new = step_case(98, [90, 3, 0], 90, H, Hkv, dh, dtype)
+    check_step(c, new, H, 90, 10)
+    for n_pre, rows, own in ((130, [1, 3], [40, 3]), (0, [2, 1], [70, 1])):
+        d = prefix_case(99, n_pre, rows, own, H, Hkv, dh, dtype)
+        want, tol = prefix_expected(d, rows, own, H, Hkv, dh)
+        got = run_prefix(d, rows, own, H, Hkv, dh)
+        assert np.all(np.abs(f64(got).reshape(want.shape) - want) <= tol)
+    B.lazy_device_status()
+
+
+@pytest.mark.parametrize("heads", [HEADS[1], HEADS[6], HEADS[7]], ids=[IDS[1], IDS[6], IDS[7]])
+def test_rows_of_no_sequence(heads):
+    """Rows before the first sequence's and behind the last one's: no weight, no part in an eviction; behind a prefix they are
+    reported and see it alone."""
+    H, Hkv, dh, dtype = heads
+    lens, n = [40, 70], 120
+    q, k, dq, dk = mass_case(100, [n], H, Hkv, dh, dtype, fused=False)
+    dq[:3], dk[:3], dq[113:], dk[113:] = (float("nan"),) * 4
+    table = torch.tensor([3, 43, 113], dtype=torch.int32).cuda()
+    out = torch.full((Hkv, n), -7.0, device="cuda")
+    B.lazy_k_attention_mass(dq, dk, table, 70, H, Hkv, dh, out=out)
+    assert torch.all(out[:, :3] == -7) and torch.all(out[:, 113:] == -7)
+    qn, kn = f64(q).reshape(n, H, dh)[3:113], f64(k).reshape(n, Hkv, dh)[3:113]
+    want = R.attention_mass(qn, kn, lens, H, Hkv, dh, 0)
+    assert np.all(np.abs(f64(out)[:, 3:113] - want) <= weight_error(qn, kn, dh) * want)
+    cache = dict(kc=torch.zeros((2, 30, Hkv, dh), dtype=dtype, device="cuda"), vc=torch.zeros((2, 30, Hkv, dh), dtype=dtype, device="cuda"),
+                 cmass=torch.zeros((2, Hkv, 30), device="cuda"), cpos=torch.zeros((2, Hkv, 30), dtype=torch.int32, device="cuda"),
+                 clen=torch.zeros((2, Hkv), dtype=torch.int32, device="cuda"))
+    out[:, :3] = out[:, 113:] = float("inf")
+    B.lazy_k_evict(dk, dk, torch.arange(n, dtype=torch.int32).cuda(), out, table, 70, 30, 4, **cache)
+    B.lazy_device_status()
+    for s, a, ln in ((0, 3, 40), (1, 43, 70)):
+        for h in range(Hkv):
+            assert (cache["cpos"][s, h].cpu() - a).tolist() == R.kept_rows(out[h, a:a + ln].cpu().numpy(), ln, 30, 4)
+    rows, own, n_pre = [2, 3], [40, 90], 75
+    d = prefix_case(101, n_pre, [1] + rows + [2], [0] + own + [0], H, Hkv, dh, dtype)
+    want, tol = prefix_expected(d, [1] + rows + [1, 1], [0] + own + [0, 0], H, Hkv, dh)
+    dev = {name: t.cuda() for name, t in d.items()}
+    got = B.lazy_k_attention_prefix(dev["q"], torch.tensor([1, 3, 6], dtype=torch.int32).cuda(), 3, dev["k_pre"], dev["v_pre"], dev["k"],
+                                    dev["v"], dev["kv_idx"], cu(own), 90, H, Hkv, dh)
+    with pytest.raises(B.LazyError, match="BADARG"):
+        B.lazy_device_status()
+    assert np.all(np.abs(f64(got).reshape(want.shape) - want) <= tol)
