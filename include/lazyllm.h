@@ -410,7 +410,9 @@ int lazy_k_gather_rows(void *stream, const void *src, const int32_t *idx, void *
 /* Accumulated attention weight of prompts: mass[g][r] (fp32 [n_kv_heads, n_total]) = sum over the last `window` rows
  * i >= r of r's sequence (0 = all its rows) and over the query heads h of key/value head g of
  * softmax_r(q_i,h . k_r,g / sqrt(head_dim)), causal.  q rows of pitch ldq, k rows of pitch ldkv elements, packed sequences
- * of at most max_len rows (any number that no sequence exceeds).  Sums in fp32 in a fixed order (the same bits every call). */
+ * of at most max_len rows (any number that no sequence exceeds).  Sums in fp32 in a fixed order (the same bits every call).  Rows
+ * of no sequence keep what mass held.  A sequence is cut into tiles of 128 (row, head) pairs and of 128 keys in bf16 up to a width
+ * of 128, else of 32; more than 65535 of either by the bounds given are refused (LAZY_E_CAPACITY). */
 size_t lazy_k_attention_mass_scratch_floats(int32_t n_seqs, int32_t n_total, int32_t max_len, int32_t n_heads,
                                             int32_t n_kv_heads, int32_t window);
 int lazy_k_attention_mass(void *stream, int32_t dtype, const void *q, int32_t ldq, const void *k, int32_t ldkv,
@@ -447,7 +449,9 @@ int lazy_k_evict_step(void *stream, int32_t dtype, const void *q, int32_t ldq, c
  * token and its drafted successors) of n_rows in all, and its own keys kv_idx[cu_kv[s] .. cu_kv[s+1]) (at most max_kv),
  * rows of the buffers k / v (kv_rows rows of pitch ldkv) in the order of their positions, its new rows' own keys last.  Row i of
  * T sees all n_pre rows of k_pre / v_pre (pitch ld_pre; the slots of one bounded cache serve too) and its own keys j
- * <= C - T + i of C; a row that sees nothing gives zeros, and so does one that sees logits of -inf alone.  The prefix is read once for the batch.  A row index outside
+ * <= C - T + i of C; a row that sees nothing gives zeros, and so does one that sees logits of -inf alone.  In bf16 up to a width of 128 the
+ * prefix is read once for every 256 (row, head) pairs of a key/value head, else once for every row and head.  A row that belongs to
+ * no sequence, or to one whose tables do not fit, is reported and sees the prefix alone.  A row index outside
  * [0, kv_rows) is reported and that key skipped.  n_rows <= 65535.  o [n_rows, n_heads * head_dim]. */
 size_t lazy_k_attention_prefix_scratch_floats(int32_t n_rows, int32_t n_seqs, int32_t max_q, int32_t n_pre,
                                               int32_t max_kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);

@@ -1,14 +1,17 @@
 // Attention of a batch of requests that share one prefix.  Every query row sees the whole prefix and the first part of
 // its request's own key list (row i of T rows: keys j <= C - T + i of C), so the prefix part is one product of all
-// rows with the prefix's keys: it is computed for the batch together and read once, not once per request.
+// rows with the prefix's keys: in the tensor-core form it is computed for the batch together and read once for every 256 (row,
+// head) pairs of a key/value head (64 rows of a group of four), not once per request.  The general form (fp32, widths above 128,
+// groups above 128) reads it for every row and head.
 //
-// bf16, head width up to 128: three launches, one for a few requests without a prefix.  (1) The prefix on tcgen05: the
+// bf16, head width up to 128: three launches; one for a few requests without a prefix, two for more of them or for requests
+// without own keys.  (1) The prefix on tcgen05: the
 // batch's (row, head) pairs of one key/value head are the lanes of 128-lane tiles, the prefix's keys are cut into ranges, every
 // CTA leaves the partial softmax of its lanes over its range.  (2) The requests' own keys on the warp-level path of
 // rows_mma.cuh, launched as a dependent that does not wait for (1): a CTA of it fits beside one of (1).  (3) A merge of the
 // parts, one warp per (row, head).  64 requests of one row behind 16384 keys, 8 heads of 128 in groups of 4, 1 to 500 own keys
-// each: 47 us (139 MB; 33 us without own keys, 24 without the prefix); four requests of five rows behind 1000 keys, 32 heads:
-// 16.5 us (24 MB).
+// each: 47.8 us (139 MB; 33 us without own keys, 24 without the prefix); four requests of five rows behind 1000 keys, 32 heads:
+// 16.6 us (24 MB).
 #include "attn_split.cuh"
 #include "rows_mma.cuh"
 
@@ -113,9 +116,10 @@ int prefix_general(cudaStream_t st, const PrefixArgs &a, float *scratch, DevStat
 //   warp 2      issues O += P V (M128 N = head width, P from TMEM);
 //   warps 3..   softmax, one thread per lane; running maximum raised only when it grows by more than 2^8.
 // TMEM columns of a tile: S (64) | P high (32) | P low (32) | O (head width).  P enters as the sum of two bf16 numbers (see
-// WEIGHT_REST), so that the only rounding of an output that counts is its own; without the low part the 64 requests above would take 2.7 % less.  Two lane
-// tiles in one CTA share the K and V tiles in shared memory.  64 keys take a CTA 1.17 us with two tiles, 0.9 with one: the products
-// alone would take 0.8 and 0.4, the softmax threads' instructions about as much, and neither hides all of the other.
+// WEIGHT_REST), so that the only rounding of an output that counts is its own; without the low part the 64 requests above
+// would take 2.7 % less.  Two lane tiles in one CTA share the K and V tiles in shared memory.  64 keys take a CTA 1.17 us
+// with two tiles, 0.9 with one: the products alone would take 0.8 and 0.4, the softmax threads' instructions about as much,
+// and neither hides all of the other.
 constexpr int PT_Q = 128, PT_K = 64;
 constexpr float PT_RESCALE = 8.f;
 constexpr int PT_REGS = 120;  // of 352 threads, which leaves the registers of a CTA of the own keys (168 x 128)

@@ -164,7 +164,7 @@ __device__ __forceinline__ void attn_split_merge(const float *part_o, const floa
 // Key ranges per (row, head): enough CTAs for four on every SM, in whole tiles.
 inline int attn_split_count(long long rows_heads, int n_keys) {
   const long long tiles = cdiv(n_keys > 0 ? n_keys : 1, AS_TILE);
-  long long want = (4LL * 148 + rows_heads - 1) / (rows_heads > 0 ? rows_heads : 1);
+  long long want = (4LL * sm_count() + rows_heads - 1) / (rows_heads > 0 ? rows_heads : 1);
   if (want < 1) want = 1;
   if (want > tiles) want = tiles;
   const long long per = (tiles + want - 1) / want;
@@ -172,7 +172,7 @@ inline int attn_split_count(long long rows_heads, int n_keys) {
 }
 // The most ranges that any number of pairs up to rows_heads makes of up to n_keys, times the pairs.
 inline size_t attn_split_parts(long long rows_heads, int n_keys) {
-  const long long tiles = cdiv(n_keys > 0 ? n_keys : 1, AS_TILE), all = rows_heads * tiles, most = rows_heads + 4LL * 148 - 1;
+  const long long tiles = cdiv(n_keys > 0 ? n_keys : 1, AS_TILE), all = rows_heads * tiles, most = rows_heads + 4LL * sm_count() - 1;
   return (size_t)(rows_heads < 1 ? 0 : (all < most ? all : most));
 }
 // Keys per range when n_keys are cut into `splits` ranges of whole tiles.

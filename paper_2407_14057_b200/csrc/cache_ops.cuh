@@ -95,8 +95,8 @@ inline int co_launch(void (*kfn)(KArgs...), dim3 grid, dim3 block, size_t smem, 
 }
 
 // CTAs that run at once in clusters of `size` (1, 2, 4, 8 or 16), up to three to an SM: a cluster stays within a group of SMs, and
-// the groups are not multiples of it (as the occupancy calculator has it for 148 SMs).  A launch of more runs its last
-// clusters after the others.
+// the groups are not multiples of it (as the occupancy calculator has it for 148 SMs and a kernel that fits one, two or
+// three times on an SM).  An estimate for choosing a launch's shape: a launch of more runs its last clusters after the others.
 inline int co_cluster_ctas(int size, int per_sm) {
   constexpr int TABLE[3][3] = {{132, 284, 416}, {120, 264, 384}, {112, 224, 336}};
   if (size <= 2) return sm_count() * per_sm;

@@ -6,8 +6,8 @@
 // between them): a radix select over order-preserving keys held in shared memory (of few keys, a comparison of each with all)
 // finds the weight at the last kept rank, every warp counts the kept rows of its contiguous part, and after one scan over the warps the rows are listed
 // in row order without a barrier per chunk.  A CTA lists and then copies only its share of the slots.  The copy is what
-// is bound by memory: kept rows are read and written once.  A prompt of 3376 rows on 32 heads cut to 1024 slots: 14.4 us (34 MB,
-// 4.6 us of it the selection, 5.3 the copy); eight prompts of 1 to 16384 rows on 8 heads cut to 2048: 31 us (119 MB, 3.8 TB/s).
+// is bound by memory: kept rows are read and written once.  A prompt of 3376 rows on 32 heads cut to 1024 slots: 15.2 us (34 MB,
+// 4.6 us of it the selection, 5.3 the copy); eight prompts of 1 to 16384 rows on 8 heads cut to 2048: 31.5 us (119 MB, 3.8 TB/s).
 #include "cache_ops.cuh"
 
 namespace lazy {
@@ -129,9 +129,9 @@ evict_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long
     if (held)
       for (int i0 = threadIdx.x; i0 < old; i0 += ES_THREADS * ES_BATCH) {
         float w[ES_BATCH];
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < ES_BATCH; ++i) w[i] = i0 + i * ES_THREADS < old ? m[i0 + i * ES_THREADS] : 0.f;
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < ES_BATCH; ++i)
           if (i0 + i * ES_THREADS < old) keys[i0 + i * ES_THREADS] = co_weight_key(w[i]);
       }
@@ -186,7 +186,7 @@ evict_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long
     const int part = ((old + ES_WARPS - 1) / ES_WARPS + 31) / 32 * 32;
     const int begin = min(warp * part, old), end = min(begin + part, old);
     int n_above = 0, n_equal = 0;
-  #pragma unroll 4
+#pragma unroll 4
     for (int i = begin + lane; i < end; i += 32) {
       const uint32_t key = key_of(i);
       n_above += cut ? key > prefix : key >= prefix;
@@ -206,7 +206,7 @@ evict_kernel(const uint4 *__restrict__ k, const uint4 *__restrict__ v, long long
     const uint32_t below = (1u << lane) - 1u;
     if (!cut) {
       if (at < last && at + n_above > first) {
-  #pragma unroll 4
+#pragma unroll 4
         for (int i0 = begin; i0 < end; i0 += 32) {
           const int i = i0 + lane;
           const bool stays = i < end && key_of(i) >= prefix;

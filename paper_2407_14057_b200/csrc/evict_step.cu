@@ -167,7 +167,7 @@ int step_general(cudaStream_t st, const EvictStepArgs &a, float *scratch, DevSta
 // shared memory when its group comes up.  The parts' maxima, sums and outputs meet in distributed shared memory, and
 // every CTA adds the final weights of its own slots to their masses from the logits it kept (in shared memory, or in
 // the scratch when a part is too long).  32 sequences of up to 2048 slots, 8 heads of 128 in groups of 4: 45 us for 232 MB, 5.2
-// TB/s (the loop alone runs at the memory's rate); one sequence of 1024 slots, 32 heads: 10.7 us, the time of its steps one
+// TB/s (the loop alone runs at the memory's rate); one sequence of 1024 slots, 32 heads: 11.3 us, the time of its steps one
 // after the other: two rounds of loads, the choice, the exchange, the masses.
 constexpr int SF_WARPS = 4, SF_THREADS = SF_WARPS * 32, SF_STAGES = 2, SF_CTAS = 3;
 constexpr int SF_MAX_CLUSTER = 8, SF_LARGE_CLUSTER = 16;  // the second is beyond what every device has to offer: see step_cluster

@@ -6,9 +6,9 @@
 // What has to be read is one row of p (and one of q after a rejection) per sequence, wherever the scan ends; the
 // other rows are touched at the drafted ids only.  A cluster of CTAs shares the row: each sums its contiguous
 // part, the totals meet in distributed shared memory, and the one warp whose part holds the crossing reads its
-// few hundred values again (from L2).  Sums run in 64 bits, differences included: with 32 the running sum's rounding would move the crossing to a
-// neighbouring id about once in a few hundred draws at a vocabulary of 32000.  One request, 32000 ids: 6.2 us, the latency of
-// three rounds of loads and two scans; 128 requests of up to 7 drafts: 12.3 us (31 MB).
+// few hundred values again (from L2).  Sums run in 64 bits, differences included: with 32 the running sum's rounding would
+// move the crossing to a neighbouring id about once in a few hundred draws at a vocabulary of 32000.  One request, 32000
+// ids: 6.4 us, the latency of three rounds of loads and two scans; 128 requests of up to 7 drafts: 12.6 us (31 MB).
 #include "attn_common.cuh"
 #include "cache_ops.cuh"
 
@@ -51,8 +51,9 @@ struct VfRow {
     return j == zeroed ? 0.0 : fmax(vf_prob_f64(p[j]) - (q ? vf_prob_f64(q[j]) : 0.0), 0.0);
   }
   // Sum over ids first, first + stride, ... < end (four consecutive ones each with VEC).  What 32 bits lose of the
-  // differences is added up as well (2^-44 of the sum is left): without it a crossing would move to a neighbouring id now and
-  // then.  Subtracting in 64 bits throughout, with another conversion per id, takes 128 requests 12.5 us in a graph, 10.3 so.
+  // differences is added up as well (2^-44 of the sum is left): without it a crossing would move to a neighbouring id now
+  // and then.  Subtracting in 64 bits throughout, with another conversion per id, takes 128 requests 12.5 us with their rows
+  // in L2, 10.3 so.
   __device__ __forceinline__ double sum(int first, int end, int stride) const {
     if (wild) {
       double total = 0.0;
