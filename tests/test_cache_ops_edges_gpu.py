@@ -298,3 +298,25 @@ def test_rows_of_no_sequence(heads):
     with pytest.raises(B.LazyError, match="BADARG"):
         B.lazy_device_status()
     assert np.all(np.abs(f64(got).reshape(want.shape) - want) <= tol)
+
+
+# ------------------------------------------------------------------------------------------- in place or not, each for itself
+@pytest.mark.parametrize("heads", [HEADS[1], HEADS[7]], ids=[IDS[1], IDS[7]])
+@pytest.mark.parametrize("apart", [(), ("mass",), ("pos",), ("len",), ("mass", "pos"), ("mass", "len"), ("pos", "len")])
+def test_evict_step_some_state_in_place(heads, apart):
+    """Masses, positions and lengths go to arrays of their own or stay, independently of one another."""
+    H, Hkv, dh, dtype = heads
+    lens, budget = [90, 41, 0], 90
+    c, new = step_case(102, lens, budget, H, Hkv, dh, dtype)
+    both = [{k: v.cuda() for k, v in {**c, **new}.items()} for _ in range(2)]
+    want = B.lazy_k_evict_step(**both[0], n_heads=H, budget=budget, n_recent=5)
+    outs = {f"{x}_out": both[1]["c" + x].clone() for x in apart}
+    got = B.lazy_k_evict_step(**both[1], **outs, n_heads=H, budget=budget, n_recent=5)
+    B.lazy_device_status()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    as_bytes = lambda t: t.contiguous().view(torch.uint8)  # noqa: E731
+    for x in ("mass", "pos", "len"):
+        after = outs[f"{x}_out"] if x in apart else both[1]["c" + x]
+        assert torch.equal(as_bytes(after), as_bytes(both[0]["c" + x])), x
+        if x in apart:
+            assert torch.equal(as_bytes(both[1]["c" + x].cpu()), as_bytes(c["c" + x])), x
