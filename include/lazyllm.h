@@ -257,7 +257,8 @@ int lazy_device_status(void *stream);
 /* Where the latest non-OK device status taken by this process came from: *where = code of the wait or
  * check that failed (1..4 GEMM roles, 5 gather index, 6 Aux look-up, 7 token id, 8 selection, 9 decode
  * planning, 10 RoPE position, 11..13 attention roles, 14 split-wave counter wait, 15 wait self-test,
- * 16 eviction and bounded caches, 17 shared-prefix attention, 18 draft verification, 19 attention weight),
+ * 16 eviction and bounded caches, 17 shared-prefix attention, 18 draft verification, 19 attention weight,
+ * 20 paged caches, 21 log probabilities),
  * *a / *b two integers of context (CTA and parity for a wait, row and value for a check).  Any pointer
  * may be NULL.  Plumbing: no counterpart in the paper. */
 int lazy_status_detail(int32_t *where, int32_t *a, int32_t *b);
@@ -475,6 +476,71 @@ int lazy_k_attention_prefix(void *stream, int32_t dtype, const void *q, int32_t 
 int lazy_k_verify(void *stream, const float *p, int32_t ldp, const float *q, int32_t ldq, const int32_t *draft,
                   const int32_t *d_cu_draft, int32_t n_seqs, int32_t n_draft, int32_t max_draft, int32_t vocab,
                   const float *u_accept, const float *u_sample, int32_t *n_accept, int32_t *tokens);
+
+/* ---- paged caches -------------------------------------------------------------------------- */
+/* Steps for serving from caches that are handed out in pages: new rows rotated and written to the pages of their sequences, and
+ * attention of the new rows over them.  The paper has no counterpart (its caches are contiguous); rows carry
+ * their original positions, so a pruned prompt's kept rows are cached like any others.  The conventions of the section above
+ * hold here too (heads, 16-byte rows, scratch, infinities and NaN, outputs that do not overlap inputs except where stated).
+ *
+ * Slot t of a page p holds one token; key/value head g of it starts at k + p * page_stride + t * slot_stride + g * head_stride
+ * (elements; head_dim contiguous; v with the same strides): [page][slot][head] and [page][head][slot] alike.  Token j of
+ * sequence s lies in slot j % page_size of page table[s * ld_table + j / page_size].  len[s] counts the cached tokens of
+ * sequence s, the new rows of the call included.  The struct is host memory, read before the call returns. */
+typedef struct {
+  void *k, *v;                                    /* device, 16-byte aligned                               */
+  int64_t page_stride, slot_stride, head_stride;  /* elements, multiples of 16 bytes, not negative         */
+  int32_t n_pages, page_size;                     /* any page size                                         */
+  const int32_t *table;                           /* device int32 [n_seqs, table_pages], pitch ld_table; entries behind a
+                                                   * sequence's last page are not read                     */
+  int32_t table_pages, ld_table;
+  const int32_t *len;                             /* device int32 [n_seqs]                                 */
+} lazy_pages;
+/* Which rows are whose, for both calls below: sequence s has rows [cu_q[s], cu_q[s+1]) of the batch, its last tokens: row i
+ * of T is token len[s] - T + i.  cu_q NULL: one row per sequence (n_rows = n_seqs), none where len[s] is 0.  Rows of no sequence
+ * (behind the last one: a padded batch) and their outputs are left as they are.  A sequence whose tables do not fit
+ * (boundaries that do not ascend or leave the rows, len below its rows or above what its pages or max_kv allow) is reported and skipped,
+ * its outputs left as they are; a page outside [0, n_pages) is reported, and its slots are neither read nor
+ * written. */
+
+/* cos and sin of p * theta^(-2 i / head_dim), i < head_dim / 2, as pairs: table fp32 [max_pos, head_dim / 2, 2], angles in
+ * 64 bits.  The table that lazy_k_paged_append takes; one made otherwise (scaled positions) serves as well. */
+int lazy_k_rope_table(void *stream, float *table, int32_t max_pos, int32_t head_dim, float theta);
+/* New rows into a paged cache.  Every head of q and k is normalised, x * rsqrt(mean(x^2) + eps) * g, where g_q / g_k
+ * ([head_dim], of the rows' type) is not NULL, then rotated by its row's position pos[r] (pairs i, i + head_dim / 2; 0 <= pos <
+ * max_pos, else the row is reported and skipped); arithmetic in fp32, rounded once.  q goes to q_out (pitch ldq_out; may be q
+ * itself), k and v to their slot, and k to k_out as well (pitch ldk_out; may be k itself) unless that is NULL.  q rows of pitch
+ * ldq, k and v rows of pitch ldkv: parts of one fused projection's rows.  rope_table: 16-byte aligned, [max_pos, head_dim / 2, 2].
+ * Two rows must not share a slot. */
+int lazy_k_paged_append(void *stream, int32_t dtype, const void *q, int32_t ldq, const void *k, const void *v, int32_t ldkv,
+                        const int32_t *pos, const float *rope_table, int32_t max_pos, const void *g_q, const void *g_k,
+                        float eps, const int32_t *d_cu_q, int32_t n_rows, int32_t n_seqs, const lazy_pages *pages,
+                        int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, void *q_out, int32_t ldq_out, void *k_out,
+                        int32_t ldk_out);
+/* Attention over a paged cache: o [n_rows, n_heads * head_dim] = softmax(q k / sqrt(head_dim)) v, row i of T over the
+ * first len - T + i + 1 tokens of its sequence (one row: all of them).  At most max_q rows and max_kv tokens to a
+ * sequence (any numbers that none exceeds; they size the launch and the scratch).  A row whose pages are all outside the pool gives zeros.  n_rows
+ * and n_seqs <= 65535. */
+size_t lazy_k_attention_paged_scratch_floats(int32_t n_rows, int32_t n_seqs, int32_t max_q, int32_t max_kv, int32_t n_heads,
+                                             int32_t n_kv_heads, int32_t head_dim);
+int lazy_k_attention_paged(void *stream, int32_t dtype, const void *q, int32_t ldq, const int32_t *d_cu_q, int32_t n_rows,
+                           int32_t n_seqs, int32_t max_q, const lazy_pages *pages, int32_t max_kv, int32_t n_heads,
+                           int32_t n_kv_heads, int32_t head_dim, float *scratch, size_t scratch_floats, void *o);
+
+/* ---- log probabilities --------------------------------------------------------------------- */
+/* What a server answers with beside a token (no counterpart in the paper).  logits [n_rows, vocab] of type dtype, pitch ld, any alignment;
+ * per row r, with log p_j = x_j - log sum_i e^(x_i):
+ *   logprob[r] = log p of tokens[r];  entropy[r] = - sum_j p_j log p_j;  rank[r] = how many ids come before the token;
+ *   top_id / top_logprob [n_rows, n_top]: the ids that come first, and their log p.
+ * Ids come in the order of their logits, the larger first, of equal ones the lower id; NaN comes last.  Logits of -infinity
+ * have probability 0 (log p -infinity); a row with a NaN, with +infinity or with nothing above -infinity has NaN for its log
+ * p and entropy, as the formula.  A negative token stands for none: logprob 0, rank -1; one >= vocab is reported and taken as none;
+ * the rank of a NaN logit is -1.  logprob, entropy and rank may be NULL; tokens too, if logprob and rank are.  n_top <= LAZY_MAX_TOP
+ * and <= vocab.  fp32 inside. */
+#define LAZY_MAX_TOP 64
+int lazy_k_token_logprobs(void *stream, int32_t dtype, const void *logits, int64_t ld, const int32_t *tokens, int32_t n_rows,
+                          int32_t vocab, int32_t n_top, float *logprob, float *entropy, int32_t *rank, int32_t *top_id,
+                          float *top_logprob);
 
 #ifdef __cplusplus
 }

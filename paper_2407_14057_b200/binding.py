@@ -70,6 +70,12 @@ class lazy_kernel_times(C.Structure):
                 ("flops", C.c_double * LAZY_N_KERNEL_KINDS), ("bytes", C.c_double * LAZY_N_KERNEL_KINDS)]
 
 
+class lazy_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("table", C.c_void_p),
+                ("table_pages", C.c_int32), ("ld_table", C.c_int32), ("len", C.c_void_p)]
+
+
 # name -> (restype, argtypes); the list mirrors include/lazyllm.h
 _P, _I, _F, _U, _Z = C.c_void_p, C.c_int32, C.c_float, C.c_uint32, C.c_size_t
 _SIGNATURES = {
@@ -131,6 +137,12 @@ _SIGNATURES = {
     "lazy_k_attention_prefix": (_I, [_P, _I, _P, _I, _P, _I, _I, _I, _P, _P, _I, _I, _P, _P, _I, _I, _P, _P] +
                                 [_I] * 5 + [_P, _Z, _P]),
     "lazy_k_verify": (_I, [_P, _P, _I, _P, _I, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P]),
+    "lazy_k_rope_table": (_I, [_P, _P, _I, _I, _F]),
+    "lazy_k_paged_append": (_I, [_P, _I, _P, _I, _P, _P, _I, _P, _P, _I, _P, _P, _F, _P, _I, _I, C.POINTER(lazy_pages)] + [_I] * 3 +
+                            [_P, _I, _P, _I]),
+    "lazy_k_attention_paged_scratch_floats": (_Z, [_I] * 7),
+    "lazy_k_attention_paged": (_I, [_P, _I, _P, _I, _P, _I, _I, _I, C.POINTER(lazy_pages)] + [_I] * 4 + [_P, _Z, _P]),
+    "lazy_k_token_logprobs": (_I, [_P, _I, _P, C.c_int64, _P, _I, _I, _I, _P, _P, _P, _P, _P]),
     "lazy_status_detail": (_I, [C.POINTER(_I), C.POINTER(_I), C.POINTER(_I)]),
     "lazy_k_wait_selftest": (_I, [_P, _I, _U]),
 }
@@ -601,7 +613,8 @@ def _native():
         spec.loader.exec_module(m)
         L = lib()
         m.bind(*[C.cast(getattr(L, f), C.c_void_p).value for f in (
-            "lazy_k_attention_mass", "lazy_k_evict", "lazy_k_evict_step", "lazy_k_attention_prefix", "lazy_k_verify")])
+            "lazy_k_attention_mass", "lazy_k_evict", "lazy_k_evict_step", "lazy_k_attention_prefix", "lazy_k_verify",
+            "lazy_k_paged_append", "lazy_k_attention_paged", "lazy_k_token_logprobs")])
         _call = m
     return _call
 
@@ -717,4 +730,67 @@ def lazy_k_verify(p: torch.Tensor, draft: torch.Tensor, cu_draft: torch.Tensor, 
         out = (torch.empty(n_seqs, dtype=torch.int32, device=p.device),
                torch.empty((n_seqs, max_draft + 1), dtype=torch.int32, device=p.device))
     _check("lazy_k_verify", _native().verify(*_here(), p, q, draft, cu_draft, u_accept, u_sample, *out, max_draft))
+    return out
+
+
+# ------------------------------------------------------------------------------- paged caches, log probabilities
+# Pages are tensors k_pages, v_pages [n_pages, page_size, n_kv_heads, head_dim] of equal strides, any but the last: a pool that holds a
+# head's slots side by side is passed as its .transpose(1, 2).  page_table int32 [n_seqs, pages of the longest], kv_len int32
+# [n_seqs] with the new rows counted in, cu_q int32 [n_seqs + 1] or None for one row per sequence.
+def lazy_k_rope_table(max_pos: int, head_dim: int, theta: float, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """fp32 [max_pos, head_dim // 2, 2]: the cosines and sines that lazy_k_paged_append rotates by."""
+    if out is None:
+        out = torch.empty((max_pos, head_dim // 2, 2), dtype=torch.float32, device="cuda")
+    elif out.numel() != max_pos * head_dim or out.dtype != torch.float32:
+        raise ValueError("out: float32 [max_pos, head_dim // 2, 2] is wanted")
+    _check("lazy_k_rope_table", lib().lazy_k_rope_table(_stream(), _ptr(out), max_pos, head_dim, theta))
+    return out
+
+
+def lazy_k_paged_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, rope_table: torch.Tensor,
+                        k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, kv_len: torch.Tensor,
+                        cu_q: Optional[torch.Tensor] = None, g_q: Optional[torch.Tensor] = None,
+                        g_k: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None,
+                        k_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Writes rows k, v [n, n_kv_heads * head_dim] to their pages, k rotated, and returns the rotated q [n, n_heads * head_dim] (q_out; q
+    itself for in place).  k_out, if given, receives the rotated k as well.  Any row pitch (parts of a fused projection's rows)."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check("lazy_k_paged_append", _native().paged_append(*_here(), q, k, v, pos, rope_table, g_q, g_k, cu_q, k_pages, v_pages,
+                                                         page_table, kv_len, q_out, k_out, eps))
+    return q_out
+
+
+def lazy_k_attention_paged_scratch(n_rows: int, n_seqs: int, max_q: int, max_kv: int, n_heads: int, n_kv_heads: int,
+                                   head_dim: int) -> torch.Tensor:
+    """Scratch for the `scratch=` argument of lazy_k_attention_paged."""
+    return _scratch(lib().lazy_k_attention_paged_scratch_floats(n_rows, n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim),
+                    torch.float32)
+
+
+def lazy_k_attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                           kv_len: torch.Tensor, max_kv: int, cu_q: Optional[torch.Tensor] = None, max_q: int = 1,
+                           scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """o [n, n_heads * head_dim]; q [n, n_heads * head_dim], any row pitch: each sequence's newest tokens."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if scratch is None:
+        n_kv_heads, head_dim = k_pages.shape[2:]
+        scratch = lazy_k_attention_paged_scratch(q.shape[0], kv_len.numel(), max_q, max_kv, q.shape[1] // head_dim, n_kv_heads,
+                                                 head_dim)
+    _check("lazy_k_attention_paged", _native().attention_paged(*_here(), q, cu_q, k_pages, v_pages, page_table, kv_len, scratch,
+                                                               out, max_q, max_kv))
+    return out
+
+
+def lazy_k_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, n_top: int = 0,
+                          out: Optional[Tuple[torch.Tensor, ...]] = None):
+    """(logprob, entropy fp32 [n], rank int32 [n], top_id int32, top_logprob fp32 [n, n_top]); logits [n, vocab], bf16 or fp32, any row
+    pitch; tokens int32 [n], negative for none."""
+    if out is None:
+        n, dev = logits.shape[0], logits.device
+        out = (torch.empty(n, dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev),
+               torch.empty(n, dtype=torch.int32, device=dev), torch.empty((n, n_top), dtype=torch.int32, device=dev),
+               torch.empty((n, n_top), dtype=torch.float32, device=dev))
+    _check("lazy_k_token_logprobs", _native().token_logprobs(*_here(), logits, tokens, *out, n_top))
     return out

@@ -1,27 +1,11 @@
 // Entry points of the operators on bounded and shared caches: argument checks, then the launchers.
-#include "cache_ops.cuh"
+#include "api_checks.cuh"
 
 using namespace lazy;
 
 namespace {
 
-constexpr int MAX_GRID_YZ = 65535;
 constexpr long long MAX_KEYS = 0x7fffff00LL;  // that a row of the shared prefix's attention sees
-
-bool bad_dtype(int dtype) { return dtype != LAZY_BF16 && dtype != LAZY_F32; }
-
-// Head layout shared by the calls below; n_kv_heads = 0 stands for n_heads.
-int check_heads(int n_heads, int &n_kv_heads, int head_dim) {
-  if (n_kv_heads == 0) n_kv_heads = n_heads;
-  if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return LAZY_E_BADARG;
-  if (head_dim < 32 || head_dim > 256 || head_dim % 32) return LAZY_E_BADARG;
-  if (n_heads > MAX_GRID_YZ) return LAZY_E_CAPACITY;
-  return LAZY_OK;
-}
-
-bool bad_rows(const void *p, long long ld, long long width, int dtype) {
-  return !p || ld < width || !co_rows_ok(p, ld, dtype);
-}
 
 }  // namespace
 

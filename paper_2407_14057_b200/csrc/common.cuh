@@ -38,6 +38,8 @@ enum DevWhere {
   W_PREFIX = 17,
   W_VERIFY = 18,
   W_MASS = 19,
+  W_PAGED = 20,
+  W_LOGPROBS = 21,
 };
 
 __device__ __forceinline__ void dev_fail(DevStatus *st, int code, int where, int a = 0, int b = 0) {
@@ -379,6 +381,53 @@ int launch_attention_prefix(cudaStream_t st, int dtype, const PrefixArgs &a, flo
 int launch_verify(cudaStream_t st, const float *p, int ldp, const float *q, int ldq, const int32_t *draft,
                   const int32_t *cu_draft, int n_seqs, int n_draft, int max_draft, int vocab, const float *u_accept,
                   const float *u_sample, int32_t *n_accept, int32_t *tokens, DevStatus *status);
+// ---- paged caches (paged_append.cu, attention_paged.cu) and what a server answers with (token_logprobs.cu) ----
+struct PagedKV {  // strides in elements
+  void *k, *v;
+  long long page_stride, slot_stride, head_stride;
+  const int32_t *table, *len;
+  int n_pages, page_size, table_pages, ld_table;
+};
+struct AppendArgs {
+  const void *q, *k, *v;
+  int ldq, ldkv;
+  const int32_t *pos;
+  const float *rope_table;
+  int max_pos;
+  const void *g_q, *g_k;
+  float eps;
+  const int32_t *cu_q;
+  int n_rows, n_seqs;
+  PagedKV kv;
+  int max_len;  // most tokens that the table names
+  int n_heads, n_kv_heads, head_dim;
+  void *q_out, *k_out;
+  int ldq_out, ldk_out;
+};
+int launch_paged_append(cudaStream_t st, int dtype, const AppendArgs &a, DevStatus *status);
+struct PagedArgs {
+  const void *q;
+  int ldq;
+  const int32_t *cu_q;
+  int n_rows, n_seqs, max_q;
+  PagedKV kv;
+  int max_kv;  // no more than the table names
+  int n_heads, n_kv_heads, head_dim;
+  void *o;
+};
+size_t attention_paged_scratch_need(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim);
+size_t attention_paged_scratch_floats(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim);
+int launch_attention_paged(cudaStream_t st, int dtype, const PagedArgs &a, float *scratch, DevStatus *status);
+struct LogprobArgs {
+  const void *logits;
+  long long ld;
+  const int32_t *tokens;
+  int n_rows, vocab, n_top;
+  float *logprob, *entropy;
+  int32_t *rank, *top_id;
+  float *top_logprob;
+};
+int launch_token_logprobs(cudaStream_t st, int dtype, const LogprobArgs &a, DevStatus *status);
 int launch_argmax(cudaStream_t st, const float *logits, int32_t *out, int n_rows, int vocab);
 int launch_fill_i32(cudaStream_t st, int32_t *p, int32_t v, size_t n);
 int launch_iota_pos(cudaStream_t st, int32_t *pos, const int32_t *cu, int n_seqs, int n_total);

@@ -113,6 +113,9 @@ decltype(&lazy_k_evict) f_evict;
 decltype(&lazy_k_evict_step) f_step;
 decltype(&lazy_k_attention_prefix) f_prefix;
 decltype(&lazy_k_verify) f_verify;
+decltype(&lazy_k_paged_append) f_append;
+decltype(&lazy_k_attention_paged) f_paged;
+decltype(&lazy_k_token_logprobs) f_logprobs;
 
 // Caches [n_seqs, cap, n_kv_heads, head_dim].
 struct Cache {
@@ -124,6 +127,33 @@ struct Cache {
     n_seqs = t.size(0), cap = t.size(1), heads = t.size(2), dim = t.size(3);
     k = c.dense<void>("kc", type, t.numel());
     v = c.dense<void>("vc", type, t.numel());
+  }
+};
+
+// Pages [n_pages, page_size, n_kv_heads, head_dim] of k and v with equal strides, then the table and the lengths: four arguments.
+struct Pages : lazy_pages {
+  int64_t heads = 0, dim = 0, n_seqs = 0;
+  Pages(Call &c, at::ScalarType type) {
+    const at::Tensor &tk = c.tensor("k_pages"), &tv = c.tensor("v_pages");
+    if (tk.scalar_type() != type || tv.scalar_type() != type) fail("k_pages, v_pages", "the type of the rows is wanted");
+    if (tk.dim() != 4 || tk.sizes() != tv.sizes()) fail("k_pages, v_pages", "[n_pages, page_size, n_kv_heads, head_dim] is wanted");
+    if (tk.strides() != tv.strides() || (tk.numel() > 0 && tk.size(3) > 1 && tk.stride(3) != 1))
+      fail("k_pages, v_pages", "equal strides and contiguous heads are wanted");
+    heads = tk.size(2), dim = tk.size(3);
+    k = tk.data_ptr(), v = tv.data_ptr();
+    // a stride that is never used may be anything
+    page_stride = tk.size(0) > 1 ? tk.stride(0) : 0;
+    slot_stride = tk.size(1) > 1 ? tk.stride(1) : 0;
+    head_stride = tk.size(2) > 1 ? tk.stride(2) : 0;
+    n_pages = fits(tk.size(0), "k_pages"), page_size = fits(tk.size(1), "k_pages");
+    const at::Tensor &t = c.tensor("page_table");
+    if (t.scalar_type() != at::kInt || t.dim() != 2 || (t.numel() > 0 && t.size(1) > 1 && t.stride(1) != 1))
+      fail("page_table", "int32 [n_seqs, pages] with contiguous rows is wanted");
+    n_seqs = t.size(0);
+    table_pages = fits(t.size(1), "page_table");
+    ld_table = t.size(0) > 1 ? fits(t.stride(0), "page_table") : table_pages;
+    table = static_cast<int32_t *>(t.data_ptr());
+    len = c.dense<int32_t>("kv_len", at::kInt, n_seqs);
   }
 };
 
@@ -259,14 +289,105 @@ PyObject *verify(PyObject *, PyObject *const *args, Py_ssize_t n) try {
   return raised();
 }
 
-// bind(attention_mass, evict, evict_step, attention_prefix, verify): the entry points' addresses.
+// (device, stream, q, k, v, pos, rope_table, g_q or None, g_k or None, cu_q or None, k_pages, v_pages, page_table, kv_len, q_out,
+//  k_out or None, eps)
+PyObject *paged_append(PyObject *, PyObject *const *args, Py_ssize_t n) try {
+  Call c(args, n, 17);
+  const at::ScalarType type = type_of(args[2]);
+  if (!THPVariable_Check(args[10]) || THPVariable_Unpack(args[10]).dim() != 4)
+    fail("k_pages", "[n_pages, page_size, n_kv_heads, head_dim] is wanted");
+  const at::Tensor &kp = THPVariable_Unpack(args[10]), &tq = THPVariable_Unpack(args[2]);
+  const int64_t dh = kp.size(3), width = kp.size(2) * dh;
+  if (tq.dim() != 2 || dh < 1 || tq.size(1) % dh) fail("q", "[n, n_heads * head_dim] is wanted");
+  const int64_t wq = tq.size(1);
+  int64_t nq, nk, nv, n_out, n_table, n_seqs = 0;
+  int32_t ldq, ldk, ldv, ldo, ldko = 0;
+  const void *q = c.rows("q", type, wq, &nq, &ldq), *k = c.rows("k", type, width, &nk, &ldk), *v = c.rows("v", type, width, &nv, &ldv);
+  if (nk != nq || nv != nq || ldk != ldv) fail("k, v", "as many rows as q, of one pitch, are wanted");
+  const int32_t *pos = c.dense<int32_t>("pos", at::kInt, nq);
+  const float *rope = c.dense<float>("rope_table", at::kFloat, -1, &n_table);
+  if (dh < 1 || n_table % dh) fail("rope_table", "[max_pos, head_dim / 2, 2] is wanted");
+  const void *gq = c.none() ? nullptr : c.dense<void>("g_q", type, dh), *gk = c.none() ? nullptr : c.dense<void>("g_k", type, dh);
+  const int32_t *cu = nullptr;
+  const bool one_each = c.none();
+  if (!one_each) cu = c.dense<int32_t>("cu_q", at::kInt, -1, &n_seqs);
+  const Pages pages(c, type);
+  if (!one_each && n_seqs - 1 != pages.n_seqs) fail("cu_q", "a boundary more than sequences is wanted");
+  if (one_each && nq != pages.n_seqs) fail("q", "a row per sequence is wanted without cu_q");
+  void *q_out = c.rows("q_out", type, wq, &n_out, &ldo), *k_out = nullptr;
+  if (n_out != nq) fail("q_out", "as many rows as q are wanted");
+  if (!c.none()) {
+    k_out = c.rows("k_out", type, width, &n_out, &ldko);
+    if (n_out != nq) fail("k_out", "as many rows as k are wanted");
+  }
+  const double eps = PyFloat_AsDouble(args[c.next]);
+  if (eps == -1.0 && PyErr_Occurred()) throw Fail();
+  return PyLong_FromLong(f_append(c.stream, code_of(type), q, ldq, k, v, ldk, pos, rope, fits(n_table / dh, "rope_table"), gq, gk,
+                                  static_cast<float>(eps), cu, fits(nq, "q"), fits(pages.n_seqs, "page_table"), &pages,
+                                  fits(wq / dh, "q"), fits(pages.heads, "k_pages"), fits(dh, "k_pages"), q_out, ldo, k_out, ldko));
+} catch (...) {
+  return raised();
+}
+
+// (device, stream, q, cu_q or None, k_pages, v_pages, page_table, kv_len, scratch, out, max_q, max_kv)
+PyObject *attention_paged(PyObject *, PyObject *const *args, Py_ssize_t n) try {
+  Call c(args, n, 12);
+  const at::ScalarType type = type_of(args[2]);
+  const at::Tensor &tq = THPVariable_Unpack(args[2]);
+  if (tq.dim() != 2) fail("q", "[n, n_heads * head_dim] is wanted");
+  const int64_t wq = tq.size(1);
+  int64_t nq, n_seqs = 0, floats;
+  int32_t ldq;
+  const void *q = c.rows("q", type, wq, &nq, &ldq);
+  const int32_t *cu = nullptr;
+  const bool one_each = c.none();
+  if (!one_each) cu = c.dense<int32_t>("cu_q", at::kInt, -1, &n_seqs);
+  const Pages pages(c, type);
+  if (!one_each && n_seqs - 1 != pages.n_seqs) fail("cu_q", "a boundary more than sequences is wanted");
+  if (one_each && nq != pages.n_seqs) fail("q", "a row per sequence is wanted without cu_q");
+  if (pages.dim < 1 || wq % pages.dim) fail("q", "[n, n_heads * head_dim] is wanted");
+  float *scratch = c.dense<float>("scratch", at::kFloat, -1, &floats);
+  void *out = c.dense<void>("out", type, nq * wq);
+  const int32_t max_q = c.int32("max_q"), max_kv = c.int32("max_kv");
+  return PyLong_FromLong(f_paged(c.stream, code_of(type), q, ldq, cu, fits(nq, "q"), fits(pages.n_seqs, "page_table"), max_q, &pages,
+                                 max_kv, fits(wq / pages.dim, "q"), fits(pages.heads, "k_pages"), fits(pages.dim, "k_pages"), scratch,
+                                 floats, out));
+} catch (...) {
+  return raised();
+}
+
+// (device, stream, logits, tokens, logprob, entropy, rank, top_id, top_logprob, n_top)
+PyObject *token_logprobs(PyObject *, PyObject *const *args, Py_ssize_t n) try {
+  Call c(args, n, 10);
+  const at::ScalarType type = type_of(args[2]);
+  const at::Tensor &t = c.tensor("logits");
+  if (t.dim() != 2 || (t.numel() > 0 && t.size(1) > 1 && t.stride(1) != 1)) fail("logits", "[n, vocab] with contiguous rows is wanted");
+  const int64_t rows = t.size(0), vocab = t.size(1), ld = rows > 1 ? t.stride(0) : vocab;
+  if (ld < vocab) fail("logits", "rows overlap");
+  const int32_t *tokens = c.dense<int32_t>("tokens", at::kInt, rows);
+  float *logprob = c.dense<float>("logprob", at::kFloat, rows), *entropy = c.dense<float>("entropy", at::kFloat, rows);
+  int32_t *rank = c.dense<int32_t>("rank", at::kInt, rows);
+  const int64_t n_top = PyLong_AsLongLong(args[9]);
+  if (PyErr_Occurred()) throw Fail();
+  if (n_top < 0 || n_top > LAZY_MAX_TOP) fail("n_top", "0 to 64 are wanted");
+  int32_t *id = c.dense<int32_t>("top_id", at::kInt, rows * n_top);
+  float *top = c.dense<float>("top_logprob", at::kFloat, rows * n_top);
+  return PyLong_FromLong(f_logprobs(c.stream, code_of(type), t.data_ptr(), ld, tokens, fits(rows, "logits"), fits(vocab, "logits"),
+                                    static_cast<int32_t>(n_top), logprob, entropy, rank, id, top));
+} catch (...) {
+  return raised();
+}
+
+// bind(attention_mass, evict, evict_step, attention_prefix, verify, paged_append, attention_paged, token_logprobs): the entry points'
+// addresses.
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
-  void *f[5];
-  if (n != 5) {
-    PyErr_SetString(PyExc_TypeError, "five addresses are wanted");
+  constexpr int COUNT = 8;
+  void *f[COUNT];
+  if (n != COUNT) {
+    PyErr_SetString(PyExc_TypeError, "eight addresses are wanted");
     return nullptr;
   }
-  for (int i = 0; i < 5; ++i) {
+  for (int i = 0; i < COUNT; ++i) {
     f[i] = PyLong_AsVoidPtr(args[i]);
     if (!f[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an address is null");
@@ -278,6 +399,9 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
   f_step = reinterpret_cast<decltype(f_step)>(f[2]);
   f_prefix = reinterpret_cast<decltype(f_prefix)>(f[3]);
   f_verify = reinterpret_cast<decltype(f_verify)>(f[4]);
+  f_append = reinterpret_cast<decltype(f_append)>(f[5]);
+  f_paged = reinterpret_cast<decltype(f_paged)>(f[6]);
+  f_logprobs = reinterpret_cast<decltype(f_logprobs)>(f[7]);
   Py_RETURN_NONE;
 }
 
@@ -288,6 +412,9 @@ PyMethodDef methods[] = {
     {"evict_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(evict_step)), METH_FASTCALL, nullptr},
     {"attention_prefix", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attention_prefix)), METH_FASTCALL, nullptr},
     {"verify", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(verify)), METH_FASTCALL, nullptr},
+    {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(paged_append)), METH_FASTCALL, nullptr},
+    {"attention_paged", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attention_paged)), METH_FASTCALL, nullptr},
+    {"token_logprobs", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(token_logprobs)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "lazycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

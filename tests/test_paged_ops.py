@@ -1,0 +1,107 @@
+"""Refusals of the operators on paged caches and of the log probabilities: every check answers before the device is touched."""
+import ctypes as C
+import math
+import random
+
+import pytest
+
+from paper_2407_14057_b200 import binding, build
+
+BADARG, CAPACITY = -1, -3
+X = 1 << 30   # an aligned non-null address that no call below gets to use
+
+PAGES = dict(k=X, v=X, page_stride=2048, slot_stride=128, head_stride=64, n_pages=4, page_size=16, table=X, table_pages=3, ld_table=3,
+             len=X)
+APPEND = dict(stream=None, dtype=0, q=X, ldq=256, k=X, v=X, ldkv=128, pos=X, rope=X, max_pos=64, g_q=X, g_k=X, eps=1e-6, cu_q=X,
+              n_rows=2, n_seqs=1, pages=PAGES, H=4, Hkv=2, dh=64, q_out=X, ldq_out=256, k_out=X, ldk_out=128)
+PAGED = dict(stream=None, dtype=0, q=X, ldq=256, cu_q=X, n_rows=2, n_seqs=1, max_q=2, pages=PAGES, max_kv=40, H=4, Hkv=2, dh=64,
+             scratch=X, floats=1 << 24, o=X)
+LOGPROBS = dict(stream=None, dtype=0, logits=X, ld=100, tokens=X, n_rows=2, vocab=100, n_top=5, logprob=X, entropy=X, rank=X, top_id=X,
+                top_logprob=X)
+HEADS = [dict(H=0), dict(H=4, Hkv=3), dict(Hkv=-1), dict(dh=48), dict(dh=0), dict(dh=288), dict(dtype=2), dict(dtype=-1)]
+BAD_PAGES = [dict(k=None), dict(v=None), dict(table=None), dict(len=None), dict(k=X + 8), dict(v=X + 2), dict(page_stride=2047),
+             dict(slot_stride=4), dict(head_stride=1), dict(page_stride=-8), dict(slot_stride=-128), dict(head_stride=-64),
+             dict(n_pages=-1), dict(page_size=0), dict(page_size=-16), dict(table_pages=-1), dict(ld_table=2)]
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return binding.lib()
+
+
+def refuse(fn, base, want, **change):
+    args = dict(base, **change)
+    assert set(args) == set(base)
+    if isinstance(args.get("pages"), dict):
+        args["pages"] = C.byref(binding.lazy_pages(*args["pages"].values()))
+    assert fn(*args.values()) == want, change
+
+
+def test_rope_table_refuses(lib):
+    f = lib.lazy_k_rope_table
+    for args in [(None, 4, 64, 1e4), (X + 4, 4, 64, 1e4), (X, -1, 64, 1e4), (X, 4, 63, 1e4), (X, 4, 0, 1e4), (X, 4, 64, 0.0),
+                 (X, 4, 64, -1.0), (X, 4, 64, math.nan)]:
+        assert f(None, *args) == BADARG, args
+    assert f(None, X, 1 << 26, 128, 1e4) == CAPACITY
+    assert f(None, None, 0, 64, 1e4) == 0
+
+
+def test_append_refuses(lib):
+    f = lib.lazy_k_paged_append
+    pointers = [{k: None} for k in ("q", "k", "v", "pos", "rope", "q_out", "pages")]
+    for change in HEADS + pointers + [dict(q=X + 8), dict(k=X + 2), dict(v=X + 8), dict(q_out=X + 8), dict(k_out=X + 8), dict(g_q=X + 8),
+                                      dict(g_k=X + 4), dict(rope=X + 8), dict(ldq=255), dict(ldq=252), dict(ldkv=124), dict(ldkv=130),
+                                      dict(ldq_out=248), dict(ldk_out=120), dict(n_rows=-1), dict(n_seqs=-1), dict(n_seqs=0),
+                                      dict(max_pos=-1), dict(eps=-1.0), dict(eps=math.nan), dict(cu_q=None)]:
+        refuse(f, APPEND, BADARG, **change)
+    for change in BAD_PAGES:
+        refuse(f, APPEND, BADARG, pages=dict(PAGES, **change))
+    refuse(f, APPEND, CAPACITY, H=65536, Hkv=2)
+    refuse(f, APPEND, 0, n_rows=0, q=None, k=None, v=None, pages=None)
+
+
+def test_attention_paged_refuses(lib):
+    f = lib.lazy_k_attention_paged
+    pointers = [{k: None} for k in ("q", "scratch", "o", "pages")]
+    for change in HEADS + pointers + [dict(q=X + 8), dict(o=X + 8), dict(ldq=248), dict(ldq=257), dict(n_rows=-1), dict(n_seqs=-1),
+                                      dict(n_seqs=0), dict(max_q=0), dict(max_q=-1), dict(max_kv=-1), dict(cu_q=None)]:
+        refuse(f, PAGED, BADARG, **change)
+    for change in BAD_PAGES:
+        refuse(f, PAGED, BADARG, pages=dict(PAGES, **change))
+    refuse(f, PAGED, CAPACITY, floats=0)
+    refuse(f, PAGED, CAPACITY, n_rows=65536)
+    refuse(f, PAGED, CAPACITY, n_seqs=65536)
+    refuse(f, PAGED, 0, n_rows=0)
+    g = lib.lazy_k_attention_paged_scratch_floats
+    assert g(2, 1, 2, 40, 4, 3, 64) == 0 and g(-1, 1, 2, 40, 4, 2, 64) == 0 and g(2, 1, 2, -1, 4, 2, 64) == 0
+    assert g(2, 1, 2, 40, 4, 2, 64) > 0
+
+
+def test_logprobs_refuses(lib):
+    f = lib.lazy_k_token_logprobs
+    for change in [dict(logits=None), dict(tokens=None), dict(tokens=None, rank=None), dict(top_id=None), dict(top_logprob=None),
+                   dict(logits=X + 1), dict(dtype=1, logits=X + 2), dict(dtype=3), dict(ld=99), dict(vocab=0), dict(n_rows=-1),
+                   dict(n_top=-1), dict(n_top=65), dict(vocab=4), dict(ld=(1 << 30), vocab=-1)]:
+        refuse(f, LOGPROBS, BADARG, **change)
+    refuse(f, LOGPROBS, CAPACITY, ld=1 << 31, vocab=(1 << 30) + 1)
+    refuse(f, LOGPROBS, 0, n_rows=0, logits=None)
+
+
+def _sizes(rng, top):
+    return max(1, min(top, int(round(2 ** rng.uniform(0, math.log2(top))))))
+
+
+def test_scratch_for_the_largest_serves_every_smaller_call(lib):
+    """The size asked for a shape is at least that of every shape that is no larger in anything."""
+    rng = random.Random(5)
+    f = lib.lazy_k_attention_paged_scratch_floats
+    for _ in range(20000):
+        H, Hkv, dh = rng.choice([(32, 32, 128), (32, 8, 128), (8, 1, 128), (16, 4, 64), (12, 4, 128), (8, 2, 96), (4, 2, 256), (40, 1, 64),
+                                 (6, 2, 32), (150, 1, 32), (200, 200, 64)])
+        n_seqs, max_q, max_kv = _sizes(rng, 300), _sizes(rng, 20), _sizes(rng, 200000)
+        rows = rng.randint(1, n_seqs * max_q)
+        a = f(rows, n_seqs, max_q, max_kv, H, Hkv, dh)
+        s, t = rng.randint(1, n_seqs), rng.randint(1, max_q)
+        less = (rng.randint(1, min(rows, s * t)), s, t, rng.randint(1, max_kv), H, Hkv, dh)
+        assert f(*less) <= a, (rows, n_seqs, max_q, max_kv, less)
