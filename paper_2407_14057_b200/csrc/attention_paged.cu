@@ -2,6 +2,7 @@
 // sees the first len - T + i + 1 of its tokens.
 #include "attn_split.cuh"
 #include "paged.cuh"
+#include "rows_mma.cuh"
 
 namespace lazy {
 
@@ -77,18 +78,363 @@ int paged_general(cudaStream_t st, const PagedArgs &a, float *scratch, DevStatus
   return co_launch(paged_merge_kernel<T>, dim3(a.n_heads, a.n_rows), dim3(AS_THREADS), 0, st, 1, false, a, part_o, part_ml, splits);
 }
 
+// ---- bf16, head width up to 128: warp-level MMA over equal shares of the batch's keys -------------------------------------------
+// The work is cut into units of 64 keys of one (sequence, key/value head, tile of columns), a column being one (row, query head); units
+// lie in the order of sequences, heads, column tiles and keys, and every CTA takes an equal range of them, whatever the
+// lengths: it runs through the end of one pair, whole pairs, and the start of another.  A warp takes every fourth 16 keys.  What a CTA
+// has of a whole pair it writes to o; of a part, the maximum, sum and unnormalised output go to the scratch, the last part of a
+// range to place 1, an earlier one to place 0.  A second launch has a CTA per place 1 and adds the parts up in order.
+constexpr int PG_WARPS = 4, PG_THREADS = PG_WARPS * 32, PG_STAGES = 2, PG_CTAS = 3;
+constexpr int PG_UNIT = PG_WARPS * RM_KEYS;
+constexpr int PG_LEAST = 4;         // units that a CTA is worth starting for
+constexpr int PG_MERGE_THREADS = 512;
+
+// A part that other CTAs continue: as many of them as `more`.
+struct PgSplit {
+  int more, s, g, ct;
+};
+struct PgScratch {
+  PgSplit *split;    // [CTAs]
+  float *ml, *o;     // [CTAs][2][columns][2], [CTAs][2][columns][HD]
+};
+inline int pg_grid() { return sm_count() * PG_CTAS; }
+constexpr int PG_MAX_COLS = 16;
+// floats; the parts' order in memory is splits, maxima and sums, outputs (+ 4: they start on a 16-byte boundary)
+inline size_t pg_scratch_floats(int head_dim) { return (size_t)pg_grid() * (4 + 2 * PG_MAX_COLS * (2 + head_dim)) + 4; }
+inline PgScratch pg_scratch(float *scratch) {
+  PgScratch c;
+  c.split = reinterpret_cast<PgSplit *>(align_up((uintptr_t)scratch, 16));
+  c.ml = reinterpret_cast<float *>(c.split + pg_grid());
+  c.o = c.ml + (size_t)pg_grid() * 2 * PG_MAX_COLS * 2;
+  return c;
+}
+
+struct PgSeq {
+  int start, rows, len, tiles, cts;  // cts: column tiles
+  __device__ __forceinline__ long long units(int n_kv_heads) const { return (long long)tiles * cts * n_kv_heads; }
+};
+template <int COLS>
+__device__ __forceinline__ PgSeq pg_seq(const PagedArgs &a, int s, int group, bool report, DevStatus *status) {
+  PgSeq q;
+  if (!paged_seq(a.kv, a.cu_q, s, a.n_rows, a.max_q, a.max_kv, report, status, q.start, q.rows, q.len)) q.rows = 0;
+  q.tiles = q.rows ? (q.len + PG_UNIT - 1) / PG_UNIT : 0;
+  q.cts = (int)(((long long)q.rows * group + COLS - 1) / COLS);
+  return q;
+}
+
+template <int HD, int NT>
+struct PgShared {
+  float wm[PG_WARPS][NT * 8], wl[PG_WARPS][NT * 8];
+  long long scan[PG_WARPS];
+  long long total, base;  // units of the batch; of the sequences before `s`
+  int s;
+};
+
+template <int HD, int NT, bool WHOLE>
+__global__ void __launch_bounds__(PG_THREADS, PG_CTAS)
+paged_mma_kernel(const PagedArgs a, int group, PgScratch scratch, DevStatus *status) {
+  using Rows = RowsMma<HD, NT>;
+  constexpr int COLS = NT * 8;
+  extern __shared__ __align__(128) uint8_t paged_smem[];
+  __shared__ PgShared<HD, NT> sh;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x, Hkv = a.n_kv_heads;
+  // ---- this CTA's range of units
+  const int per = (a.n_seqs + PG_THREADS - 1) / PG_THREADS, s0 = threadIdx.x * per, s1 = min(s0 + per, a.n_seqs);
+  long long mine = 0;
+  for (int s = s0; s < s1; ++s) mine += pg_seq<COLS>(a, s, group, cta == 0, status).units(Hkv);
+  long long incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) sh.scan[warp] = incl;
+  __syncthreads();
+  long long total = 0;
+#pragma unroll
+  for (int w = 0; w < PG_WARPS; ++w) {
+    if (w < warp) incl += sh.scan[w];
+    total += sh.scan[w];
+  }
+  const int ctas = (int)min((long long)gridDim.x, (total + PG_LEAST - 1) / PG_LEAST);
+  if (cta >= ctas) {
+    if (threadIdx.x == 0) scratch.split[cta] = {0, 0, 0, 0};
+    return;
+  }
+  auto first_of = [&](int c) { return total * c / ctas; };
+  const long long u0 = first_of(cta), u1 = first_of(cta + 1);
+  if (incl - mine <= u0 && u0 < incl) {
+    long long base = incl - mine;
+    int s = s0;
+    while (s + 1 < s1) {
+      const long long n = pg_seq<COLS>(a, s, group, false, status).units(Hkv);
+      if (u0 < base + n) break;
+      base += n;
+      ++s;
+    }
+    sh.s = s;
+    sh.base = base;
+  }
+  __syncthreads();
+  int s = sh.s;
+  long long base = sh.base;
+  PgSeq seq = pg_seq<COLS>(a, s, group, false, status);
+  const uint32_t stages = smem_u32(paged_smem) + warp * PG_STAGES * Rows::STAGE;
+  PgSplit split = {0, 0, 0, 0};
+  for (long long u = u0; u < u1;) {
+    while (u >= base + seq.units(Hkv)) {
+      if (s + 1 >= a.n_seqs) return;  // the tables changed meanwhile
+      base += seq.units(Hkv);
+      seq = pg_seq<COLS>(a, ++s, group, false, status);
+    }
+    // ---- units [ta, tb) of pair (s, g, ct)
+    const int pair = (int)((u - base) / seq.tiles), g = pair / seq.cts, ct = pair - g * seq.cts;
+    const long long pair0 = base + (long long)pair * seq.tiles;
+    const int ta = (int)(u - pair0), tb = (int)min((long long)seq.tiles, u1 - pair0);
+    const int c0 = ct * COLS, cols = min(COLS, seq.rows * group - c0);
+    const int32_t *table = a.kv.table + (size_t)s * a.kv.ld_table;
+    const bf16 *kp = (const bf16 *)a.kv.k + (long long)g * a.kv.head_stride, *vp = (const bf16 *)a.kv.v + (long long)g * a.kv.head_stride;
+    // group i of this warp: keys [j0, j0 + 16); the page of its keys (WHOLE: one for all of them) is asked for a group ahead
+    auto first_key = [&](int i) { return ((ta + i) * PG_WARPS + warp) * RM_KEYS; };
+    auto ask = [&](int i) {
+      const int j = min(first_key(i) + (WHOLE ? 0 : lane & 15), seq.len - 1);
+      return ta + i < tb ? table[j / a.kv.page_size] : 0;
+    };
+    int next = ask(0);
+    uint32_t there[PG_STAGES];  // of the stages in flight: keys whose pages are in the pool
+    auto request = [&](int i, uint32_t &ok) {
+      const int j0 = first_key(i), page = next;
+      next = ask(i + 1);
+      ok = 0u;
+      if (ta + i < tb && j0 < seq.len) {
+        const bool in = (uint32_t)page < (uint32_t)a.kv.n_pages;
+        if (!in && (WHOLE ? lane == 0 : j0 + (lane & 15) < seq.len)) dev_fail(status, LAZY_E_BADARG, W_PAGED, s, page);
+        const int j = WHOLE ? j0 : min(j0 + (lane & 15), seq.len - 1), at = j % a.kv.page_size;
+        const long long off = (long long)page * a.kv.page_stride + (long long)at * a.kv.slot_stride;
+        const uint32_t pages = __ballot_sync(0xffffffffu, in);
+        ok = WHOLE ? (in ? 0xffffu : 0u) : pages & 0xffffu;
+        const int left = seq.len - j0;
+        rows_load<HD>(stages + (i % PG_STAGES) * Rows::STAGE, [&](int r, const bf16 *&kr, const bf16 *&vr) {
+          const long long o = WHOLE ? off + r * a.kv.slot_stride : __shfl_sync(0xffffffffu, off, r);
+          const bool there = (ok >> r & 1u) && r < left;
+          kr = kp + (there ? o : 0);
+          vr = vp + (there ? o : 0);
+          return there;
+        });
+      }
+      rm_cp_commit();
+    };
+    request(0, there[0]);
+    Rows rows;
+    int t_vis[NT][2];  // tokens that this lane's columns see
+    rows.init([&](int c) -> const bf16 * {
+      if (c >= cols) return nullptr;
+      const int t = (c0 + c) / group, h = c0 + c - t * group;
+      return (const bf16 *)a.q + (size_t)(seq.start + t) * a.ldq + (size_t)(g * group + h) * HD;
+    });
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        t_vis[t][i] = seq.len - seq.rows + min((c0 + t * 8 + (lane & 3) * 2 + i) / group, seq.rows - 1) + 1;
+    const int least = seq.len - seq.rows + 1;  // what every row sees
+#pragma unroll 1
+    for (int i = 0; ta + i < tb; i += PG_STAGES) {
+#pragma unroll
+      for (int b = 0; b < PG_STAGES; ++b) {  // stages by name: `there` stays in registers
+        if (ta + i + b >= tb) break;
+        request(i + b + PG_STAGES - 1, there[(b + PG_STAGES - 1) % PG_STAGES]);
+        rm_cp_wait<PG_STAGES - 1>();
+        __syncwarp();
+        const int j0 = first_key(i + b);
+        if (j0 < seq.len) {
+          int vis[NT][2];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) vis[t][0] = t_vis[t][0] - j0, vis[t][1] = t_vis[t][1] - j0;
+          const uint32_t stage = stages + b * Rows::STAGE;
+          auto no_logits = [](int, int, float, float) {};
+          if (j0 + RM_KEYS > least && seq.rows > 1) rows.template process<true>(stage, vis, there[b], no_logits);
+          else rows.template process<false>(stage, vis, there[b], no_logits);
+        }
+        __syncwarp();  // the stage may be requested again
+      }
+    }
+    rm_cp_wait<0>();
+    rows.finish();
+    // ---- the CTA's part: the warps' outputs against the common maximum, added in warp order
+    if (lane < 4) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          sh.wm[warp][t * 8 + lane * 2 + i] = rows.m[t][i];
+          sh.wl[warp][t * 8 + lane * 2 + i] = rows.l[t][i];
+        }
+    }
+    __syncthreads();  // also: no warp reads its stages any more
+    float *wo = reinterpret_cast<float *>(paged_smem);  // [warp][column][HD]
+    static_assert(PG_WARPS * COLS * HD * 4 <= PG_WARPS * PG_STAGES * Rows::STAGE, "the stages hold the outputs in the end");
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int c = t * 8 + (lane & 3) * 2 + i;
+        if (c >= cols) continue;
+        float mx = sh.wm[0][c];
+#pragma unroll
+        for (int w = 1; w < PG_WARPS; ++w) mx = fmaxf(mx, sh.wm[w][c]);
+        const float f = ex2_approx(rows.m[t][i] - (mx == -INFINITY ? 0.f : mx)) * WEIGHT_UNLIFT;
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          wo[(warp * COLS + c) * HD + k * 16 + (lane >> 2)] = rows.o[t][k][i] * f;
+          wo[(warp * COLS + c) * HD + k * 16 + 8 + (lane >> 2)] = rows.o[t][k][2 + i] * f;
+        }
+      }
+    __syncthreads();
+    const bool all = ta == 0 && tb == seq.tiles;
+    const size_t place = ((size_t)cta * 2 + (ta == 0)) * PG_MAX_COLS;
+    for (int e = threadIdx.x; e < cols * (HD / 8); e += PG_THREADS) {
+      const int c = e / (HD / 8), d = e % (HD / 8) * 8;
+      float m = -INFINITY, l = 0.f, x[8];
+#pragma unroll
+      for (int w = 0; w < PG_WARPS; ++w) m = fmaxf(m, sh.wm[w][c]);
+#pragma unroll
+      for (int w = 0; w < PG_WARPS; ++w) l += sh.wl[w][c] * ex2_approx(sh.wm[w][c] - (m == -INFINITY ? 0.f : m));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < PG_WARPS; ++w)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] += wo[(w * COLS + c) * HD + d + i];
+      if (all) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int t = (c0 + c) / group, h = c0 + c - t * group;
+        Vec16<bf16> y;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= inv;
+        y.pack(x);
+        y.store((bf16 *)a.o + ((size_t)(seq.start + t) * a.n_heads + g * group + h) * HD + d);
+      } else {
+        if (d == 0) *reinterpret_cast<float2 *>(scratch.ml + (place + c) * 2) = make_float2(m, l);
+        float4 *o = reinterpret_cast<float4 *>(scratch.o + (place + c) * HD + d);
+        o[0] = make_float4(x[0], x[1], x[2], x[3]);
+        o[1] = make_float4(x[4], x[5], x[6], x[7]);
+      }
+    }
+    if (ta == 0 && !all) {  // the range ends here: how many CTAs have the rest of the pair
+      int more = 1;
+      while (cta + 1 + more < ctas && first_of(cta + 1 + more) < pair0 + seq.tiles) ++more;
+      split = {more, s, g, ct};
+    }
+    u = pair0 + tb;
+    if (u < u1) __syncthreads();  // the stages and the maxima have been read
+  }
+  if (threadIdx.x == 0) scratch.split[cta] = split;
+}
+
+// Adds up the parts of the pair that CTA blockIdx.x began and did not finish.  A warp per column, several to one where there are few.
+template <int HD, int COLS>
+__global__ void __launch_bounds__(PG_MERGE_THREADS)
+paged_mma_merge_kernel(const PagedArgs a, int group, PgScratch scratch, DevStatus *status) {
+  constexpr int WARPS = PG_MERGE_THREADS / 32, WIDE = HD / 4, BATCH = 8;  // lanes 0..WIDE-1 hold four of a column's elements each
+  __shared__ float4 part[WARPS][32];
+  __shared__ float part_ml[WARPS][2];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const PgSplit p = scratch.split[cta];
+  if (p.more == 0) return;
+  const PgSeq seq = pg_seq<COLS>(a, p.s, group, false, status);
+  const int c0 = p.ct * COLS, cols = min(COLS, seq.rows * group - c0), n = p.more + 1;
+  int share = 1;  // warps to a column
+  while (share * 2 * cols <= WARPS) share *= 2;
+  const int c = warp / share, first = warp % share;
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto place = [&](int i) { return ((size_t)(cta + i) * 2 + (i == 0)) * PG_MAX_COLS + c; };
+  if (c < cols) {
+    for (int i0 = first; i0 < n; i0 += share * BATCH) {
+      float2 ml[BATCH];
+      float4 x[BATCH];
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b) {
+        const int i = i0 + b * share;
+        ml[b] = i < n ? *reinterpret_cast<const float2 *>(scratch.ml + place(i) * 2) : make_float2(-INFINITY, 0.f);
+        x[b] = i < n && lane < WIDE ? *reinterpret_cast<const float4 *>(scratch.o + place(i) * HD + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      float mx = m;
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b) mx = fmaxf(mx, ml[b].x);
+      const float ref = mx == -INFINITY ? 0.f : mx, f = ex2_approx(m - ref);
+      l *= f;
+      o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+      m = mx;
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b) {
+        const float w = ex2_approx(ml[b].x - ref);
+        l = fmaf(ml[b].y, w, l);
+        o = make_float4(fmaf(x[b].x, w, o.x), fmaf(x[b].y, w, o.y), fmaf(x[b].z, w, o.z), fmaf(x[b].w, w, o.w));
+      }
+    }
+  }
+  part[warp][lane] = o;
+  if (lane == 0) part_ml[warp][0] = m, part_ml[warp][1] = l;
+  __syncthreads();
+  if (c >= cols || first != 0 || lane >= WIDE) return;
+  for (int w = 0; w < share; ++w) m = fmaxf(m, part_ml[warp + w][0]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  l = 0.f;
+  o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int w = 0; w < share; ++w) {
+    const float f = ex2_approx(part_ml[warp + w][0] - ref);
+    const float4 x = part[warp + w][lane];
+    l = fmaf(part_ml[warp + w][1], f, l);
+    o = make_float4(fmaf(x.x, f, o.x), fmaf(x.y, f, o.y), fmaf(x.z, f, o.z), fmaf(x.w, f, o.w));
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int t = (c0 + c) / group, h = c0 + c - t * group;
+  *reinterpret_cast<uint2 *>((bf16 *)a.o + ((size_t)(seq.start + t) * a.n_heads + p.g * group + h) * HD + lane * 4) =
+      make_uint2(bf16x2_pack(o.x * inv, o.y * inv), bf16x2_pack(o.z * inv, o.w * inv));
+}
+
+template <int HD, int NT, bool WHOLE>
+int paged_mma_launch(cudaStream_t st, const PagedArgs &a, float *scratch, DevStatus *status) {
+  constexpr int SMEM = PG_WARPS * PG_STAGES * RowsMma<HD, NT>::STAGE;
+  const int group = a.n_heads / a.n_kv_heads;
+  const PgScratch c = pg_scratch(scratch);
+  LAZY_TRY((co_allow_smem<paged_mma_kernel<HD, NT, WHOLE>>(SMEM)));
+  LAZY_TRY(co_launch(paged_mma_kernel<HD, NT, WHOLE>, dim3(pg_grid()), dim3(PG_THREADS), SMEM, st, 1, false, a, group, c, status));
+  return co_launch(paged_mma_merge_kernel<HD, NT * 8>, dim3(pg_grid()), dim3(PG_MERGE_THREADS), 0, st, 1, true, a, group, c, status);
+}
+
+bool paged_mma_eligible(int dtype, int head_dim) { return dtype == LAZY_BF16 && head_dim <= 128; }
+
 }  // namespace
 
-size_t attention_paged_scratch_need(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
+// What the call needs, or (`any`) as much as any smaller one does.
+static size_t paged_scratch_floats(int n_rows, int max_kv, int n_heads, int head_dim, bool any) {
   const long long rh = (long long)n_rows * n_heads;
-  return (size_t)rh * attn_split_count(rh, max_kv) * (head_dim + 2);
+  const size_t parts = any ? attn_split_parts(rh, max_kv) : (size_t)rh * attn_split_count(rh, max_kv);
+  const size_t general = parts * (head_dim + 2), mma = head_dim <= 128 ? pg_scratch_floats(head_dim) : 0;
+  return general > mma ? general : mma;
 }
-size_t attention_paged_scratch_floats(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
-  return attn_split_parts((long long)n_rows * n_heads, max_kv) * (head_dim + 2);
+size_t attention_paged_scratch_need(int n_rows, int max_kv, int n_heads, int head_dim) {
+  return paged_scratch_floats(n_rows, max_kv, n_heads, head_dim, false);
+}
+size_t attention_paged_scratch_floats(int n_rows, int max_kv, int n_heads, int head_dim) {
+  return paged_scratch_floats(n_rows, max_kv, n_heads, head_dim, true);
 }
 
 int launch_attention_paged(cudaStream_t st, int dtype, const PagedArgs &a, float *scratch, DevStatus *status) {
   if (a.n_rows == 0) return LAZY_OK;
+  if (paged_mma_eligible(dtype, a.head_dim)) {
+    const bool narrow = (long long)a.max_q * (a.n_heads / a.n_kv_heads) <= 8, whole = a.kv.page_size % RM_KEYS == 0;
+    return co_head_dim(a.head_dim, [&](auto hd) {
+      constexpr int HD = hd.value;
+      if (whole) return narrow ? paged_mma_launch<HD, 1, true>(st, a, scratch, status) : paged_mma_launch<HD, 2, true>(st, a, scratch, status);
+      return narrow ? paged_mma_launch<HD, 1, false>(st, a, scratch, status) : paged_mma_launch<HD, 2, false>(st, a, scratch, status);
+    });
+  }
   return dtype == LAZY_F32 ? paged_general<float>(st, a, scratch, status) : paged_general<bf16>(st, a, scratch, status);
 }
 
