@@ -492,7 +492,7 @@ typedef struct {
   int64_t page_stride, slot_stride, head_stride;  /* elements, multiples of 16 bytes, not negative         */
   int32_t n_pages, page_size;                     /* any page size                                         */
   const int32_t *table;                           /* device int32 [n_seqs, table_pages], pitch ld_table; entries behind a
-                                                   * sequence's last page are not read                     */
+                                                   * sequence's last page may be anything                  */
   int32_t table_pages, ld_table;
   const int32_t *len;                             /* device int32 [n_seqs]                                 */
 } lazy_pages;

@@ -88,6 +88,10 @@ constexpr int PG_WARPS = 4, PG_THREADS = PG_WARPS * 32, PG_STAGES = 2, PG_CTAS =
 constexpr int PG_UNIT = PG_WARPS * RM_KEYS;
 constexpr int PG_LEAST = 4;         // units that a CTA is worth starting for
 constexpr int PG_MERGE_THREADS = 512;
+// Where all pairs run at once in clusters of up to eight CTAs, and a CTA has few units of its pair, a cluster holds a pair, every CTA
+// every eighth unit of it, and the parts meet in distributed shared memory: one launch, and the first pages are asked for with the length.
+constexpr int PG_MAX_CLUSTER = 8;
+constexpr int PG_JOIN_UNITS = 16;
 
 // A part that other CTAs continue: as many of them as `more`.
 struct PgSplit {
@@ -124,90 +128,117 @@ __device__ __forceinline__ PgSeq pg_seq(const PagedArgs &a, int s, int group, bo
 
 template <int HD, int NT>
 struct PgShared {
+  float m[NT * 8], l[NT * 8];  // the CTA's part, read by the cluster
   float wm[PG_WARPS][NT * 8], wl[PG_WARPS][NT * 8];
   long long scan[PG_WARPS];
-  long long total, base;  // units of the batch; of the sequences before `s`
+  long long base;  // units of the sequences before `s`
   int s;
 };
 
-template <int HD, int NT, bool WHOLE>
+// JOIN: a cluster per pair, see above.
+template <int HD, int NT, bool WHOLE, bool JOIN>
 __global__ void __launch_bounds__(PG_THREADS, PG_CTAS)
-paged_mma_kernel(const PagedArgs a, int group, PgScratch scratch, DevStatus *status) {
+paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, DevStatus *status) {
   using Rows = RowsMma<HD, NT>;
   constexpr int COLS = NT * 8;
   extern __shared__ __align__(128) uint8_t paged_smem[];
   __shared__ PgShared<HD, NT> sh;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x, Hkv = a.n_kv_heads;
-  // ---- this CTA's range of units
-  const int per = (a.n_seqs + PG_THREADS - 1) / PG_THREADS, s0 = threadIdx.x * per, s1 = min(s0 + per, a.n_seqs);
-  long long mine = 0;
-  for (int s = s0; s < s1; ++s) mine += pg_seq<COLS>(a, s, group, cta == 0, status).units(Hkv);
-  long long incl = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long up = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += up;
-  }
-  if (lane == 31) sh.scan[warp] = incl;
-  __syncthreads();
-  long long total = 0;
-#pragma unroll
-  for (int w = 0; w < PG_WARPS; ++w) {
-    if (w < warp) incl += sh.scan[w];
-    total += sh.scan[w];
-  }
-  const int ctas = (int)min((long long)gridDim.x, (total + PG_LEAST - 1) / PG_LEAST);
-  if (cta >= ctas) {
-    if (threadIdx.x == 0) scratch.split[cta] = {0, 0, 0, 0};
-    return;
-  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, Hkv = a.n_kv_heads;
+  const int csize = JOIN ? (int)co_cluster_size() : 1, rank = JOIN ? (int)co_cluster_rank() : 0, cta = blockIdx.x;
+  int s, g, ct, first, jump, early = 0;  // the pair, and this CTA's units of it: first, first + jump, ...
+  long long base = 0, total = 0, u0 = 0, u1 = 1;
+  int ctas = 1;
+  PgSeq seq;
+  auto page_of = [&](int s, int j) { return a.kv.table[(size_t)s * a.kv.ld_table + j / a.kv.page_size]; };
   auto first_of = [&](int c) { return total * c / ctas; };
-  const long long u0 = first_of(cta), u1 = first_of(cta + 1);
-  if (incl - mine <= u0 && u0 < incl) {
-    long long base = incl - mine;
-    int s = s0;
-    while (s + 1 < s1) {
-      const long long n = pg_seq<COLS>(a, s, group, false, status).units(Hkv);
-      if (u0 < base + n) break;
-      base += n;
-      ++s;
+  if (JOIN) {
+    int pair = blockIdx.x / csize;
+    ct = pair % max_cts;
+    pair /= max_cts;
+    s = pair / Hkv;
+    g = pair - s * Hkv;
+    first = rank;
+    jump = csize;
+    // asked for before the length is known: it may name a page that the sequence has not
+    early = page_of(s, min((first * PG_WARPS + warp) * RM_KEYS + (WHOLE ? 0 : lane & 15), a.max_kv - 1));
+    seq = pg_seq<COLS>(a, s, group, g == 0 && ct == 0 && rank == 0 && threadIdx.x == 0, status);
+    if (ct >= seq.cts) return;  // the whole cluster alike
+  } else {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // ---- this CTA's range of units
+    const int per = (a.n_seqs + PG_THREADS - 1) / PG_THREADS, s0 = threadIdx.x * per, s1 = min(s0 + per, a.n_seqs);
+    long long mine = 0;
+    for (int i = s0; i < s1; ++i) mine += pg_seq<COLS>(a, i, group, cta == 0, status).units(Hkv);
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
     }
-    sh.s = s;
-    sh.base = base;
+    if (lane == 31) sh.scan[warp] = incl;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < PG_WARPS; ++w) {
+      if (w < warp) incl += sh.scan[w];
+      total += sh.scan[w];
+    }
+    ctas = (int)min((long long)gridDim.x, (total + PG_LEAST - 1) / PG_LEAST);
+    if (cta >= ctas) {
+      if (threadIdx.x == 0) scratch.split[cta] = {0, 0, 0, 0};
+      return;
+    }
+    u0 = first_of(cta);
+    u1 = first_of(cta + 1);
+    if (incl - mine <= u0 && u0 < incl) {
+      long long at = incl - mine;
+      int i = s0;
+      while (i + 1 < s1) {
+        const long long n = pg_seq<COLS>(a, i, group, false, status).units(Hkv);
+        if (u0 < at + n) break;
+        at += n;
+        ++i;
+      }
+      sh.s = i;
+      sh.base = at;
+    }
+    __syncthreads();
+    s = sh.s;
+    base = sh.base;
+    seq = pg_seq<COLS>(a, s, group, false, status);
+    jump = 1;
   }
-  __syncthreads();
-  int s = sh.s;
-  long long base = sh.base;
-  PgSeq seq = pg_seq<COLS>(a, s, group, false, status);
   const uint32_t stages = smem_u32(paged_smem) + warp * PG_STAGES * Rows::STAGE;
   PgSplit split = {0, 0, 0, 0};
   for (long long u = u0; u < u1;) {
-    while (u >= base + seq.units(Hkv)) {
-      if (s + 1 >= a.n_seqs) return;  // the tables changed meanwhile
-      base += seq.units(Hkv);
-      seq = pg_seq<COLS>(a, ++s, group, false, status);
+    int count;           // units of this CTA
+    long long pair0 = 0;  // the pair's first unit
+    if (JOIN) {
+      count = first < seq.tiles ? (seq.tiles - first + jump - 1) / jump : 0;
+    } else {
+      while (u >= base + seq.units(Hkv)) {
+        if (s + 1 >= a.n_seqs) return;  // the tables changed meanwhile
+        base += seq.units(Hkv);
+        seq = pg_seq<COLS>(a, ++s, group, false, status);
+      }
+      const int pair = (int)((u - base) / seq.tiles);
+      g = pair / seq.cts;
+      ct = pair - g * seq.cts;
+      pair0 = base + (long long)pair * seq.tiles;
+      first = (int)(u - pair0);
+      count = (int)min((long long)seq.tiles, u1 - pair0) - first;
     }
-    // ---- units [ta, tb) of pair (s, g, ct)
-    const int pair = (int)((u - base) / seq.tiles), g = pair / seq.cts, ct = pair - g * seq.cts;
-    const long long pair0 = base + (long long)pair * seq.tiles;
-    const int ta = (int)(u - pair0), tb = (int)min((long long)seq.tiles, u1 - pair0);
     const int c0 = ct * COLS, cols = min(COLS, seq.rows * group - c0);
-    const int32_t *table = a.kv.table + (size_t)s * a.kv.ld_table;
     const bf16 *kp = (const bf16 *)a.kv.k + (long long)g * a.kv.head_stride, *vp = (const bf16 *)a.kv.v + (long long)g * a.kv.head_stride;
     // group i of this warp: keys [j0, j0 + 16); the page of its keys (WHOLE: one for all of them) is asked for a group ahead
-    auto first_key = [&](int i) { return ((ta + i) * PG_WARPS + warp) * RM_KEYS; };
-    auto ask = [&](int i) {
-      const int j = min(first_key(i) + (WHOLE ? 0 : lane & 15), seq.len - 1);
-      return ta + i < tb ? table[j / a.kv.page_size] : 0;
-    };
-    int next = ask(0);
+    auto first_key = [&](int i) { return ((first + i * jump) * PG_WARPS + warp) * RM_KEYS; };
+    auto ask = [&](int i) { return i < count ? page_of(s, min(first_key(i) + (WHOLE ? 0 : lane & 15), seq.len - 1)) : 0; };
+    int next = JOIN && WHOLE ? early : ask(0);  // an early page beyond the length is not looked at
     uint32_t there[PG_STAGES];  // of the stages in flight: keys whose pages are in the pool
     auto request = [&](int i, uint32_t &ok) {
       const int j0 = first_key(i), page = next;
       next = ask(i + 1);
       ok = 0u;
-      if (ta + i < tb && j0 < seq.len) {
+      if (i < count && j0 < seq.len) {
         const bool in = (uint32_t)page < (uint32_t)a.kv.n_pages;
         if (!in && (WHOLE ? lane == 0 : j0 + (lane & 15) < seq.len)) dev_fail(status, LAZY_E_BADARG, W_PAGED, s, page);
         const int j = WHOLE ? j0 : min(j0 + (lane & 15), seq.len - 1), at = j % a.kv.page_size;
@@ -240,10 +271,10 @@ paged_mma_kernel(const PagedArgs a, int group, PgScratch scratch, DevStatus *sta
         t_vis[t][i] = seq.len - seq.rows + min((c0 + t * 8 + (lane & 3) * 2 + i) / group, seq.rows - 1) + 1;
     const int least = seq.len - seq.rows + 1;  // what every row sees
 #pragma unroll 1
-    for (int i = 0; ta + i < tb; i += PG_STAGES) {
+    for (int i = 0; i < count; i += PG_STAGES) {
 #pragma unroll
       for (int b = 0; b < PG_STAGES; ++b) {  // stages by name: `there` stays in registers
-        if (ta + i + b >= tb) break;
+        if (i + b >= count) break;
         request(i + b + PG_STAGES - 1, there[(b + PG_STAGES - 1) % PG_STAGES]);
         rm_cp_wait<PG_STAGES - 1>();
         __syncwarp();
@@ -274,7 +305,8 @@ paged_mma_kernel(const PagedArgs a, int group, PgScratch scratch, DevStatus *sta
     }
     __syncthreads();  // also: no warp reads its stages any more
     float *wo = reinterpret_cast<float *>(paged_smem);  // [warp][column][HD]
-    static_assert(PG_WARPS * COLS * HD * 4 <= PG_WARPS * PG_STAGES * Rows::STAGE, "the stages hold the outputs in the end");
+    float *co = wo + PG_WARPS * COLS * HD;              // [column][HD]: the part, read by the cluster
+    static_assert((PG_WARPS + 1) * COLS * HD * 4 <= PG_WARPS * PG_STAGES * Rows::STAGE, "the stages hold the outputs in the end");
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -292,8 +324,12 @@ paged_mma_kernel(const PagedArgs a, int group, PgScratch scratch, DevStatus *sta
         }
       }
     __syncthreads();
-    const bool all = ta == 0 && tb == seq.tiles;
-    const size_t place = ((size_t)cta * 2 + (ta == 0)) * PG_MAX_COLS;
+    const bool all = !JOIN && first == 0 && count == seq.tiles;
+    const size_t place = JOIN ? 0 : ((size_t)cta * 2 + (first == 0)) * PG_MAX_COLS;
+    auto output = [&](int c, int d) {
+      const int t = (c0 + c) / group, h = c0 + c - t * group;
+      return (bf16 *)a.o + ((size_t)(seq.start + t) * a.n_heads + g * group + h) * HD + d;
+    };
     for (int e = threadIdx.x; e < cols * (HD / 8); e += PG_THREADS) {
       const int c = e / (HD / 8), d = e % (HD / 8) * 8;
       float m = -INFINITY, l = 0.f, x[8];
@@ -307,27 +343,60 @@ paged_mma_kernel(const PagedArgs a, int group, PgScratch scratch, DevStatus *sta
       for (int w = 0; w < PG_WARPS; ++w)
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] += wo[(w * COLS + c) * HD + d + i];
-      if (all) {
+      if (all || (JOIN && csize == 1)) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const int t = (c0 + c) / group, h = c0 + c - t * group;
         Vec16<bf16> y;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] *= inv;
         y.pack(x);
-        y.store((bf16 *)a.o + ((size_t)(seq.start + t) * a.n_heads + g * group + h) * HD + d);
+        y.store(output(c, d));
       } else {
-        if (d == 0) *reinterpret_cast<float2 *>(scratch.ml + (place + c) * 2) = make_float2(m, l);
-        float4 *o = reinterpret_cast<float4 *>(scratch.o + (place + c) * HD + d);
+        if (d == 0) {
+          if (JOIN) sh.m[c] = m, sh.l[c] = l;
+          else *reinterpret_cast<float2 *>(scratch.ml + (place + c) * 2) = make_float2(m, l);
+        }
+        float4 *o = reinterpret_cast<float4 *>(JOIN ? co + c * HD + d : scratch.o + (place + c) * HD + d);
         o[0] = make_float4(x[0], x[1], x[2], x[3]);
         o[1] = make_float4(x[4], x[5], x[6], x[7]);
       }
     }
-    if (ta == 0 && !all) {  // the range ends here: how many CTAs have the rest of the pair
+    if (JOIN) {
+      if (csize == 1) return;
+      co_cluster_sync();
+      // every CTA a share of the outputs, four elements to a thread; all reads of the others' memory are in flight together
+      for (int e = rank * PG_THREADS + threadIdx.x; e < cols * (HD / 4); e += csize * PG_THREADS) {
+        const int c = e / (HD / 4), d = e % (HD / 4) * 4;
+        float m[PG_MAX_CLUSTER], l[PG_MAX_CLUSTER];
+        float4 x[PG_MAX_CLUSTER];
+#pragma unroll
+        for (int r = 0; r < PG_MAX_CLUSTER; ++r) {
+          m[r] = r < csize ? *co_map_shared(&sh.m[c], r) : -INFINITY;
+          l[r] = r < csize ? *co_map_shared(&sh.l[c], r) : 0.f;
+          x[r] = r < csize ? *co_map_shared(reinterpret_cast<float4 *>(co + c * HD + d), r) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float most = -INFINITY, sum = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int r = 0; r < PG_MAX_CLUSTER; ++r) most = fmaxf(most, m[r]);
+#pragma unroll
+        for (int r = 0; r < PG_MAX_CLUSTER; ++r) {
+          const float f = ex2_approx(m[r] - (most == -INFINITY ? 0.f : most));
+          sum = fmaf(l[r], f, sum);
+          o = make_float4(fmaf(x[r].x, f, o.x), fmaf(x[r].y, f, o.y), fmaf(x[r].z, f, o.z), fmaf(x[r].w, f, o.w));
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        *reinterpret_cast<uint2 *>(output(c, d)) = make_uint2(bf16x2_pack(o.x * inv, o.y * inv), bf16x2_pack(o.z * inv, o.w * inv));
+      }
+      __syncwarp();
+      co_cluster_sync();  // nobody leaves while its part is being read
+      return;
+    }
+    if (first == 0 && !all) {  // the range ends here: how many CTAs have the rest of the pair
       int more = 1;
       while (cta + 1 + more < ctas && first_of(cta + 1 + more) < pair0 + seq.tiles) ++more;
       split = {more, s, g, ct};
     }
-    u = pair0 + tb;
+    u = pair0 + first + count;
     if (u < u1) __syncthreads();  // the stages and the maxima have been read
   }
   if (threadIdx.x == 0) scratch.split[cta] = split;
@@ -397,13 +466,26 @@ paged_mma_merge_kernel(const PagedArgs a, int group, PgScratch scratch, DevStatu
       make_uint2(bf16x2_pack(o.x * inv, o.y * inv), bf16x2_pack(o.z * inv, o.w * inv));
 }
 
+// CTAs of a cluster per pair, 0: equal shares of all keys.
+int paged_join(const PagedArgs &a, int max_cts) {
+  const long long pairs = (long long)a.n_seqs * a.n_kv_heads * max_cts;
+  int c = 1;
+  while (c < PG_MAX_CLUSTER && pairs * c * 2 <= co_cluster_ctas(c * 2, PG_CTAS) && a.max_kv > c * PG_UNIT) c *= 2;
+  return a.max_kv > 0 && pairs * c <= co_cluster_ctas(c, PG_CTAS) && a.max_kv <= c * PG_UNIT * PG_JOIN_UNITS ? c : 0;
+}
+
 template <int HD, int NT, bool WHOLE>
 int paged_mma_launch(cudaStream_t st, const PagedArgs &a, float *scratch, DevStatus *status) {
   constexpr int SMEM = PG_WARPS * PG_STAGES * RowsMma<HD, NT>::STAGE;
-  const int group = a.n_heads / a.n_kv_heads;
+  const int group = a.n_heads / a.n_kv_heads, max_cts = (int)(((long long)a.max_q * group + NT * 8 - 1) / (NT * 8));
   const PgScratch c = pg_scratch(scratch);
-  LAZY_TRY((co_allow_smem<paged_mma_kernel<HD, NT, WHOLE>>(SMEM)));
-  LAZY_TRY(co_launch(paged_mma_kernel<HD, NT, WHOLE>, dim3(pg_grid()), dim3(PG_THREADS), SMEM, st, 1, false, a, group, c, status));
+  if (const int join = paged_join(a, max_cts)) {
+    LAZY_TRY((co_allow_smem<paged_mma_kernel<HD, NT, WHOLE, true>>(SMEM)));
+    return co_launch(paged_mma_kernel<HD, NT, WHOLE, true>, dim3((unsigned)(a.n_seqs * a.n_kv_heads * max_cts * join)), dim3(PG_THREADS), SMEM,
+                     st, join, false, a, group, max_cts, c, status);
+  }
+  LAZY_TRY((co_allow_smem<paged_mma_kernel<HD, NT, WHOLE, false>>(SMEM)));
+  LAZY_TRY(co_launch(paged_mma_kernel<HD, NT, WHOLE, false>, dim3(pg_grid()), dim3(PG_THREADS), SMEM, st, 1, false, a, group, 0, c, status));
   return co_launch(paged_mma_merge_kernel<HD, NT * 8>, dim3(pg_grid()), dim3(PG_MERGE_THREADS), 0, st, 1, true, a, group, c, status);
 }
 
