@@ -8,6 +8,8 @@ namespace lazy {
 
 namespace {
 
+typedef unsigned long long u64;
+
 // ---- general form: every type and head width, on CUDA cores; partial softmaxes of split key ranges, then their merge ----------
 
 // Row r's sequence and how many tokens it sees (0: it belongs to none, or its tables do not fit).  By whole warps.
@@ -82,40 +84,54 @@ int paged_general(cudaStream_t st, const PagedArgs &a, float *scratch, DevStatus
 // The work is cut into units of 64 keys of one (sequence, key/value head, tile of columns), a column being one (row, query head); units
 // lie in the order of sequences, heads, column tiles and keys, and every CTA takes an equal range of them, whatever the
 // lengths: it runs through the end of one pair, whole pairs, and the start of another.  A warp takes every fourth 16 keys.  What a CTA
-// has of a whole pair it writes to o; of a part, the maximum, sum and unnormalised output go to the scratch, the last part of a
-// range to place 1, an earlier one to place 0.  A second launch has a CTA per place 1 and adds the parts up in order.
-constexpr int PG_WARPS = 4, PG_THREADS = PG_WARPS * 32, PG_STAGES = 2, PG_CTAS = 3;
-constexpr int PG_UNIT = PG_WARPS * RM_KEYS;
-constexpr int PG_LEAST = 4;         // units that a CTA is worth starting for
+// has of a whole pair it writes to o; of a part, the maximum, sum and unnormalised output go to the scratch, a
+// pair's first to place 1, a later one to place 0.  A second launch has a CTA per place 1 and adds the parts up in order.
+constexpr int PG_UNIT = 64;
+constexpr int PG_LEAST = 4;          // units that a CTA is worth starting for
+constexpr int PG_SWITCH = 2;         // units that go by while a CTA turns to another pair: they count at the pair's start
 constexpr int PG_MERGE_THREADS = 512;
-// Where all pairs run at once in clusters of up to eight CTAs, and a CTA has few units of its pair, a cluster holds a pair, every CTA
-// every eighth unit of it, and the parts meet in distributed shared memory: one launch, and the first pages are asked for with the length.
-constexpr int PG_MAX_CLUSTER = 8;
+// Where all pairs run at once in clusters of up to 16 CTAs, and a CTA has few units of its pair, a cluster holds a pair, its CTAs
+// taking turns at the units, and the parts meet in distributed shared memory: one launch, and the first pages are asked for with the
+// length.
+constexpr int PG_MAX_CLUSTER = 16;
 constexpr int PG_JOIN_UNITS = 16;
+// Warps of a CTA, groups of 16 keys that a warp has asked for or at hand, CTAs to an SM.  12 warps keep the memory busy; a warp by itself
+// takes a microsecond for 16 keys, whatever is at hand, so that a few large CTAs finish sooner than as many small ones.
+struct PgDepth {
+  int warps, stages, ctas;
+};
+constexpr PgDepth PG_WIDE = {4, 2, 3};
+constexpr PgDepth PG_DEEP = {8, 2, 1};
 
-// A part that other CTAs continue: as many of them as `more`.
-struct PgSplit {
-  int more, s, g, ct;
+// A part that other CTAs continue, as many of them as `more`, and where the pair's outputs are: columns [c0, c0 + cols) of key/value
+// head g for the rows from `start` on.
+struct __align__(16) PgSplit {
+  int more, start, g, c0, cols, unused[3];
 };
 struct PgScratch {
   PgSplit *split;    // [CTAs]
   float *ml, *o;     // [CTAs][2][columns][2], [CTAs][2][columns][HD]
 };
-inline int pg_grid() { return sm_count() * PG_CTAS; }
-constexpr int PG_MAX_COLS = 16;
+// Blocks of eight columns that a CTA takes, by the columns that a key/value head may have.  Four at a time read the keys of 32 columns
+// once instead of twice, but take the registers of a third CTA and spill: 16 sequences of 3000 tokens, 8 rows of 4 heads, 66 us with
+// four blocks, 69 with two; four sequences with drafts 25 and 20.
+inline int pg_blocks(long long columns) { return columns <= 8 ? 1 : 2; }
+inline int pg_grid() { return sm_count() * PG_WIDE.ctas; }
 // floats; the parts' order in memory is splits, maxima and sums, outputs (+ 4: they start on a 16-byte boundary)
-inline size_t pg_scratch_floats(int head_dim) { return (size_t)pg_grid() * (4 + 2 * PG_MAX_COLS * (2 + head_dim)) + 4; }
-inline PgScratch pg_scratch(float *scratch) {
+inline size_t pg_scratch_floats(int blocks, int head_dim) { return (size_t)pg_grid() * (8 + 16 * blocks * (2 + head_dim)) + 4; }
+inline PgScratch pg_scratch(float *scratch, int blocks) {
   PgScratch c;
   c.split = reinterpret_cast<PgSplit *>(align_up((uintptr_t)scratch, 16));
   c.ml = reinterpret_cast<float *>(c.split + pg_grid());
-  c.o = c.ml + (size_t)pg_grid() * 2 * PG_MAX_COLS * 2;
+  c.o = c.ml + (size_t)pg_grid() * 16 * blocks * 2;
   return c;
 }
 
 struct PgSeq {
   int start, rows, len, tiles, cts;  // cts: column tiles
-  __device__ __forceinline__ long long units(int n_kv_heads) const { return (long long)tiles * cts * n_kv_heads; }
+  // what a pair counts for in the CTAs' shares, and the sequence
+  __device__ __forceinline__ int share() const { return tiles + PG_SWITCH; }
+  __device__ __forceinline__ long long units(int n_kv_heads) const { return rows ? (long long)share() * cts * n_kv_heads : 0; }
 };
 template <int COLS>
 __device__ __forceinline__ PgSeq pg_seq(const PagedArgs &a, int s, int group, bool report, DevStatus *status) {
@@ -126,23 +142,23 @@ __device__ __forceinline__ PgSeq pg_seq(const PagedArgs &a, int s, int group, bo
   return q;
 }
 
-template <int HD, int NT>
+template <int HD, int NT, int WARPS>
 struct PgShared {
   float m[NT * 8], l[NT * 8];  // the CTA's part, read by the cluster
-  float wm[PG_WARPS][NT * 8], wl[PG_WARPS][NT * 8];
-  long long scan[PG_WARPS];
+  float wm[WARPS][NT * 8], wl[WARPS][NT * 8];
+  long long scan[WARPS];
   long long base;  // units of the sequences before `s`
   int s;
 };
 
-// JOIN: a cluster per pair, see above.
-template <int HD, int NT, bool WHOLE, bool JOIN>
-__global__ void __launch_bounds__(PG_THREADS, PG_CTAS)
+// JOIN: a cluster per pair, see above.  WHOLE: 16 keys from a multiple of 16 on lie in one page.
+template <int HD, int NT, bool WHOLE, bool JOIN, int WARPS, int STAGES, int CTAS>
+__global__ void __launch_bounds__(WARPS * 32, CTAS)
 paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, DevStatus *status) {
   using Rows = RowsMma<HD, NT>;
-  constexpr int COLS = NT * 8;
+  constexpr int COLS = NT * 8, THREADS = WARPS * 32, PER_UNIT = PG_UNIT / RM_KEYS;  // a unit is four groups of 16 keys
   extern __shared__ __align__(128) uint8_t paged_smem[];
-  __shared__ PgShared<HD, NT> sh;
+  __shared__ PgShared<HD, NT, WARPS> sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, Hkv = a.n_kv_heads;
   const int csize = JOIN ? (int)co_cluster_size() : 1, rank = JOIN ? (int)co_cluster_rank() : 0, cta = blockIdx.x;
   int s, g, ct, first, jump, early = 0;  // the pair, and this CTA's units of it: first, first + jump, ...
@@ -160,13 +176,15 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
     first = rank;
     jump = csize;
     // asked for before the length is known: it may name a page that the sequence has not
-    early = page_of(s, min((first * PG_WARPS + warp) * RM_KEYS + (WHOLE ? 0 : lane & 15), a.max_kv - 1));
+    first += warp / PER_UNIT * jump;  // four warps to a unit
+    jump *= WARPS / PER_UNIT;
+    early = page_of(s, min((first * PER_UNIT + warp % PER_UNIT) * RM_KEYS + (WHOLE ? 0 : lane & 15), a.max_kv - 1));
     seq = pg_seq<COLS>(a, s, group, g == 0 && ct == 0 && rank == 0 && threadIdx.x == 0, status);
     if (ct >= seq.cts) return;  // the whole cluster alike
   } else {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // ---- this CTA's range of units
-    const int per = (a.n_seqs + PG_THREADS - 1) / PG_THREADS, s0 = threadIdx.x * per, s1 = min(s0 + per, a.n_seqs);
+    const int per = (a.n_seqs + THREADS - 1) / THREADS, s0 = threadIdx.x * per, s1 = min(s0 + per, a.n_seqs);
     long long mine = 0;
     for (int i = s0; i < s1; ++i) mine += pg_seq<COLS>(a, i, group, cta == 0, status).units(Hkv);
     long long incl = mine;
@@ -178,13 +196,13 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
     if (lane == 31) sh.scan[warp] = incl;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < PG_WARPS; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
       if (w < warp) incl += sh.scan[w];
       total += sh.scan[w];
     }
     ctas = (int)min((long long)gridDim.x, (total + PG_LEAST - 1) / PG_LEAST);
     if (cta >= ctas) {
-      if (threadIdx.x == 0) scratch.split[cta] = {0, 0, 0, 0};
+      if (threadIdx.x == 0) scratch.split[cta].more = 0;
       return;
     }
     u0 = first_of(cta);
@@ -207,56 +225,68 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
     seq = pg_seq<COLS>(a, s, group, false, status);
     jump = 1;
   }
-  const uint32_t stages = smem_u32(paged_smem) + warp * PG_STAGES * Rows::STAGE;
-  PgSplit split = {0, 0, 0, 0};
-  for (long long u = u0; u < u1;) {
+  const uint32_t stages = smem_u32(paged_smem) + warp * STAGES * Rows::STAGE;
+  PgSplit split = {};
+  for (long long u = u0; u < u1; u = JOIN ? u1 : u) {
     int count;           // units of this CTA
     long long pair0 = 0;  // the pair's first unit
     if (JOIN) {
       count = first < seq.tiles ? (seq.tiles - first + jump - 1) / jump : 0;
     } else {
       while (u >= base + seq.units(Hkv)) {
-        if (s + 1 >= a.n_seqs) return;  // the tables changed meanwhile
+        if (s + 1 >= a.n_seqs) {  // the tables changed meanwhile
+          if (threadIdx.x == 0) scratch.split[cta].more = 0;
+          return;
+        }
         base += seq.units(Hkv);
         seq = pg_seq<COLS>(a, ++s, group, false, status);
       }
-      const int pair = (int)((u - base) / seq.tiles);
+      const int pair = (int)((u - base) / seq.share());
       g = pair / seq.cts;
       ct = pair - g * seq.cts;
-      pair0 = base + (long long)pair * seq.tiles;
-      first = (int)(u - pair0);
-      count = (int)min((long long)seq.tiles, u1 - pair0) - first;
+      pair0 = base + (long long)pair * seq.share();
+      first = max((int)(u - pair0) - PG_SWITCH, 0);
+      const int share_end = (int)min((long long)seq.share(), u1 - pair0);
+      u = pair0 + share_end;
+      count = share_end - PG_SWITCH - first;
+      if (count <= 0) continue;  // the range ends before the pair's keys
     }
     const int c0 = ct * COLS, cols = min(COLS, seq.rows * group - c0);
     const bf16 *kp = (const bf16 *)a.kv.k + (long long)g * a.kv.head_stride, *vp = (const bf16 *)a.kv.v + (long long)g * a.kv.head_stride;
     // group i of this warp: keys [j0, j0 + 16); the page of its keys (WHOLE: one for all of them) is asked for a group ahead
-    auto first_key = [&](int i) { return ((first + i * jump) * PG_WARPS + warp) * RM_KEYS; };
+    auto first_key = [&](int i) { return ((first + i * jump) * PER_UNIT + warp % PER_UNIT) * RM_KEYS; };
     auto ask = [&](int i) { return i < count ? page_of(s, min(first_key(i) + (WHOLE ? 0 : lane & 15), seq.len - 1)) : 0; };
     int next = JOIN && WHOLE ? early : ask(0);  // an early page beyond the length is not looked at
-    uint32_t there[PG_STAGES];  // of the stages in flight: keys whose pages are in the pool
-    auto request = [&](int i, uint32_t &ok) {
+    u64 there = 0;  // of the stages in flight, 16 bits each: keys whose pages are in the pool
+    int put = 0, take = 0;
+    auto request = [&](int i) {
       const int j0 = first_key(i), page = next;
       next = ask(i + 1);
-      ok = 0u;
       if (i < count && j0 < seq.len) {
         const bool in = (uint32_t)page < (uint32_t)a.kv.n_pages;
         if (!in && (WHOLE ? lane == 0 : j0 + (lane & 15) < seq.len)) dev_fail(status, LAZY_E_BADARG, W_PAGED, s, page);
-        const int j = WHOLE ? j0 : min(j0 + (lane & 15), seq.len - 1), at = j % a.kv.page_size;
+        const int j = WHOLE ? j0 : min(j0 + (lane & 15), seq.len - 1), at = j % a.kv.page_size, left = seq.len - j0;
         const long long off = (long long)page * a.kv.page_stride + (long long)at * a.kv.slot_stride;
-        const uint32_t pages = __ballot_sync(0xffffffffu, in);
-        ok = WHOLE ? (in ? 0xffffu : 0u) : pages & 0xffffu;
-        const int left = seq.len - j0;
-        rows_load<HD>(stages + (i % PG_STAGES) * Rows::STAGE, [&](int r, const bf16 *&kr, const bf16 *&vr) {
-          const long long o = WHOLE ? off + r * a.kv.slot_stride : __shfl_sync(0xffffffffu, off, r);
-          const bool there = (ok >> r & 1u) && r < left;
-          kr = kp + (there ? o : 0);
-          vr = vp + (there ? o : 0);
-          return there;
-        });
+        const uint32_t pages = __ballot_sync(0xffffffffu, in), ok = WHOLE ? (in ? 0xffffu : 0u) : pages & 0xffffu;
+        const uint32_t to = stages + put * Rows::STAGE;
+        if (WHOLE && in && left >= RM_KEYS) {
+          rows_load_run<HD>(to, kp + off, vp + off, a.kv.slot_stride);
+        } else {
+          rows_load<HD>(to, [&](int r, const bf16 *&kr, const bf16 *&vr) {
+            const long long o = WHOLE ? off + r * a.kv.slot_stride : __shfl_sync(0xffffffffu, off, r);
+            const bool there = (ok >> r & 1u) && r < left;
+            kr = kp + (there ? o : 0);
+            vr = vp + (there ? o : 0);
+            return there;
+          });
+        }
+        there = (there & ~(0xffffull << (16 * put))) | (u64)ok << (16 * put);
       }
+      put = put + 1 == STAGES ? 0 : put + 1;
       rm_cp_commit();
     };
-    request(0, there[0]);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) request(i);
     Rows rows;
     int t_vis[NT][2];  // tokens that this lane's columns see
     rows.init([&](int c) -> const bf16 * {
@@ -271,25 +301,25 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
         t_vis[t][i] = seq.len - seq.rows + min((c0 + t * 8 + (lane & 3) * 2 + i) / group, seq.rows - 1) + 1;
     const int least = seq.len - seq.rows + 1;  // what every row sees
 #pragma unroll 1
-    for (int i = 0; i < count; i += PG_STAGES) {
-#pragma unroll
-      for (int b = 0; b < PG_STAGES; ++b) {  // stages by name: `there` stays in registers
-        if (i + b >= count) break;
-        request(i + b + PG_STAGES - 1, there[(b + PG_STAGES - 1) % PG_STAGES]);
-        rm_cp_wait<PG_STAGES - 1>();
-        __syncwarp();
-        const int j0 = first_key(i + b);
-        if (j0 < seq.len) {
-          int vis[NT][2];
+    for (int i = 0; i < count; ++i) {
+      request(i + STAGES - 1);
+      rm_cp_wait<STAGES - 1>();
+      __syncwarp();
+      const int j0 = first_key(i);
+      if (j0 < seq.len) {
+        int vis[NT][2];
+        const uint32_t stage = stages + take * Rows::STAGE, ok = (uint32_t)(there >> (16 * take)) & 0xffffu;
+        if (j0 + RM_KEYS <= least && ok == 0xffffu) {
+          rows.template step<false, true>(stage, vis, ok);
+        } else {
 #pragma unroll
           for (int t = 0; t < NT; ++t) vis[t][0] = t_vis[t][0] - j0, vis[t][1] = t_vis[t][1] - j0;
-          const uint32_t stage = stages + b * Rows::STAGE;
-          auto no_logits = [](int, int, float, float) {};
-          if (j0 + RM_KEYS > least && seq.rows > 1) rows.template process<true>(stage, vis, there[b], no_logits);
-          else rows.template process<false>(stage, vis, there[b], no_logits);
+          if (j0 + RM_KEYS > least && seq.rows > 1) rows.template step<true, false>(stage, vis, ok);
+          else rows.template step<false, false>(stage, vis, ok);
         }
-        __syncwarp();  // the stage may be requested again
       }
+      take = take + 1 == STAGES ? 0 : take + 1;
+      __syncwarp();  // the stage may be requested again
     }
     rm_cp_wait<0>();
     rows.finish();
@@ -305,8 +335,8 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
     }
     __syncthreads();  // also: no warp reads its stages any more
     float *wo = reinterpret_cast<float *>(paged_smem);  // [warp][column][HD]
-    float *co = wo + PG_WARPS * COLS * HD;              // [column][HD]: the part, read by the cluster
-    static_assert((PG_WARPS + 1) * COLS * HD * 4 <= PG_WARPS * PG_STAGES * Rows::STAGE, "the stages hold the outputs in the end");
+    float *co = wo;                                     // [column][HD]: the part, read by the cluster; written where warp 0's was
+    static_assert(WARPS * COLS * HD * 4 <= WARPS * STAGES * Rows::STAGE, "the stages hold the outputs in the end");
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -315,7 +345,7 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
         if (c >= cols) continue;
         float mx = sh.wm[0][c];
 #pragma unroll
-        for (int w = 1; w < PG_WARPS; ++w) mx = fmaxf(mx, sh.wm[w][c]);
+        for (int w = 1; w < WARPS; ++w) mx = fmaxf(mx, sh.wm[w][c]);
         const float f = ex2_approx(rows.m[t][i] - (mx == -INFINITY ? 0.f : mx)) * WEIGHT_UNLIFT;
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k) {
@@ -325,22 +355,22 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
       }
     __syncthreads();
     const bool all = !JOIN && first == 0 && count == seq.tiles;
-    const size_t place = JOIN ? 0 : ((size_t)cta * 2 + (first == 0)) * PG_MAX_COLS;
+    const size_t place = JOIN ? 0 : ((size_t)cta * 2 + (first == 0)) * COLS;
     auto output = [&](int c, int d) {
       const int t = (c0 + c) / group, h = c0 + c - t * group;
       return (bf16 *)a.o + ((size_t)(seq.start + t) * a.n_heads + g * group + h) * HD + d;
     };
-    for (int e = threadIdx.x; e < cols * (HD / 8); e += PG_THREADS) {
+    for (int e = threadIdx.x; e < cols * (HD / 8); e += THREADS) {
       const int c = e / (HD / 8), d = e % (HD / 8) * 8;
       float m = -INFINITY, l = 0.f, x[8];
 #pragma unroll
-      for (int w = 0; w < PG_WARPS; ++w) m = fmaxf(m, sh.wm[w][c]);
+      for (int w = 0; w < WARPS; ++w) m = fmaxf(m, sh.wm[w][c]);
 #pragma unroll
-      for (int w = 0; w < PG_WARPS; ++w) l += sh.wl[w][c] * ex2_approx(sh.wm[w][c] - (m == -INFINITY ? 0.f : m));
+      for (int w = 0; w < WARPS; ++w) l += sh.wl[w][c] * ex2_approx(sh.wm[w][c] - (m == -INFINITY ? 0.f : m));
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = 0.f;
 #pragma unroll
-      for (int w = 0; w < PG_WARPS; ++w)
+      for (int w = 0; w < WARPS; ++w)
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] += wo[(w * COLS + c) * HD + d + i];
       if (all || (JOIN && csize == 1)) {
@@ -364,25 +394,33 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
       if (csize == 1) return;
       co_cluster_sync();
       // every CTA a share of the outputs, four elements to a thread; all reads of the others' memory are in flight together
-      for (int e = rank * PG_THREADS + threadIdx.x; e < cols * (HD / 4); e += csize * PG_THREADS) {
+      for (int e = rank * THREADS + threadIdx.x; e < cols * (HD / 4); e += csize * THREADS) {
         const int c = e / (HD / 4), d = e % (HD / 4) * 4;
         float m[PG_MAX_CLUSTER], l[PG_MAX_CLUSTER];
-        float4 x[PG_MAX_CLUSTER];
 #pragma unroll
         for (int r = 0; r < PG_MAX_CLUSTER; ++r) {
           m[r] = r < csize ? *co_map_shared(&sh.m[c], r) : -INFINITY;
           l[r] = r < csize ? *co_map_shared(&sh.l[c], r) : 0.f;
-          x[r] = r < csize ? *co_map_shared(reinterpret_cast<float4 *>(co + c * HD + d), r) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
         float most = -INFINITY, sum = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int r = 0; r < PG_MAX_CLUSTER; ++r) most = fmaxf(most, m[r]);
+        for (int r0 = 0; r0 < PG_MAX_CLUSTER; r0 += 8) {
+          if (r0 >= csize) break;
+          float4 x[8];
 #pragma unroll
-        for (int r = 0; r < PG_MAX_CLUSTER; ++r) {
-          const float f = ex2_approx(m[r] - (most == -INFINITY ? 0.f : most));
-          sum = fmaf(l[r], f, sum);
-          o = make_float4(fmaf(x[r].x, f, o.x), fmaf(x[r].y, f, o.y), fmaf(x[r].z, f, o.z), fmaf(x[r].w, f, o.w));
+          for (int r = 0; r < 8; ++r)
+            x[r] = r0 + r < csize ? *co_map_shared(reinterpret_cast<float4 *>(co + c * HD + d), r0 + r) : make_float4(0.f, 0.f, 0.f, 0.f);
+          if (r0 == 0) {
+#pragma unroll
+            for (int r = 0; r < PG_MAX_CLUSTER; ++r) most = fmaxf(most, m[r]);
+          }
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            const float f = ex2_approx(m[r0 + r] - (most == -INFINITY ? 0.f : most));
+            sum = fmaf(l[r0 + r], f, sum);
+            o = make_float4(fmaf(x[r].x, f, o.x), fmaf(x[r].y, f, o.y), fmaf(x[r].z, f, o.z), fmaf(x[r].w, f, o.w));
+          }
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         *reinterpret_cast<uint2 *>(output(c, d)) = make_uint2(bf16x2_pack(o.x * inv, o.y * inv), bf16x2_pack(o.z * inv, o.w * inv));
@@ -391,12 +429,10 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
       co_cluster_sync();  // nobody leaves while its part is being read
       return;
     }
-    if (first == 0 && !all) {  // the range ends here: how many CTAs have the rest of the pair
-      int more = 1;
-      while (cta + 1 + more < ctas && first_of(cta + 1 + more) < pair0 + seq.tiles) ++more;
-      split = {more, s, g, ct};
+    if (first == 0 && !all) {  // the range ends here; the pair's last unit is that of the last CTA that begins before it
+      const long long last = pair0 + seq.share() - 1;
+      split = {(int)(((last + 1) * ctas + total - 1) / total) - 1 - cta, seq.start, g, c0, cols, {}};
     }
-    u = pair0 + first + count;
     if (u < u1) __syncthreads();  // the stages and the maxima have been read
   }
   if (threadIdx.x == 0) scratch.split[cta] = split;
@@ -405,23 +441,23 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
 // Adds up the parts of the pair that CTA blockIdx.x began and did not finish.  A warp per column, several to one where there are few.
 template <int HD, int COLS>
 __global__ void __launch_bounds__(PG_MERGE_THREADS)
-paged_mma_merge_kernel(const PagedArgs a, int group, PgScratch scratch, DevStatus *status) {
+paged_mma_merge_kernel(const PagedArgs a, int group, PgScratch scratch) {
   constexpr int WARPS = PG_MERGE_THREADS / 32, WIDE = HD / 4, BATCH = 8;  // lanes 0..WIDE-1 hold four of a column's elements each
+  static_assert(COLS <= WARPS, "a warp per column");
   __shared__ float4 part[WARPS][32];
-  __shared__ float part_ml[WARPS][2];
+  __shared__ float2 part_ml[WARPS];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int cta = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const PgSplit p = scratch.split[cta];
   if (p.more == 0) return;
-  const PgSeq seq = pg_seq<COLS>(a, p.s, group, false, status);
-  const int c0 = p.ct * COLS, cols = min(COLS, seq.rows * group - c0), n = p.more + 1;
+  const int n = p.more + 1;
   int share = 1;  // warps to a column
-  while (share * 2 * cols <= WARPS) share *= 2;
+  while (share * 2 * p.cols <= WARPS) share *= 2;
   const int c = warp / share, first = warp % share;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto place = [&](int i) { return ((size_t)(cta + i) * 2 + (i == 0)) * PG_MAX_COLS + c; };
-  if (c < cols) {
+  auto place = [&](int i) { return ((size_t)(cta + i) * 2 + (i == 0)) * COLS + c; };
+  if (c < p.cols) {
     for (int i0 = first; i0 < n; i0 += share * BATCH) {
       float2 ml[BATCH];
       float4 x[BATCH];
@@ -447,46 +483,71 @@ paged_mma_merge_kernel(const PagedArgs a, int group, PgScratch scratch, DevStatu
     }
   }
   part[warp][lane] = o;
-  if (lane == 0) part_ml[warp][0] = m, part_ml[warp][1] = l;
+  if (lane == 0) part_ml[warp] = make_float2(m, l);
   __syncthreads();
-  if (c >= cols || first != 0 || lane >= WIDE) return;
-  for (int w = 0; w < share; ++w) m = fmaxf(m, part_ml[warp + w][0]);
+  if (c >= p.cols || first != 0 || lane >= WIDE) return;
+  for (int w = 0; w < share; ++w) m = fmaxf(m, part_ml[warp + w].x);
   const float ref = m == -INFINITY ? 0.f : m;
   l = 0.f;
   o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int w = 0; w < share; ++w) {
-    const float f = ex2_approx(part_ml[warp + w][0] - ref);
+    const float2 ml = part_ml[warp + w];
+    const float f = ex2_approx(ml.x - ref);
     const float4 x = part[warp + w][lane];
-    l = fmaf(part_ml[warp + w][1], f, l);
+    l = fmaf(ml.y, f, l);
     o = make_float4(fmaf(x.x, f, o.x), fmaf(x.y, f, o.y), fmaf(x.z, f, o.z), fmaf(x.w, f, o.w));
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int t = (c0 + c) / group, h = c0 + c - t * group;
-  *reinterpret_cast<uint2 *>((bf16 *)a.o + ((size_t)(seq.start + t) * a.n_heads + p.g * group + h) * HD + lane * 4) =
+  const int t = (p.c0 + c) / group, h = p.c0 + c - t * group;
+  *reinterpret_cast<uint2 *>((bf16 *)a.o + ((size_t)(p.start + t) * a.n_heads + p.g * group + h) * HD + lane * 4) =
       make_uint2(bf16x2_pack(o.x * inv, o.y * inv), bf16x2_pack(o.z * inv, o.w * inv));
 }
 
-// CTAs of a cluster per pair, 0: equal shares of all keys.
-int paged_join(const PagedArgs &a, int max_cts) {
+// How a launch is shaped: CTAs of a cluster per pair (0: equal shares of all keys), and whether they are the large ones.
+struct PgShape {
+  int cluster;
+  bool deep;
+};
+PgShape paged_shape(const PagedArgs &a, int max_cts) {
   const long long pairs = (long long)a.n_seqs * a.n_kv_heads * max_cts;
-  int c = 1;
-  while (c < PG_MAX_CLUSTER && pairs * c * 2 <= co_cluster_ctas(c * 2, PG_CTAS) && a.max_kv > c * PG_UNIT) c *= 2;
-  return a.max_kv > 0 && pairs * c <= co_cluster_ctas(c, PG_CTAS) && a.max_kv <= c * PG_UNIT * PG_JOIN_UNITS ? c : 0;
+  if (a.max_kv < 1) return {0, false};
+  auto largest = [&](PgDepth d) {  // of which all run at once, and every warp has something to do
+    int c = 1;
+    while (c < PG_MAX_CLUSTER && pairs * c * 2 <= co_cluster_ctas(c * 2, d.ctas) && a.max_kv > c * d.warps * RM_KEYS) c *= 2;
+    return pairs * c <= co_cluster_ctas(c, d.ctas) ? c : 0;
+  };
+  const PgDepth d = PG_WIDE;
+  const int wide = largest(d), deep = largest(PG_DEEP);
+  // as many SMs as possible, then as many warps
+  const long long sms = sm_count(), wide_sms = min(pairs * wide, sms), deep_sms = min(pairs * deep, sms);
+  const bool large = deep_sms > wide_sms || (deep_sms == wide_sms && deep * PG_DEEP.warps >= wide * d.warps);
+  const int c = large ? deep : wide, warps = c * (large ? PG_DEEP : d).warps;
+  if (c == 0 || a.max_kv > warps * RM_KEYS * PG_JOIN_UNITS) return {0, false};
+  return {c, large};
 }
 
 template <int HD, int NT, bool WHOLE>
 int paged_mma_launch(cudaStream_t st, const PagedArgs &a, float *scratch, DevStatus *status) {
-  constexpr int SMEM = PG_WARPS * PG_STAGES * RowsMma<HD, NT>::STAGE;
+  constexpr PgDepth D = PG_WIDE, E = PG_DEEP;
+  constexpr int GROUP = RowsMma<HD, NT>::STAGE, SMEM = GROUP * D.warps * D.stages, DEEP = GROUP * E.warps * E.stages;
   const int group = a.n_heads / a.n_kv_heads, max_cts = (int)(((long long)a.max_q * group + NT * 8 - 1) / (NT * 8));
-  const PgScratch c = pg_scratch(scratch);
-  if (const int join = paged_join(a, max_cts)) {
-    LAZY_TRY((co_allow_smem<paged_mma_kernel<HD, NT, WHOLE, true>>(SMEM)));
-    return co_launch(paged_mma_kernel<HD, NT, WHOLE, true>, dim3((unsigned)(a.n_seqs * a.n_kv_heads * max_cts * join)), dim3(PG_THREADS), SMEM,
-                     st, join, false, a, group, max_cts, c, status);
+  const PgScratch c = pg_scratch(scratch, NT);
+  const PgShape shape = paged_shape(a, max_cts);
+  if (shape.cluster) {
+    const dim3 grid((unsigned)(a.n_seqs * a.n_kv_heads * max_cts * shape.cluster));
+    if (shape.deep) {
+      constexpr auto kernel = paged_mma_kernel<HD, NT, WHOLE, true, E.warps, E.stages, E.ctas>;
+      LAZY_TRY((co_allow_smem<kernel>(DEEP, false, true)));
+      return co_launch(kernel, grid, dim3(E.warps * 32), DEEP, st, shape.cluster, false, a, group, max_cts, c, status);
+    }
+    constexpr auto kernel = paged_mma_kernel<HD, NT, WHOLE, true, D.warps, D.stages, D.ctas>;
+    LAZY_TRY((co_allow_smem<kernel>(SMEM, false, true)));
+    return co_launch(kernel, grid, dim3(D.warps * 32), SMEM, st, shape.cluster, false, a, group, max_cts, c, status);
   }
-  LAZY_TRY((co_allow_smem<paged_mma_kernel<HD, NT, WHOLE, false>>(SMEM)));
-  LAZY_TRY(co_launch(paged_mma_kernel<HD, NT, WHOLE, false>, dim3(pg_grid()), dim3(PG_THREADS), SMEM, st, 1, false, a, group, 0, c, status));
-  return co_launch(paged_mma_merge_kernel<HD, NT * 8>, dim3(pg_grid()), dim3(PG_MERGE_THREADS), 0, st, 1, true, a, group, c, status);
+  constexpr auto kernel = paged_mma_kernel<HD, NT, WHOLE, false, D.warps, D.stages, D.ctas>;
+  LAZY_TRY((co_allow_smem<kernel>(SMEM)));
+  LAZY_TRY(co_launch(kernel, dim3(pg_grid()), dim3(D.warps * 32), SMEM, st, 1, false, a, group, 0, c, status));
+  return co_launch(paged_mma_merge_kernel<HD, NT * 8>, dim3(pg_grid()), dim3(PG_MERGE_THREADS), 0, st, 1, true, a, group, c);
 }
 
 bool paged_mma_eligible(int dtype, int head_dim) { return dtype == LAZY_BF16 && head_dim <= 128; }
@@ -494,27 +555,32 @@ bool paged_mma_eligible(int dtype, int head_dim) { return dtype == LAZY_BF16 && 
 }  // namespace
 
 // What the call needs, or (`any`) as much as any smaller one does.
-static size_t paged_scratch_floats(int n_rows, int max_kv, int n_heads, int head_dim, bool any) {
+static size_t paged_scratch_floats(int n_rows, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim, bool any) {
   const long long rh = (long long)n_rows * n_heads;
   const size_t parts = any ? attn_split_parts(rh, max_kv) : (size_t)rh * attn_split_count(rh, max_kv);
-  const size_t general = parts * (head_dim + 2), mma = head_dim <= 128 ? pg_scratch_floats(head_dim) : 0;
+  const size_t general = parts * (head_dim + 2);
+  const size_t mma = head_dim <= 128 ? pg_scratch_floats(pg_blocks((long long)max_q * (n_heads / n_kv_heads)), head_dim) : 0;
   return general > mma ? general : mma;
 }
-size_t attention_paged_scratch_need(int n_rows, int max_kv, int n_heads, int head_dim) {
-  return paged_scratch_floats(n_rows, max_kv, n_heads, head_dim, false);
+size_t attention_paged_scratch_need(int n_rows, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
+  return paged_scratch_floats(n_rows, max_q, max_kv, n_heads, n_kv_heads, head_dim, false);
 }
-size_t attention_paged_scratch_floats(int n_rows, int max_kv, int n_heads, int head_dim) {
-  return paged_scratch_floats(n_rows, max_kv, n_heads, head_dim, true);
+size_t attention_paged_scratch_floats(int n_rows, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
+  return paged_scratch_floats(n_rows, max_q, max_kv, n_heads, n_kv_heads, head_dim, true);
+}
+
+template <int HD, bool WHOLE>
+static int paged_mma(cudaStream_t st, const PagedArgs &a, float *scratch, DevStatus *status) {
+  return pg_blocks((long long)a.max_q * (a.n_heads / a.n_kv_heads)) == 1 ? paged_mma_launch<HD, 1, WHOLE>(st, a, scratch, status)
+                                                                        : paged_mma_launch<HD, 2, WHOLE>(st, a, scratch, status);
 }
 
 int launch_attention_paged(cudaStream_t st, int dtype, const PagedArgs &a, float *scratch, DevStatus *status) {
   if (a.n_rows == 0) return LAZY_OK;
   if (paged_mma_eligible(dtype, a.head_dim)) {
-    const bool narrow = (long long)a.max_q * (a.n_heads / a.n_kv_heads) <= 8, whole = a.kv.page_size % RM_KEYS == 0;
+    const bool whole = a.kv.page_size % RM_KEYS == 0;
     return co_head_dim(a.head_dim, [&](auto hd) {
-      constexpr int HD = hd.value;
-      if (whole) return narrow ? paged_mma_launch<HD, 1, true>(st, a, scratch, status) : paged_mma_launch<HD, 2, true>(st, a, scratch, status);
-      return narrow ? paged_mma_launch<HD, 1, false>(st, a, scratch, status) : paged_mma_launch<HD, 2, false>(st, a, scratch, status);
+      return whole ? paged_mma<hd.value, true>(st, a, scratch, status) : paged_mma<hd.value, false>(st, a, scratch, status);
     });
   }
   return dtype == LAZY_F32 ? paged_general<float>(st, a, scratch, status) : paged_general<bf16>(st, a, scratch, status);

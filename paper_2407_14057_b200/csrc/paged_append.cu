@@ -14,10 +14,11 @@ namespace lazy {
 namespace {
 
 constexpr int PA_THREADS = 256, PA_WARPS = PA_THREADS / 32;
-constexpr int PA_BATCH = 4;  // heads of a lane in flight
+constexpr int PA_BATCH = 2;  // heads of a lane in flight
+constexpr int PA_CTAS = 3;   // to an SM
 
 template <typename T>
-__global__ void __launch_bounds__(PA_THREADS)
+__global__ void __launch_bounds__(PA_THREADS, PA_CTAS)
 paged_append_kernel(const AppendArgs a, int lanes_log2, int parts, int steps, DevStatus *status) {
   constexpr int V = Elem<T>::kPerVec;
   const int lane = threadIdx.x & 31;

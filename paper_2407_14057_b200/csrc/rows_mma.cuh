@@ -76,6 +76,35 @@ __device__ __forceinline__ void rows_load(uint32_t stage, Rows rows) {
   }
 }
 
+// The same for 16 rows that lie `stride` elements apart from kr / vr on, all of them there: fewer instructions to an address.
+template <int HD>
+__device__ __forceinline__ void rows_load_run(uint32_t stage, const bf16 *kr, const bf16 *vr, long long stride) {
+  const int lane = threadIdx.x & 31;
+  constexpr int CHUNKS = HD / 8;
+  if constexpr (32 % CHUNKS == 0) {  // a lane stays in its column, rows advance by 32 / CHUNKS
+    constexpr int STEP = 32 / CHUNKS;
+    const int r0 = lane / CHUNKS, c = lane % CHUNKS;
+    kr += r0 * stride + c * 8;
+    vr += r0 * stride + c * 8;
+#pragma unroll
+    for (int i = 0; i < RM_KEYS / STEP; ++i) {
+      const uint32_t to = stage + rows_at<HD>(r0 + i * STEP, c);
+      rm_cp_async16(to, kr, true);
+      rm_cp_async16(to + RM_KEYS * rows_pitch<HD>, vr, true);
+      kr += STEP * stride;
+      vr += STEP * stride;
+    }
+  } else {
+    rows_load<HD>(stage, [&](int r, const bf16 *&k, const bf16 *&v) {
+      k = kr + r * stride;
+      v = vr + r * stride;
+      return true;
+    });
+  }
+}
+
+constexpr float RM_SLACK = 8.f;
+
 template <int HD, int NT>
 struct RowsMma {
   static constexpr int CHUNKS = HD / 8;              // 16-byte pieces per row
@@ -182,6 +211,102 @@ struct RowsMma {
         rm_mma(o[t][k], a, hi[t][0], hi[t][1]);
         rm_mma(o[t][k], a, lo[t][0], lo[t][1]);
       }
+    }
+  }
+
+  // The same without logits for the caller, with less between its products: a column's reference m is raised only when a logit exceeds it
+  // by more than RM_SLACK (weights are then up to 2^RM_SLACK), so that most groups need neither their maximum nor a pass over the
+  // outputs, and products that depend on one another have others between them.  ALL: every column sees all 16 keys.
+  template <bool CUT, bool ALL>
+  __device__ __forceinline__ void step(uint32_t stage, const int (&vis)[NT][2], uint32_t there) {
+    const int lane = threadIdx.x & 31, kr = lane >> 2;
+    const float sl2 = rsqrtf((float)HD) * CO_LOG2E;
+    constexpr int CHAINS = NT == 1 ? 2 : 1;  // sums over the head that run side by side
+    float s[NT][4], x[CHAINS][NT][4];
+#pragma unroll
+    for (int c = 0; c < CHAINS; ++c)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[c][t][i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k) {
+      uint32_t a[4];  // keys 0-7 | 8-15 of columns k * 16 .. + 7, then of the next eight
+      rm_ldmatrix(stage + at(lane & 15, k * 2 + (lane >> 4)), a);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) rm_mma(x[k % CHAINS][t], a, qf[t][k][0], qf[t][k][1]);
+    }
+    const uint32_t wild = CUT ? take_out_wild(stage) : 0u;
+    bool grown = false;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[t][i] = (CHAINS == 2 ? x[0][t][i] + x[CHAINS - 1][t][i] : x[0][t][i]) * sl2;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (!ALL) {
+          if (kr >= vis[t][i] || !(there >> kr & 1u)) s[t][i] = -INFINITY;
+          if (kr + 8 >= vis[t][i] || !(there >> (kr + 8) & 1u)) s[t][2 + i] = -INFINITY;
+        }
+        grown |= fmaxf(s[t][i], s[t][2 + i]) > m[t][i] + RM_SLACK;
+      }
+    }
+    if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float mx = fmaxf(s[t][i], s[t][2 + i]);
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          mx = fmaxf(mx, m[t][i]);
+          const float alpha = ex2_approx(m[t][i] - (mx == -INFINITY ? 0.f : mx));
+          m[t][i] = mx;
+          l[t][i] *= alpha;
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) {
+            o[t][k][i] *= alpha;
+            o[t][k][2 + i] *= alpha;
+          }
+        }
+    }
+    uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float p[4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float ref = m[t][i] == -INFINITY ? 0.f : m[t][i];  // nothing seen so far: every weight is 2^-inf = 0
+        p[i] = ex2_approx(s[t][i] - ref);
+        p[2 + i] = ex2_approx(s[t][2 + i] - ref);
+        l[t][i] += p[i] + p[2 + i];
+      }
+      if (CUT && wild) add_wild(stage, wild, t, vis[t], there, p);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t h = bf16x2_pack_rz(p[2 * i], p[2 * i + 1]);
+        float h0, h1;
+        bf16x2_unpack(h, h0, h1);
+        hi[t][i] = rm_transpose(h);
+        lo[t][i] = rm_transpose(bf16x2_pack(fmaf(h0, -WEIGHT_REST, p[2 * i]), fmaf(h1, -WEIGHT_REST, p[2 * i + 1])));
+      }
+    }
+    constexpr int BATCH = HD % 64 == 0 ? 4 : 2;  // pieces of the head at a time
+#pragma unroll
+    for (int k0 = 0; k0 < HD / 16; k0 += BATCH) {
+      uint32_t a[BATCH][4];  // head columns 0-7 | 8-15 of keys 0-7, then of keys 8-15
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b)
+        rm_ldmatrix_trans(stage + HALF + at((lane & 7) + ((lane >> 4) << 3), (k0 + b) * 2 + ((lane >> 3) & 1)), a[b]);
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) rm_mma(o[t][k0 + b], a[b], hi[t][0], hi[t][1]);
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) rm_mma(o[t][k0 + b], a[b], lo[t][0], lo[t][1]);
     }
   }
 
