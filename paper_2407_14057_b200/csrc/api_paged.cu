@@ -55,7 +55,7 @@ int lazy_k_paged_append(void *stream, int32_t dtype, const void *q, int32_t ldq,
 size_t lazy_k_attention_paged_scratch_floats(int32_t n_rows, int32_t n_seqs, int32_t max_q, int32_t max_kv, int32_t n_heads,
                                              int32_t n_kv_heads, int32_t head_dim) {
   if (n_rows < 0 || n_seqs < 0 || max_q < 0 || max_kv < 0 || check_heads(n_heads, n_kv_heads, head_dim) != LAZY_OK) return 0;
-  return attention_paged_scratch_floats(n_rows, max_q, max_kv, n_heads, n_kv_heads, head_dim);
+  return attention_paged_scratch_floats(n_rows, n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim);
 }
 
 int lazy_k_attention_paged(void *stream, int32_t dtype, const void *q, int32_t ldq, const int32_t *d_cu_q, int32_t n_rows,
@@ -71,7 +71,8 @@ int lazy_k_attention_paged(void *stream, int32_t dtype, const void *q, int32_t l
   LAZY_TRY(take_pages(pages, dtype, a.kv));
   const int most = paged_capacity(a.kv);
   if (a.max_kv > most) a.max_kv = most;
-  if (scratch_floats < attention_paged_scratch_need(n_rows, max_q, a.max_kv, n_heads, n_kv_heads, head_dim)) return LAZY_E_CAPACITY;
+  if (a.max_q > n_rows) a.max_q = n_rows;
+  if (scratch_floats < attention_paged_scratch_need(n_rows, n_seqs, a.max_q, a.max_kv, n_heads, n_kv_heads, head_dim)) return LAZY_E_CAPACITY;
   DevStatus *status = dev_status_ptr();
   if (!status) return LAZY_E_CUDA;
   return launch_attention_paged((cudaStream_t)stream, dtype, a, scratch, status);

@@ -10,74 +10,197 @@ namespace {
 
 typedef unsigned long long u64;
 
-// ---- general form: every type and head width, on CUDA cores; partial softmaxes of split key ranges, then their merge ----------
+// ---- general form: fp32 and wide heads, on CUDA cores; partial softmaxes of split key ranges, then their merge ----------------------
+// A CTA takes a range of keys for four columns (a column being one (row, query head)) of a key/value head, a warp eight keys at a time
+// with its lanes along the head: 32 dot products, whose sums over the lanes are scattered to one a lane in 31 exchanges (each on its own
+// takes five); the weights go back by 32 broadcasts.  16 sequences of 3000 tokens, 8 on 2 heads of 64, fp32 (49 MB): 25 us, with a row and
+// head to a CTA 63.
+constexpr int PW_COLS = 4, PW_KEYS = 8, PW_WARPS = 4, PW_THREADS = PW_WARPS * 32;
 
-// Row r's sequence and how many tokens it sees (0: it belongs to none, or its tables do not fit).  By whole warps.
-__device__ __forceinline__ int paged_row_sees(const PagedArgs &a, int r, bool report, DevStatus *status, int &s) {
-  s = a.cu_q ? paged_find_seq(a.cu_q, a.n_seqs, r) : r;
-  int start, rows, len;
-  if (s < 0 || !paged_seq(a.kv, a.cu_q, s, a.n_rows, a.max_q, a.max_kv, report, status, start, rows, len) || rows == 0) return 0;
-  if (r < start || r >= start + rows) {  // boundaries that do not ascend
-    if (report) dev_fail(status, LAZY_E_BADARG, W_PAGED, s, r);
-    return 0;
-  }
-  return len - rows + (r - start) + 1;
+// Key ranges: enough CTAs for four on every SM, in whole tiles of keys.
+inline int paged_wide_splits(long long pairs, int max_kv) { return attn_split_count(pairs, max_kv); }
+inline long long paged_wide_tiles(int max_q, int n_heads, int n_kv_heads) {
+  return ((long long)max_q * (n_heads / n_kv_heads) + PW_COLS - 1) / PW_COLS;
 }
 
-// grid (splits, n_heads, n_rows)
-template <typename T>
-__global__ void __launch_bounds__(AS_THREADS)
-paged_partial_kernel(const PagedArgs a, int group, int per_split, float *__restrict__ part_o, float *__restrict__ part_ml,
-                     DevStatus *status) {
-  __shared__ AttnSplitSmem<T> sm;
-  const int h = blockIdx.y, r = blockIdx.z, g = h / group;
-  int s;
-  const int n = paged_row_sees(a, r, blockIdx.x == 0 && h == 0 && threadIdx.x == 0, status, s);
-  if (n == 0) return;
-  const size_t part = ((size_t)r * gridDim.y + h) * gridDim.x + blockIdx.x;
+// grid (n_kv_heads * column tiles * splits, n_seqs); head width 32 E
+template <typename T, int E>
+__global__ void __launch_bounds__(PW_THREADS)
+paged_wide_kernel(const PagedArgs a, int group, int tiles, int splits, int per_split, float *__restrict__ part_o,
+                  float *__restrict__ part_ml, DevStatus *status) {
+  constexpr int HD = 32 * E;
+  __shared__ float so[PW_WARPS][PW_COLS][HD];
+  __shared__ float2 sml[PW_WARPS][PW_COLS];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = blockIdx.y;
+  int x = blockIdx.x;
+  const int split = x % splits;
+  x /= splits;
+  const int g = x / tiles, c0 = (x - g * tiles) * PW_COLS;
+  int start, rows, len;
+  if (!paged_seq(a.kv, a.cu_q, s, a.n_rows, a.max_q, a.max_kv, blockIdx.x == 0 && threadIdx.x == 0, status, start, rows, len)) return;
+  const int cols = min(PW_COLS, (int)min((long long)rows * group - c0, (long long)PW_COLS));
+  if (cols <= 0) return;
+  const int k0 = split * per_split, k1 = min(len, k0 + per_split);
   const int32_t *table = a.kv.table + (size_t)s * a.kv.ld_table;
-  auto at = [&](int j) -> long long {
-    const int nth = j / a.kv.page_size, page = table[nth];
-    if (page < 0 || page >= a.kv.n_pages) {
-      dev_fail(status, LAZY_E_BADARG, W_PAGED, s, page);
-      return -1;
+  const T *kp = (const T *)a.kv.k + (long long)g * a.kv.head_stride + lane, *vp = (const T *)a.kv.v + (long long)g * a.kv.head_stride + lane;
+  auto row_of = [&](int c) { return (c0 + c) / group; };
+  auto head_of = [&](int c) { return g * group + (c0 + c) % group; };
+  float q[PW_COLS][E], o[PW_COLS][E], m = -INFINITY, l = 0.f;  // m and l of column lane % 4, l of this lane's keys
+  const float scale = rsqrtf((float)HD) * CO_LOG2E;
+#pragma unroll
+  for (int c = 0; c < PW_COLS; ++c)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      q[c][e] = c < cols ? Elem<T>::to_f(((const T *)a.q)[(size_t)(start + row_of(c)) * a.ldq + (size_t)head_of(c) * HD + e * 32 + lane]) * scale : 0.f;
+      o[c][e] = 0.f;
     }
-    return (long long)page * a.kv.page_stride + (long long)(j - nth * a.kv.page_size) * a.kv.slot_stride + (long long)g * a.kv.head_stride;
-  };
-  attn_split_partial<T>(
-      sm, (const T *)a.q + (size_t)r * a.ldq + (size_t)h * a.head_dim, a.head_dim, blockIdx.x * per_split,
-      min(n, (int)blockIdx.x * per_split + per_split),
-      [&](int j) -> const T * {
-        const long long i = at(j);
-        return i < 0 ? nullptr : (const T *)a.kv.k + i;
-      },
-      [&](int j) -> const T * {
-        const long long i = at(j);
-        return i < 0 ? nullptr : (const T *)a.kv.v + i;
-      },
-      part_o + part * a.head_dim, part_ml + part * 2, nullptr);
+  const int my_c = lane & 3, my_key = lane >> 2;
+  const int vis = my_c < cols ? min(len - rows + row_of(my_c) + 1, k1) : 0;  // keys below it are seen by this lane's column
+  for (int j0 = k0 + warp * PW_KEYS; j0 < k1; j0 += PW_WARPS * PW_KEYS) {
+    const int j = min(j0 + (lane & 7), k1 - 1), nth = j / a.kv.page_size, page = table[nth];
+    const bool in = page >= 0 && page < a.kv.n_pages;
+    if (!in && lane < PW_KEYS) dev_fail(status, LAZY_E_BADARG, W_PAGED, s, page);
+    const long long off = (long long)page * a.kv.page_stride + (long long)(j - nth * a.kv.page_size) * a.kv.slot_stride;
+    const uint32_t there = __ballot_sync(0xffffffffu, in && j0 + (lane & 7) < k1) & 0xffu;
+    float v[PW_KEYS][E], d[PW_KEYS * PW_COLS];
+    {
+      float k[PW_KEYS][E];
+#pragma unroll
+      for (int i = 0; i < PW_KEYS; ++i) {
+        const long long at = __shfl_sync(0xffffffffu, off, i);
+#pragma unroll
+        for (int e = 0; e < E; ++e) k[i][e] = there >> i & 1u ? Elem<T>::to_f(kp[at + e * 32]) : 0.f;
+        if (E <= 4) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[i][e] = there >> i & 1u ? Elem<T>::to_f(vp[at + e * 32]) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < PW_KEYS; ++i)
+#pragma unroll
+        for (int c = 0; c < PW_COLS; ++c) {
+          float sum = q[c][0] * k[i][0];
+#pragma unroll
+          for (int e = 1; e < E; ++e) sum = fmaf(q[c][e], k[i][e], sum);
+          d[i * PW_COLS + c] = sum;
+        }
+    }
+    if (E > 4) {
+#pragma unroll
+      for (int i = 0; i < PW_KEYS; ++i) {
+        const long long at = __shfl_sync(0xffffffffu, off, i);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[i][e] = there >> i & 1u ? Elem<T>::to_f(vp[at + e * 32]) : 0.f;
+      }
+    }
+    // sums over the lanes, that of key i and column c to lane 4 i + c
+#pragma unroll
+    for (int n = 16; n > 0; n >>= 1)
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const float keep = lane & n ? d[i + n] : d[i], give = lane & n ? d[i] : d[i + n];
+        d[i] = keep + __shfl_xor_sync(0xffffffffu, give, n);
+      }
+    const float logit = (there >> my_key & 1u) && j0 + my_key < vis ? d[0] : -INFINITY;
+    float most = fmaxf(logit, __shfl_xor_sync(0xffffffffu, logit, 4));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 8));
+    most = fmaxf(m, fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 16)));
+    const float ref = most == -INFINITY ? 0.f : most;  // nothing seen so far: every weight is 2^-inf = 0
+    const float alpha = exp2f(m - ref), p = exp2f(logit - ref);
+    m = most;
+    l = fmaf(l, alpha, p);
+    if (__any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll
+      for (int c = 0; c < PW_COLS; ++c) {
+        const float f = __shfl_sync(0xffffffffu, alpha, c);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[c][e] *= f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < PW_KEYS; ++i)
+#pragma unroll
+      for (int c = 0; c < PW_COLS; ++c) {
+        const float w = __shfl_sync(0xffffffffu, p, i * PW_COLS + c);
+        if (w != 0.f) {  // the whole warp alike; a value that a column does not see must not reach it as 0 x inf
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[c][e] = fmaf(w, v[i][e], o[c][e]);
+        }
+      }
+  }
+  l += __shfl_xor_sync(0xffffffffu, l, 4);
+  l += __shfl_xor_sync(0xffffffffu, l, 8);
+  l += __shfl_xor_sync(0xffffffffu, l, 16);
+  if (lane < PW_COLS) sml[warp][lane] = make_float2(m, l);
+#pragma unroll
+  for (int c = 0; c < PW_COLS; ++c)
+#pragma unroll
+    for (int e = 0; e < E; ++e) so[warp][c][e * 32 + lane] = o[c][e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < cols * HD; i += PW_THREADS) {
+    const int c = i / HD, at = i - c * HD;
+    float top = -INFINITY, sum = 0.f, out = 0.f;
+#pragma unroll
+    for (int w = 0; w < PW_WARPS; ++w) top = fmaxf(top, sml[w][c].x);
+#pragma unroll
+    for (int w = 0; w < PW_WARPS; ++w) {
+      const float f = exp2f(sml[w][c].x - (top == -INFINITY ? 0.f : top));
+      sum = fmaf(sml[w][c].y, f, sum);
+      if (f != 0.f) out = fmaf(so[w][c][at], f, out);
+    }
+    if (splits == 1) {
+      ((T *)a.o)[((size_t)(start + row_of(c)) * a.n_heads + head_of(c)) * HD + at] = Elem<T>::from_f(sum == 0.f ? 0.f : out / sum);
+    } else {
+      const size_t part = (((size_t)s * (gridDim.x / splits) + x) * PW_COLS + c) * splits + split;
+      part_o[part * HD + at] = out;
+      if (at == 0) {
+        part_ml[part * 2] = top;
+        part_ml[part * 2 + 1] = sum;
+      }
+    }
+  }
 }
 
 // grid (n_heads, n_rows)
 template <typename T>
 __global__ void __launch_bounds__(AS_THREADS)
-paged_merge_kernel(const PagedArgs a, const float *__restrict__ part_o, const float *__restrict__ part_ml, int splits) {
+paged_merge_kernel(const PagedArgs a, const float *__restrict__ part_o, const float *__restrict__ part_ml, int tiles, int splits) {
   const int h = blockIdx.x, r = blockIdx.y;
-  int s;
-  if (paged_row_sees(a, r, false, nullptr, s) == 0) return;  // the row is left as it was
-  const size_t rh = (size_t)r * gridDim.x + h;
-  attn_split_merge<T>(part_o + rh * splits * a.head_dim, part_ml + rh * splits * 2, splits, a.head_dim, (T *)a.o + rh * a.head_dim,
+  const int s = a.cu_q ? paged_find_seq(a.cu_q, a.n_seqs, r) : r;
+  int start, rows, len;
+  if (s < 0 || !paged_seq(a.kv, a.cu_q, s, a.n_rows, a.max_q, a.max_kv, false, nullptr, start, rows, len) || r < start || r >= start + rows)
+    return;  // the row is left as it was
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int group = a.n_heads / a.n_kv_heads, g = h / group, c = (r - start) * group + h - g * group;
+  const size_t part = ((((size_t)s * a.n_kv_heads + g) * tiles + c / PW_COLS) * PW_COLS + c % PW_COLS) * splits;
+  attn_split_merge<T>(part_o + part * a.head_dim, part_ml + part * 2, splits, a.head_dim, (T *)a.o + ((size_t)r * gridDim.x + h) * a.head_dim,
                       nullptr);
 }
 
-template <typename T>
-int paged_general(cudaStream_t st, const PagedArgs &a, float *scratch, DevStatus *status) {
-  const long long rh = (long long)a.n_rows * a.n_heads;
-  const int splits = attn_split_count(rh, a.max_kv);
-  float *part_o = scratch, *part_ml = scratch + (size_t)rh * splits * a.head_dim;
-  LAZY_TRY(co_launch(paged_partial_kernel<T>, dim3(splits, a.n_heads, a.n_rows), dim3(AS_THREADS), 0, st, 1, false, a,
-                     a.n_heads / a.n_kv_heads, attn_split_keys(a.max_kv, splits), part_o, part_ml, status));
-  return co_launch(paged_merge_kernel<T>, dim3(a.n_heads, a.n_rows), dim3(AS_THREADS), 0, st, 1, false, a, part_o, part_ml, splits);
+template <typename T, int E>
+int paged_wide(cudaStream_t st, const PagedArgs &a, float *scratch, DevStatus *status) {
+  const long long tiles = paged_wide_tiles(a.max_q, a.n_heads, a.n_kv_heads), pairs = tiles * a.n_kv_heads;  // of a sequence
+  const int splits = paged_wide_splits(pairs * a.n_seqs, a.max_kv);
+  if (pairs * splits > 0x7fffffffLL) return LAZY_E_CAPACITY;
+  float *part_o = scratch, *part_ml = scratch + (size_t)pairs * a.n_seqs * PW_COLS * splits * a.head_dim;
+  LAZY_TRY(co_launch(paged_wide_kernel<T, E>, dim3((unsigned)(pairs * splits), a.n_seqs), dim3(PW_THREADS), 0, st, 1, false, a,
+                     a.n_heads / a.n_kv_heads, (int)tiles, splits, attn_split_keys(a.max_kv, splits), part_o, part_ml, status));
+  if (splits == 1) return LAZY_OK;
+  return co_launch(paged_merge_kernel<T>, dim3(a.n_heads, a.n_rows), dim3(AS_THREADS), 0, st, 1, true, a, part_o, part_ml, (int)tiles, splits);
+}
+int paged_f32(cudaStream_t st, const PagedArgs &a, float *scratch, DevStatus *status) {
+  switch (a.head_dim) {
+    case 32: return paged_wide<float, 1>(st, a, scratch, status);
+    case 64: return paged_wide<float, 2>(st, a, scratch, status);
+    case 96: return paged_wide<float, 3>(st, a, scratch, status);
+    case 128: return paged_wide<float, 4>(st, a, scratch, status);
+    case 160: return paged_wide<float, 5>(st, a, scratch, status);
+    case 192: return paged_wide<float, 6>(st, a, scratch, status);
+    case 224: return paged_wide<float, 7>(st, a, scratch, status);
+    case 256: return paged_wide<float, 8>(st, a, scratch, status);
+  }
+  return LAZY_E_BADARG;
 }
 
 // ---- bf16, head width up to 128: warp-level MMA over equal shares of the batch's keys -------------------------------------------
@@ -555,18 +678,19 @@ bool paged_mma_eligible(int dtype, int head_dim) { return dtype == LAZY_BF16 && 
 }  // namespace
 
 // What the call needs, or (`any`) as much as any smaller one does.
-static size_t paged_scratch_floats(int n_rows, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim, bool any) {
-  const long long rh = (long long)n_rows * n_heads;
-  const size_t parts = any ? attn_split_parts(rh, max_kv) : (size_t)rh * attn_split_count(rh, max_kv);
-  const size_t general = parts * (head_dim + 2);
+static size_t paged_scratch_floats(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim, bool any) {
+  max_q = min(max_q, n_rows);
+  const long long pairs = paged_wide_tiles(max_q, n_heads, n_kv_heads) * n_kv_heads * n_seqs;
+  const size_t parts = any ? attn_split_parts(pairs, max_kv) : (size_t)pairs * paged_wide_splits(pairs, max_kv);
+  const size_t wide = parts * PW_COLS * (head_dim + 2);
   const size_t mma = head_dim <= 128 ? pg_scratch_floats(pg_blocks((long long)max_q * (n_heads / n_kv_heads)), head_dim) : 0;
-  return general > mma ? general : mma;
+  return wide > mma ? wide : mma;
 }
-size_t attention_paged_scratch_need(int n_rows, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
-  return paged_scratch_floats(n_rows, max_q, max_kv, n_heads, n_kv_heads, head_dim, false);
+size_t attention_paged_scratch_need(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
+  return paged_scratch_floats(n_rows, n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim, false);
 }
-size_t attention_paged_scratch_floats(int n_rows, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
-  return paged_scratch_floats(n_rows, max_q, max_kv, n_heads, n_kv_heads, head_dim, true);
+size_t attention_paged_scratch_floats(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
+  return paged_scratch_floats(n_rows, n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim, true);
 }
 
 template <int HD, bool WHOLE>
@@ -583,7 +707,14 @@ int launch_attention_paged(cudaStream_t st, int dtype, const PagedArgs &a, float
       return whole ? paged_mma<hd.value, true>(st, a, scratch, status) : paged_mma<hd.value, false>(st, a, scratch, status);
     });
   }
-  return dtype == LAZY_F32 ? paged_general<float>(st, a, scratch, status) : paged_general<bf16>(st, a, scratch, status);
+  if (dtype == LAZY_F32) return paged_f32(st, a, scratch, status);
+  switch (a.head_dim) {
+    case 160: return paged_wide<bf16, 5>(st, a, scratch, status);
+    case 192: return paged_wide<bf16, 6>(st, a, scratch, status);
+    case 224: return paged_wide<bf16, 7>(st, a, scratch, status);
+    case 256: return paged_wide<bf16, 8>(st, a, scratch, status);
+  }
+  return LAZY_E_BADARG;
 }
 
 }  // namespace lazy
