@@ -140,6 +140,33 @@ __device__ __forceinline__ float lp_largest(uint32_t from, int step) {
   return sizeof(T) == 4 ? big : fmaxf(__low2float(big2), __high2float(big2));
 }
 
+// How many of a thread's round are larger than x or, in the loads that lie before the token's (u * THREADS < before), no smaller.  bf16 are
+// compared two at a time: the counts of either half stay below 256, exact in bf16.
+template <typename T, int THREADS>
+__device__ __forceinline__ int lp_count(uint32_t from, float x, int before) {
+  int n = 0;
+  const float above = x == INFINITY ? NAN : nextafterf(x, INFINITY);  // the least number that is larger
+  const __nv_bfloat162 x2 = __float2bfloat162_rn(x);
+  __nv_bfloat162 n2 = __float2bfloat162_rn(0.f);
+#pragma unroll
+  for (int u = 0; u < LP_LOADS<T>; ++u) {
+    uint32_t y[4];
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(from + u * THREADS * 16) : "memory");
+    const bool equal = u * THREADS < before;
+    const float bar = equal ? x : above;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (sizeof(T) == 4) {
+        n += __uint_as_float(y[j]) >= bar;
+      } else {
+        const __nv_bfloat162 y2 = *reinterpret_cast<__nv_bfloat162 *>(&y[j]);
+        n2 = __hadd2(n2, equal ? __hge2(y2, x2) : __hgt2(y2, x2));
+      }
+    }
+  }
+  return sizeof(T) == 4 ? n : (int)(__low2float(n2) + __high2float(n2));
+}
+
 // A key that at least k of the threads' maxima reach, the k-th largest of them or one below it that no more reach.  By one
 // warp; 0 where fewer than k threads have seen anything.
 template <int THREADS>
@@ -257,7 +284,6 @@ token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
       token = -1;
     }
     const int later = r + step < a.n_rows && a.tokens ? a.tokens[r + step] : -1;
-    const float above = given == INFINITY ? NAN : nextafterf(given, INFINITY);  // the least number that is larger
     const int token_piece = token < row.offset ? -1 : (token - row.offset) / V;
     LpSums sums;
     int higher = 0;
@@ -309,15 +335,8 @@ token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
       if (big >= given) {
         const int p = row.piece(i, 0), before = token_piece - p;  // loads u with u * THREADS < before lie before the token's
         if (given > -3.3e38f) {                                   // else what stands behind the last piece would count
-#pragma unroll
-          for (int u = 0; u < LOADS; ++u) {
-            float f[V];
-            fetch(from + u * STEP, f);
-            const float bar = u * THREADS < before ? given : above;
-#pragma unroll
-            for (int j = 0; j < V; ++j) higher += f[j] >= bar;
-          }
-          if (before >= 0 && before < LOADS * THREADS && before % THREADS == 0) {
+          higher += lp_count<T, THREADS>(from, given, before);
+          if (before >= 0 && before < LOADS * THREADS && before % THREADS == 0) {  // the token's own piece
             float f[V];
             fetch(from + before / THREADS * STEP, f);
 #pragma unroll
@@ -328,8 +347,9 @@ token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
           for (int u = 0; u < LOADS && p + u * THREADS < row.p1; ++u) {
             float f[V];
             fetch(from + u * STEP, f);
+            const int id = row.offset + (p + u * THREADS) * V;
 #pragma unroll
-            for (int j = 0; j < V; ++j) higher += f[j] > given || (f[j] == given && row.offset + (p + u * THREADS) * V + j < token);
+            for (int j = 0; j < V; ++j) higher += f[j] > given || (f[j] == given && id + j < token);
           }
         }
       }
