@@ -6,6 +6,8 @@ using namespace lazy;
 
 namespace {
 
+constexpr long long MAX_COLUMNS = 1 << 30;  // rows of a sequence times query heads of a key/value head
+
 // The pages as the kernels take them.
 int take_pages(const lazy_pages *p, int dtype, PagedKV &kv) {
   if (!p || p->n_pages < 0 || p->page_size < 1 || p->table_pages < 0 || p->ld_table < p->table_pages) return LAZY_E_BADARG;
@@ -72,6 +74,7 @@ int lazy_k_attention_paged(void *stream, int32_t dtype, const void *q, int32_t l
   const int most = paged_capacity(a.kv);
   if (a.max_kv > most) a.max_kv = most;
   if (a.max_q > n_rows) a.max_q = n_rows;
+  if ((long long)a.max_q * (n_heads / n_kv_heads) > MAX_COLUMNS) return LAZY_E_CAPACITY;
   if (scratch_floats < attention_paged_scratch_need(n_rows, n_seqs, a.max_q, a.max_kv, n_heads, n_kv_heads, head_dim)) return LAZY_E_CAPACITY;
   DevStatus *status = dev_status_ptr();
   if (!status) return LAZY_E_CUDA;

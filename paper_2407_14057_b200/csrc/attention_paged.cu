@@ -166,12 +166,12 @@ paged_wide_kernel(const PagedArgs a, int group, int tiles, int splits, int per_s
 template <typename T>
 __global__ void __launch_bounds__(AS_THREADS)
 paged_merge_kernel(const PagedArgs a, const float *__restrict__ part_o, const float *__restrict__ part_ml, int tiles, int splits) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int h = blockIdx.x, r = blockIdx.y;
   const int s = a.cu_q ? paged_find_seq(a.cu_q, a.n_seqs, r) : r;
   int start, rows, len;
   if (s < 0 || !paged_seq(a.kv, a.cu_q, s, a.n_rows, a.max_q, a.max_kv, false, nullptr, start, rows, len) || r < start || r >= start + rows)
     return;  // the row is left as it was
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int group = a.n_heads / a.n_kv_heads, g = h / group, c = (r - start) * group + h - g * group;
   const size_t part = ((((size_t)s * a.n_kv_heads + g) * tiles + c / PW_COLS) * PW_COLS + c % PW_COLS) * splits;
   attn_split_merge<T>(part_o + part * a.head_dim, part_ml + part * 2, splits, a.head_dim, (T *)a.o + ((size_t)r * gridDim.x + h) * a.head_dim,

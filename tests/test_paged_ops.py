@@ -72,6 +72,7 @@ def test_attention_paged_refuses(lib):
     refuse(f, PAGED, CAPACITY, floats=0)
     refuse(f, PAGED, CAPACITY, n_rows=65536)
     refuse(f, PAGED, CAPACITY, n_seqs=65536)
+    refuse(f, PAGED, CAPACITY, n_rows=65535, max_q=1 << 30, H=65535, Hkv=1, ldq=65535 * 64, floats=1 << 60)
     refuse(f, PAGED, 0, n_rows=0)
     g = lib.lazy_k_attention_paged_scratch_floats
     assert g(2, 1, 2, 40, 4, 3, 64) == 0 and g(-1, 1, 2, 40, 4, 2, 64) == 0 and g(2, 1, 2, -1, 4, 2, 64) == 0

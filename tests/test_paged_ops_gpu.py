@@ -406,6 +406,46 @@ def test_attention_paged_leaves_others_alone(heads):
     assert torch.equal(got[2], want[2])
 
 
+@pytest.mark.parametrize("page", [1, 5, 16, 48, 64, 100])
+@pytest.mark.parametrize("heads", [(28, 4, 128, BF16), (40, 2, 64, BF16), (8, 8, 96, BF16), (6, 2, 192, BF16), (9, 3, 128, F32)])
+def test_attention_paged_page_sizes_and_columns(heads, page):
+    """Pages that end inside a group of keys or hold several, heads and rows that do not divide a tile of columns; both launch shapes."""
+    rows, lens = [1, 9, 3, 2], [64, 128, 3, 1500]
+    pool, q, dq = attention_case(page, rows, lens, heads, page, "wide" if page == 48 else "heads")
+    for bound in (1500, 1 << 20):
+        got = B.lazy_k_attention_paged(dq, *pool.args(), bound, cu_q=cu(rows), max_q=9)
+        B.lazy_device_status()
+        check_attention(pool, q, rows, lens, heads, got)
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128, BF16), (4, 4, 64, F32)])
+def test_attention_paged_large_logits(heads):
+    """Logits that grow along the keys by far more than the exponential's range, and that are all the same."""
+    H, Hkv, dh, dtype = heads
+    for lens in ([300], [5000]):
+        pool, q, dq = attention_case(2, [1], lens, heads, 16, "slots")
+        p, t = R.slots(pool.table[0], 16, lens[0])
+        ramp = torch.linspace(-40.0, 40.0, lens[0])[:, None, None].expand(-1, Hkv, dh).to(dtype).cuda()
+        for k, want_row in ((ramp, None), (torch.zeros_like(ramp), None), (-ramp, None)):
+            pool.k[p.tolist(), t.tolist()] = k
+            dq.fill_(1.0)
+            got = B.lazy_k_attention_paged(dq, *pool.args(), lens[0])
+            check_attention(pool, torch.ones_like(q), [1], lens, heads, got)
+    B.lazy_device_status()
+
+
+def test_attention_paged_shares_pages():
+    """Sequences that share the pages of a prefix, and a page named twice by one sequence."""
+    heads = (8, 2, 128, BF16)
+    pool, q, dq = attention_case(8, [1, 1, 1], [100, 90, 64], heads, 16, "slots")
+    pool.table[1, :4] = pool.table[0, :4]
+    pool.table[2, 3] = pool.table[2, 0]
+    table = torch.from_numpy(pool.table).cuda()
+    got = B.lazy_k_attention_paged(dq, pool.k, pool.v, table, pool.d_len, 100)
+    B.lazy_device_status()
+    check_attention(pool, q, [1, 1, 1], [100, 90, 64], heads, got)
+
+
 @pytest.mark.parametrize("heads", [(8, 2, 128, BF16), (4, 4, 64, F32)])
 def test_attention_paged_infinite_values(heads):
     """A token's infinite value reaches the rows that see it, and no row before."""
@@ -589,6 +629,22 @@ def test_logprobs_of_masked_and_odd_rows(V, k, dtype):
     got = B.lazy_k_token_logprobs(x.cuda(), tokens.cuda(), k)
     B.lazy_device_status()
     check_logprobs(x, tokens, k, got)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,V,k", [(300, 9000, 64), (900, 4099, 20), (1, 131072, 64), (40, 70000, 33), (2000, 300, 3)])
+def test_logprobs_shapes_of_a_launch(n, V, k, dtype):
+    """Rows to a CTA, rows in turn, rows to clusters: a few of them by the formula, others against themselves alone (two sums that are
+    off by (V / 512 + 24) u each: 3.4e-5 for the largest)."""
+    x, tokens, dx = logits_case(n, n, V, dtype, 2)
+    got = B.lazy_k_token_logprobs(dx, tokens.cuda(), k)
+    B.lazy_device_status()
+    some = sorted({0, 1 % n, n // 2, n - 1})
+    check_logprobs(x[some], tokens[some], k, [t[some] for t in got])
+    for a in range(0, n, max(1, n // 3)):
+        one = B.lazy_k_token_logprobs(dx[a:a + 1], tokens[a:a + 1].cuda(), k)
+        assert torch.equal(one[3][0], got[3][a]) and torch.equal(one[2][0], got[2][a])
+        assert torch.allclose(one[0][0], got[0][a], rtol=1e-5, atol=4e-5) and torch.allclose(one[1][0], got[1][a], rtol=1e-5, atol=4e-5)
 
 
 def test_logprobs_report_a_token_that_is_not_there():
