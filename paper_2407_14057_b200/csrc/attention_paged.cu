@@ -288,7 +288,10 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
   long long base = 0, total = 0, u0 = 0, u1 = 1;
   int ctas = 1;
   PgSeq seq;
-  auto page_of = [&](int s, int j) { return a.kv.table[(size_t)s * a.kv.ld_table + j / a.kv.page_size]; };
+  const int shift = (a.kv.page_size & (a.kv.page_size - 1)) == 0 ? __ffs(a.kv.page_size) - 1 : -1;  // of a power of two: no divisions
+  auto nth_page = [&](int j) { return shift >= 0 ? j >> shift : j / a.kv.page_size; };
+  auto page_of = [&](int s, int j) { return a.kv.table[(size_t)s * a.kv.ld_table + nth_page(j)]; };
+  const long long slot_stride = a.kv.slot_stride, mine_in_run = rows_mine<HD>(slot_stride);
   auto first_of = [&](int c) { return total * c / ctas; };
   if (JOIN) {
     int pair = blockIdx.x / csize;
@@ -387,16 +390,18 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
       next = ask(i + 1);
       if (i < count && j0 < seq.len) {
         const bool in = (uint32_t)page < (uint32_t)a.kv.n_pages;
-        if (!in && (WHOLE ? lane == 0 : j0 + (lane & 15) < seq.len)) dev_fail(status, LAZY_E_BADARG, W_PAGED, s, page);
-        const int j = WHOLE ? j0 : min(j0 + (lane & 15), seq.len - 1), at = j % a.kv.page_size, left = seq.len - j0;
-        const long long off = (long long)page * a.kv.page_stride + (long long)at * a.kv.slot_stride;
-        const uint32_t pages = __ballot_sync(0xffffffffu, in), ok = WHOLE ? (in ? 0xffffu : 0u) : pages & 0xffffu;
+        const int j = WHOLE ? j0 : min(j0 + (lane & 15), seq.len - 1), left = seq.len - j0;
+        const int at = shift >= 0 ? j & (a.kv.page_size - 1) : j - nth_page(j) * a.kv.page_size;
+        const long long off = page * a.kv.page_stride + at * slot_stride;
         const uint32_t to = stages + put * Rows::STAGE;
+        uint32_t ok = 0xffffu;
         if (WHOLE && in && left >= RM_KEYS) {
-          rows_load_run<HD>(to, kp + off, vp + off, a.kv.slot_stride);
+          rows_load_run<HD>(to, kp + off, vp + off, slot_stride, mine_in_run);
         } else {
+          if (!in && (WHOLE ? lane == 0 : j0 + (lane & 15) < seq.len)) dev_fail(status, LAZY_E_BADARG, W_PAGED, s, page);
+          ok &= __ballot_sync(0xffffffffu, in);  // WHOLE: all lanes alike
           rows_load<HD>(to, [&](int r, const bf16 *&kr, const bf16 *&vr) {
-            const long long o = WHOLE ? off + r * a.kv.slot_stride : __shfl_sync(0xffffffffu, off, r);
+            const long long o = WHOLE ? off + r * slot_stride : __shfl_sync(0xffffffffu, off, r);
             const bool there = (ok >> r & 1u) && r < left;
             kr = kp + (there ? o : 0);
             vr = vp + (there ? o : 0);

@@ -76,16 +76,22 @@ __device__ __forceinline__ void rows_load(uint32_t stage, Rows rows) {
   }
 }
 
-// The same for 16 rows that lie `stride` elements apart from kr / vr on, all of them there: fewer instructions to an address.
+// The same for 16 rows that lie `stride` elements apart from kr / vr on, all of them there: fewer instructions to an address.  `mine` is
+// rows_mine(stride), this lane's place in the first of them.
 template <int HD>
-__device__ __forceinline__ void rows_load_run(uint32_t stage, const bf16 *kr, const bf16 *vr, long long stride) {
+__device__ __forceinline__ long long rows_mine(long long stride) {
   const int lane = threadIdx.x & 31;
+  constexpr int CHUNKS = HD / 8;
+  return 32 % CHUNKS == 0 ? (lane / CHUNKS) * stride + lane % CHUNKS * 8 : 0;
+}
+template <int HD>
+__device__ __forceinline__ void rows_load_run(uint32_t stage, const bf16 *kr, const bf16 *vr, long long stride, long long mine) {
   constexpr int CHUNKS = HD / 8;
   if constexpr (32 % CHUNKS == 0) {  // a lane stays in its column, rows advance by 32 / CHUNKS
     constexpr int STEP = 32 / CHUNKS;
-    const int r0 = lane / CHUNKS, c = lane % CHUNKS;
-    kr += r0 * stride + c * 8;
-    vr += r0 * stride + c * 8;
+    const int lane = threadIdx.x & 31, r0 = lane / CHUNKS, c = lane % CHUNKS;
+    kr += mine;
+    vr += mine;
 #pragma unroll
     for (int i = 0; i < RM_KEYS / STEP; ++i) {
       const uint32_t to = stage + rows_at<HD>(r0 + i * STEP, c);
