@@ -229,7 +229,7 @@ template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS, (LP_CTAS<T, THREADS>))
 token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
   constexpr int V = Elem<T>::kPerVec, LOADS = LP_LOADS<T>, AHEAD = LP_AHEAD<T>, STEP = THREADS * 16, WARPS = THREADS / 32;
-  extern __shared__ __align__(16) uint4 lp_rounds[];  // [AHEAD][LOADS][THREADS]
+  extern __shared__ __align__(128) uint4 lp_rounds[];  // [AHEAD][LOADS][THREADS]
   __shared__ LpShared<THREADS> sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, k = a.n_top;
   const int rank = (int)co_cluster_rank(), size = (int)co_cluster_size(), size_log2 = 31 - __clz(size);
