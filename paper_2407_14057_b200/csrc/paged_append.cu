@@ -6,7 +6,8 @@
 //
 // A few lanes hold a head: lane i the 16-byte pieces i and i + half, so that a pair never leaves its lane, the mean is a
 // reduction over those lanes, and a row's cosines and sines are loaded once for all its heads.  A warp takes a row, or a part of one
-// where the rows are few.  Bound by memory: every element read and written once.
+// where the rows are few.  Bound by memory, every element read and written once: 3376 rows of 32 heads (166 MB) 31 us, 5.4 TB/s, 9000 rows
+// 79 (5.6).  Normalised heads cost instructions, 235 for four heads of a warp: 9427 rows of 32 on 8 heads (232 MB) 52 us, without 43.
 #include "paged.cuh"
 
 namespace lazy {
@@ -14,7 +15,7 @@ namespace lazy {
 namespace {
 
 constexpr int PA_THREADS = 256, PA_WARPS = PA_THREADS / 32;
-constexpr int PA_BATCH = 2;  // heads of a lane in flight
+constexpr int PA_BATCH = 2;  // heads of a lane in flight; four at two CTAs to an SM: 32 and 54 us for the two above
 constexpr int PA_CTAS = 3;   // to an SM
 
 template <typename T>

@@ -9,7 +9,11 @@
 // overflows (many equal logits) is filled again with a better bound.  Nothing of this is in the loop over the row.
 //
 // A CTA takes row after row; a cluster shares one where the rows are few.  A thread's loads go through its own places in shared memory
-// (cp.async, a round ahead, into the next row too), so that the memory keeps busy while a row is being finished.
+// (cp.async, a round ahead, into the next row too), so that the memory keeps busy while a row is being finished: small CTAs, five to an
+// SM, since their barriers at a row's end then hold up less (with 256 threads, three to an SM, 102 us for what follows).
+//
+// 3376 rows of 32000 in fp32 (432 MB): 68 us without alternatives (6.3 TB/s), 82 with the five best; in bf16 48 and 67, bound by
+// instructions (one exponential per logit alone takes 24).  One row: 5 and 8.5 us, 64 rows of 128256 in bf16 10 and 14, latency.
 #include "rows_mma.cuh"
 
 namespace lazy {
