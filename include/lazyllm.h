@@ -511,7 +511,7 @@ int lazy_k_rope_table(void *stream, float *table, int32_t max_pos, int32_t head_
  * max_pos, else the row is reported and skipped); arithmetic in fp32, rounded once.  q goes to q_out (pitch ldq_out; may be q
  * itself), k and v to their slot, and k to k_out as well (pitch ldk_out; may be k itself) unless that is NULL.  q rows of pitch
  * ldq, k and v rows of pitch ldkv: parts of one fused projection's rows.  rope_table: 16-byte aligned, [max_pos, head_dim / 2, 2].
- * Two rows must not share a slot. */
+ * Two rows must not share a slot.  n_rows and n_seqs <= 2^30. */
 int lazy_k_paged_append(void *stream, int32_t dtype, const void *q, int32_t ldq, const void *k, const void *v, int32_t ldkv,
                         const int32_t *pos, const float *rope_table, int32_t max_pos, const void *g_q, const void *g_k,
                         float eps, const int32_t *d_cu_q, int32_t n_rows, int32_t n_seqs, const lazy_pages *pages,
@@ -519,7 +519,7 @@ int lazy_k_paged_append(void *stream, int32_t dtype, const void *q, int32_t ldq,
                         int32_t ldk_out);
 /* Attention over a paged cache: o [n_rows, n_heads * head_dim] = softmax(q k / sqrt(head_dim)) v, row i of T over the
  * first len - T + i + 1 tokens of its sequence (one row: all of them).  At most max_q rows and max_kv tokens to a
- * sequence (any numbers that none exceeds; they size the launch and the scratch).  A row whose pages are all outside the pool gives zeros.  n_rows
+ * sequence (any numbers that none exceeds; they size the launch and the scratch, and close ones let small calls run in one launch).  A row whose pages are all outside the pool gives zeros.  n_rows
  * and n_seqs <= 65535, rows of a sequence times query heads of a key/value head <= 2^30.  bf16 up to a width of 128 runs on tensor cores,
  * the keys read once for every 16 columns ((row, head) pairs of a key/value head), else on CUDA cores, once for every four. */
 size_t lazy_k_attention_paged_scratch_floats(int32_t n_rows, int32_t n_seqs, int32_t max_q, int32_t max_kv, int32_t n_heads,
@@ -537,7 +537,7 @@ int lazy_k_attention_paged(void *stream, int32_t dtype, const void *q, int32_t l
  * have probability 0 (log p -infinity); a row with a NaN, with +infinity or with nothing above -infinity has NaN for its log
  * p and entropy, as the formula.  A negative token stands for none: logprob 0, rank -1; one >= vocab is reported and taken as none;
  * the rank of a NaN logit is -1.  logprob, entropy and rank may be NULL; tokens too, if logprob and rank are.  n_top <= LAZY_MAX_TOP
- * and <= vocab.  fp32 inside. */
+ * and <= vocab; n_rows and vocab <= 2^30.  fp32 inside. */
 #define LAZY_MAX_TOP 64
 int lazy_k_token_logprobs(void *stream, int32_t dtype, const void *logits, int64_t ld, const int32_t *tokens, int32_t n_rows,
                           int32_t vocab, int32_t n_top, float *logprob, float *entropy, int32_t *rank, int32_t *top_id,

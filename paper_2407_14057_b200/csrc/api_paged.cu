@@ -6,6 +6,7 @@ using namespace lazy;
 
 namespace {
 
+constexpr int MAX_ROWS = 1 << 30;
 constexpr long long MAX_COLUMNS = 1 << 30;  // rows of a sequence times query heads of a key/value head
 
 // The pages as the kernels take them.
@@ -38,6 +39,7 @@ int lazy_k_paged_append(void *stream, int32_t dtype, const void *q, int32_t ldq,
                         int32_t ldk_out) {
   if (bad_dtype(dtype) || n_rows < 0 || n_seqs < 0 || max_pos < 0 || !(eps >= 0.f)) return LAZY_E_BADARG;
   LAZY_TRY(check_heads(n_heads, n_kv_heads, head_dim));
+  if (n_rows > MAX_ROWS || n_seqs > MAX_ROWS) return LAZY_E_CAPACITY;
   if (n_rows == 0) return LAZY_OK;
   if (n_seqs == 0 || (!d_cu_q && n_rows != n_seqs)) return LAZY_E_BADARG;
   const long long wq = (long long)n_heads * head_dim, wk = (long long)n_kv_heads * head_dim;
@@ -85,7 +87,7 @@ int lazy_k_token_logprobs(void *stream, int32_t dtype, const void *logits, int64
                           int32_t vocab, int32_t n_top, float *logprob, float *entropy, int32_t *rank, int32_t *top_id,
                           float *top_logprob) {
   if (bad_dtype(dtype) || n_rows < 0 || vocab < 1 || ld < vocab || n_top < 0 || n_top > LAZY_MAX_TOP || n_top > vocab) return LAZY_E_BADARG;
-  if (vocab > (1 << 30)) return LAZY_E_CAPACITY;
+  if (vocab > (1 << 30) || n_rows > MAX_ROWS) return LAZY_E_CAPACITY;
   if (n_rows == 0) return LAZY_OK;
   if (!logits || ((uintptr_t)logits & (dtype == LAZY_F32 ? 3 : 1)) || (n_top > 0 && (!top_id || !top_logprob))) return LAZY_E_BADARG;
   if (!tokens && (logprob || rank)) return LAZY_E_BADARG;

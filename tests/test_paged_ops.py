@@ -58,6 +58,8 @@ def test_append_refuses(lib):
     for change in BAD_PAGES:
         refuse(f, APPEND, BADARG, pages=dict(PAGES, **change))
     refuse(f, APPEND, CAPACITY, H=65536, Hkv=2)
+    refuse(f, APPEND, CAPACITY, n_rows=(1 << 30) + 1)
+    refuse(f, APPEND, CAPACITY, n_seqs=2 ** 31 - 1)
     refuse(f, APPEND, 0, n_rows=0, q=None, k=None, v=None, pages=None)
 
 
@@ -86,6 +88,7 @@ def test_logprobs_refuses(lib):
                    dict(n_top=-1), dict(n_top=65), dict(vocab=4), dict(ld=(1 << 30), vocab=-1)]:
         refuse(f, LOGPROBS, BADARG, **change)
     refuse(f, LOGPROBS, CAPACITY, ld=1 << 31, vocab=(1 << 30) + 1)
+    refuse(f, LOGPROBS, CAPACITY, n_rows=2 ** 31 - 1)
     refuse(f, LOGPROBS, 0, n_rows=0, logits=None)
 
 
