@@ -210,15 +210,16 @@ __device__ __noinline__ int lp_before(const u64 *list, int n, u64 mine, int shar
   for (int o = share >> 1; o > 0; o >>= 1) at += __shfl_xor_sync(0xffffffffu, at, o);
   return at;
 }
-// Calls write(place, key) for the `want` best of n keys (0: no key), a few threads to a key; by the whole CTA.
+// Calls write(place, key) for those of keys [from, from + count) that are among the `want` best of all n (0: no key), a few threads to a
+// key; by the whole CTA.
 template <int THREADS, typename Write>
-__device__ __forceinline__ void lp_best(const u64 *list, int n, int want, Write write) {
+__device__ __forceinline__ void lp_best(const u64 *list, int n, int from, int count, int want, Write write) {
   int share = 1;
-  while (share < 32 && share * 2 * n <= THREADS) share *= 2;
+  while (share < 32 && share * 2 * count <= THREADS) share *= 2;
   const int each = THREADS / share, first = (threadIdx.x & ~31) / share;
-  for (int i0 = 0; i0 + first < n; i0 += each) {  // the whole warp alike
+  for (int i0 = 0; i0 + first < count; i0 += each) {  // the whole warp alike
     const int i = i0 + threadIdx.x / share;
-    const u64 mine = i < n ? list[i] : 0ull;
+    const u64 mine = i < count ? list[from + i] : 0ull;
     const int at = lp_before(list, n, mine, share);
     if (mine != 0ull && at < want && (threadIdx.x & (share - 1)) == 0) write(at, mine);
   }
@@ -482,13 +483,13 @@ token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
         __syncthreads();
         n = (int)sh.bound;
       }
-      lp_best<THREADS>(sh.list, n, want, [&](int at, u64 key) { sh.best[at] = key; });
+      lp_best<THREADS>(sh.list, n, 0, n, want, [&](int at, u64 key) { sh.best[at] = key; });
     }
     for (int i = want + tid; i < k; i += THREADS) sh.best[i] = 0ull;  // less than everything
     if (size > 1) co_cluster_sync();
     else __syncthreads();
     // ---- the row's outputs
-    if (rank == 0) {
+    if (rank == 0 || k > 0) {
       LpTotal total = sh.total;
       higher = sh.all_higher;
       if (size > 1) {
@@ -503,7 +504,7 @@ token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
         higher = __reduce_add_sync(0xffffffffu, higher);
       }
       const float log2_s = log2f(total.s), log_s = LP_LN2 * log2_s;
-      if (tid == 0) {
+      if (tid == 0 && rank == 0) {
         if (a.logprob) a.logprob[r] = token >= 0 ? (given - total.m) - log_s : 0.f;
         if (a.entropy) a.entropy[r] = LP_LN2 * (log2_s - total.t / total.s);
         if (a.rank) a.rank[r] = token >= 0 && given == given ? higher : -1;
@@ -514,10 +515,10 @@ token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
       };
       if (size == 1) {
         if (tid < k) write(tid, sh.best[tid]);
-      } else if (k > 0) {
+      } else if (k > 0) {  // every CTA places its own among all
         for (int i = tid; i < size * k; i += THREADS) sh.list[i] = *co_map_shared(&sh.best[i % k], i / k);
         __syncthreads();
-        lp_best<THREADS>(sh.list, size * k, k, write);
+        lp_best<THREADS>(sh.list, size * k, rank * k, k, k, write);
       }
     }
     if (size > 1) co_cluster_sync();  // the parts have been read
