@@ -13,7 +13,7 @@
 // SM, since their barriers at a row's end then hold up less (with 256 threads, three to an SM, 102 us for what follows).
 //
 // 3376 rows of 32000 in fp32 (432 MB): 68 us without alternatives (6.3 TB/s), 82 with the five best; in bf16 48 and 67, bound by
-// instructions (one exponential per logit alone takes 24).  One row: 5 and 8.5 us, 64 rows of 128256 in bf16 10 and 14, latency.
+// instructions (one exponential per logit alone takes 24).  One row: 4.6 and 7.6 us, 64 rows of 128256 in bf16 10 and 14, latency.
 #include "rows_mma.cuh"
 
 namespace lazy {
@@ -535,14 +535,16 @@ struct LpShape {
   double us;
 };
 // A row takes the longest of its share of the memory's rate (44 B/ns to an SM), of what an SM sums (13 logits a ns), and of a round trip
-// to every round, and then some time to be finished: 2 us, another 2 to join the parts of a cluster.
+// to every round, and then some time to be finished: 2 us; to join the parts of a cluster of two another 2, and 0.75 for each doubling.
+// One row with five alternatives, by one CTA, four and eight: of 16000 logits 7.7 us / - / 8.9, 32000 - / 8.0 / 9.0, 50257 - / 9.5 / 8.5.
 template <typename T, int THREADS>
 LpShape lp_shape(const LogprobArgs &a, int cluster) {
   constexpr int CTAS = LP_CTAS<T, THREADS>;
   const int at_once = (cluster <= 2 ? sm_count() * CTAS : co_cluster_ctas(cluster, CTAS < 3 ? CTAS : 3)) / cluster;
   auto wave = [&](int rows) {
     const double per_sm = rows * cluster <= sm_count() ? 1.0 : (double)rows * cluster / sm_count(), n = (double)a.vocab / cluster;
-    return rows == 0 ? 0.0 : fmax(n * per_sm * fmax(sizeof(T) / 44.0, 1.0 / 13.0), n / (0.025 * THREADS)) * 1e-3 + (cluster > 1 ? 4.0 : 2.0);
+    const double finish = 2.0 + (cluster > 1 ? 1.25 + 0.75 * log2(cluster) : 0.0);
+    return rows == 0 ? 0.0 : fmax(n * per_sm * fmax(sizeof(T) / 44.0, 1.0 / 13.0), n / (0.025 * THREADS)) * 1e-3 + finish;
   };
   return {THREADS, cluster, at_once, a.n_rows / at_once * wave(at_once) + wave(a.n_rows % at_once)};
 }
