@@ -77,7 +77,8 @@ int lazy_k_attention_paged(void *stream, int32_t dtype, const void *q, int32_t l
   if (a.max_kv > most) a.max_kv = most;
   if (a.max_q > n_rows) a.max_q = n_rows;
   if ((long long)a.max_q * (n_heads / n_kv_heads) > MAX_COLUMNS) return LAZY_E_CAPACITY;
-  if (scratch_floats < attention_paged_scratch_need(n_rows, n_seqs, a.max_q, a.max_kv, n_heads, n_kv_heads, head_dim)) return LAZY_E_CAPACITY;
+  if (scratch_floats < attention_paged_scratch_need(dtype, n_rows, n_seqs, a.max_q, a.max_kv, n_heads, n_kv_heads, head_dim))
+    return LAZY_E_CAPACITY;
   DevStatus *status = dev_status_ptr();
   if (!status) return LAZY_E_CUDA;
   return launch_attention_paged((cudaStream_t)stream, dtype, a, scratch, status);

@@ -687,20 +687,21 @@ bool paged_mma_eligible(int dtype, int head_dim) { return dtype == LAZY_BF16 && 
 
 }  // namespace
 
-// What the call needs, or (`any`) as much as any smaller one does.
-static size_t paged_scratch_floats(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim, bool any) {
+// What the call needs: parts of keys that are not split go straight to the outputs.
+size_t attention_paged_scratch_need(int dtype, int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
+  max_q = min(max_q, n_rows);
+  if (paged_mma_eligible(dtype, head_dim)) return pg_scratch_floats(pg_blocks((long long)max_q * (n_heads / n_kv_heads)), head_dim);
+  const long long pairs = paged_wide_tiles(max_q, n_heads, n_kv_heads) * n_kv_heads * n_seqs;
+  const int splits = paged_wide_splits(pairs, max_kv);
+  return splits == 1 ? 0 : (size_t)pairs * splits * PW_COLS * (head_dim + 2);
+}
+// As much as that call or any smaller one needs, of either type.
+size_t attention_paged_scratch_floats(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
   max_q = min(max_q, n_rows);
   const long long pairs = paged_wide_tiles(max_q, n_heads, n_kv_heads) * n_kv_heads * n_seqs;
-  const size_t parts = any ? attn_split_parts(pairs, max_kv) : (size_t)pairs * paged_wide_splits(pairs, max_kv);
-  const size_t wide = parts * PW_COLS * (head_dim + 2);
+  const size_t wide = attn_split_parts(min(pairs, attn_split_most()), max_kv) * PW_COLS * (head_dim + 2);
   const size_t mma = head_dim <= 128 ? pg_scratch_floats(pg_blocks((long long)max_q * (n_heads / n_kv_heads)), head_dim) : 0;
   return wide > mma ? wide : mma;
-}
-size_t attention_paged_scratch_need(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
-  return paged_scratch_floats(n_rows, n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim, false);
-}
-size_t attention_paged_scratch_floats(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim) {
-  return paged_scratch_floats(n_rows, n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim, true);
 }
 
 template <int HD, bool WHOLE>

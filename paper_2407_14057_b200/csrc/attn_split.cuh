@@ -170,6 +170,8 @@ inline int attn_split_count(long long rows_heads, int n_keys) {
   const long long per = (tiles + want - 1) / want;
   return (int)((tiles + per - 1) / per);
 }
+// Pairs whose keys may be split: with more there are CTAs enough without.
+inline long long attn_split_most() { return 4LL * sm_count() - 1; }
 // The most ranges that any number of pairs up to rows_heads makes of up to n_keys, times the pairs.
 inline size_t attn_split_parts(long long rows_heads, int n_keys) {
   const long long tiles = cdiv(n_keys > 0 ? n_keys : 1, AS_TILE), all = rows_heads * tiles, most = rows_heads + 4LL * sm_count() - 1;

@@ -415,7 +415,7 @@ struct PagedArgs {
   int n_heads, n_kv_heads, head_dim;
   void *o;
 };
-size_t attention_paged_scratch_need(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim);
+size_t attention_paged_scratch_need(int dtype, int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim);
 size_t attention_paged_scratch_floats(int n_rows, int n_seqs, int max_q, int max_kv, int n_heads, int n_kv_heads, int head_dim);
 int launch_attention_paged(cudaStream_t st, int dtype, const PagedArgs &a, float *scratch, DevStatus *status);
 struct LogprobArgs {

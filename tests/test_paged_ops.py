@@ -109,3 +109,24 @@ def test_scratch_for_the_largest_serves_every_smaller_call(lib):
         s, t = rng.randint(1, n_seqs), rng.randint(1, max_q)
         less = (rng.randint(1, min(rows, s * t)), s, t, rng.randint(1, max_kv), H, Hkv, dh)
         assert f(*less) <= a, (rows, n_seqs, max_q, max_kv, less)
+
+
+@pytest.mark.parametrize("heads", [(32, 8, 128), (32, 32, 64), (8, 1, 128), (32, 8, 256)])
+def test_scratch_of_a_mixed_batch(lib, heads):
+    """A chunk among single tokens, a server's ordinary step: parts of keys that are not split need no place."""
+    f = lib.lazy_k_attention_paged_scratch_floats
+    for n_seqs, chunk in [(64, 512), (64, 4096), (256, 8192), (2000, 30000)]:
+        assert f(n_seqs - 1 + chunk, n_seqs, chunk, 32768, *heads) * 4 < 16 << 20, (n_seqs, chunk)
+        refuse(lib.lazy_k_attention_paged, PAGED, CAPACITY, n_rows=n_seqs - 1 + chunk, n_seqs=n_seqs, max_q=chunk, floats=0)
+
+
+def test_scratch_of_mixed_batches_serves_smaller_calls(lib):
+    """As above, where the largest call's keys are not split and a smaller one's are."""
+    rng = random.Random(6)
+    f = lib.lazy_k_attention_paged_scratch_floats
+    for _ in range(20000):
+        H, Hkv, dh = rng.choice([(32, 8, 128), (8, 1, 128), (16, 4, 64), (4, 2, 256), (40, 1, 64), (12, 2, 192)])
+        n_seqs, max_q, max_kv = _sizes(rng, 3000), _sizes(rng, 20000), _sizes(rng, 200000)
+        rows = min(65535, n_seqs - 1 + max_q)
+        s, t, r, L = _sizes(rng, n_seqs), _sizes(rng, max_q), _sizes(rng, rows), _sizes(rng, max_kv)
+        assert f(r, s, t, L, H, Hkv, dh) <= f(rows, n_seqs, max_q, max_kv, H, Hkv, dh), (rows, n_seqs, max_q, max_kv, r, s, t, L)

@@ -824,3 +824,21 @@ def test_a_prompt_then_tokens_from_pages():
     accepted, tokens = B.lazy_k_verify(p, draft, i32([0, 3]), 3, u, torch.tensor([0.0], device="cuda"))
     assert accepted.item() == 3 and torch.equal(tokens[0, :3], draft)
     B.lazy_device_status()
+
+
+# ------------------------------------------------------------------------------------------- mixed batches
+@pytest.mark.parametrize("heads", [(8, 2, 128, BF16), (4, 4, 64, BF16), (4, 2, 64, F32), (2, 1, 256, BF16)])
+def test_attention_paged_of_a_mixed_batch(heads):
+    """A long chunk behind cached tokens among single tokens, with scratch of the size asked for and no more."""
+    H, Hkv, dh, dtype = heads
+    rows = [1] * 20 + [1100, 0] + [1] * 9
+    lens = [1 + 97 * i % 700 for i in range(20)] + [1500, 40] + [2000, 1, 16, 17, 300, 5, 64, 1024, 33]
+    pool, q, dq = attention_case(60, rows, lens, heads, 16, "slots")
+    floats = B.lazy_k_attention_paged_scratch(sum(rows), len(rows), 1100, 2000, H, Hkv, dh).numel()
+    assert floats * 4 < 16 << 20
+    scratch = torch.full((floats + 64,), float("nan"), device="cuda")
+    scratch[floats:] = 7.0
+    got = B.lazy_k_attention_paged(dq, *pool.args(), 2000, cu_q=cu(rows), max_q=1100, scratch=scratch[:floats])
+    B.lazy_device_status()
+    assert torch.all(scratch[floats:] == 7.0)
+    check_attention(pool, q, rows, lens, heads, got)
