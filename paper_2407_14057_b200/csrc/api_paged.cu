@@ -1,4 +1,6 @@
 // Entry points of the operators on paged caches and of the log probabilities: argument checks, then the launchers.
+#include <algorithm>
+
 #include "api_checks.cuh"
 #include "paged.cuh"
 
@@ -59,6 +61,9 @@ int lazy_k_paged_append(void *stream, int32_t dtype, const void *q, int32_t ldq,
 size_t lazy_k_attention_paged_scratch_floats(int32_t n_rows, int32_t n_seqs, int32_t max_q, int32_t max_kv, int32_t n_heads,
                                              int32_t n_kv_heads, int32_t head_dim) {
   if (n_rows < 0 || n_seqs < 0 || max_q < 0 || max_kv < 0 || check_heads(n_heads, n_kv_heads, head_dim) != LAZY_OK) return 0;
+  // bounds may be any numbers: no call has more rows or sequences
+  n_rows = std::min(n_rows, MAX_GRID_YZ);
+  n_seqs = std::min(n_seqs, MAX_GRID_YZ);
   return attention_paged_scratch_floats(n_rows, n_seqs, max_q, max_kv, n_heads, n_kv_heads, head_dim);
 }
 

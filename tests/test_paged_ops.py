@@ -130,3 +130,13 @@ def test_scratch_of_mixed_batches_serves_smaller_calls(lib):
         rows = min(65535, n_seqs - 1 + max_q)
         s, t, r, L = _sizes(rng, n_seqs), _sizes(rng, max_q), _sizes(rng, rows), _sizes(rng, max_kv)
         assert f(r, s, t, L, H, Hkv, dh) <= f(rows, n_seqs, max_q, max_kv, H, Hkv, dh), (rows, n_seqs, max_q, max_kv, r, s, t, L)
+
+
+@pytest.mark.parametrize("heads", [(32, 8, 128), (4, 2, 256), (1, 1, 64), (65535, 1, 64), (65535, 65535, 32)])
+def test_scratch_with_bounds_that_bind_nothing(lib, heads):
+    """Any numbers serve as bounds, the largest among them."""
+    f, most = lib.lazy_k_attention_paged_scratch_floats, 2 ** 31 - 1
+    for n_rows, n_seqs, max_q in [(1, 1, 1), (4, 4, most), (65535, 65535, most), (most, most, most)]:
+        want = f(min(n_rows, 65535), min(n_seqs, 65535), min(max_q, 65535), 1 << 30, *heads)
+        for max_kv in (1 << 30, most - 300, most - 127, most - 126, most):
+            assert f(n_rows, n_seqs, max_q, max_kv, *heads) == want < 1 << 24, (n_rows, n_seqs, max_q, max_kv)
