@@ -558,7 +558,6 @@ paged_mma_kernel(const PagedArgs a, int group, int max_cts, PgScratch scratch, D
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         *reinterpret_cast<uint2 *>(output(c, d)) = make_uint2(bf16x2_pack(o.x * inv, o.y * inv), bf16x2_pack(o.z * inv, o.w * inv));
       }
-      __syncwarp();
       co_cluster_sync();  // nobody leaves while its part is being read
       return;
     }

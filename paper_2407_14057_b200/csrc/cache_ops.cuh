@@ -113,13 +113,21 @@ __device__ __forceinline__ uint32_t co_cluster_size() {
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
-// All threads of all CTAs of the cluster; shared-memory writes before it are visible cluster-wide after it.
+// All threads of all CTAs of the cluster; shared-memory writes before it are visible cluster-wide after it.  The instructions want the
+// warp's lanes together: after a loop whose length differs between them, or a branch, nothing else promises that.
 __device__ __forceinline__ void co_cluster_sync() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 // The same in two steps, with work between them that needs no word from the others.
-__device__ __forceinline__ void co_cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
-__device__ __forceinline__ void co_cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+__device__ __forceinline__ void co_cluster_arrive() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void co_cluster_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
 // Address of `p` (this CTA's shared memory) in CTA `rank` of the cluster.
 template <typename T>
 __device__ __forceinline__ T *co_map_shared(T *p, uint32_t rank) {

@@ -448,7 +448,6 @@ step_fused_kernel(const EvictStepArgs a, int group, int part_slots, int logits_i
       if (j0 + i * SF_THREADS < hi) mo[j[i]] = (j[i] == slot ? 0.f : bw[i]) + w[i];
   }
   if (rank == 0 && threadIdx.x == 0) a.len_out[sg] = n;  // the cluster has read the old length long ago
-  __syncwarp();
   if (csize > 1) co_cluster_wait();                      // nobody leaves while its parts are being read
 }
 

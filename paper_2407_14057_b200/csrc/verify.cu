@@ -258,7 +258,6 @@ verify_kernel(const float *__restrict__ p, int ldp, const float *__restrict__ q,
       for (int t = threadIdx.x; t <= max_draft; t += VF_THREADS)
         if (t != acc) tokens[(size_t)s * (max_draft + 1) + t] = t < acc ? draft[d0 + t] : -1;
     }
-    __syncwarp();
     co_cluster_wait();
     return;
   }

@@ -1,6 +1,8 @@
 """Refusals of the operators on paged caches and of the log probabilities: every check answers before the device is touched."""
 import ctypes as C
+import glob
 import math
+import os
 import random
 
 import pytest
@@ -140,3 +142,18 @@ def test_scratch_with_bounds_that_bind_nothing(lib, heads):
         want = f(min(n_rows, 65535), min(n_seqs, 65535), min(max_q, 65535), 1 << 30, *heads)
         for max_kv in (1 << 30, most - 300, most - 127, most - 126, most):
             assert f(n_rows, n_seqs, max_q, max_kv, *heads) == want < 1 << 24, (n_rows, n_seqs, max_q, max_kv)
+
+
+def test_cluster_barriers_find_the_warp_together():
+    """The .aligned forms are undefined for a warp whose lanes are apart: each stands right behind a barrier that joins them."""
+    found = 0
+    for path in sorted(glob.glob(os.path.join(os.path.dirname(build.__file__), "csrc", "*.cu*"))):
+        with open(path) as f:
+            code = [line.split("//")[0].strip() for line in f]
+        for i, line in enumerate(code):
+            if "barrier.cluster." in line and ".aligned" in line and "barrier.cluster.arrive" not in code[i - 1]:
+                before = code[i - 1] if code[i - 1].startswith("__sync") else None
+                if before is None:   # at the head of a function: its callers have the barrier
+                    assert os.path.basename(path) == "tc_pair.cuh" and code[i - 1].endswith("{"), (path, i + 1)
+                found += 1
+    assert found >= 4

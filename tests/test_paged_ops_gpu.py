@@ -842,3 +842,27 @@ def test_attention_paged_of_a_mixed_batch(heads):
     B.lazy_device_status()
     assert torch.all(scratch[floats:] == 7.0)
     check_attention(pool, q, rows, lens, heads, got)
+
+
+@pytest.mark.parametrize("heads", [(1, 1, 32, BF16), (3, 3, 32, BF16), (1, 1, 96, BF16), (5, 5, 64, BF16), (2, 1, 128, BF16)])
+@pytest.mark.parametrize("lens", [[700], [3000], [130, 1, 2000]])
+def test_attention_paged_few_outputs_to_a_cluster(heads, lens):
+    """A column or two: a few lanes of one warp write the cluster's parts, and the others wait; the same bits every time."""
+    rows = [1] * len(lens)
+    pool, q, dq = attention_case(lens[0] + heads[0], rows, lens, heads, 16, "slots")
+    got = B.lazy_k_attention_paged(dq, *pool.args(), max(lens))
+    B.lazy_device_status()
+    check_attention(pool, q, rows, lens, heads, got)
+    for _ in range(20):
+        assert torch.equal(B.lazy_k_attention_paged(dq, *pool.args(), max(lens)), got)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V,k", [(9001, 1), (20011, 3), (50257, 33), (131075, 7)])
+def test_logprobs_lists_of_odd_sizes_in_clusters(V, k, dtype):
+    x, tokens, dx = logits_case(V, 3, V, dtype, 1)
+    got = B.lazy_k_token_logprobs(dx, tokens.cuda(), k)
+    B.lazy_device_status()
+    check_logprobs(x, tokens, k, got)
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(B.lazy_k_token_logprobs(dx, tokens.cuda(), k), got))
