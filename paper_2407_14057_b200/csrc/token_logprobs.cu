@@ -245,7 +245,9 @@ token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(z.raw.x), "=r"(z.raw.y), "=r"(z.raw.z), "=r"(z.raw.w) : "r"(at) : "memory");
     z.unpack(f);
   };
-  const uint32_t none = sizeof(T) == 4 ? 0xff7fffffu : 0xff7fff7fu;  // the type's lowest: adds nothing, and no NaN
+  // behind the last piece stands the type's lowest: nothing's maximum, and not summed (times log2(e) it is -infinity, which would call for
+  // the round once more)
+  const uint32_t none = sizeof(T) == 4 ? 0xff7fffffu : 0xff7fff7fu;
   // ---- rounds are asked for AHEAD - 1 ahead, row after row
   int ask_row = first, ask_i = 0, asked = 0;
   LpRow<T, THREADS> ask(a, min(ask_row, a.n_rows - 1), rank, size_log2);
@@ -319,17 +321,21 @@ token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
       if (big > sums.m) sums.raise(big);
       const u64 minus_m2 = f32x2_pack(-sums.m2, -sums.m2);
       const LpSums before_round = sums;
+      const int piece0 = row.piece(i, 0);
+      const bool whole = piece0 - lane + 31 + (LOADS - 1) * THREADS < row.p1;  // the whole warp alike
+      if (whole) {
 #pragma unroll
-      for (int u = 0; u < LOADS; ++u) {
-        float f[V];
-        fetch(from + u * STEP, f);
+        for (int u = 0; u < LOADS; ++u) {
+          float f[V];
+          fetch(from + u * STEP, f);
 #pragma unroll
-        for (int j = 0; j < V; j += 2) sums.add<false>(f[j], f[j + 1], minus_m2);
+          for (int j = 0; j < V; j += 2) sums.add<false>(f[j], f[j + 1], minus_m2);
+        }
       }
-      if (sums.wild()) {  // there are -infinities (or NaN): the round once more
+      if (!whole || sums.wild()) {  // the end of the part, or there are -infinities (or NaN): the round once more
         sums = before_round;
 #pragma unroll 1
-        for (int u = 0; u < LOADS; ++u) {
+        for (int u = 0; u < LOADS && piece0 + u * THREADS < row.p1; ++u) {
           float f[V];
           fetch(from + u * STEP, f);
 #pragma unroll
@@ -338,8 +344,8 @@ token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
       }
       // ---- ids before the token
       if (big >= given) {
-        const int p = row.piece(i, 0), before = token_piece - p;  // loads u with u * THREADS < before lie before the token's
-        if (given > -3.3e38f) {                                   // else what stands behind the last piece would count
+        const int before = token_piece - piece0;  // loads u with u * THREADS < before lie before the token's
+        if (given > -3.3e38f) {                   // else what stands behind the last piece would count
           higher += lp_count<T, THREADS>(from, given, before);
           if (before >= 0 && before < LOADS * THREADS && before % THREADS == 0) {  // the token's own piece
             float f[V];
@@ -349,10 +355,10 @@ token_logprobs_kernel(const LogprobArgs a, DevStatus *status) {
           }
         } else {
 #pragma unroll 1
-          for (int u = 0; u < LOADS && p + u * THREADS < row.p1; ++u) {
+          for (int u = 0; u < LOADS && piece0 + u * THREADS < row.p1; ++u) {
             float f[V];
             fetch(from + u * STEP, f);
-            const int id = row.offset + (p + u * THREADS) * V;
+            const int id = row.offset + (piece0 + u * THREADS) * V;
 #pragma unroll
             for (int j = 0; j < V; ++j) higher += f[j] > given || (f[j] == given && id + j < token);
           }

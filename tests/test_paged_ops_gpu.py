@@ -866,3 +866,19 @@ def test_logprobs_lists_of_odd_sizes_in_clusters(V, k, dtype):
     check_logprobs(x, tokens, k, got)
     for _ in range(20):
         assert all(torch.equal(a, b) for a, b in zip(B.lazy_k_token_logprobs(dx, tokens.cuda(), k), got))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [3, 640])
+def test_logprobs_of_parts_that_end_anywhere_in_a_round(n, dtype):
+    """The last 16 bytes of a row belong to any lane and load of a round, in a row to a CTA and in rows in turn, the rest of which is not
+    there; among masks of -infinity and of the type's lowest value."""
+    per = 16 // dtype.itemsize
+    for V in [per * (128 * u + t) + per - 1 for u, t in [(0, 1), (0, 31), (0, 33), (1, 0), (3, 127), (5, 64), (7, 32), (7, 127), (8, 0), (8, 1)]]:
+        x, tokens, dx = logits_case(V + n, n, V, dtype, V % 5)
+        x[1, V // 3:], x[2, :V // 2] = -float("inf"), torch.finfo(dtype).min
+        dx.copy_(x)
+        got = B.lazy_k_token_logprobs(dx, tokens.cuda(), 4)
+        B.lazy_device_status()
+        check_logprobs(x[:3], tokens[:3], 4, [t[:3] for t in got])
+        check_logprobs(x[-1:], tokens[-1:], 4, [t[-1:] for t in got])
