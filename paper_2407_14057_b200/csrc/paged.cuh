@@ -41,6 +41,14 @@ __device__ __forceinline__ bool paged_seq(const PagedKV &kv, const int32_t *cu, 
   return ok;
 }
 
+// Reports boundaries that do not ascend or leave the rows, those that no row leads to among them: thread `id` of `n` takes every n-th.
+__device__ __forceinline__ void paged_check_bounds(const int32_t *cu, int n_seqs, int n_rows, long long id, long long n, DevStatus *status) {
+  for (long long s = id; s < n_seqs; s += n) {
+    const int start = cu[s], end = cu[s + 1];
+    if (start < 0 || end < start || end > n_rows) dev_fail(status, LAZY_E_BADARG, W_PAGED, (int)s, end);
+  }
+}
+
 // Most tokens that a sequence's row of the table names.
 inline int paged_capacity(const PagedKV &kv) {
   const long long n = (long long)kv.table_pages * kv.page_size;

@@ -53,6 +53,7 @@ paged_append_kernel(const AppendArgs a, int lanes_log2, int parts, int steps, De
   fetch(h0);  // needs no table
   // ---- the row's place
   const int s = a.cu_q ? paged_find_seq(a.cu_q, a.n_seqs, r) : r;
+  if (a.cu_q) paged_check_bounds(a.cu_q, a.n_seqs, a.n_rows, w * 32 + lane, (long long)a.n_rows * parts * 32, status);
   if (s < 0) return;
   const int p = a.pos[r];
   int start, rows, len;

@@ -882,3 +882,17 @@ def test_logprobs_of_parts_that_end_anywhere_in_a_round(n, dtype):
         B.lazy_device_status()
         check_logprobs(x[:3], tokens[:3], 4, [t[:3] for t in got])
         check_logprobs(x[-1:], tokens[-1:], 4, [t[-1:] for t in got])
+
+
+@pytest.mark.parametrize("bounds", [[0, 4, 2], [3, 0, 7], [0, 7, 7, 5], [0, 0, 7, 9], [0, 7, -1, 7], [2, 1, 2, 7]])
+def test_append_reports_boundaries_that_no_row_leads_to(bounds):
+    """Boundaries that do not ascend or leave the rows are reported wherever they are; nothing outside the sequences' slots is written."""
+    heads, n = (2, 2, 64, BF16), len(bounds) - 1
+    pool, x, dev, pos, _ = append_case(8, [6] * n, [7] * n, heads, 4, "slots", False, False)
+    dev = [t[:7] for t in dev]
+    rope = B.lazy_k_rope_table(64, 64, 1e4)
+    before = pool.k.clone()
+    B.lazy_k_paged_append(*dev, i32(list(range(7))), rope, *pool.args(), cu_q=i32(bounds))
+    assert reported(20) == -1
+    free = [p for p in range(before.shape[0]) if p not in set(pool.table.ravel().tolist())]
+    assert free and torch.equal(pool.k[free], before[free])
