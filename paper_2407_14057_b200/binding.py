@@ -741,8 +741,10 @@ def lazy_k_rope_table(max_pos: int, head_dim: int, theta: float, out: Optional[t
     """fp32 [max_pos, head_dim // 2, 2]: the cosines and sines that lazy_k_paged_append rotates by."""
     if out is None:
         out = torch.empty((max_pos, head_dim // 2, 2), dtype=torch.float32, device="cuda")
-    elif out.numel() != max_pos * head_dim or out.dtype != torch.float32:
-        raise ValueError("out: float32 [max_pos, head_dim // 2, 2] is wanted")
+    elif out.numel() != max_pos * head_dim or out.dtype != torch.float32 or not out.is_contiguous():
+        raise ValueError("out: contiguous float32 [max_pos, head_dim // 2, 2] is wanted")
+    elif not out.is_cuda or out.get_device() != torch.cuda.current_device():
+        raise ValueError("out: a tensor on the current CUDA device is wanted")
     _check("lazy_k_rope_table", lib().lazy_k_rope_table(_stream(), _ptr(out), max_pos, head_dim, theta))
     return out
 

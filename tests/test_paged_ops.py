@@ -6,6 +6,7 @@ import os
 import random
 
 import pytest
+import torch
 
 from paper_2407_14057_b200 import binding, build
 
@@ -157,3 +158,21 @@ def test_cluster_barriers_find_the_warp_together():
                     assert os.path.basename(path) == "tc_pair.cuh" and code[i - 1].endswith("{"), (path, i + 1)
                 found += 1
     assert found >= 4
+
+
+def test_rope_table_checks_its_output():
+    t = torch.empty
+    for out in (t(4, 32, 2), t(4, 32, 4)[..., :2], t(4, 16, 2), t((4, 32, 2), dtype=torch.float64)):
+        with pytest.raises(ValueError):
+            binding.lazy_k_rope_table(4, 64, 1e4, out=out)
+
+
+def test_rope_table_refuses_another_devices_output(monkeypatch):
+    class There:
+        """As much of a tensor on device 1 as is looked at."""
+        dtype, is_cuda = torch.float32, True
+        numel, is_contiguous, get_device = (lambda self: 256), (lambda self: True), (lambda self: 1)
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="current CUDA device"):
+        binding.lazy_k_rope_table(4, 64, 1e4, out=There())
