@@ -519,8 +519,9 @@ int lazy_k_paged_append(void *stream, int32_t dtype, const void *q, int32_t ldq,
                         int32_t ldk_out);
 /* Attention over a paged cache: o [n_rows, n_heads * head_dim] = softmax(q k / sqrt(head_dim)) v, row i of T over the
  * first len - T + i + 1 tokens of its sequence (one row: all of them).  At most max_q rows and max_kv tokens to a
- * sequence (any numbers that none exceeds; they size the launch and the scratch, and close ones let small calls run in one launch).  A row whose pages are all outside the pool gives zeros.  n_rows
- * and n_seqs <= 65535, rows of a sequence times query heads of a key/value head <= 2^30.  bf16 up to a width of 128 runs on tensor cores,
+ * sequence (any numbers that none exceeds; they size the launch and the scratch, and close ones let small calls run in one launch).
+ * A row whose pages are all outside the pool gives zeros, as does one whose logits are all -infinity.  n_rows and n_seqs <= 65535,
+ * rows of a sequence times query heads of a key/value head <= 2^30.  bf16 up to a width of 128 runs on tensor cores,
  * the keys read once for every 16 columns ((row, head) pairs of a key/value head), else on CUDA cores, once for every four. */
 size_t lazy_k_attention_paged_scratch_floats(int32_t n_rows, int32_t n_seqs, int32_t max_q, int32_t max_kv, int32_t n_heads,
                                              int32_t n_kv_heads, int32_t head_dim);

@@ -896,3 +896,83 @@ def test_append_reports_boundaries_that_no_row_leads_to(bounds):
     assert reported(20) == -1
     free = [p for p in range(before.shape[0]) if p not in set(pool.table.ravel().tolist())]
     assert free and torch.equal(pool.k[free], before[free])
+
+
+# ------------------------------------------------------------------------------------------- large and odd numbers
+@pytest.mark.parametrize("offset", [9.9e6, -9.9e6, 1e7, -1e7, 1.1e7, -1.1e7, 3e7, -3e7, 2.0 ** 24 + 2, -1e12, 1e30])
+@pytest.mark.parametrize("n,V", [(3, 300), (2, 40001), (600, 1003)])
+def test_logprobs_of_rows_far_from_zero(n, V, offset):
+    """Logits that differ by a few around a large number, either side of the size from which a row is summed from the differences: the
+    rounding of the largest logit's product with log2(e), up to half a unit there, must not show."""
+    g = gen(V)
+    step = max(1.0, float(np.spacing(np.float32(abs(offset)))))
+    level = torch.floor(13.0 * torch.rand((n, V), generator=g) ** 3)          # few large ones
+    level[0] = 2.0 * (torch.arange(V) % 7 == 3)
+    x = (offset + step * level.double()).float()
+    x[1, V // 2:] = -float("inf")
+    tokens = torch.randint(0, V // 2, (n,), generator=g).to(torch.int32)
+    got = B.lazy_k_token_logprobs(x.cuda(), tokens.cuda(), 9)
+    B.lazy_device_status()
+    some = sorted({0, 1, n // 2, n - 1})
+    check_logprobs(x[some], tokens[some], 9, [t[some] for t in got])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,V", [(2, 500), (3, 32001)])
+def test_logprobs_tells_the_smallest_numbers_apart(n, V, dtype):
+    """Numbers below the smallest normal one are neither zero nor equal."""
+    g = gen(n)
+    x = torch.zeros((n, V), dtype=dtype)
+    raw = torch.int16 if dtype == BF16 else torch.int32
+    x.view(raw).copy_(torch.randint(0, 100, (n, V), generator=g).to(raw))
+    x[1] = -x[1]
+    tokens = torch.randint(0, V, (n,), generator=g).to(torch.int32)
+    got = B.lazy_k_token_logprobs(x.cuda(), tokens.cuda(), 20)
+    B.lazy_device_status()
+    check_logprobs(x, tokens, 20, got)
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128, BF16), (12, 2, 96, BF16), (4, 4, 64, F32), (2, 2, 256, BF16)])
+@pytest.mark.parametrize("length", [50, 3000])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_attention_paged_of_keys_that_are_not_finite(heads, length, bad):
+    """A key's infinity makes its logit one: all of the row is NaN, or the key has no weight; a NaN is the whole row's.  Rows that do not
+    see it have the bits that they have without."""
+    H, Hkv, dh, dtype = heads
+    rows, lens, at, col = [4], [length], length - 3, 5
+    pool, q, dq = attention_case(length + H, rows, lens, heads, 16, "slots")
+    want = f64(B.lazy_k_attention_paged(dq, *pool.args(), length, cu_q=cu(rows), max_q=4)).reshape(4, H, dh)
+    k, v = pool.rows(0, length)
+    p, t = R.slots(pool.table[0], 16, length)
+    pool.k[int(p[at]), int(t[at]), :, col] = bad
+    got = f64(B.lazy_k_attention_paged(dq, *pool.args(), length, cu_q=cu(rows), max_q=4)).reshape(4, H, dh)
+    B.lazy_device_status()
+    qn = f64(q).reshape(4, H, dh)
+    assert np.array_equal(got[0], want[0])
+    others = np.arange(length) != at
+    S = np.sqrt((qn ** 2).sum(-1).max() * (k ** 2).sum(-1).max()) * dh ** -0.5
+    E = 2 * (dh + 4) * 2 * U * S + 2.0 ** -19 + length / 16 * 4 * U
+    seen = set()
+    for i in range(1, 4):
+        for h in range(H):
+            if np.isnan(bad) or qn[i, h, col] * bad > 0:
+                assert np.all(np.isnan(got[i, h])), (i, h)
+                seen.add("nan")
+            else:
+                g, see = h // (H // Hkv), length - 4 + i + 1
+                y, size = R.attention_row(qn[i, h], k[:see, g], v[:see, g], others[:see])
+                assert np.all(np.abs(got[i, h] - y) <= E * size + half_step(dtype) * (np.abs(y) + E * size)), (i, h)
+                seen.add("left out")
+    assert seen == {"nan"} if np.isnan(bad) else seen == {"nan", "left out"}
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128, BF16), (4, 4, 64, F32), (2, 2, 256, BF16)])
+def test_attention_paged_of_a_row_without_a_finite_logit(heads):
+    """Where every logit is -infinity no key has weight: zeros, as for a row that sees no page."""
+    H, Hkv, dh, dtype = heads
+    for length in (1, 40, 2500):
+        pool, q, dq = attention_case(length, [1], [length], heads, 16, "slots")
+        dq.fill_(1.0)
+        pool.k[..., 3] = -float("inf")
+        assert torch.all(B.lazy_k_attention_paged(dq, *pool.args(), length) == 0)
+    B.lazy_device_status()
