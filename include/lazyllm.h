@@ -500,8 +500,8 @@ typedef struct {
  * of T is token len[s] - T + i.  cu_q NULL: one row per sequence (n_rows = n_seqs), none where len[s] is 0.  Rows of no sequence
  * (behind the last one: a padded batch) and their outputs are left as they are.  A sequence whose tables do not fit
  * (boundaries that do not ascend or leave the rows, len below its rows or above what its pages or max_kv allow) is reported and skipped,
- * its outputs left as they are (and, where boundaries do not ascend, maybe those of rows beside it); a page outside [0, n_pages) is reported, and its slots are neither read nor
- * written. */
+ * its outputs left as they are (and, where boundaries do not ascend, maybe those of rows beside it); a page outside [0, n_pages) is
+ * reported, and its slots are neither read nor written. */
 
 /* cos and sin of p * theta^(-2 i / head_dim), i < head_dim / 2, as pairs: table fp32 [max_pos, head_dim / 2, 2], angles in
  * 64 bits.  The table that lazy_k_paged_append takes; one made otherwise (scaled positions) serves as well. */

@@ -83,8 +83,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     try:
         build_call(force)
     except (ImportError, OSError, subprocess.CalledProcessError) as e:
-        sys.stderr.write(f"{os.path.basename(CALL_LIB)} was not built ({e}): the Python wrappers of the operators on bounded "
-                         "and shared caches will raise\n")
+        sys.stderr.write(f"{os.path.basename(CALL_LIB)} was not built ({e}): the Python wrappers of the operators on bounded, "
+                         "shared and paged caches and of the log probabilities will raise\n")
     return path
 
 

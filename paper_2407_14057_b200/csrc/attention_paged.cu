@@ -241,8 +241,8 @@ struct PgScratch {
   float *ml, *o;     // [CTAs][2][columns][2], [CTAs][2][columns][HD]
 };
 // Blocks of eight columns that a CTA takes, by the columns that a key/value head may have.  Four at a time read the keys of 32 columns
-// once instead of twice, but take the registers of a third CTA and spill: 16 sequences of 3000 tokens, 8 rows of 4 heads, 66 us with
-// four blocks, 69 with two; four sequences with drafts 25 and 20 (65 and 18.6 now).
+// once instead of twice, but take the registers of a third CTA and spill: when tried, 16 sequences of 3000 tokens, 8 rows of 4 heads, took 66 us
+// with four blocks and 69 with two, four sequences with drafts 25 and 20.  With two, later steps have brought them to 65 and 18.6.
 inline int pg_blocks(long long columns) { return columns <= 8 ? 1 : 2; }
 inline int pg_grid() { return sm_count() * PG_WIDE.ctas; }
 // floats; the parts' order in memory is splits, maxima and sums, outputs (+ 4: they start on a 16-byte boundary)

@@ -1,5 +1,5 @@
-// Marshals the arguments of the operators on bounded and shared caches: torch tensors in, the C entry points of
-// include/lazyllm.h out, their status back.  It does what the ctypes layer does for the other calls (checks of types, sizes and
+// Marshals the arguments of the operators on bounded, shared and paged caches and of the log probabilities: torch tensors in, the C
+// entry points of include/lazyllm.h out, their status back.  It does what the ctypes layer does for the other calls (checks of types, sizes and
 // devices, addresses, pitches) in one call from Python: with a dozen tensors per operator and a few microseconds of device
 // time, checking them one by one in Python costs more than the operator (14.8 us a call for the step, 9.7 for the verification).
 // No arithmetic, no state but the entry points' addresses.

@@ -1,5 +1,5 @@
 // Attention of a few query rows over keys that lie anywhere in memory, one warp at a time: the inner loop shared by
-// the step on bounded caches and by the requests' own keys behind a shared prefix.
+// the step on bounded caches, the requests' own keys behind a shared prefix, and new rows over paged caches.
 //
 // A warp takes 16 keys at a time and up to 8 NT columns, a column being one (query row, head) that reads the same
 // key/value head.  Keys are the M side of both products, so few columns waste nothing of the instruction:
@@ -8,8 +8,10 @@
 // product's operand without shared memory.  P enters as the sum of two bf16 numbers (see WEIGHT_REST), so that the only
 // rounding of an output that counts is its own: the step is bound by reading K and V, and the second product's extra
 // instructions (24 instead of 16 per 16 keys of a head width of 128, about 3 clocks per key of an SM against 22 that
-// the key's 512 bytes take) cost no time.  This is the warp-level tensor path, not tcgen05: with at most 16 columns a
-// 128-row instruction would be 7/8 padding, and keys named by lists cannot come through tensor maps.
+// the key's 512 bytes take) cost no time.  This is the warp-level tensor path, not tcgen05: with at most 16 columns the step is bound by
+// reading the keys, which a warp alone does without a wait for others, whereas a 128-row instruction wants 128 keys brought
+// together by a CTA, a tile's P back through shared or tensor memory, and barriers between.  Keys named by lists cannot come through
+// tensor maps either way.  With many columns (drafts, chunks of a prompt) the products bound the step, and that reason ends.
 //
 // Every warp owns its shared memory stages (cp.async, 16 bytes a lane, rows that do not exist read as zeros), so the
 // loop has no barrier wider than the warp.

@@ -12,8 +12,9 @@
 // (cp.async, a round ahead, into the next row too), so that the memory keeps busy while a row is being finished: small CTAs, five to an
 // SM, since their barriers at a row's end then hold up less (with 256 threads, three to an SM, 102 us for what follows).
 //
-// 3376 rows of 32000 in fp32 (432 MB): 68 us without alternatives (6.3 TB/s), 82 with the five best; in bf16 48 and 67, bound by
-// instructions (one exponential per logit alone takes 24).  One row: 4.6 and 7.6 us, 64 rows of 128256 in bf16 10 and 14, latency.
+// 3376 rows of 32000 in fp32 (432 MB), with the ranks of their tokens: 69 us without alternatives (6.2 TB/s), 83 with the five best; in bf16 53
+// and 67, bound by instructions (one exponential per logit alone takes 24), and by what finishing a row holds up.  One row: 5.0 and
+// 8.0 us, 64 rows of 128256 in bf16 9.0 and 14.0 with the 20 best, latency.
 #include "rows_mma.cuh"
 
 namespace lazy {
@@ -542,7 +543,8 @@ struct LpShape {
 };
 // A row takes the longest of its share of the memory's rate (44 B/ns to an SM), of what an SM sums (13 logits a ns), and of a round trip
 // to every round, and then some time to be finished: 2 us; to join the parts of a cluster of two another 2, and 0.75 for each doubling.
-// One row with five alternatives, by one CTA, four and eight: of 16000 logits 7.7 us / - / 8.9, 32000 - / 8.0 / 9.0, 50257 - / 9.5 / 8.5.
+// The times to finish and to join are those of five alternatives, whatever n_top is.
+// One row with five of them, by one CTA, four and eight: of 16000 logits 7.7 us / - / 8.9, 32000 - / 8.0 / 9.0, 50257 - / 9.5 / 8.5.
 template <typename T, int THREADS>
 LpShape lp_shape(const LogprobArgs &a, int cluster) {
   constexpr int CTAS = LP_CTAS<T, THREADS>;
