@@ -41,7 +41,7 @@ paged_wide_kernel(const PagedArgs a, int group, int tiles, int splits, int per_s
   if (!paged_seq(a.kv, a.cu_q, s, a.n_rows, a.max_q, a.max_kv, blockIdx.x == 0 && threadIdx.x == 0, status, start, rows, len)) return;
   const int cols = min(PW_COLS, (int)min((long long)rows * group - c0, (long long)PW_COLS));
   if (cols <= 0) return;
-  const int k0 = split * per_split, k1 = min(len, k0 + per_split);
+  const int k0 = split * per_split, k1 = k0 + min(len - k0, per_split);  // k0 + per_split may pass 2^31
   const int32_t *table = a.kv.table + (size_t)s * a.kv.ld_table;
   const T *kp = (const T *)a.kv.k + (long long)g * a.kv.head_stride + lane, *vp = (const T *)a.kv.v + (long long)g * a.kv.head_stride + lane;
   auto row_of = [&](int c) { return (c0 + c) / group; };

@@ -80,7 +80,7 @@ prefix_partial_kernel(const PrefixArgs a, int per_split, float *__restrict__ par
     return (const T *)own + (size_t)i * a.ldkv + col;
   };
   attn_split_partial<T>(sm, (const T *)a.q + (size_t)r * a.ldq + (size_t)h * a.head_dim, a.head_dim, k0,
-                        min(n, k0 + per_split), [&](int j) { return row(a.k_pre, a.k, j); },
+                        k0 + min(n - k0, per_split), [&](int j) { return row(a.k_pre, a.k, j); },
                         [&](int j) { return row(a.v_pre, a.v, j); }, part_o + part * a.head_dim, part_ml + part * 2,
                         nullptr);
 }

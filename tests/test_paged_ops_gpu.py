@@ -976,3 +976,22 @@ def test_attention_paged_of_a_row_without_a_finite_logit(heads):
         pool.k[..., 3] = -float("inf")
         assert torch.all(B.lazy_k_attention_paged(dq, *pool.args(), length) == 0)
     B.lazy_device_status()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attention_paged_of_nearly_2_to_31_tokens(dtype):
+    """A table that names one page 2046 times and another last, whose keys outweigh all before: the last range of keys ends behind 2^31 by
+    the bounds.  Every token of the last page has the same weight and value: o is that value, off by the sums of weights alone, at most
+    2^20 / 8 terms one after the other in either."""
+    page, dh = 1 << 20, 32
+    k, v = [torch.zeros((2, page, 1, dh), dtype=dtype, device="cuda") for _ in range(2)]
+    k[1] = 4.0
+    want = (1.0 + torch.arange(dh) / 16).to(dtype)
+    v[1] = want.cuda()
+    table = torch.zeros((1, 2048), dtype=torch.int32, device="cuda")
+    table[0, 2046] = 1
+    q = torch.ones((1, dh), dtype=dtype, device="cuda")
+    got = B.lazy_k_attention_paged(q, k, v, table, i32([2047 * page]), 2 ** 31 - 1)
+    B.lazy_device_status()
+    # a token of the others weighs e^-22.6 as much: 2046 times that is 3.2e-7
+    assert torch.all(torch.abs(got[0].cpu().double() - want.double()) <= (2.0 ** 17 * 2 * U + 1e-6 + half_step(dtype)) * want.double())
